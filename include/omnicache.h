@@ -48,7 +48,7 @@ enum {
 };
 
 enum { OC_KIND_TOKEN = 0, OC_KIND_FRAME = 1, OC_KIND_BLOCK = 2 };
-enum { OC_DTYPE_F32 = 0, OC_DTYPE_BF16 = 1 };
+enum { OC_DTYPE_F32 = 0, OC_DTYPE_BF16 = 1, OC_DTYPE_I8 = 2 /* rows with a scale each: oc_block_norm only */ };
 enum { OC_SELECT_THRESHOLD = 0, OC_SELECT_COUNT = 1 };
 enum { OC_RESTORE_FROM_CACHE = 0, OC_RESTORE_FROM_REPRESENTATIVE = 1 };
 enum { OC_FRAME_MEAN_POS_COS = 0, OC_FRAME_FLAT_COS = 1 };
@@ -142,7 +142,11 @@ enum {
     OC_K_RESTORE = 10,
     OC_K_COPY = 11,       /* layered-cache put / copying get                          */
     OC_K_LINEAR = 12,     /* projection with gather / scatter folded in               */
-    OC_K_COUNT = 13
+    OC_K_BLOCK_NORM = 13, /* restore + gate + residual + norms between two blocks      */
+    OC_K_ROPE = 14,       /* rotary positions                                           */
+    OC_K_QUANT = 15,      /* rows to 8-bit integers                                     */
+    OC_K_LINEAR_I8 = 16,  /* 8-bit matrix product                                       */
+    OC_K_COUNT = 17
 };
 const char* oc_kernel_name(int kernel_id);
 
@@ -434,6 +438,125 @@ oc_status oc_schedule_propose(const double* latency, const double* quality_loss,
 oc_status oc_cache_step_host(oc_ctx* ctx, const oc_layout* layout, int mode, float thr,
                              int64_t n_reuse_per_group, const void* x_host, const void* cache_host,
                              void* out_host, int32_t* kept_count_host, void* stream);
+
+/* =============================================================================================
+ * The wrapped block on kept tokens: norms with gate and residual, rotary positions, 8-bit products
+ * ============================================================================================= */
+
+/* (In every call of this part, no rows at all -- n_rows or M of 0 -- is OC_OK whatever the pointers.) */
+enum { OC_NORM_NONE = 0, OC_NORM_RMS = 1, OC_NORM_LAYER = 2 };
+enum { OC_ROPE_ADJACENT = 0, OC_ROPE_HALVES = 1 };
+
+/* What happens to the rows between two blocks of a transformer, in one pass over them.  Rows belong
+ * to units of unit_rows rows (1: tokens of Token Cache; H*W: frames of Frame Cache); for row i of
+ * unit u = i / unit_rows, with s = slot_of[u] (no slot_of: s = u),
+ *     v            = row (s*unit_rows + i % unit_rows) of z if s >= 0, else row i of cache     (restore)
+ *     cache_out[i] = v
+ *     r            = res_scale * x[i] + gate * post(v)
+ *     out[i]       = r
+ *     h[s*unit_rows + i % unit_rows] = pre(r) * (1 + scale) + shift       only where s >= 0 (gather)
+ * post / pre: OC_NORM_RMS  v / sqrt(mean(v^2) + eps) * w + b,
+ *             OC_NORM_LAYER the same of v - mean(v),   OC_NORM_NONE  v * w + b;
+ * w, b, gate, scale, shift may each be null (1, 0, 1, 0, 0).  gate, scale and shift are vectors of C
+ * elements, one for each group of rows_per_group rows (a batch element, a frame): group g's vector
+ * begins g * mod_stride elements after the pointer, so the three may lie side by side in what a
+ * modulation projection wrote; mod_stride = 0 is one vector for all rows.
+ * All arithmetic is in fp32; r is rounded for `out` and enters pre() unrounded; cache_out is a bit
+ * copy.  h is fp32, bf16 or OC_DTYPE_I8: h[s][c] = rint(y[c] * 127 / max|y|) with h_scale[s] =
+ * max|y| / 127 (a row whose max|y| is under 2^-100: zeros and scale 0; a row with an infinity or NaN
+ * keeps it in its scale).
+ * x and slot_of are read, everything else is optional: without z there is no v (cache, cache_out,
+ * gate and post_* are then null, post_norm NONE), without h nothing is done for it.  Without z and
+ * out, rows that have no slot are not read.
+ * Errors: OC_ERR_INVALID_ARG (also: slot_of and z without cache; rows not a whole number of units);
+ * OC_ERR_ALIGNMENT (a pointer or mod_stride not a multiple of 16 bytes -- 8 for bf16 parameters of
+ * fp32 rows, 4 for slot_of and h_scale --, C not a multiple of 16 bytes of dtype, or of 16 elements for
+ * OC_DTYPE_I8); OC_ERR_UNSUPPORTED (rows
+ * over 49152 bytes, 2^31 rows or more).  A slot outside dense_rows is recorded as OC_ERR_INVALID_ARG
+ * in the device status word and its unit treated as reused (with no cache: left out).
+ * out may be x, and cache_out may be cache (then only computed rows are written); otherwise outputs
+ * overlap nothing. */
+typedef struct oc_block_norm_desc {
+    int dtype;               /* x, z, cache, cache_out, out: OC_DTYPE_F32 or OC_DTYPE_BF16 */
+    int h_dtype;             /* OC_DTYPE_F32, OC_DTYPE_BF16 or OC_DTYPE_I8 */
+    int param_dtype;         /* post_w .. shift: OC_DTYPE_F32 or OC_DTYPE_BF16 */
+    int post_norm, pre_norm; /* OC_NORM_* */
+    float post_eps, pre_eps, res_scale;
+    int64_t n_rows, C;
+    int64_t rows_per_group, mod_stride;
+    int64_t unit_rows, dense_rows;    /* dense_rows: rows of z and h, a multiple of unit_rows */
+} oc_block_norm_desc;
+oc_status oc_block_norm(oc_ctx* ctx, const oc_block_norm_desc* desc, const void* x, const void* z, const int32_t* slot_of,
+                        const void* cache, void* cache_out, void* out, const void* post_w, const void* post_b,
+                        const void* gate, const void* pre_w, const void* pre_b, const void* scale, const void* shift,
+                        void* h, float* h_scale, void* stream);
+
+/* Rotary positions with up to three axes on queries and keys, after an optional RMS norm of each head.
+ * The leading axis_dims[0] + axis_dims[1] + axis_dims[2] elements of a head are rotated, the rest
+ * pass through.  They form P = half as many pairs: OC_ROPE_ADJACENT pair p = elements (2p, 2p + 1),
+ * OC_ROPE_HALVES pair p = elements (p, P + p).  The first axis_dims[0]/2 pairs turn by the position
+ * on axis 0, the next axis_dims[1]/2 by that on axis 1, and so on (axes: time, height, width):
+ *     a' = a cos - b sin,   b' = b cos + a sin        (inverse: sin taken negative)
+ * table: fp32 (cos, sin) for every position and pair of an axis, [axis_len[a]][axis_dims[a]/2][2],
+ * the axes one after the other; oc_rope_table writes the usual one.  It may hold any rotation.
+ * Row r's position is pos[r] (int32 [n_rows][3]) or, without pos, that of token
+ *     idx[r / unit_rows] * unit_rows + r % unit_rows      (no idx: r)
+ * of a [..., axis_len[0], axis_len[1], axis_len[2]] grid: rows gathered by a kept list keep the
+ * position of the token they came from.  Rows whose idx is negative (the list's unused tail) are
+ * neither read nor written, nor is a row with a position outside the table (recorded as
+ * OC_ERR_INVALID_ARG in the device status word).
+ * Head h of row r = (b, i), b = r / rows_per_batch, i = r % rows_per_batch, begins
+ *     in:  r * row_stride + h * head_stride              (q and k may be parts of one projection)
+ *     out: b * batch_stride + i * row_stride + h * head_stride
+ * elements after its pointer; elements of a head are contiguous.  k, k_out may be null, and k_heads
+ * may differ from q_heads.  q_w / k_w: fp32 [head_dim], null for no norm (both or neither):
+ * v / sqrt(mean(v^2) + eps) * w before the rotation.  All arithmetic is in fp32, rounded once.
+ * In place (out = in with the same strides) is allowed; otherwise inputs and outputs do not overlap.
+ * Errors: OC_ERR_INVALID_ARG; OC_ERR_ALIGNMENT (a pointer not aligned to its element, or for ADJACENT
+ * to its pair; odd strides there); OC_ERR_UNSUPPORTED (a head of more than 64 units: one unit is 16
+ * bytes of a head, twice that with HALVES, or as much less as strides, pointers and pairs are aligned
+ * to; 2^31 rows or more). */
+typedef struct oc_rope_view { int64_t batch_stride, row_stride, head_stride; } oc_rope_view;
+typedef struct oc_rope_desc {
+    int dtype;                        /* OC_DTYPE_F32 or OC_DTYPE_BF16 */
+    int head_dim, q_heads, k_heads;
+    int pairing;                      /* OC_ROPE_* */
+    int inverse;
+    int axis_dims[3];                 /* even, may be 0 */
+    int axis_len[3];                  /* positions of each axis, >= 1 */
+    float eps;
+    int64_t n_rows, rows_per_batch, unit_rows;
+    oc_rope_view q, q_out, k, k_out;  /* batch_stride of q and k: unused */
+} oc_rope_desc;
+/* Host only: elements of the table, and the table with angle = position * theta^(-2j / axis_dims[a])
+ * for pair j of axis a, computed in double and rounded; table_host is host memory. */
+oc_status oc_rope_table_size(const oc_rope_desc* desc, int64_t* n_floats);
+oc_status oc_rope_table(const oc_rope_desc* desc, double theta, float* table_host);
+oc_status oc_rope(oc_ctx* ctx, const oc_rope_desc* desc, const float* table, const int32_t* idx, const int32_t* pos,
+                  const void* q, void* q_out, const float* q_w, const void* k, void* k_out, const float* k_w, void* stream);
+
+/* Rows to 8-bit integers with a scale each, as oc_block_norm's OC_DTYPE_I8 form:
+ *     scale[r] = max|x_r| / 127,   q[r][c] = rint(x_r[c] * 127 / max|x_r|)
+ * x_r is row idx[r] of x (no idx: row r); rows are x_stride elements apart.  Rows whose idx is
+ * negative are left untouched; an idx outside x_rows too (recorded in the device status word).
+ * Also makes the weights of oc_linear_int8 (a row is an output channel).
+ * Errors: OC_ERR_ALIGNMENT (K not a multiple of 16, x_stride * element size not of 16 bytes, a pointer
+ * not 16-byte aligned -- scale: 4), OC_ERR_UNSUPPORTED (rows over 49152 bytes, 2^31 rows or more). */
+oc_status oc_quantize_rows(oc_ctx* ctx, const void* x, int dtype, int64_t x_rows, int64_t x_stride, const int32_t* idx,
+                           int64_t n_rows, int64_t K, int8_t* q, float* scale, void* stream);
+
+/* Matrix product in 8-bit integers, one scale per token and one per output channel:
+ *     out[dst(m)][n] = a_scale[m] * w_scale[n] * sum_k a[m][k] * w[n][k] + bias[n],  m = 0 .. M-1
+ * a int8 [M][K], w int8 [N][K], scales and bias fp32 (bias nullable); out fp32 or bf16, rows
+ * out_stride elements apart.  dst(m) = out_idx[m] (no out_idx: m); a negative one is not stored, one
+ * outside out_rows neither (recorded in the device status word).  Sums are exact; the scales and the
+ * bias are applied in fp32 and the result is rounded once.  Any M, N and out_stride (rows of out that
+ * are multiples of 16 bytes are stored fastest); K at most 131056, so that no sum leaves 32 bits.
+ * Errors: OC_ERR_ALIGNMENT (K not a multiple of 16; a or w not 16-byte aligned), OC_ERR_INVALID_ARG (out_stride < N; out_rows < M without out_idx),
+ * OC_ERR_UNSUPPORTED (sizes). */
+oc_status oc_linear_int8(oc_ctx* ctx, const int8_t* a, const float* a_scale, int64_t M, int64_t K, const int8_t* w,
+                         const float* w_scale, int64_t N, const float* bias, void* out, int out_dtype, int64_t out_rows,
+                         int64_t out_stride, const int32_t* out_idx, void* stream);
 
 #ifdef __cplusplus
 }

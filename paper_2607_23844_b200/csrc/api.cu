@@ -143,7 +143,8 @@ const char* oc_status_str(oc_status s) {
 const char* oc_kernel_name(int k) {
     static const char* names[OC_K_COUNT] = {"norms", "match_tc", "match_simt", "match_finalize", "frame_pair",
                                             "frame_finalize", "block_partial", "block_finalize", "select",
-                                            "gather", "restore", "copy", "linear"};
+                                            "gather", "restore", "copy", "linear", "block_norm", "rope", "quantize",
+                                            "linear_int8"};
     return (k >= 0 && k < OC_K_COUNT) ? names[k] : "unknown";
 }
 
@@ -427,6 +428,139 @@ oc_status oc_linear_gather_scatter(oc_ctx* c, const void* a, int64_t a_rows, int
     DeviceGuard guard(c->device);
     if (!guard.ok) return OC_ERR_CUDA;
     return launch_linear_gs(c, a, a_rows, K, a_idx, n_rows, w, N, out, out_rows, out_idx, (cudaStream_t)stream);
+}
+
+// ---- the wrapped block on kept tokens -------------------------------------------------------------
+static inline bool float_type(int t) { return t == OC_DTYPE_F32 || t == OC_DTYPE_BF16; }
+static inline bool norm_kind(int k) { return k == OC_NORM_NONE || k == OC_NORM_RMS || k == OC_NORM_LAYER; }
+static inline bool bad_eps(float e) { return !(e >= 0.0f) || !isfinite(e); }
+static const int64_t ROWS_MAX = 0x7FFFFFFFll;
+
+oc_status oc_block_norm(oc_ctx* c, const oc_block_norm_desc* d, const void* x, const void* z, const int32_t* slot_of,
+                        const void* cache, void* cache_out, void* out, const void* post_w, const void* post_b,
+                        const void* gate, const void* pre_w, const void* pre_b, const void* scale, const void* shift,
+                        void* h, float* h_scale, void* stream) {
+    if (!c || !d) return OC_ERR_INVALID_ARG;
+    if (!float_type(d->dtype) || !float_type(d->param_dtype) || !norm_kind(d->post_norm) || !norm_kind(d->pre_norm)) return OC_ERR_INVALID_ARG;
+    if (!float_type(d->h_dtype) && d->h_dtype != OC_DTYPE_I8) return OC_ERR_INVALID_ARG;
+    if (bad_eps(d->post_eps) || bad_eps(d->pre_eps) || !isfinite(d->res_scale)) return OC_ERR_INVALID_ARG;
+    if (d->n_rows < 0 || d->C <= 0 || d->rows_per_group <= 0 || d->mod_stride < 0 || d->unit_rows <= 0 || d->dense_rows < 0) return OC_ERR_INVALID_ARG;
+    if (d->n_rows > ROWS_MAX || d->dense_rows > ROWS_MAX || d->C > ROWS_MAX) return OC_ERR_UNSUPPORTED;
+    if (d->n_rows % d->unit_rows != 0 || d->dense_rows % d->unit_rows != 0) return OC_ERR_INVALID_ARG;
+    if (d->n_rows == 0) return OC_OK;                                       // (empty tensors have no addresses)
+    if (!x || (!out && !h && !cache_out)) return OC_ERR_INVALID_ARG;
+    if (!z && (cache || cache_out || gate || post_w || post_b || d->post_norm != OC_NORM_NONE)) return OC_ERR_INVALID_ARG;
+    if (z && slot_of && !cache) return OC_ERR_INVALID_ARG;                  // reused rows would come from nowhere
+    if ((z || h) && !slot_of && d->dense_rows < d->n_rows) return OC_ERR_INVALID_ARG;
+    if (h && d->h_dtype == OC_DTYPE_I8 && !h_scale) return OC_ERR_INVALID_ARG;
+    if (out && (out == z || out == cache || out == cache_out)) return OC_ERR_INVALID_ARG;
+    if (cache_out && (cache_out == x || cache_out == z)) return OC_ERR_INVALID_ARG;
+    if (h && (h == x || h == z || h == cache || h == cache_out || h == out)) return OC_ERR_INVALID_ARG;
+    const int64_t eb = d->dtype == OC_DTYPE_F32 ? 4 : 2;
+    if (d->C * eb % 16 != 0 || (h && d->h_dtype == OC_DTYPE_I8 && d->C % 16 != 0)) return OC_ERR_ALIGNMENT;
+    const void* rows[] = {x, z, cache, cache_out, out, h};
+    for (const void* p : rows) if (p && misaligned(p)) return OC_ERR_ALIGNMENT;
+    // parameters are read as many elements at a time as 16 bytes of a row hold
+    const int64_t pb = d->param_dtype == OC_DTYPE_F32 ? 4 : 2, param_align = std::min<int64_t>(16, 16 / eb * pb);
+    const void* params[] = {post_w, post_b, gate, pre_w, pre_b, scale, shift};
+    for (const void* p : params) if ((uintptr_t)p & (uintptr_t)(param_align - 1)) return OC_ERR_ALIGNMENT;
+    if ((gate || scale || shift) && d->mod_stride * pb % param_align != 0) return OC_ERR_ALIGNMENT;
+    if (((uintptr_t)slot_of & 3u) || ((uintptr_t)h_scale & 3u)) return OC_ERR_ALIGNMENT;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return OC_ERR_CUDA;
+    return launch_block_norm(c, *d, x, z, slot_of, cache, cache_out, out, post_w, post_b, gate, pre_w, pre_b, scale, shift,
+                             h, h_scale, (cudaStream_t)stream);
+}
+
+// Sizes and axes of a rotation; the number of (cos, sin) pairs of its table.
+static oc_status check_rope(const oc_rope_desc* d, int64_t* table_pairs) {
+    if (!d || !float_type(d->dtype) || d->head_dim <= 0 || (d->pairing != OC_ROPE_ADJACENT && d->pairing != OC_ROPE_HALVES)) return OC_ERR_INVALID_ARG;
+    int64_t rot = 0, n = 0, grid = 1;
+    for (int a = 0; a < 3; ++a) {
+        if (d->axis_dims[a] < 0 || d->axis_dims[a] % 2 != 0 || d->axis_len[a] < 1) return OC_ERR_INVALID_ARG;
+        rot += d->axis_dims[a];
+        n += (int64_t)d->axis_len[a] * (d->axis_dims[a] / 2);
+        if (grid <= ROWS_MAX) grid *= d->axis_len[a];
+    }
+    if (rot == 0 || rot > d->head_dim) return OC_ERR_INVALID_ARG;
+    if (n > ROWS_MAX || grid > ROWS_MAX) return OC_ERR_UNSUPPORTED;
+    *table_pairs = n;
+    return OC_OK;
+}
+
+oc_status oc_rope_table_size(const oc_rope_desc* d, int64_t* n_floats) {
+    int64_t n;
+    if (!n_floats) return OC_ERR_INVALID_ARG;
+    oc_status st = check_rope(d, &n);
+    if (st != OC_OK) return st;
+    *n_floats = 2 * n;
+    return OC_OK;
+}
+
+oc_status oc_rope_table(const oc_rope_desc* d, double theta, float* table) {
+    int64_t n;
+    if (!table || !(theta > 0.0) || !std::isfinite(theta)) return OC_ERR_INVALID_ARG;
+    oc_status st = check_rope(d, &n);
+    if (st != OC_OK) return st;
+    for (int a = 0; a < 3; ++a)
+        for (int p = 0; p < d->axis_len[a]; ++p)
+            for (int j = 0; j < d->axis_dims[a] / 2; ++j) {
+                const double angle = p * std::pow(theta, -2.0 * j / d->axis_dims[a]);
+                *table++ = (float)std::cos(angle);
+                *table++ = (float)std::sin(angle);
+            }
+    return OC_OK;
+}
+
+oc_status oc_rope(oc_ctx* c, const oc_rope_desc* d, const float* table, const int32_t* idx, const int32_t* pos, const void* q,
+                  void* q_out, const float* q_w, const void* k, void* k_out, const float* k_w, void* stream) {
+    if (!c) return OC_ERR_INVALID_ARG;
+    int64_t n;
+    oc_status st = check_rope(d, &n);
+    if (st != OC_OK) return st;
+    if (d->q_heads <= 0 || (k && d->k_heads <= 0) || d->n_rows < 0 || d->rows_per_batch <= 0 || d->unit_rows <= 0) return OC_ERR_INVALID_ARG;
+    if (d->n_rows == 0) return OC_OK;                                       // (empty tensors have no addresses)
+    if (!table || !q || !q_out) return OC_ERR_INVALID_ARG;
+    if ((k != nullptr) != (k_out != nullptr) || (idx && pos)) return OC_ERR_INVALID_ARG;
+    if ((q_w != nullptr) != (k_w != nullptr) && k) return OC_ERR_INVALID_ARG;
+    if (k_w && !k) return OC_ERR_INVALID_ARG;
+    if (q_w && bad_eps(d->eps)) return OC_ERR_INVALID_ARG;
+    const oc_rope_view* views[4] = {&d->q, &d->q_out, &d->k, &d->k_out};
+    for (int i = 0; i < (k ? 4 : 2); ++i)
+        if (views[i]->batch_stride < 0 || views[i]->row_stride < 0 || views[i]->head_stride < 0) return OC_ERR_INVALID_ARG;
+    if (d->n_rows > ROWS_MAX || d->rows_per_batch > ROWS_MAX || d->unit_rows > ROWS_MAX || d->q_heads > 65535 || d->k_heads > 65535) return OC_ERR_UNSUPPORTED;
+    if (((uintptr_t)table & 7u) || ((uintptr_t)idx & 3u) || ((uintptr_t)pos & 3u) || ((uintptr_t)q_w & 3u) || ((uintptr_t)k_w & 3u)) return OC_ERR_ALIGNMENT;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return OC_ERR_CUDA;
+    return launch_rope(c, *d, table, idx, pos, q, q_out, q_w, k, k_out, k_w, (cudaStream_t)stream);
+}
+
+oc_status oc_quantize_rows(oc_ctx* c, const void* x, int dtype, int64_t x_rows, int64_t x_stride, const int32_t* idx,
+                           int64_t n_rows, int64_t K, int8_t* q, float* scale, void* stream) {
+    if (!c || !float_type(dtype) || n_rows < 0 || K <= 0 || x_rows < 0 || x_stride < K) return OC_ERR_INVALID_ARG;
+    if (n_rows == 0) return OC_OK;                                          // (empty tensors have no addresses)
+    if (!x || !q || !scale || (!idx && n_rows > x_rows)) return OC_ERR_INVALID_ARG;
+    if (n_rows > ROWS_MAX || x_rows > ROWS_MAX || K > ROWS_MAX) return OC_ERR_UNSUPPORTED;
+    if (K % 16 != 0 || x_stride * (dtype == OC_DTYPE_F32 ? 4 : 2) % 16 != 0 || misaligned(x) || misaligned(q)) return OC_ERR_ALIGNMENT;
+    if (((uintptr_t)scale & 3u) || ((uintptr_t)idx & 3u)) return OC_ERR_ALIGNMENT;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return OC_ERR_CUDA;
+    return launch_quantize_rows(c, x, dtype, x_rows, x_stride, idx, n_rows, K, q, scale, (cudaStream_t)stream);
+}
+
+oc_status oc_linear_int8(oc_ctx* c, const int8_t* a, const float* a_scale, int64_t M, int64_t K, const int8_t* w,
+                         const float* w_scale, int64_t N, const float* bias, void* out, int out_dtype, int64_t out_rows,
+                         int64_t out_stride, const int32_t* out_idx, void* stream) {
+    if (!c || !float_type(out_dtype) || M < 0 || K <= 0 || N <= 0 || out_rows < 0 || out_stride < N) return OC_ERR_INVALID_ARG;
+    if (M == 0) return OC_OK;                                               // (empty tensors have no addresses)
+    if (!a || !a_scale || !w || !w_scale || !out || (!out_idx && out_rows < M)) return OC_ERR_INVALID_ARG;
+    if (M > ROWS_MAX || N > ROWS_MAX || out_rows > ROWS_MAX || K > 131056) return OC_ERR_UNSUPPORTED;
+    if (K % 16 != 0 || misaligned(a) || misaligned(w)) return OC_ERR_ALIGNMENT;
+    if ((uintptr_t)out & (out_dtype == OC_DTYPE_F32 ? 3u : 1u)) return OC_ERR_ALIGNMENT;
+    if (((uintptr_t)a_scale & 3u) || ((uintptr_t)w_scale & 3u) || ((uintptr_t)bias & 3u) || ((uintptr_t)out_idx & 3u)) return OC_ERR_ALIGNMENT;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return OC_ERR_CUDA;
+    return launch_linear_int8(c, a, a_scale, M, K, w, w_scale, N, bias, out, out_dtype, out_rows, out_stride, out_idx, (cudaStream_t)stream);
 }
 
 // ---- Token Cache on the frame pairs of Frame Cache (Section 3.2.3) ---------------------------------

@@ -192,6 +192,17 @@ oc_status launch_match_token(oc_ctx*, const Geo&, const void* x, float* best_sim
 bool tc_match_supported(const Geo&);
 oc_status launch_linear_gs(oc_ctx*, const void* a, int64_t a_rows, int64_t K, const int32_t* a_idx, int64_t n_rows,
                            const void* w, int64_t N, void* out, int64_t out_rows, const int32_t* out_idx, cudaStream_t);
+oc_status launch_block_norm(oc_ctx*, const oc_block_norm_desc&, const void* x, const void* z, const int32_t* slot_of,
+                            const void* cache, void* cache_out, void* out, const void* post_w, const void* post_b,
+                            const void* gate, const void* pre_w, const void* pre_b, const void* scale, const void* shift,
+                            void* h, float* h_scale, cudaStream_t);
+oc_status launch_rope(oc_ctx*, const oc_rope_desc&, const float* table, const int32_t* idx, const int32_t* pos, const void* q,
+                      void* q_out, const float* q_w, const void* k, void* k_out, const float* k_w, cudaStream_t);
+oc_status launch_quantize_rows(oc_ctx*, const void* x, int dtype, int64_t x_rows, int64_t x_stride, const int32_t* idx,
+                               int64_t n_rows, int64_t K, int8_t* q, float* scale, cudaStream_t);
+oc_status launch_linear_int8(oc_ctx*, const int8_t* a, const float* a_scale, int64_t M, int64_t K, const int8_t* w,
+                             const float* w_scale, int64_t N, const float* bias, void* out, int out_dtype, int64_t out_rows,
+                             int64_t out_stride, const int32_t* out_idx, cudaStream_t);
 size_t joint_workspace_bytes(const Geo&);
 oc_status launch_joint_groups(oc_ctx*, int B, int T, const float* frame_best_sim, const int32_t* frame_best_idx,
                               const int32_t* frame_slot_of, int2* frames, cudaStream_t);

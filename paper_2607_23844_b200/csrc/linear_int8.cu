@@ -1,0 +1,510 @@
+// Matrix product in 8-bit integers with one scale per token and one per output channel:
+//     out[dst(m), n] = a_scale[m] * w_scale[n] * sum_k a[m, k] * w[n, k] + bias[n]
+// The sums are exact (32-bit integers), the scales and the bias are applied in fp32, the result is rounded once.
+//
+// Many tokens: tcgen05.mma kind::i8 (8-bit operands, 32-bit accumulators in tensor memory).  One persistent CTA
+// (or CTA pair, cta_group::2) per SM walks over output tiles of 128 x N_TILE (256 x 256 for a pair):
+//   warp 0       copies: TMA boxes of 128 bytes of K by 128 rows, 128-byte swizzle, into a ring of stages
+//   warp 1       the MMAs (128 bytes of K = four steps of 32); owns the tensor memory
+//   warps 2..3   idle (the epilogue's warps have to start at a multiple of four)
+//   warps 4..11  epilogue: thread = row; scales, bias, rounding, then through shared memory so that a warp
+//                stores whole 64- or 128-byte pieces of rows, to the rows that out_idx names
+// Two accumulators take turns, so the epilogue of a tile runs under the MMAs of the next.
+// Few tokens (at most 8): one warp per pair of output channels, dp4a, the weights read once as they lie.
+// K and N tails are zero-filled by TMA and not stored.  Every wait is bounded (OC_ERR_TIMEOUT in the status word).
+#include <string.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "rows.cuh"
+#include "tc_ptx.cuh"
+
+namespace oc {
+
+static constexpr int I8_BM = 128, I8_BK = 128;                      // rows of a CTA's tile; bytes of K per stage
+static constexpr int I8_THREADS = 384, I8_EPI_WARPS = 8;
+static constexpr int I8_A_BYTES = I8_BM * I8_BK;
+static constexpr int I8_STAGES_MAX = 8;
+static constexpr int I8_PITCH = 144;                                // bytes per staged row: 128 and a bank step of 16
+static constexpr int I8_OUT_STAGE = 32 * I8_PITCH;                  // per epilogue warp
+
+struct I8Params {
+    CUtensorMap mapA, mapW;      // {K, rows}: boxes {128, 128} and {128, rows of W per CTA}
+    const float *a_scale, *w_scale, *bias;
+    const int32_t* out_idx;
+    void* out;
+    long long out_stride;
+    int M, N, out_rows;
+    int kblocks, m_tiles, n_tiles, n_first, n_stages;
+    int wide;                    // rows of `out` may be stored in 16-byte pieces
+    int* status;
+};
+
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void tc_mma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate, uint32_t issue) {
+    if (PAIR)
+        asm volatile("{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+                     "@e tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                     :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+                     "@e tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                     :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
+}
+// arrive on `bar` (of both CTAs in a pair) once every MMA issued so far has retired
+template <bool PAIR>
+__device__ __forceinline__ void tc_commit_all(uint32_t bar, uint32_t issue) {
+    if (PAIR)
+        asm volatile("{\n\t.reg .pred e;\n\t.reg .b16 both;\n\tmov.b16 both, 3;\n\tsetp.ne.b32 e, %1, 0;\n\t"
+                     "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], both;\n\t}"
+                     :: "r"(bar), "r"(issue) : "memory");
+    else
+        tc_commit<false>(bar, issue);
+}
+
+// The tiles of a walker, in order.  The larger operand is walked through once, the smaller one again for each
+// tile of it (it stays in L2).
+struct I8Walk {
+    int tile, step, total;
+    __device__ __forceinline__ bool next(const I8Params& P, int& m, int& n) {
+        if (tile >= total) return false;
+        if (P.n_first) { m = tile / P.n_tiles; n = tile - m * P.n_tiles; }
+        else { n = tile / P.m_tiles; m = tile - n * P.m_tiles; }
+        tile += step;
+        return true;
+    }
+};
+
+template <int N_TILE, bool PAIR, int OT>
+__global__ void __launch_bounds__(I8_THREADS, 1)
+linear_int8_kernel(const __grid_constant__ I8Params P) {
+    constexpr int W_ROWS = PAIR ? N_TILE / 2 : N_TILE;               // rows of W that this CTA fetches
+    constexpr int STAGE_BYTES = I8_A_BYTES + W_ROWS * I8_BK;
+    constexpr int TMEM_COLS = 2 * N_TILE;
+    constexpr int OB = OT == OC_DTYPE_F32 ? 4 : 2;
+    constexpr int PASS = (OB == 2 && N_TILE >= 128) ? 64 : 32;       // columns that a warp stages together
+    constexpr int SEG = PASS * OB, LPR = SEG / 16, RPI = 32 / LPR;   // a staged row: bytes, lanes that store it; rows per store
+    constexpr int PITCH = SEG + 16;
+    extern __shared__ __align__(1024) uint8_t i8_smem[];
+    uint8_t* after = i8_smem + (size_t)P.n_stages * STAGE_BYTES;
+    uint8_t* out_stage = after;                                      // [8 warps][32 rows][PITCH]
+    float* col_tab = (float*)(after + I8_EPI_WARPS * I8_OUT_STAGE);  // [2 tiles][scale, bias][N_TILE]
+    uint64_t* bars = (uint64_t*)(col_tab + 4 * N_TILE);
+    const uint32_t tiles = smem_u32(i8_smem);
+    const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * I8_STAGES_MAX;
+    const uint32_t bar_acc_full = bar_empty + 8 * I8_STAGES_MAX, bar_acc_empty = bar_acc_full + 16, bar_drain = bar_acc_empty + 16;
+    uint32_t* tmem_slot = (uint32_t*)(bars + 2 * I8_STAGES_MAX + 5);
+    volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
+    const bool leader = rank == 0;
+    const int STAGES = P.n_stages;
+
+    if ((tiles & 1023u) != 0) {                                      // never expected; refuse rather than compute garbage
+        if (threadIdx.x == 0) atomicCAS(P.status, 0, OC_ERR_ALIGNMENT);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < I8_STAGES_MAX; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(bar_acc_full + 8 * b, 1); mbar_init(bar_acc_empty + 8 * b, (PAIR ? 2 : 1) * I8_EPI_WARPS); }
+        mbar_init(bar_drain, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        tma_prefetch_map(&P.mapA);
+        tma_prefetch_map(&P.mapW);
+    }
+    if (warp == 1) {
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            tmem_alloc_cta1(smem_u32(tmem_slot), TMEM_COLS);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();                                    // the other CTA's barriers exist before anything signals them
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    pdl_wait();                                                      // the operands may come from the kernel before this one
+    if (threadIdx.x == 0) pdl_launch_dependents();
+    I8Walk walk;
+    walk.tile = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
+    walk.step = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+    walk.total = P.m_tiles * P.n_tiles;
+    int m, n;
+
+    if (warp == 0) {
+        // ================================ copies ================================================
+        if (lane == 0) {
+            int stage = 0; uint32_t phase = 0, armed = 0;
+            bool ok = true;
+            while (ok && walk.next(P, m, n)) {
+                const int row0 = m * (PAIR ? 2 * I8_BM : I8_BM) + (int)rank * I8_BM, col0 = n * N_TILE + (int)rank * W_ROWS;
+                for (int kb = 0; kb < P.kblocks; ++kb) {
+                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
+                    const uint32_t dst = tiles + (uint32_t)(stage * STAGE_BYTES), full = bar_full + 8 * stage;
+                    if (leader) mbar_arrive_expect_tx(full, (PAIR ? 2 : 1) * STAGE_BYTES);
+                    if (PAIR) {
+                        const uint32_t bar = map_to_cta(full, 0);    // both CTAs' copies report to the leader
+                        tma_load_2d_pair(dst, &P.mapA, kb * I8_BK, row0, bar);
+                        tma_load_2d_pair(dst + I8_A_BYTES, &P.mapW, kb * I8_BK, col0, bar);
+                    } else {
+                        tma_load_2d(dst, &P.mapA, kb * I8_BK, row0, full);
+                        tma_load_2d(dst + I8_A_BYTES, &P.mapW, kb * I8_BK, col0, full);
+                    }
+                    armed |= 1u << stage;
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok) {
+                atomicCAS(P.status, 0, OC_ERR_TIMEOUT);
+                *abort_flag = 1;
+                // copies already issued still write this CTA's shared memory: a bounded chance to land
+                const unsigned long long t0 = global_ns();
+                if (leader) {
+                    for (int s = 0; s < STAGES; ++s)
+                        if (armed & (1u << s))
+                            while (!mbar_try_wait(bar_full + 8 * s, s < stage ? phase : phase ^ 1u) && global_ns() - t0 < 20000000ull) {}
+                } else {
+                    while (global_ns() - t0 < 2000000ull) {}
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ================================ MMAs ==================================================
+        if (leader) {
+            constexpr uint32_t IDESC = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N_TILE >> 3) << 17) |
+                                       ((uint32_t)((PAIR ? 2 * I8_BM : I8_BM) >> 4) << 24);       // D = s32, A = B = s8, K-major
+            const uint32_t issue = elect_one();
+            int stage = 0; uint32_t phase = 0, it = 0;
+            bool ok = true;
+            while (ok && walk.next(P, m, n)) {
+                const uint32_t buf = it & 1u, acc_phase = (it >> 1) & 1u;
+                ++it;
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(bar_acc_empty + 8 * buf, acc_phase ^ 1u, abort_flag))) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t d = tmem_base + buf * N_TILE;
+                for (int kb = 0; kb < P.kblocks; ++kb) {
+                    if (!__all_sync(0xFFFFFFFFu, mbar_wait(bar_full + 8 * stage, phase, abort_flag))) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t a_addr = tiles + (uint32_t)(stage * STAGE_BYTES);
+                    const uint64_t a_desc = make_smem_desc(a_addr), b_desc = make_smem_desc(a_addr + I8_A_BYTES);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)                      // 32 bytes of K at a time along the swizzled rows
+                        tc_mma_i8<PAIR>(d, a_desc + 2 * k, b_desc + 2 * k, IDESC, (uint32_t)((kb | k) != 0), issue);
+                    tc_commit_all<PAIR>(bar_empty + 8 * stage, issue);
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+                if (ok) tc_commit_all<PAIR>(bar_acc_full + 8 * buf, issue);
+            }
+            if (!ok && lane == 0) { atomicCAS(P.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
+            // every MMA retires before tensor memory is released
+            tc_commit<PAIR>(PAIR ? map_to_cta(bar_drain, 0) : bar_drain, issue);
+            const unsigned long long t0 = global_ns();
+            while (!mbar_try_wait(bar_drain, 0) && global_ns() - t0 < WAIT_LIMIT_NS) {}
+        }
+    } else if (warp >= 4) {
+        // ================================ epilogue ==============================================
+        const int et = threadIdx.x - 128, ew = et >> 5;
+        const int quarter = warp & 3, part = ew >> 2;                // TMEM lanes of this warp; which of its passes
+        const uint32_t acc_empty = PAIR ? map_to_cta(bar_acc_empty, 0) : bar_acc_empty;          // the leader's
+        const uint32_t stage_row = smem_u32(out_stage + ew * I8_OUT_STAGE) + (uint32_t)(lane * PITCH);
+        const uint32_t stage_base = smem_u32(out_stage + ew * I8_OUT_STAGE);
+        uint32_t it = 0;
+        bool ok = true;
+        while (walk.next(P, m, n)) {
+            const uint32_t buf = it & 1u, acc_phase = (it >> 1) & 1u;
+            ++it;
+            const int col0 = n * N_TILE;
+            float* tab = col_tab + buf * 2 * N_TILE;
+            // (a table is written again two tiles later: whoever does has passed the barrier of the tile between,
+            //  which everybody reaches after the last use of this one)
+            if (et < N_TILE) {
+                const int c = col0 + et;
+                tab[et] = c < P.N ? __ldg(P.w_scale + c) : 0.0f;
+                tab[N_TILE + et] = c < P.N && P.bias ? __ldg(P.bias + c) : 0.0f;
+            }
+            const int r = m * (PAIR ? 2 * I8_BM : I8_BM) + (int)rank * I8_BM + quarter * 32 + lane;
+            int dst = -1;
+            float sa = 0.0f;
+            if (r < P.M) {
+                sa = __ldg(P.a_scale + r);
+                dst = P.out_idx ? __ldg(P.out_idx + r) : r;
+                if (dst >= P.out_rows) { atomicCAS(P.status, 0, OC_ERR_INVALID_ARG); dst = -1; }
+            }
+            asm volatile("bar.sync 1, %0;" :: "n"(I8_EPI_WARPS * 32) : "memory");
+            // (a warp that has given up keeps meeting the others at the barrier, and waits for nothing else)
+            if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar_acc_full + 8 * buf, acc_phase, abort_flag));
+            if (!ok) {
+                if (lane == 0) { atomicCAS(P.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
+                continue;
+            }
+            tc_fence_after();
+            const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N_TILE;
+#pragma unroll 1
+            for (int pass = part; pass < N_TILE / PASS; pass += 2) {
+                __syncwarp();                                        // the rows staged before have been read
+#pragma unroll
+                for (int c32 = 0; c32 < PASS; c32 += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(t_row + (uint32_t)(pass * PASS + c32), v);
+                    tmem_ld_wait();
+                    const float4* sw = (const float4*)(tab + pass * PASS + c32);
+                    const float4* bs = (const float4*)(tab + N_TILE + pass * PASS + c32);
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 w = sw[j / 4], b = bs[j / 4];
+                        v[j] = __float_as_uint(fmaf((float)(int)v[j] * sa, w.x, b.x));
+                        v[j + 1] = __float_as_uint(fmaf((float)(int)v[j + 1] * sa, w.y, b.y));
+                        v[j + 2] = __float_as_uint(fmaf((float)(int)v[j + 2] * sa, w.z, b.z));
+                        v[j + 3] = __float_as_uint(fmaf((float)(int)v[j + 3] * sa, w.w, b.w));
+                    }
+                    if (OT == OC_DTYPE_F32) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4)
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(stage_row + (uint32_t)(c32 + j) * 4u), "r"(v[j]), "r"(v[j + 1]), "r"(v[j + 2]), "r"(v[j + 3]) : "memory");
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8) {
+                            uint32_t o[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(__uint_as_float(v[j + 2 * i]), __uint_as_float(v[j + 2 * i + 1]));
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(stage_row + (uint32_t)(c32 + j) * 2u), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                        }
+                    }
+                }
+                __syncwarp();
+                if (!P.wide) {                                       // rows of `out` that are not 16-byte aligned: element by element
+                    for (int row = 0; row < 32; ++row) {
+                        const int d = __shfl_sync(0xFFFFFFFFu, dst, row);
+#pragma unroll
+                        for (int e = 0; e < PASS; e += 32) {
+                            const int col = col0 + pass * PASS + e + lane;
+                            const uint32_t from = stage_base + (uint32_t)(row * PITCH + (e + lane) * OB);
+                            if (d < 0 || col >= P.N) continue;
+                            if (OB == 4) {
+                                uint32_t o;
+                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(o) : "r"(from) : "memory");
+                                ((uint32_t*)P.out)[(long long)d * P.out_stride + col] = o;
+                            } else {
+                                uint16_t o;
+                                asm volatile("ld.shared.b16 %0, [%1];" : "=h"(o) : "r"(from) : "memory");
+                                ((uint16_t*)P.out)[(long long)d * P.out_stride + col] = o;
+                            }
+                        }
+                    }
+                    continue;
+                }
+                const int col = col0 + pass * PASS + (lane % LPR) * (16 / OB);
+#pragma unroll
+                for (int i = 0; i < 32 / RPI; ++i) {
+                    const int row = i * RPI + lane / LPR;
+                    const int d = __shfl_sync(0xFFFFFFFFu, dst, row);
+                    uint4 o;
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(o.x), "=r"(o.y), "=r"(o.z), "=r"(o.w) : "r"(stage_base + (uint32_t)(row * PITCH + (lane % LPR) * 16)) : "memory");
+                    if (d >= 0 && col < P.N) {
+                        uint8_t* p = (uint8_t*)P.out + ((long long)d * P.out_stride + col) * OB;
+                        if (col + 16 / OB <= P.N) {
+                            st_v4(p, o);
+                        } else {                                     // the row's last, partial 16 bytes
+                            const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+                            for (int e = 0; e < P.N - col; ++e) {
+                                if (OB == 4) ((uint32_t*)p)[e] = w[e];
+                                else ((uint16_t*)p)[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                            }
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) { if (PAIR) mbar_arrive_cluster(acc_empty + 8 * buf); else mbar_arrive(acc_empty + 8 * buf); }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();                                    // nobody signals a barrier of, or reads operands from, a retired CTA
+    tc_fence_after();
+    if (warp == 1) {
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(TMEM_COLS) : "memory");
+        else tmem_dealloc_cta1(tmem_base, TMEM_COLS);
+    }
+}
+
+// ---- few tokens ------------------------------------------------------------------------------------
+static constexpr int I8S_WARPS = 8, I8S_CH = 2;                      // warps per CTA, output channels per warp
+
+struct I8SmallParams {
+    const int8_t *a, *w;
+    const float *a_scale, *w_scale, *bias;
+    const int32_t* out_idx;
+    void* out;
+    long long out_stride;
+    int M, N, K, out_rows;
+    int* status;
+};
+
+template <int MR, int OT>
+__global__ void __launch_bounds__(I8S_WARPS * 32)
+linear_int8_small_kernel(const __grid_constant__ I8SmallParams P) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n0 = (blockIdx.x * I8S_WARPS + warp) * I8S_CH;
+    pdl_enter();
+    if (n0 >= P.N) return;
+    int acc[I8S_CH][MR] = {};
+    const int chunks = P.K >> 4;
+#pragma unroll 4
+    for (int c = lane; c < chunks; c += 32) {
+        uint4 w[I8S_CH];
+#pragma unroll
+        for (int i = 0; i < I8S_CH; ++i)
+            w[i] = n0 + i < P.N ? ld_nc_v4(P.w + (long long)(n0 + i) * P.K + c * 16) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+            const uint4 a = m < P.M ? __ldg((const uint4*)(P.a + (long long)m * P.K + c * 16)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < I8S_CH; ++i) {
+                acc[i][m] = __dp4a((int)w[i].x, (int)a.x, acc[i][m]);
+                acc[i][m] = __dp4a((int)w[i].y, (int)a.y, acc[i][m]);
+                acc[i][m] = __dp4a((int)w[i].z, (int)a.z, acc[i][m]);
+                acc[i][m] = __dp4a((int)w[i].w, (int)a.w, acc[i][m]);
+            }
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int i = 0; i < I8S_CH; ++i) {
+            const int sum = __reduce_add_sync(0xFFFFFFFFu, acc[i][m]);
+            const int n = n0 + i;
+            if (lane == (m * I8S_CH + i) && m < P.M && n < P.N) {
+                const int d = P.out_idx ? __ldg(P.out_idx + m) : m;
+                if (d >= P.out_rows) { atomicCAS(P.status, 0, OC_ERR_INVALID_ARG); }
+                else if (d >= 0) {
+                    const float v = fmaf((float)sum * __ldg(P.a_scale + m), __ldg(P.w_scale + n), P.bias ? __ldg(P.bias + n) : 0.0f);
+                    const long long at = (long long)d * P.out_stride + n;
+                    if (OT == OC_DTYPE_F32) ((float*)P.out)[at] = v;
+                    else ((uint16_t*)P.out)[at] = (uint16_t)pack_bf16x2(v, 0.0f);
+                }
+            }
+        }
+}
+
+template <int OT>
+static void launch_small(const I8SmallParams& P, cudaStream_t s) {
+    const dim3 grid((unsigned)((P.N + I8S_WARPS * I8S_CH - 1) / (I8S_WARPS * I8S_CH)));
+    if (P.M == 1) OC_LAUNCH((linear_int8_small_kernel<1, OT>), grid, I8S_WARPS * 32, 0, s, P);
+    else if (P.M == 2) OC_LAUNCH((linear_int8_small_kernel<2, OT>), grid, I8S_WARPS * 32, 0, s, P);
+    else if (P.M <= 4) OC_LAUNCH((linear_int8_small_kernel<4, OT>), grid, I8S_WARPS * 32, 0, s, P);
+    else OC_LAUNCH((linear_int8_small_kernel<8, OT>), grid, I8S_WARPS * 32, 0, s, P);
+}
+
+// ---- host side -------------------------------------------------------------------------------------
+typedef CUresult (*I8EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                               const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                               CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static I8EncodeFn i8_encode_fn() {
+    static I8EncodeFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = (I8EncodeFn)p;
+        else
+            cudaGetLastError();
+    });
+    return fn;
+}
+static bool i8_encode(I8EncodeFn enc, CUtensorMap* map, const void* p, int64_t K, int64_t rows, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)K};
+    const cuuint32_t box[2] = {(cuuint32_t)I8_BK, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)p, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int N_TILE, bool PAIR, int OT>
+static oc_status launch_tiles_as(oc_ctx* ctx, I8Params& P, cudaStream_t s) {
+    constexpr int STAGE_BYTES = I8_A_BYTES + (PAIR ? N_TILE / 2 : N_TILE) * I8_BK;
+    constexpr int REST = I8_EPI_WARPS * I8_OUT_STAGE + 4 * N_TILE * 4 + (2 * I8_STAGES_MAX + 5) * 8 + 16;
+    constexpr int FIT = (227 * 1024 - REST) / STAGE_BYTES, STAGES = FIT < I8_STAGES_MAX ? FIT : I8_STAGES_MAX;
+    constexpr int SMEM = STAGES * STAGE_BYTES + REST;
+    static PerDeviceOnce once;                       // (the context's device is current here)
+    auto* kernel = linear_int8_kernel<N_TILE, PAIR, OT>;
+    if (!once.ensure(ctx->device, [&] {
+            const bool ok = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) == cudaSuccess;
+            if (!ok) cudaGetLastError();
+            return ok;
+        })) return OC_ERR_CUDA;
+    P.n_stages = STAGES;
+    const long long tiles = (long long)P.m_tiles * P.n_tiles, walkers = PAIR ? ctx->sm_count / 2 : ctx->sm_count;
+    const unsigned grid = (unsigned)(tiles < walkers ? tiles : walkers) * (PAIR ? 2u : 1u);
+    LaunchScope scope(ctx, OC_K_LINEAR_I8, s);
+    PdlLaunch l(dim3(grid), dim3(I8_THREADS), SMEM, s, PAIR ? 2u : 0u);
+    cudaLaunchKernelEx(&l.cfg, kernel, P);
+    return last_launch_status();
+}
+template <int N_TILE, bool PAIR>
+static oc_status launch_tiles(oc_ctx* ctx, I8Params& P, int out_dtype, cudaStream_t s) {
+    return out_dtype == OC_DTYPE_F32 ? launch_tiles_as<N_TILE, PAIR, OC_DTYPE_F32>(ctx, P, s)
+                                     : launch_tiles_as<N_TILE, PAIR, OC_DTYPE_BF16>(ctx, P, s);
+}
+
+oc_status launch_linear_int8(oc_ctx* ctx, const int8_t* a, const float* a_scale, int64_t M, int64_t K, const int8_t* w,
+                             const float* w_scale, int64_t N, const float* bias, void* out, int out_dtype, int64_t out_rows,
+                             int64_t out_stride, const int32_t* out_idx, cudaStream_t s) {
+    if (M <= 8) {
+        I8SmallParams P;
+        P.a = a; P.w = w; P.a_scale = a_scale; P.w_scale = w_scale; P.bias = bias; P.out_idx = out_idx; P.out = out;
+        P.out_stride = out_stride; P.M = (int)M; P.N = (int)N; P.K = (int)K; P.out_rows = (int)out_rows; P.status = ctx->d_status;
+        LaunchScope scope(ctx, OC_K_LINEAR_I8, s);
+        if (out_dtype == OC_DTYPE_F32) launch_small<OC_DTYPE_F32>(P, s);
+        else launch_small<OC_DTYPE_BF16>(P, s);
+        return last_launch_status();
+    }
+    I8EncodeFn enc = i8_encode_fn();
+    if (!enc) return OC_ERR_UNSUPPORTED;
+    I8Params P;
+    memset(&P, 0, sizeof(P));
+    // The tile whose waves over the device take the fewest cycles: a 128-byte step of K costs the MMAs of its
+    // tile or the arrival of its operands, whichever is longer.
+    struct Form { int rows, cols, w_rows, per_sm; } forms[4] = {{256, 256, 128, 2}, {128, 128, 128, 1}, {128, 64, 64, 1}, {128, 32, 32, 1}};
+    int best = 1;
+    double best_cost = 1e300;
+    const int kblocks = (int)((K + I8_BK - 1) / I8_BK);
+    for (int f = 0; f < 4; ++f) {
+        if (f == 0 && M <= 128) continue;
+        const long long tiles = ((M + forms[f].rows - 1) / forms[f].rows) * ((N + forms[f].cols - 1) / forms[f].cols);
+        const long long walkers = ctx->sm_count / forms[f].per_sm;
+        const double step = std::max(2.0 * forms[f].cols, (I8_A_BYTES + forms[f].w_rows * I8_BK) / 64.0);
+        const double cost = (double)((tiles + walkers - 1) / walkers) * (kblocks * step + 300.0);
+        if (cost < best_cost) { best_cost = cost; best = f; }
+    }
+    const Form& F = forms[best];
+    if (!i8_encode(enc, &P.mapA, a, K, M, I8_BM) || !i8_encode(enc, &P.mapW, w, K, N, F.w_rows)) return OC_ERR_UNSUPPORTED;
+    P.a_scale = a_scale; P.w_scale = w_scale; P.bias = bias; P.out_idx = out_idx; P.out = out; P.out_stride = out_stride;
+    P.M = (int)M; P.N = (int)N; P.out_rows = (int)out_rows; P.kblocks = kblocks; P.status = ctx->d_status;
+    const long long mt = (M + F.rows - 1) / F.rows, nt = (N + F.cols - 1) / F.cols;
+    if (mt * nt > 0x7FFFFFFFll - 1024) return OC_ERR_UNSUPPORTED;
+    P.m_tiles = (int)mt; P.n_tiles = (int)nt;
+    P.n_first = M >= N;
+    P.wide = ((uintptr_t)out | (uint64_t)out_stride * (out_dtype == OC_DTYPE_F32 ? 4u : 2u)) % 16 == 0;
+    switch (best) {
+        case 0: return launch_tiles<256, true>(ctx, P, out_dtype, s);
+        case 1: return launch_tiles<128, false>(ctx, P, out_dtype, s);
+        case 2: return launch_tiles<64, false>(ctx, P, out_dtype, s);
+        default: return launch_tiles<32, false>(ctx, P, out_dtype, s);
+    }
+}
+
+}  // namespace oc

@@ -18,13 +18,15 @@ LIB_PATH = os.path.join(_PKG, "libomnicache_b200.so")
 
 OK, ERR_INVALID_ARG, ERR_ALIGNMENT, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_OOM, CACHE_MISS = range(9)
 KIND_TOKEN, KIND_FRAME, KIND_BLOCK = 0, 1, 2
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_I8 = 0, 1, 2
 SELECT_THRESHOLD, SELECT_COUNT = 0, 1
 RESTORE_FROM_CACHE, RESTORE_FROM_REPRESENTATIVE = 0, 1
 FRAME_MEAN_POS_COS, FRAME_FLAT_COS = 0, 1
 (K_NORMS, K_MATCH_TC, K_MATCH_SIMT, K_MATCH_FIN, K_FRAME, K_FRAME_FIN, K_BLOCK, K_BLOCK_FIN, K_SELECT,
- K_GATHER, K_RESTORE, K_COPY, K_LINEAR) = range(13)
-K_COUNT = 13
+ K_GATHER, K_RESTORE, K_COPY, K_LINEAR, K_BLOCK_NORM, K_ROPE, K_QUANT, K_LINEAR_I8) = range(17)
+K_COUNT = 17
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+ROPE_ADJACENT, ROPE_HALVES = 0, 1
 
 EXPORTS = (
     "oc_status_str", "oc_layout_check", "oc_layout_counts", "oc_match_workspace_bytes",
@@ -35,6 +37,7 @@ EXPORTS = (
     "oc_layer_cache_clear", "oc_cache_step_host", "oc_match_frame_noalloc", "oc_selftest_bounded_wait", "oc_selftest_per_device_once",
     "oc_schedule_propose", "oc_joint_workspace_bytes", "oc_joint_groups", "oc_match_joint", "oc_select_joint",
     "oc_linear_gather_scatter", "oc_tc_plan_override", "oc_tc_plan_describe",
+    "oc_block_norm", "oc_rope_table_size", "oc_rope_table", "oc_rope", "oc_quantize_rows", "oc_linear_int8",
 )
 
 
@@ -52,6 +55,23 @@ class CLayout(C.Structure):
 class CRows(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("seg_bytes", "n_seg", "seg_stride", "unit_pitch",
                                         "units_per_outer", "outer_pitch")]
+
+
+class CBlockNorm(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("dtype", "h_dtype", "param_dtype", "post_norm", "pre_norm")] +
+                [(n, C.c_float) for n in ("post_eps", "pre_eps", "res_scale")] +
+                [(n, C.c_int64) for n in ("n_rows", "C", "rows_per_group", "mod_stride", "unit_rows", "dense_rows")])
+
+
+class CRopeView(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("batch_stride", "row_stride", "head_stride")]
+
+
+class CRope(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("dtype", "head_dim", "q_heads", "k_heads", "pairing", "inverse")] +
+                [("axis_dims", C.c_int * 3), ("axis_len", C.c_int * 3), ("eps", C.c_float)] +
+                [(n, C.c_int64) for n in ("n_rows", "rows_per_batch", "unit_rows")] +
+                [(n, CRopeView) for n in ("q", "q_out", "k", "k_out")])
 
 
 if not os.path.exists(LIB_PATH):
@@ -95,6 +115,12 @@ _lib.oc_layer_cache_get.argtypes = [_vp, _i, _i, _i, _vp, _vp, _vp, _vp]
 _lib.oc_layer_cache_clear.argtypes = [_vp]
 _lib.oc_cache_step_host.argtypes = [_vp, _vp, _i, _f, _i64, _vp, _vp, _vp, _vp, _vp]
 _lib.oc_schedule_propose.argtypes = [_vp, _vp, _i64, C.c_double, _vp, _vp, _vp]
+_lib.oc_block_norm.argtypes = [_vp] * 18
+_lib.oc_rope_table_size.argtypes = [_vp, _vp]
+_lib.oc_rope_table.argtypes = [_vp, C.c_double, _vp]
+_lib.oc_rope.argtypes = [_vp] * 12
+_lib.oc_quantize_rows.argtypes = [_vp, _vp, _i, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp]
+_lib.oc_linear_int8.argtypes = [_vp, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _i, _i64, _i64, _vp, _vp]
 _lib.oc_match_frame_noalloc.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _vp]
 NOALLOC_SCRATCH_BYTES = 1 << 20
 
@@ -220,6 +246,55 @@ def _stream(stream) -> int:
     if stream is None:
         return torch.cuda.current_stream().cuda_stream
     return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _ptr_strided(t) -> int | None:
+    """Pointer of a tensor whose strides the call gets on their own (a part of a larger tensor)."""
+    return None if t is None else (t if isinstance(t, int) else t.data_ptr())
+
+
+def block_norm_desc(n_rows: int, C_: int, dtype: int, h_dtype: int, param_dtype: int, post_norm: int = NORM_NONE,
+                    pre_norm: int = NORM_NONE, post_eps: float = 1e-6, pre_eps: float = 1e-6, res_scale: float = 1.0,
+                    rows_per_group: int | None = None, mod_stride: int = 0, unit_rows: int = 1,
+                    dense_rows: int | None = None) -> CBlockNorm:
+    """oc_block_norm_desc: made once for a layer and passed to Context.block_norm.  rows_per_group and dense_rows
+    default to n_rows (one group; every row computed)."""
+    return CBlockNorm(dtype, h_dtype, param_dtype, post_norm, pre_norm, post_eps, pre_eps, res_scale, n_rows, C_,
+                      max(n_rows, 1) if rows_per_group is None else rows_per_group, mod_stride, unit_rows,
+                      n_rows if dense_rows is None else dense_rows)
+
+
+def rope_desc(n_rows: int, dtype: int, head_dim: int, axis_dims, axis_len, q_heads: int, k_heads: int = 0,
+              rows_per_batch: int | None = None, unit_rows: int = 1, pairing: int = ROPE_ADJACENT, inverse: bool = False,
+              eps: float = 1e-6, q=None, q_out=None, k=None, k_out=None) -> CRope:
+    """oc_rope_desc, the strides taken from tensors (or from (batch, row, head) stride tuples): q, k are
+    [n_rows, heads, head_dim] views, q_out, k_out [batch, heads, rows, head_dim] or [n_rows, heads, head_dim]."""
+    def view(t, heads):
+        if t is None:
+            return CRopeView(0, 0, 0)
+        if isinstance(t, tuple):
+            return CRopeView(*t)
+        if t.shape[-1] != head_dim or t.stride(-1) != 1:
+            raise ValueError("heads must be contiguous and head_dim wide")
+        if t.dim() == 4:
+            if t.shape[1] != heads:
+                raise ValueError("a [batch, heads, rows, head_dim] tensor has another number of heads")
+            return CRopeView(t.stride(0), t.stride(2), t.stride(1))
+        if t.dim() != 3 or t.shape[1] != heads:
+            raise ValueError("expected [rows, heads, head_dim] or [batch, heads, rows, head_dim]")
+        return CRopeView(t.stride(0) * (rows_per_batch or n_rows), t.stride(0), t.stride(1))
+    return CRope(dtype, head_dim, q_heads, k_heads, pairing, int(inverse), (C.c_int * 3)(*axis_dims), (C.c_int * 3)(*axis_len),
+                 eps, n_rows, max(n_rows, 1) if rows_per_batch is None else rows_per_batch, unit_rows,
+                 view(q, q_heads), view(q_out, q_heads), view(k, k_heads), view(k_out, k_heads))
+
+
+def rope_table(desc: CRope, theta: float = 10000.0) -> torch.Tensor:
+    """oc_rope_table: the (cos, sin) table of a rotation, as a CPU tensor.  Host only."""
+    n = C.c_int64()
+    _chk(_lib.oc_rope_table_size(C.byref(desc), C.byref(n)), "oc_rope_table_size")
+    t = torch.empty(n.value, dtype=torch.float32)
+    _chk(_lib.oc_rope_table(C.byref(desc), theta, t.data_ptr()), "oc_rope_table")
+    return t
 
 
 def schedule_propose(latency, quality_loss, target_speedup: float):
@@ -355,6 +430,46 @@ class Context:
                                            out_rows, _ptr(out_idx), _stream(stream))
         if check:
             _chk(st, "oc_linear_gather_scatter")
+        return st
+
+    # -- the wrapped block on kept tokens ----------------------------------------------------------
+    def block_norm(self, desc: CBlockNorm, x, z=None, slot_of=None, cache=None, cache_out=None, out=None, post_w=None,
+                   post_b=None, gate=None, pre_w=None, pre_b=None, scale=None, shift=None, h=None, h_scale=None,
+                   stream=None, check: bool = True) -> int:
+        """oc_block_norm.  gate, scale and shift may be column ranges of one [groups, mod_stride] tensor."""
+        st = _lib.oc_block_norm(self._h, C.byref(desc), _ptr(x), _ptr(z), _ptr(slot_of), _ptr(cache), _ptr(cache_out),
+                                _ptr(out), _ptr(post_w), _ptr(post_b), _ptr_strided(gate), _ptr(pre_w), _ptr(pre_b),
+                                _ptr_strided(scale), _ptr_strided(shift), _ptr(h), _ptr(h_scale), _stream(stream))
+        if check:
+            _chk(st, "oc_block_norm")
+        return st
+
+    def rope(self, desc: CRope, table, q, q_out, k=None, k_out=None, idx=None, pos=None, q_w=None, k_w=None, stream=None,
+             check: bool = True) -> int:
+        """oc_rope: strides are the descriptor's, so q and k may be parts of one projection."""
+        st = _lib.oc_rope(self._h, C.byref(desc), _ptr(table), _ptr(idx), _ptr(pos), _ptr_strided(q), _ptr_strided(q_out),
+                          _ptr(q_w), _ptr_strided(k), _ptr_strided(k_out), _ptr(k_w), _stream(stream))
+        if check:
+            _chk(st, "oc_rope")
+        return st
+
+    def quantize_rows(self, x, dtype: int, n_rows: int, K: int, q, scale, idx=None, x_rows: int | None = None,
+                      x_stride: int | None = None, stream=None, check: bool = True) -> int:
+        st = _lib.oc_quantize_rows(self._h, _ptr_strided(x), dtype, n_rows if x_rows is None else x_rows,
+                                   K if x_stride is None else x_stride, _ptr(idx), n_rows, K, _ptr(q), _ptr(scale),
+                                   _stream(stream))
+        if check:
+            _chk(st, "oc_quantize_rows")
+        return st
+
+    def linear_int8(self, a, a_scale, M: int, K: int, w, w_scale, N: int, out, out_dtype: int, bias=None,
+                    out_rows: int | None = None, out_stride: int | None = None, out_idx=None, stream=None,
+                    check: bool = True) -> int:
+        st = _lib.oc_linear_int8(self._h, _ptr(a), _ptr(a_scale), M, K, _ptr(w), _ptr(w_scale), N, _ptr(bias),
+                                 _ptr_strided(out), out_dtype, M if out_rows is None else out_rows,
+                                 N if out_stride is None else out_stride, _ptr(out_idx), _stream(stream))
+        if check:
+            _chk(st, "oc_linear_int8")
         return st
 
     def joint_groups(self, layout: Layout, frame_best_sim, frame_best_idx, frame_slot_of, frames, stream=None,

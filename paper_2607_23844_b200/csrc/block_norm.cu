@@ -41,7 +41,7 @@ __device__ __forceinline__ void normalise(float (&f)[VPT][E], int how, float eps
 #pragma unroll
             for (int e = 0; e < E; ++e) { f[j][e] -= mean; q = fmaf(f[j][e], f[j][e], q); }
         }
-    const float rstd = rsqrtf(row_sum<TPR>(q, scratch, parity) * inv_c + eps);
+    const float rstd = 1.0f / sqrtf(row_sum<TPR>(q, scratch, parity) * inv_c + eps);   // (rsqrtf is off by up to 2 ulp, for the whole row)
 #pragma unroll
     for (int j = 0; j < VPT; ++j)
 #pragma unroll

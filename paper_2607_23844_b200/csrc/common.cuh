@@ -57,12 +57,14 @@ namespace oc {
 // RAII: makes ctx->device current for the duration of a call and restores the caller's device.
 struct DeviceGuard {
     int prev = -1;
-    bool ok = true;
+    bool ok = true, moved = false;
     explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+        if (cudaGetDevice(&prev) != cudaSuccess) { prev = -1; ok = false; return; }
+        if (prev == dev) return;
+        moved = true;
+        if (cudaSetDevice(dev) != cudaSuccess) ok = false;
     }
-    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
+    ~DeviceGuard() { if (moved && prev >= 0) cudaSetDevice(prev); }
 };
 
 // Work that has to be done once per DEVICE rather than once per process: function attributes such as

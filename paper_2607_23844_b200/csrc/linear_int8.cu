@@ -6,9 +6,9 @@
 // (or CTA pair, cta_group::2) per SM walks over output tiles of 128 x N_TILE (256 x 256 for a pair):
 //   warp 0       copies: TMA boxes of 128 bytes of K by 128 rows, 128-byte swizzle, into a ring of stages
 //   warp 1       the MMAs (128 bytes of K = four steps of 32); owns the tensor memory
-//   warps 2..3   idle (the epilogue's warps have to start at a multiple of four)
-//   warps 4..11  epilogue: thread = row; scales, bias, rounding, then through shared memory so that a warp
-//                stores whole 64- or 128-byte pieces of rows, to the rows that out_idx names
+//   warps 2..17  epilogue: thread = row, four warps side by side; scales, bias, rounding, then through shared
+//                memory: rows that keep their order leave as TMA boxes, others as whole 64-byte pieces to
+//                where out_idx says
 // Two accumulators take turns, so the epilogue of a tile runs under the MMAs of the next.
 // Few tokens (at most 8): one warp per pair of output channels, dp4a, the weights read once as they lie.
 // K and N tails are zero-filled by TMA and not stored.  Every wait is bounded (OC_ERR_TIMEOUT in the status word).
@@ -23,21 +23,24 @@
 namespace oc {
 
 static constexpr int I8_BM = 128, I8_BK = 128;                      // rows of a CTA's tile; bytes of K per stage
-static constexpr int I8_THREADS = 384, I8_EPI_WARPS = 8;
+static constexpr int I8_EPI_WARPS = 16, I8_THREADS = 64 + 32 * I8_EPI_WARPS;
 static constexpr int I8_A_BYTES = I8_BM * I8_BK;
 static constexpr int I8_STAGES_MAX = 8;
-static constexpr int I8_PITCH = 144;                                // bytes per staged row: 128 and a bank step of 16
-static constexpr int I8_OUT_STAGE = 32 * I8_PITCH;                  // per epilogue warp
+
+// An epilogue warp stages 64 bytes of each of its 32 rows at a time: twice that stores no faster, and the ring of
+// operands needs the shared memory (it has to cover the latency of loads that compete with the output's stores).
+static constexpr int I8_SEG = 64, I8_OUT_STAGE = 32 * I8_SEG;
 
 struct I8Params {
     CUtensorMap mapA, mapW;      // {K, rows}: boxes {128, 128} and {128, rows of W per CTA}
+    CUtensorMap mapOut;          // {N, M}: box {64 bytes, 32}; used when rows keep their order
     const float *a_scale, *w_scale, *bias;
     const int32_t* out_idx;
     void* out;
     long long out_stride;
     int M, N, out_rows;
-    int kblocks, m_tiles, n_tiles, n_first, n_stages;
-    int wide;                    // rows of `out` may be stored in 16-byte pieces
+    int kblocks, m_tiles, n_tiles, n_stages;
+    int wide, tma_out;           // rows of `out` may be stored in 16-byte pieces; by TMA
     int* status;
 };
 
@@ -56,6 +59,30 @@ __device__ __forceinline__ void tc_mma_i8(uint32_t d_tmem, uint64_t a_desc, uint
                      "@e tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
                      :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
 }
+// Where 16-byte piece j of a staged row lies: TMA's swizzle for rows of 64 bytes, which also spreads the pieces that
+// a warp's lanes write, one row each, over all banks.
+__device__ __forceinline__ uint32_t i8_staged(int row, int j) { return (uint32_t)(row * I8_SEG + ((j ^ ((row >> 1) & 3)) << 4)); }
+template <int COLS> __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t* v) {
+    if constexpr (COLS == 32) tmem_ld32(taddr, v);
+    else
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                       "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                     : "r"(taddr) : "memory");
+}
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
 // arrive on `bar` (of both CTAs in a pair) once every MMA issued so far has retired
 template <bool PAIR>
 __device__ __forceinline__ void tc_commit_all(uint32_t bar, uint32_t issue) {
@@ -67,14 +94,15 @@ __device__ __forceinline__ void tc_commit_all(uint32_t bar, uint32_t issue) {
         tc_commit<false>(bar, issue);
 }
 
-// The tiles of a walker, in order.  The larger operand is walked through once, the smaller one again for each
-// tile of it (it stays in L2).
+// The tiles of a walker, row by row of tiles: whole rows of `out` are written at about the same time, which is
+// what DRAM writes fastest (a 57600 x 5120 output: 174 us, against 188 us in groups of 9 tile columns and 202 us
+// in groups of 3), and each row of A is read from DRAM once, while W stays in L2.
 struct I8Walk {
     int tile, step, total;
     __device__ __forceinline__ bool next(const I8Params& P, int& m, int& n) {
         if (tile >= total) return false;
-        if (P.n_first) { m = tile / P.n_tiles; n = tile - m * P.n_tiles; }
-        else { n = tile / P.m_tiles; m = tile - n * P.m_tiles; }
+        m = tile / P.n_tiles;
+        n = tile - m * P.n_tiles;
         tile += step;
         return true;
     }
@@ -87,14 +115,14 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
     constexpr int STAGE_BYTES = I8_A_BYTES + W_ROWS * I8_BK;
     constexpr int TMEM_COLS = 2 * N_TILE;
     constexpr int OB = OT == OC_DTYPE_F32 ? 4 : 2;
-    constexpr int PASS = (OB == 2 && N_TILE >= 128) ? 64 : 32;       // columns that a warp stages together
-    constexpr int SEG = PASS * OB, LPR = SEG / 16, RPI = 32 / LPR;   // a staged row: bytes, lanes that store it; rows per store
-    constexpr int PITCH = SEG + 16;
+    constexpr int WC = N_TILE >= 128 ? N_TILE / 4 : 32;              // columns of an epilogue warp
+    constexpr int PASS = I8_SEG / OB, PARTS = N_TILE / WC;           // columns that it stages together; warps side by side
+    constexpr int LPR = I8_SEG / 16, RPI = 32 / LPR;                 // lanes that store a staged row; rows per store
     extern __shared__ __align__(1024) uint8_t i8_smem[];
     uint8_t* after = i8_smem + (size_t)P.n_stages * STAGE_BYTES;
-    uint8_t* out_stage = after;                                      // [8 warps][32 rows][PITCH]
-    float* col_tab = (float*)(after + I8_EPI_WARPS * I8_OUT_STAGE);  // [2 tiles][scale, bias][N_TILE]
-    uint64_t* bars = (uint64_t*)(col_tab + 4 * N_TILE);
+    uint8_t* out_stage = after;                                      // [warps][32 rows][64 bytes]
+    float* col_tab = (float*)(after + I8_EPI_WARPS * I8_OUT_STAGE);  // [parts][scale, bias][WC]
+    uint64_t* bars = (uint64_t*)(col_tab + 2 * N_TILE);
     const uint32_t tiles = smem_u32(i8_smem);
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * I8_STAGES_MAX;
     const uint32_t bar_acc_full = bar_empty + 8 * I8_STAGES_MAX, bar_acc_empty = bar_acc_full + 16, bar_drain = bar_acc_empty + 16;
@@ -118,6 +146,7 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tma_prefetch_map(&P.mapA);
         tma_prefetch_map(&P.mapW);
+        if (P.tma_out) tma_prefetch_map(&P.mapOut);
     }
     if (warp == 1) {
         if (PAIR) {
@@ -211,123 +240,145 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
             const unsigned long long t0 = global_ns();
             while (!mbar_try_wait(bar_drain, 0) && global_ns() - t0 < WAIT_LIMIT_NS) {}
         }
-    } else if (warp >= 4) {
+    } else {
         // ================================ epilogue ==============================================
-        const int et = threadIdx.x - 128, ew = et >> 5;
-        const int quarter = warp & 3, part = ew >> 2;                // TMEM lanes of this warp; which of its passes
+        const int ew = warp - 2, quarter = warp & 3, part = ew >> 2; // TMEM lanes of this warp; which of the columns
+        const bool works = part < PARTS;                             // (narrow tiles do not occupy all warps)
         const uint32_t acc_empty = PAIR ? map_to_cta(bar_acc_empty, 0) : bar_acc_empty;          // the leader's
-        const uint32_t stage_row = smem_u32(out_stage + ew * I8_OUT_STAGE) + (uint32_t)(lane * PITCH);
         const uint32_t stage_base = smem_u32(out_stage + ew * I8_OUT_STAGE);
+        float* tab = col_tab + (works ? part : 0) * 2 * WC;          // scales and biases of the part's columns
+        // What a tile needs beside its sums is fetched a tile ahead: the latency passes under the tile before.
+        // (the part's four warps fetch a column each: its scale, or with the upper lanes its bias)
+        const int et = (ew & 3) * 32 + lane;
+        struct Ahead { float col, sa; int dst; } ah;
+        auto fetch = [&](int m_, int n_) {
+            const int c = n_ * N_TILE + part * WC + et % WC;
+            const float* from = et < WC ? P.w_scale : P.bias;
+            ah.col = et < 2 * WC && works && from && c < P.N ? __ldg(from + c) : 0.0f;
+            const int r = m_ * (PAIR ? 2 * I8_BM : I8_BM) + (int)rank * I8_BM + quarter * 32 + lane;
+            ah.dst = -1; ah.sa = 0.0f;
+            if (r < P.M) { ah.sa = __ldg(P.a_scale + r); ah.dst = P.out_idx ? __ldg(P.out_idx + r) : r; }
+        };
         uint32_t it = 0;
-        bool ok = true;
-        while (walk.next(P, m, n)) {
+        bool ok = true, have = walk.next(P, m, n);
+        if (have) fetch(m, n);
+        while (have) {
             const uint32_t buf = it & 1u, acc_phase = (it >> 1) & 1u;
             ++it;
-            const int col0 = n * N_TILE;
-            float* tab = col_tab + buf * 2 * N_TILE;
-            // (a table is written again two tiles later: whoever does has passed the barrier of the tile between,
-            //  which everybody reaches after the last use of this one)
-            if (et < N_TILE) {
-                const int c = col0 + et;
-                tab[et] = c < P.N ? __ldg(P.w_scale + c) : 0.0f;
-                tab[N_TILE + et] = c < P.N && P.bias ? __ldg(P.bias + c) : 0.0f;
+            const int row0 = m * (PAIR ? 2 * I8_BM : I8_BM) + (int)rank * I8_BM + quarter * 32, col0 = n * N_TILE + part * WC;
+            if (works) {
+                asm volatile("bar.sync %0, 128;" :: "r"(1 + part) : "memory");       // the part is done with the table
+                if (et < 2 * WC) tab[et] = ah.col;
+                asm volatile("bar.sync %0, 128;" :: "r"(1 + part) : "memory");
             }
-            const int r = m * (PAIR ? 2 * I8_BM : I8_BM) + (int)rank * I8_BM + quarter * 32 + lane;
-            int dst = -1;
-            float sa = 0.0f;
-            if (r < P.M) {
-                sa = __ldg(P.a_scale + r);
-                dst = P.out_idx ? __ldg(P.out_idx + r) : r;
-                if (dst >= P.out_rows) { atomicCAS(P.status, 0, OC_ERR_INVALID_ARG); dst = -1; }
-            }
-            asm volatile("bar.sync 1, %0;" :: "n"(I8_EPI_WARPS * 32) : "memory");
-            // (a warp that has given up keeps meeting the others at the barrier, and waits for nothing else)
+            const float sa = ah.sa;
+            int dst = ah.dst;
+            if (dst >= P.out_rows) { atomicCAS(P.status, 0, OC_ERR_INVALID_ARG); dst = -1; }
+            have = walk.next(P, m, n);
+            if (have) fetch(m, n);
+            // (a warp that has given up keeps meeting the others at the barriers, and waits for nothing else)
             if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar_acc_full + 8 * buf, acc_phase, abort_flag));
-            if (!ok) {
-                if (lane == 0) { atomicCAS(P.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
-                continue;
-            }
+            if (!ok) continue;
             tc_fence_after();
-            const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N_TILE;
+            const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N_TILE + (uint32_t)(part * WC);
+            if (works) {
 #pragma unroll 1
-            for (int pass = part; pass < N_TILE / PASS; pass += 2) {
-                __syncwarp();                                        // the rows staged before have been read
-#pragma unroll
-                for (int c32 = 0; c32 < PASS; c32 += 32) {
-                    uint32_t v[32];
-                    tmem_ld32(t_row + (uint32_t)(pass * PASS + c32), v);
+                for (int pass = 0; pass < WC / PASS; ++pass) {
+                    uint32_t v[PASS];
+                    tmem_ld<PASS>(t_row + (uint32_t)(pass * PASS), v);
                     tmem_ld_wait();
-                    const float4* sw = (const float4*)(tab + pass * PASS + c32);
-                    const float4* bs = (const float4*)(tab + N_TILE + pass * PASS + c32);
+                    if ((pass + 1) * PASS == WC) {                   // the last read of this accumulator is over
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) { if (PAIR) mbar_arrive_cluster(acc_empty + 8 * buf); else mbar_arrive(acc_empty + 8 * buf); }
+                    }
+                    const float4* sw = (const float4*)(tab + pass * PASS);
+                    const float4* bs = (const float4*)(tab + WC + pass * PASS);
+                    const float2 s2 = make_float2(sa, sa);
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
+                    for (int j = 0; j < PASS; j += 4) {
                         const float4 w = sw[j / 4], b = bs[j / 4];
-                        v[j] = __float_as_uint(fmaf((float)(int)v[j] * sa, w.x, b.x));
-                        v[j + 1] = __float_as_uint(fmaf((float)(int)v[j + 1] * sa, w.y, b.y));
-                        v[j + 2] = __float_as_uint(fmaf((float)(int)v[j + 2] * sa, w.z, b.z));
-                        v[j + 3] = __float_as_uint(fmaf((float)(int)v[j + 3] * sa, w.w, b.w));
-                    }
-                    if (OT == OC_DTYPE_F32) {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4)
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(stage_row + (uint32_t)(c32 + j) * 4u), "r"(v[j]), "r"(v[j + 1]), "r"(v[j + 2]), "r"(v[j + 3]) : "memory");
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 8) {
-                            uint32_t o[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(__uint_as_float(v[j + 2 * i]), __uint_as_float(v[j + 2 * i + 1]));
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(stage_row + (uint32_t)(c32 + j) * 2u), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                        const float2 lo = fma2(mul2(make_float2((float)(int)v[j], (float)(int)v[j + 1]), s2), make_float2(w.x, w.y), make_float2(b.x, b.y));
+                        const float2 hi = fma2(mul2(make_float2((float)(int)v[j + 2], (float)(int)v[j + 3]), s2), make_float2(w.z, w.w), make_float2(b.z, b.w));
+                        if (OT == OC_DTYPE_F32) {
+                            v[j] = __float_as_uint(lo.x); v[j + 1] = __float_as_uint(lo.y);
+                            v[j + 2] = __float_as_uint(hi.x); v[j + 3] = __float_as_uint(hi.y);
+                        } else {
+                            v[j / 2] = pack_bf16x2(lo.x, lo.y);
+                            v[j / 2 + 1] = pack_bf16x2(hi.x, hi.y);
                         }
                     }
-                }
-                __syncwarp();
-                if (!P.wide) {                                       // rows of `out` that are not 16-byte aligned: element by element
-                    for (int row = 0; row < 32; ++row) {
+                    // the piece staged before has left (it had this one's arithmetic to do so)
+                    if (P.tma_out && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < I8_SEG / 16; ++j)
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(stage_base + i8_staged(lane, j)),
+                                     "r"(v[4 * j]), "r"(v[4 * j + 1]), "r"(v[4 * j + 2]), "r"(v[4 * j + 3]) : "memory");
+                    if (P.tma_out) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            // (rows and columns past the end are clipped; a box wholly outside starts past the last row or column)
+                            if (row0 < P.M && col0 + pass * PASS < P.N)
+                                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                                             :: "l"(&P.mapOut), "r"(col0 + pass * PASS), "r"(row0), "r"(stage_base) : "memory");
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                        continue;
+                    }
+                    __syncwarp();
+                    if (!P.wide) {                                   // rows of `out` that are not 16-byte aligned: element by element
+                        for (int row = 0; row < 32; ++row) {
+                            const int d = __shfl_sync(0xFFFFFFFFu, dst, row);
+#pragma unroll
+                            for (int e = 0; e < PASS; e += 32) {
+                                if (PASS < 32 && lane >= PASS) continue;
+                                const int col = col0 + pass * PASS + e + lane, at = (e + lane) * OB;
+                                const uint32_t from = stage_base + i8_staged(row, at >> 4) + (uint32_t)(at & 15);
+                                if (d < 0 || col >= P.N) continue;
+                                if (OB == 4) {
+                                    uint32_t x;
+                                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(from) : "memory");
+                                    ((uint32_t*)P.out)[(long long)d * P.out_stride + col] = x;
+                                } else {
+                                    uint16_t x;
+                                    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(from) : "memory");
+                                    ((uint16_t*)P.out)[(long long)d * P.out_stride + col] = x;
+                                }
+                            }
+                        }
+                        continue;
+                    }
+                    const int col = col0 + pass * PASS + (lane % LPR) * (16 / OB);
+#pragma unroll
+                    for (int i = 0; i < 32 / RPI; ++i) {
+                        const int row = i * RPI + lane / LPR;
                         const int d = __shfl_sync(0xFFFFFFFFu, dst, row);
-#pragma unroll
-                        for (int e = 0; e < PASS; e += 32) {
-                            const int col = col0 + pass * PASS + e + lane;
-                            const uint32_t from = stage_base + (uint32_t)(row * PITCH + (e + lane) * OB);
-                            if (d < 0 || col >= P.N) continue;
-                            if (OB == 4) {
-                                uint32_t o;
-                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(o) : "r"(from) : "memory");
-                                ((uint32_t*)P.out)[(long long)d * P.out_stride + col] = o;
-                            } else {
-                                uint16_t o;
-                                asm volatile("ld.shared.b16 %0, [%1];" : "=h"(o) : "r"(from) : "memory");
-                                ((uint16_t*)P.out)[(long long)d * P.out_stride + col] = o;
-                            }
-                        }
-                    }
-                    continue;
-                }
-                const int col = col0 + pass * PASS + (lane % LPR) * (16 / OB);
-#pragma unroll
-                for (int i = 0; i < 32 / RPI; ++i) {
-                    const int row = i * RPI + lane / LPR;
-                    const int d = __shfl_sync(0xFFFFFFFFu, dst, row);
-                    uint4 o;
-                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(o.x), "=r"(o.y), "=r"(o.z), "=r"(o.w) : "r"(stage_base + (uint32_t)(row * PITCH + (lane % LPR) * 16)) : "memory");
-                    if (d >= 0 && col < P.N) {
-                        uint8_t* p = (uint8_t*)P.out + ((long long)d * P.out_stride + col) * OB;
-                        if (col + 16 / OB <= P.N) {
-                            st_v4(p, o);
-                        } else {                                     // the row's last, partial 16 bytes
-                            const uint32_t w[4] = {o.x, o.y, o.z, o.w};
-                            for (int e = 0; e < P.N - col; ++e) {
-                                if (OB == 4) ((uint32_t*)p)[e] = w[e];
-                                else ((uint16_t*)p)[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                        uint4 x;
+                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(stage_base + i8_staged(row, lane % LPR)) : "memory");
+                        if (d >= 0 && col < P.N) {
+                            uint8_t* p = (uint8_t*)P.out + ((long long)d * P.out_stride + col) * OB;
+                            if (col + 16 / OB <= P.N) {
+                                st_v4(p, x);
+                            } else {                                 // the row's last, partial 16 bytes
+                                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                                for (int e = 0; e < P.N - col; ++e) {
+                                    if (OB == 4) ((uint32_t*)p)[e] = w[e];
+                                    else ((uint16_t*)p)[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                                }
                             }
                         }
                     }
                 }
+            } else {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) { if (PAIR) mbar_arrive_cluster(acc_empty + 8 * buf); else mbar_arrive(acc_empty + 8 * buf); }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) { if (PAIR) mbar_arrive_cluster(acc_empty + 8 * buf); else mbar_arrive(acc_empty + 8 * buf); }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");                 // its pieces are written
+        if (!ok && lane == 0) { atomicCAS(P.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
     }
     tc_fence_before();
     __syncthreads();
@@ -433,10 +484,21 @@ static bool i8_encode(I8EncodeFn enc, CUtensorMap* map, const void* p, int64_t K
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+static bool i8_encode_out(I8EncodeFn enc, CUtensorMap* map, void* p, int dtype, int64_t N, int64_t M, int64_t stride) {
+    const bool f32 = dtype == OC_DTYPE_F32;
+    const cuuint64_t dims[2] = {(cuuint64_t)N, (cuuint64_t)M};
+    const cuuint64_t strides[1] = {(cuuint64_t)stride * (f32 ? 4 : 2)};
+    const cuuint32_t box[2] = {(cuuint32_t)(f32 ? I8_SEG / 4 : I8_SEG / 2), 32}, estr[2] = {1, 1};
+    return strides[0] < (1ull << 40) &&
+           enc(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int N_TILE, bool PAIR, int OT>
 static oc_status launch_tiles_as(oc_ctx* ctx, I8Params& P, cudaStream_t s) {
     constexpr int STAGE_BYTES = I8_A_BYTES + (PAIR ? N_TILE / 2 : N_TILE) * I8_BK;
-    constexpr int REST = I8_EPI_WARPS * I8_OUT_STAGE + 4 * N_TILE * 4 + (2 * I8_STAGES_MAX + 5) * 8 + 16;
+    constexpr int REST = I8_EPI_WARPS * I8_OUT_STAGE + 2 * N_TILE * 4 + (2 * I8_STAGES_MAX + 5) * 8 + 16;
     constexpr int FIT = (227 * 1024 - REST) / STAGE_BYTES, STAGES = FIT < I8_STAGES_MAX ? FIT : I8_STAGES_MAX;
     constexpr int SMEM = STAGES * STAGE_BYTES + REST;
     static PerDeviceOnce once;                       // (the context's device is current here)
@@ -451,7 +513,7 @@ static oc_status launch_tiles_as(oc_ctx* ctx, I8Params& P, cudaStream_t s) {
     const unsigned grid = (unsigned)(tiles < walkers ? tiles : walkers) * (PAIR ? 2u : 1u);
     LaunchScope scope(ctx, OC_K_LINEAR_I8, s);
     PdlLaunch l(dim3(grid), dim3(I8_THREADS), SMEM, s, PAIR ? 2u : 0u);
-    cudaLaunchKernelEx(&l.cfg, kernel, P);
+    cudaLaunchKernelEx(&l.cfg, kernel, (const I8Params&)P);
     return last_launch_status();
 }
 template <int N_TILE, bool PAIR>
@@ -494,11 +556,13 @@ oc_status launch_linear_int8(oc_ctx* ctx, const int8_t* a, const float* a_scale,
     if (!i8_encode(enc, &P.mapA, a, K, M, I8_BM) || !i8_encode(enc, &P.mapW, w, K, N, F.w_rows)) return OC_ERR_UNSUPPORTED;
     P.a_scale = a_scale; P.w_scale = w_scale; P.bias = bias; P.out_idx = out_idx; P.out = out; P.out_stride = out_stride;
     P.M = (int)M; P.N = (int)N; P.out_rows = (int)out_rows; P.kblocks = kblocks; P.status = ctx->d_status;
+    P.wide = ((uintptr_t)out | (uint64_t)out_stride * (out_dtype == OC_DTYPE_F32 ? 4u : 2u)) % 16 == 0;
+    // (a TMA store clips at 16 bytes, not at an element: a row's end in mid-piece is stored by hand)
+    P.tma_out = P.wide && !out_idx && N * (out_dtype == OC_DTYPE_F32 ? 4 : 2) % 16 == 0 &&
+                i8_encode_out(enc, &P.mapOut, out, out_dtype, N, M, out_stride);
     const long long mt = (M + F.rows - 1) / F.rows, nt = (N + F.cols - 1) / F.cols;
     if (mt * nt > 0x7FFFFFFFll - 1024) return OC_ERR_UNSUPPORTED;
     P.m_tiles = (int)mt; P.n_tiles = (int)nt;
-    P.n_first = M >= N;
-    P.wide = ((uintptr_t)out | (uint64_t)out_stride * (out_dtype == OC_DTYPE_F32 ? 4u : 2u)) % 16 == 0;
     switch (best) {
         case 0: return launch_tiles<256, true>(ctx, P, out_dtype, s);
         case 1: return launch_tiles<128, false>(ctx, P, out_dtype, s);

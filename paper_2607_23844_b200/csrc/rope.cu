@@ -182,7 +182,7 @@ rope_kernel(const __grid_constant__ RopeParams P) {
                         s = half;
                     }
                     q = __shfl_sync(0xFFFFFFFFu, q, sub * P.lph);
-                    const float rstd = rsqrtf(q * P.inv_d + P.eps);
+                    const float rstd = 1.0f / sqrtf(q * P.inv_d + P.eps);
 #pragma unroll
                     for (int k = 0; k < UPL; ++k)
 #pragma unroll

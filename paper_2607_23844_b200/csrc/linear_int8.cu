@@ -70,19 +70,6 @@ template <int COLS> __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint
                        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
                      : "r"(taddr) : "memory");
 }
-// two fp32 operations in one instruction
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 r;
-    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 r;
-    asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return r;
-}
 // arrive on `bar` (of both CTAs in a pair) once every MMA issued so far has retired
 template <bool PAIR>
 __device__ __forceinline__ void tc_commit_all(uint32_t bar, uint32_t issue) {
@@ -294,18 +281,18 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
                     }
                     const float4* sw = (const float4*)(tab + pass * PASS);
                     const float4* bs = (const float4*)(tab + WC + pass * PASS);
-                    const float2 s2 = make_float2(sa, sa);
+                    const f32x2 s2 = f2(sa);
 #pragma unroll
                     for (int j = 0; j < PASS; j += 4) {
                         const float4 w = sw[j / 4], b = bs[j / 4];
-                        const float2 lo = fma2(mul2(make_float2((float)(int)v[j], (float)(int)v[j + 1]), s2), make_float2(w.x, w.y), make_float2(b.x, b.y));
-                        const float2 hi = fma2(mul2(make_float2((float)(int)v[j + 2], (float)(int)v[j + 3]), s2), make_float2(w.z, w.w), make_float2(b.z, b.w));
+                        const f32x2 lo = f2_fma(f2_mul(f2((float)(int)v[j], (float)(int)v[j + 1]), s2), f2(w.x, w.y), f2(b.x, b.y));
+                        const f32x2 hi = f2_fma(f2_mul(f2((float)(int)v[j + 2], (float)(int)v[j + 3]), s2), f2(w.z, w.w), f2(b.z, b.w));
                         if (OT == OC_DTYPE_F32) {
-                            v[j] = __float_as_uint(lo.x); v[j + 1] = __float_as_uint(lo.y);
-                            v[j + 2] = __float_as_uint(hi.x); v[j + 3] = __float_as_uint(hi.y);
+                            v[j] = __float_as_uint(f2_lo(lo)); v[j + 1] = __float_as_uint(f2_hi(lo));
+                            v[j + 2] = __float_as_uint(f2_lo(hi)); v[j + 3] = __float_as_uint(f2_hi(hi));
                         } else {
-                            v[j / 2] = pack_bf16x2(lo.x, lo.y);
-                            v[j / 2 + 1] = pack_bf16x2(hi.x, hi.y);
+                            v[j / 2] = pack_bf16x2(lo);
+                            v[j / 2 + 1] = pack_bf16x2(hi);
                         }
                     }
                     // the piece staged before has left (it had this one's arithmetic to do so)

@@ -5,22 +5,47 @@
 
 namespace oc {
 
-static constexpr int ROW_THREADS = 256;          // threads per CTA while a row fits one warp
+// threads per CTA: that of the row if it takes more than a warp
+template <int TPR> struct RowCta { static constexpr int threads = TPR > 32 ? TPR : 128, rows = threads / TPR; };
 
-// One 16-byte vector of a row as floats.
+// Two fp32 values in one 64-bit register, and the instructions that work on both.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 f2(float lo, float hi) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ f32x2 f2(float v) { return f2(v, v); }
+__device__ __forceinline__ float f2_lo(f32x2 v) { float a, b; asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); return a; }
+__device__ __forceinline__ float f2_hi(f32x2 v) { float a, b; asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); return b; }
+__device__ __forceinline__ f32x2 f2_add(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 f2_mul(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 f2_fma(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 f2_bits(uint32_t lo, uint32_t hi) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi)); return r; }
+
+// One 16-byte vector of a row as pairs of floats.
 template <int DT> struct RowVec;
 template <> struct RowVec<OC_DTYPE_BF16> {
     static constexpr int E = 8;                                              // elements
-    static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
-        f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
-        f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+    static __device__ __forceinline__ void unpack(const uint4& v, f32x2* f) {
+        f[0] = f2_bits(v.x << 16, v.x & 0xFFFF0000u); f[1] = f2_bits(v.y << 16, v.y & 0xFFFF0000u);
+        f[2] = f2_bits(v.z << 16, v.z & 0xFFFF0000u); f[3] = f2_bits(v.w << 16, v.w & 0xFFFF0000u);
     }
 };
 template <> struct RowVec<OC_DTYPE_F32> {
     static constexpr int E = 4;
-    static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
-        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+    static __device__ __forceinline__ void unpack(const uint4& v, f32x2* f) { f[0] = f2_bits(v.x, v.y); f[1] = f2_bits(v.z, v.w); }
+};
+
+// n / d for n < 2^31 with a multiplication (d >= 1): with 2^(L-1) < d <= 2^L and mul = ceil(2^(31+L) / d), the
+// product exceeds n 2^(31+L) / d by less than 2^(31+L) / d.
+struct FastDiv {
+    uint32_t d, mul, shift;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t d_) : d(d_), mul(0), shift(0) {
+        if (d == 1) return;
+        uint32_t L = 1;
+        while (L < 31 && (1u << L) < d) ++L;
+        mul = (uint32_t)(((1ull << (31 + L)) + d - 1) / d);
+        shift = L - 1;
     }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return d == 1 ? n : __umulhi(n, mul) >> shift; }
 };
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
@@ -37,33 +62,37 @@ __device__ __forceinline__ uint4 ld_v4(const void* p) {
 // E consecutive parameters starting at element `at` (a multiple of E), widened to fp32.  Parameters are
 // read by every row, so they go through the read-only path and stay in L1.
 template <int PT, int E>
-__device__ __forceinline__ void load_param(const void* base, long long at, float* f) {
+__device__ __forceinline__ void load_param(const void* base, long long at, f32x2* f) {
     if (PT == OC_DTYPE_F32) {
 #pragma unroll
-        for (int i = 0; i < E; i += 4) {
-            const float4 v = __ldg((const float4*)((const float*)base + at + i));
-            f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
-        }
+        for (int i = 0; i < E / 4; ++i) RowVec<OC_DTYPE_F32>::unpack(__ldg((const uint4*)((const float*)base + at) + i), f + 2 * i);
     } else if (E == 8) {
         RowVec<OC_DTYPE_BF16>::unpack(__ldg((const uint4*)((const uint16_t*)base + at)), f);
     } else {
         const uint2 v = __ldg((const uint2*)((const uint16_t*)base + at));
-        f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+        f[0] = f2_bits(v.x << 16, v.x & 0xFFFF0000u); f[1] = f2_bits(v.y << 16, v.y & 0xFFFF0000u);
     }
 }
 
 // E consecutive floats of a row rounded to type DT and stored at element `at`.
+__device__ __forceinline__ uint32_t pack_bf16x2(f32x2 v) { return pack_bf16x2(f2_lo(v), f2_hi(v)); }
 template <int DT, int E>
-__device__ __forceinline__ void store_row(void* base, long long at, const float* f) {
+__device__ __forceinline__ void store_row(void* base, long long at, const f32x2* f) {
     if (DT == OC_DTYPE_F32) {
 #pragma unroll
-        for (int i = 0; i < E; i += 4)
-            st_v4((float*)base + at + i, make_uint4(__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3])));
+        for (int i = 0; i < E / 4; ++i)
+            st_v4((float*)base + at + 4 * i, make_uint4(__float_as_uint(f2_lo(f[2 * i])), __float_as_uint(f2_hi(f[2 * i])),
+                                                        __float_as_uint(f2_lo(f[2 * i + 1])), __float_as_uint(f2_hi(f[2 * i + 1]))));
     } else if (E == 8) {
-        st_v4((uint16_t*)base + at, make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])));
+        st_v4((uint16_t*)base + at, make_uint4(pack_bf16x2(f[0]), pack_bf16x2(f[1]), pack_bf16x2(f[2]), pack_bf16x2(f[3])));
     } else {
-        *(uint2*)((uint16_t*)base + at) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+        *(uint2*)((uint16_t*)base + at) = make_uint2(pack_bf16x2(f[0]), pack_bf16x2(f[1]));
     }
+}
+
+template <int E> __device__ __forceinline__ void store_row_smem(float* to, const f32x2* f) {
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) *(float4*)(to + 4 * i) = make_float4(f2_lo(f[2 * i]), f2_hi(f[2 * i]), f2_lo(f[2 * i + 1]), f2_hi(f[2 * i + 1]));
 }
 
 // Sum / maximum over the TPR threads of a row; every one of them gets the same result (butterflies within a
@@ -112,43 +141,53 @@ __device__ __forceinline__ RowQuant row_quant(uint32_t max_bits) {
     else { r.scale = m * (1.0f / 127.0f); r.inv = 127.0f / m; }
     return r;
 }
-// (inv = 0 has to give q = 0 even where x is not finite: 0 * inf is NaN, which cvt.rni.s32 turns into 0)
-__device__ __forceinline__ uint32_t pack_s8x4(const float* f, float inv) {
-    uint32_t r = 0;
+template <int E>
+__device__ __forceinline__ uint32_t max_bits(const f32x2* f, uint32_t m) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r |= ((uint32_t)__float2int_rn(f[i] * inv) & 0xFFu) << (8 * i);
-    return r;
+    for (int i = 0; i < E / 2; ++i) m = max(m, max(__float_as_uint(f2_lo(f[i])) & 0x7FFFFFFFu, __float_as_uint(f2_hi(f[i])) & 0x7FFFFFFFu));
+    return m;
+}
+// (inv = 0 has to give q = 0 even where x is not finite: 0 * inf is NaN, which cvt.rni.s32 turns into 0)
+__device__ __forceinline__ uint32_t pack_s8x4(f32x2 a, f32x2 b, float inv) {
+    const f32x2 x = f2_mul(a, f2(inv)), y = f2_mul(b, f2(inv));
+    return ((uint32_t)__float2int_rn(f2_lo(x)) & 0xFFu) | (((uint32_t)__float2int_rn(f2_hi(x)) & 0xFFu) << 8) |
+           (((uint32_t)__float2int_rn(f2_lo(y)) & 0xFFu) << 16) | ((uint32_t)__float2int_rn(f2_hi(y)) << 24);
 }
 template <int E>
-__device__ __forceinline__ void store_row_s8(void* base, long long at, const float* f, float inv) {
+__device__ __forceinline__ void store_row_s8(void* base, long long at, const f32x2* f, float inv) {
     int8_t* p = (int8_t*)base + at;
-    if (E == 8) *(uint2*)p = make_uint2(pack_s8x4(f, inv), pack_s8x4(f + 4, inv));
-    else *(uint32_t*)p = pack_s8x4(f, inv);
+    if (E == 8) *(uint2*)p = make_uint2(pack_s8x4(f[0], f[1], inv), pack_s8x4(f[2], f[3], inv));
+    else *(uint32_t*)p = pack_s8x4(f[0], f[1], inv);
 }
 
+// The split of a row of more than MIN vectors over TPR threads with up to VPT each.
+template <int TPR, int VPT, int MIN> struct RowSplit {
+    static constexpr int tpr = TPR, vpt = VPT;
+    // whether thread t has a j-th vector (known without looking for all but the last few)
+    static __device__ __forceinline__ bool has(int j, int t, int nvec) { return (j + 1) * TPR <= MIN + 1 || j * TPR + t < nvec; }
+};
 // Picks the row split for nvec vectors: the fewest threads that hold the row in at most 6 vectors each, so that
-// few lanes idle and several 16-byte loads per thread are in flight.  Calls f with the two sizes as
-// std::integral_constant; false if the row is too wide (more than 3072 vectors).
-template <int TPR, int VPT> struct RowSplit { static constexpr int tpr = TPR, vpt = VPT; };
+// few lanes idle and several 16-byte loads per thread are in flight.  Calls f with the
+// split; false if the row is too wide (more than 3072 vectors).
 template <class F>
 inline bool row_split(long long nvec, F&& f) {
-    if (nvec <= 8) f(RowSplit<8, 1>());
-    else if (nvec <= 16) f(RowSplit<8, 2>());
-    else if (nvec <= 24) f(RowSplit<8, 3>());
-    else if (nvec <= 32) f(RowSplit<8, 4>());
-    else if (nvec <= 40) f(RowSplit<8, 5>());
-    else if (nvec <= 48) f(RowSplit<8, 6>());
-    else if (nvec <= 64) f(RowSplit<16, 4>());
-    else if (nvec <= 80) f(RowSplit<16, 5>());
-    else if (nvec <= 96) f(RowSplit<16, 6>());
-    else if (nvec <= 128) f(RowSplit<32, 4>());
-    else if (nvec <= 160) f(RowSplit<32, 5>());
-    else if (nvec <= 192) f(RowSplit<32, 6>());
-    else if (nvec <= 256) f(RowSplit<128, 2>());
-    else if (nvec <= 384) f(RowSplit<128, 3>());
-    else if (nvec <= 768) f(RowSplit<128, 6>());
-    else if (nvec <= 1536) f(RowSplit<512, 3>());
-    else if (nvec <= 3072) f(RowSplit<512, 6>());
+    if (nvec <= 8) f(RowSplit<8, 1, 0>());
+    else if (nvec <= 16) f(RowSplit<8, 2, 8>());
+    else if (nvec <= 24) f(RowSplit<8, 3, 16>());
+    else if (nvec <= 32) f(RowSplit<8, 4, 24>());
+    else if (nvec <= 40) f(RowSplit<8, 5, 32>());
+    else if (nvec <= 48) f(RowSplit<8, 6, 40>());
+    else if (nvec <= 64) f(RowSplit<16, 4, 48>());
+    else if (nvec <= 80) f(RowSplit<16, 5, 64>());
+    else if (nvec <= 96) f(RowSplit<16, 6, 80>());
+    else if (nvec <= 128) f(RowSplit<32, 4, 96>());
+    else if (nvec <= 160) f(RowSplit<32, 5, 128>());
+    else if (nvec <= 192) f(RowSplit<32, 6, 160>());
+    else if (nvec <= 256) f(RowSplit<128, 2, 192>());
+    else if (nvec <= 384) f(RowSplit<128, 3, 256>());
+    else if (nvec <= 768) f(RowSplit<128, 6, 384>());
+    else if (nvec <= 1536) f(RowSplit<512, 3, 768>());
+    else if (nvec <= 3072) f(RowSplit<512, 6, 1536>());
     else return false;
     return true;
 }

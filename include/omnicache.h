@@ -503,8 +503,8 @@ oc_status oc_block_norm(oc_ctx* ctx, const oc_block_norm_desc* desc, const void*
  *     idx[r / unit_rows] * unit_rows + r % unit_rows      (no idx: r)
  * of a [..., axis_len[0], axis_len[1], axis_len[2]] grid: rows gathered by a kept list keep the
  * position of the token they came from.  Rows whose idx is negative (the list's unused tail) are
- * neither read nor written, nor is a row with a position outside the table (recorded as
- * OC_ERR_INVALID_ARG in the device status word).
+ * not written, nor is a row with a position outside the table (recorded as OC_ERR_INVALID_ARG in the
+ * device status word).
  * Head h of row r = (b, i), b = r / rows_per_batch, i = r % rows_per_batch, begins
  *     in:  r * row_stride + h * head_stride              (q and k may be parts of one projection)
  *     out: b * batch_stride + i * row_stride + h * head_stride
@@ -513,9 +513,9 @@ oc_status oc_block_norm(oc_ctx* ctx, const oc_block_norm_desc* desc, const void*
  * v / sqrt(mean(v^2) + eps) * w before the rotation.  All arithmetic is in fp32, rounded once.
  * In place (out = in with the same strides) is allowed; otherwise inputs and outputs do not overlap.
  * Errors: OC_ERR_INVALID_ARG; OC_ERR_ALIGNMENT (a pointer not aligned to its element, or for ADJACENT
- * to its pair; odd strides there); OC_ERR_UNSUPPORTED (a head of more than 64 units: one unit is 16
- * bytes of a head, twice that with HALVES, or as much less as strides, pointers and pairs are aligned
- * to; 2^31 rows or more). */
+ * to its pair; odd strides there); OC_ERR_UNSUPPORTED (a head of more than 64 units: a unit is 8
+ * elements, 4 for fp32 ADJACENT, or as much less as strides, pointers and pairs are aligned to less
+ * than 16 bytes; 2^31 rows or more). */
 typedef struct oc_rope_view { int64_t batch_stride, row_stride, head_stride; } oc_rope_view;
 typedef struct oc_rope_desc {
     int dtype;                        /* OC_DTYPE_F32 or OC_DTYPE_BF16 */

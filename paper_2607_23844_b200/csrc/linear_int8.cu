@@ -10,7 +10,7 @@
 //                memory: rows that keep their order leave as TMA boxes, others as whole 64-byte pieces to
 //                where out_idx says
 // Two accumulators take turns, so the epilogue of a tile runs under the MMAs of the next.
-// Few tokens (at most 8): one warp per pair of output channels, dp4a, the weights read once as they lie.
+// One or two tokens: one warp per pair of output channels, dp4a, the weights read once as they lie.
 // K and N tails are zero-filled by TMA and not stored.  Every wait is bounded (OC_ERR_TIMEOUT in the status word).
 #include <string.h>
 
@@ -27,8 +27,10 @@ static constexpr int I8_EPI_WARPS = 16, I8_THREADS = 64 + 32 * I8_EPI_WARPS;
 static constexpr int I8_A_BYTES = I8_BM * I8_BK;
 static constexpr int I8_STAGES_MAX = 8;
 
-// An epilogue warp stages 64 bytes of each of its 32 rows at a time: twice that stores no faster, and the ring of
-// operands needs the shared memory (it has to cover the latency of loads that compete with the output's stores).
+// An epilogue warp stages 64 bytes of each of its 32 rows at a time.  128 would save a wait, but the shared memory is
+// worth more as ring: loads that compete with 148 SMs' stores come back late, and 57600 x 640 x 5120 takes 139 us
+// with seven resident-form stages and 177 with the four that 128-byte pieces leave (8192 x 1536 x 6144: 48 us with six
+// ring-form stages, 55 with four).
 static constexpr int I8_SEG = 64, I8_OUT_STAGE = 32 * I8_SEG;
 
 struct I8Params {
@@ -40,13 +42,22 @@ struct I8Params {
     long long out_stride;
     int M, N, out_rows;
     int kblocks, m_tiles, n_tiles, n_stages;
+    int a_bytes;                 // of A per stage: fewer than a tile's where there are not that many tokens
+    int rows_of_walkers, main_rows;    // see I8Walk
     int wide, tma_out;           // rows of `out` may be stored in 16-byte pieces; by TMA
     int* status;
 };
 
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 :: "r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+template <bool PAIR>
+__device__ __forceinline__ void tma_load_2d_elected(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar, uint32_t issue) {
+    if (PAIR)
+        asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+                     "@e cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+                     :: "r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar), "r"(issue) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+                     "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+                     :: "r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar), "r"(issue) : "memory");
 }
 template <bool PAIR>
 __device__ __forceinline__ void tc_mma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate, uint32_t issue) {
@@ -62,14 +73,6 @@ __device__ __forceinline__ void tc_mma_i8(uint32_t d_tmem, uint64_t a_desc, uint
 // Where 16-byte piece j of a staged row lies: TMA's swizzle for rows of 64 bytes, which also spreads the pieces that
 // a warp's lanes write, one row each, over all banks.
 __device__ __forceinline__ uint32_t i8_staged(int row, int j) { return (uint32_t)(row * I8_SEG + ((j ^ ((row >> 1) & 3)) << 4)); }
-template <int COLS> __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t* v) {
-    if constexpr (COLS == 32) tmem_ld32(taddr, v);
-    else
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-                       "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-                     : "r"(taddr) : "memory");
-}
 // arrive on `bar` (of both CTAs in a pair) once every MMA issued so far has retired
 template <bool PAIR>
 __device__ __forceinline__ void tc_commit_all(uint32_t bar, uint32_t issue) {
@@ -81,39 +84,57 @@ __device__ __forceinline__ void tc_commit_all(uint32_t bar, uint32_t issue) {
         tc_commit<false>(bar, issue);
 }
 
-// The tiles of a walker, row by row of tiles: whole rows of `out` are written at about the same time, which is
-// what DRAM writes fastest (a 57600 x 5120 output: 174 us, against 188 us in groups of 9 tile columns and 202 us
-// in groups of 3), and each row of A is read from DRAM once, while W stays in L2.
+// The tiles of a walker.  Whole rows of `out` are written at about the same time, which is what DRAM writes fastest
+// (a 57600 x 5120 output: 174 us, against 188 us in groups of 9 tile columns and 202 us in groups of 3), and each row
+// of A is read from DRAM once.
+//   ring form      tile after tile along a row of tiles; W comes back from L2 for every tile
+//   resident form  a walker keeps its tile column, so that its rows of W stay in shared memory (57600 x 640 x 5120
+//                  under the power limit: 157 us, ring form 175): the walkers form as many whole rows of tiles as
+//                  there are (`rows_of_walkers`), which go down the first `main_rows` rows together; the walkers
+//                  left over share out the other rows, column after column
 struct I8Walk {
-    int tile, step, total;
-    __device__ __forceinline__ bool next(const I8Params& P, int& m, int& n) {
-        if (tile >= total) return false;
-        m = tile / P.n_tiles;
-        n = tile - m * P.n_tiles;
+    int n_tiles, m_tiles, tile, step, end, column, above;            // column: of a walker that keeps it, or -1
+    template <bool RES> __device__ __forceinline__ void start(const I8Params& P, int walker, int walkers) {
+        n_tiles = P.n_tiles; m_tiles = P.m_tiles; column = -1; above = 0;
+        if (!RES) { tile = walker; step = walkers; end = m_tiles * n_tiles; return; }
+        const int mains = P.rows_of_walkers * n_tiles;
+        if (walker < mains) { tile = walker / n_tiles; column = walker - tile * n_tiles; step = P.rows_of_walkers; end = P.main_rows; return; }
+        above = P.main_rows;
+        const long long rest = (long long)(m_tiles - above) * n_tiles, x = walker - mains, of = walkers - mains;
+        tile = (int)(rest * x / of); end = (int)(rest * (x + 1) / of); step = 1;
+    }
+    template <bool RES> __device__ __forceinline__ bool next(int& m, int& n) {
+        if (tile >= end) return false;
+        if (!RES) { m = tile / n_tiles; n = tile - m * n_tiles; }
+        else if (column >= 0) { m = tile; n = column; }
+        else { const int rows = m_tiles - above; n = tile / rows; m = above + tile - n * rows; }
         tile += step;
         return true;
     }
 };
 
-template <int N_TILE, bool PAIR, int OT>
+template <int N_TILE, bool PAIR, bool RES, int OT>
 __global__ void __launch_bounds__(I8_THREADS, 1)
 linear_int8_kernel(const __grid_constant__ I8Params P) {
     constexpr int W_ROWS = PAIR ? N_TILE / 2 : N_TILE;               // rows of W that this CTA fetches
-    constexpr int STAGE_BYTES = I8_A_BYTES + W_ROWS * I8_BK;
+    constexpr int W_BYTES = W_ROWS * I8_BK;
+    constexpr int STAGE_BYTES = RES ? I8_A_BYTES : I8_A_BYTES + W_BYTES;
     constexpr int TMEM_COLS = 2 * N_TILE;
     constexpr int OB = OT == OC_DTYPE_F32 ? 4 : 2;
     constexpr int WC = N_TILE >= 128 ? N_TILE / 4 : 32;              // columns of an epilogue warp
     constexpr int PASS = I8_SEG / OB, PARTS = N_TILE / WC;           // columns that it stages together; warps side by side
     constexpr int LPR = I8_SEG / 16, RPI = 32 / LPR;                 // lanes that store a staged row; rows per store
     extern __shared__ __align__(1024) uint8_t i8_smem[];
-    uint8_t* after = i8_smem + (size_t)P.n_stages * STAGE_BYTES;
+    const uint32_t w_bytes = RES ? (uint32_t)(P.kblocks * W_BYTES) : 0u;       // W of this walker's column, in front of the ring
+    uint8_t* after = i8_smem + w_bytes + (size_t)P.n_stages * STAGE_BYTES;
     uint8_t* out_stage = after;                                      // [warps][32 rows][64 bytes]
     float* col_tab = (float*)(after + I8_EPI_WARPS * I8_OUT_STAGE);  // [parts][scale, bias][WC]
     uint64_t* bars = (uint64_t*)(col_tab + 2 * N_TILE);
-    const uint32_t tiles = smem_u32(i8_smem);
+    const uint32_t resident = smem_u32(i8_smem), tiles = resident + w_bytes;
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * I8_STAGES_MAX;
     const uint32_t bar_acc_full = bar_empty + 8 * I8_STAGES_MAX, bar_acc_empty = bar_acc_full + 16, bar_drain = bar_acc_empty + 16;
-    uint32_t* tmem_slot = (uint32_t*)(bars + 2 * I8_STAGES_MAX + 5);
+    const uint32_t bar_w_full = bar_drain + 8, bar_w_empty = bar_drain + 16;
+    uint32_t* tmem_slot = (uint32_t*)(bars + 2 * I8_STAGES_MAX + 7);
     volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
@@ -127,7 +148,7 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
     if (threadIdx.x == 0) {
         for (int s = 0; s < I8_STAGES_MAX; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(bar_acc_full + 8 * b, 1); mbar_init(bar_acc_empty + 8 * b, (PAIR ? 2 : 1) * I8_EPI_WARPS); }
-        mbar_init(bar_drain, 1);
+        mbar_init(bar_drain, 1); mbar_init(bar_w_full, 1); mbar_init(bar_w_empty, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -152,47 +173,52 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
     pdl_wait();                                                      // the operands may come from the kernel before this one
     if (threadIdx.x == 0) pdl_launch_dependents();
     I8Walk walk;
-    walk.tile = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
-    walk.step = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
-    walk.total = P.m_tiles * P.n_tiles;
+    walk.template start<RES>(P, PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x);
     int m, n;
 
     if (warp == 0) {
         // ================================ copies ================================================
-        if (lane == 0) {
-            int stage = 0; uint32_t phase = 0, armed = 0;
-            bool ok = true;
-            while (ok && walk.next(P, m, n)) {
-                const int row0 = m * (PAIR ? 2 * I8_BM : I8_BM) + (int)rank * I8_BM, col0 = n * N_TILE + (int)rank * W_ROWS;
-                for (int kb = 0; kb < P.kblocks; ++kb) {
-                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
-                    const uint32_t dst = tiles + (uint32_t)(stage * STAGE_BYTES), full = bar_full + 8 * stage;
-                    if (leader) mbar_arrive_expect_tx(full, (PAIR ? 2 : 1) * STAGE_BYTES);
-                    if (PAIR) {
-                        const uint32_t bar = map_to_cta(full, 0);    // both CTAs' copies report to the leader
-                        tma_load_2d_pair(dst, &P.mapA, kb * I8_BK, row0, bar);
-                        tma_load_2d_pair(dst + I8_A_BYTES, &P.mapW, kb * I8_BK, col0, bar);
-                    } else {
-                        tma_load_2d(dst, &P.mapA, kb * I8_BK, row0, full);
-                        tma_load_2d(dst + I8_A_BYTES, &P.mapW, kb * I8_BK, col0, full);
-                    }
-                    armed |= 1u << stage;
-                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        // The whole warp runs this and an elected lane issues: addresses and coordinates then are warp-uniform, where a
+        // lone lane would have them moved for every copy, which takes it longer than the copies' MMAs.
+        const uint32_t issue = elect_one();
+        int stage = 0, held = -1; uint32_t phase = 0, armed = 0, w_phase = 0;
+        bool ok = true, have = walk.template next<RES>(m, n);
+        while (ok && have) {
+            const int row0 = m * (PAIR ? 2 * I8_BM : I8_BM) + (int)rank * I8_BM, col0 = n * N_TILE + (int)rank * W_ROWS;
+            if (RES && n != held) {                                  // another column: its W, once the last one's MMAs are over
+                if (held >= 0) {
+                    if (!__all_sync(0xFFFFFFFFu, mbar_wait(bar_w_empty, w_phase, abort_flag))) { ok = false; break; }
+                    w_phase ^= 1u;
                 }
+                held = n;
+                for (int kb = 0; kb < P.kblocks; ++kb)
+                    tma_load_2d_elected<PAIR>(resident + (uint32_t)(kb * W_BYTES), &P.mapW, kb * I8_BK, col0, PAIR ? map_to_cta(bar_w_full, 0) : bar_w_full, issue);
+                if (leader) mbar_arrive_expect_tx_elected(bar_w_full, (PAIR ? 2 : 1) * w_bytes, issue);
             }
-            if (!ok) {
-                atomicCAS(P.status, 0, OC_ERR_TIMEOUT);
-                *abort_flag = 1;
-                // copies already issued still write this CTA's shared memory: a bounded chance to land
-                const unsigned long long t0 = global_ns();
-                if (leader) {
-                    for (int s = 0; s < STAGES; ++s)
-                        if (armed & (1u << s))
-                            while (!mbar_try_wait(bar_full + 8 * s, s < stage ? phase : phase ^ 1u) && global_ns() - t0 < 20000000ull) {}
-                } else {
-                    while (global_ns() - t0 < 2000000ull) {}
-                }
+            for (int kb = 0; kb < P.kblocks; ++kb) {
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag))) { ok = false; break; }
+                const uint32_t dst = tiles + (uint32_t)(stage * STAGE_BYTES), full = bar_full + 8 * stage;
+                const uint32_t bar = PAIR ? map_to_cta(full, 0) : full;               // both CTAs' copies report to the leader
+                // (the copies first: the barrier cannot complete before the arrival that carries their byte count)
+                tma_load_2d_elected<PAIR>(dst, &P.mapA, kb * I8_BK, row0, bar, issue);
+                if (!RES) tma_load_2d_elected<PAIR>(dst + I8_A_BYTES, &P.mapW, kb * I8_BK, col0, bar, issue);
+                if (leader) mbar_arrive_expect_tx_elected(full, (PAIR ? 2 : 1) * (uint32_t)(P.a_bytes + (RES ? 0 : W_BYTES)), issue);
+                armed |= 1u << stage;
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                if (kb == 0) have = walk.template next<RES>(m, n);
             }
+        }
+        if (!ok && lane == 0) {
+            atomicCAS(P.status, 0, OC_ERR_TIMEOUT);
+            *abort_flag = 1;
+            // copies already issued still write this CTA's shared memory: a bounded chance to land
+            const unsigned long long t0 = global_ns();
+            if (leader) {
+                for (int s = 0; s < STAGES; ++s)
+                    if (armed & (1u << s))
+                        while (!mbar_try_wait(bar_full + 8 * s, s < stage ? phase : phase ^ 1u) && global_ns() - t0 < 20000000ull) {}
+            }
+            if (!leader || RES) while (global_ns() - t0 < 2000000ull) {}       // (the peer's, and W's, report elsewhere)
         }
     } else if (warp == 1) {
         // ================================ MMAs ==================================================
@@ -200,19 +226,25 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
             constexpr uint32_t IDESC = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N_TILE >> 3) << 17) |
                                        ((uint32_t)((PAIR ? 2 * I8_BM : I8_BM) >> 4) << 24);       // D = s32, A = B = s8, K-major
             const uint32_t issue = elect_one();
-            int stage = 0; uint32_t phase = 0, it = 0;
-            bool ok = true;
-            while (ok && walk.next(P, m, n)) {
+            int stage = 0, held = -1; uint32_t phase = 0, it = 0, w_phase = 0;
+            bool ok = true, have = walk.template next<RES>(m, n);
+            while (ok && have) {
+                const int column = n;
+                have = walk.template next<RES>(m, n);
                 const uint32_t buf = it & 1u, acc_phase = (it >> 1) & 1u;
                 ++it;
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(bar_acc_empty + 8 * buf, acc_phase ^ 1u, abort_flag))) { ok = false; break; }
+                if (RES && column != held) {
+                    if (!__all_sync(0xFFFFFFFFu, mbar_wait(bar_w_full, w_phase, abort_flag))) { ok = false; break; }
+                    w_phase ^= 1u; held = column;
+                }
                 tc_fence_after();
                 const uint32_t d = tmem_base + buf * N_TILE;
                 for (int kb = 0; kb < P.kblocks; ++kb) {
                     if (!__all_sync(0xFFFFFFFFu, mbar_wait(bar_full + 8 * stage, phase, abort_flag))) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t a_addr = tiles + (uint32_t)(stage * STAGE_BYTES);
-                    const uint64_t a_desc = make_smem_desc(a_addr), b_desc = make_smem_desc(a_addr + I8_A_BYTES);
+                    const uint64_t a_desc = make_smem_desc(a_addr), b_desc = make_smem_desc(RES ? resident + (uint32_t)(kb * W_BYTES) : a_addr + I8_A_BYTES);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)                      // 32 bytes of K at a time along the swizzled rows
                         tc_mma_i8<PAIR>(d, a_desc + 2 * k, b_desc + 2 * k, IDESC, (uint32_t)((kb | k) != 0), issue);
@@ -220,6 +252,7 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                 }
                 if (ok) tc_commit_all<PAIR>(bar_acc_full + 8 * buf, issue);
+                if (RES && ok && have && n != column) tc_commit_all<PAIR>(bar_w_empty, issue);
             }
             if (!ok && lane == 0) { atomicCAS(P.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
             // every MMA retires before tensor memory is released
@@ -247,52 +280,58 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
             if (r < P.M) { ah.sa = __ldg(P.a_scale + r); ah.dst = P.out_idx ? __ldg(P.out_idx + r) : r; }
         };
         uint32_t it = 0;
-        bool ok = true, have = walk.next(P, m, n);
+        int tab_n = -1;                                              // the tile column that the table is of
+        bool ok = true, have = walk.template next<RES>(m, n);
         if (have) fetch(m, n);
         while (have) {
             const uint32_t buf = it & 1u, acc_phase = (it >> 1) & 1u;
             ++it;
             const int row0 = m * (PAIR ? 2 * I8_BM : I8_BM) + (int)rank * I8_BM + quarter * 32, col0 = n * N_TILE + part * WC;
-            if (works) {
+            if (works && n != tab_n) {
                 asm volatile("bar.sync %0, 128;" :: "r"(1 + part) : "memory");       // the part is done with the table
                 if (et < 2 * WC) tab[et] = ah.col;
                 asm volatile("bar.sync %0, 128;" :: "r"(1 + part) : "memory");
+                tab_n = n;
             }
             const float sa = ah.sa;
             int dst = ah.dst;
             if (dst >= P.out_rows) { atomicCAS(P.status, 0, OC_ERR_INVALID_ARG); dst = -1; }
-            have = walk.next(P, m, n);
+            have = walk.template next<RES>(m, n);
             if (have) fetch(m, n);
             // (a warp that has given up keeps meeting the others at the barriers, and waits for nothing else)
             if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar_acc_full + 8 * buf, acc_phase, abort_flag));
             if (!ok) continue;
             tc_fence_after();
             const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N_TILE + (uint32_t)(part * WC);
+            // The sums go into registers at once and the accumulator back to the MMAs; scaling and storing them then
+            // delays nobody but this warp.
+            uint32_t v[WC];
             if (works) {
-#pragma unroll 1
+#pragma unroll
+                for (int c = 0; c < WC; c += 32) tmem_ld32(t_row + (uint32_t)c, v + c);
+                tmem_ld_wait();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) { if (PAIR) mbar_arrive_cluster(acc_empty + 8 * buf); else mbar_arrive(acc_empty + 8 * buf); }
+            if (works) {
+#pragma unroll
                 for (int pass = 0; pass < WC / PASS; ++pass) {
-                    uint32_t v[PASS];
-                    tmem_ld<PASS>(t_row + (uint32_t)(pass * PASS), v);
-                    tmem_ld_wait();
-                    if ((pass + 1) * PASS == WC) {                   // the last read of this accumulator is over
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) { if (PAIR) mbar_arrive_cluster(acc_empty + 8 * buf); else mbar_arrive(acc_empty + 8 * buf); }
-                    }
+                    uint32_t* o = v + pass * PASS;
                     const float4* sw = (const float4*)(tab + pass * PASS);
                     const float4* bs = (const float4*)(tab + WC + pass * PASS);
                     const f32x2 s2 = f2(sa);
 #pragma unroll
                     for (int j = 0; j < PASS; j += 4) {
                         const float4 w = sw[j / 4], b = bs[j / 4];
-                        const f32x2 lo = f2_fma(f2_mul(f2((float)(int)v[j], (float)(int)v[j + 1]), s2), f2(w.x, w.y), f2(b.x, b.y));
-                        const f32x2 hi = f2_fma(f2_mul(f2((float)(int)v[j + 2], (float)(int)v[j + 3]), s2), f2(w.z, w.w), f2(b.z, b.w));
+                        const f32x2 lo = f2_fma(f2_mul(f2((float)(int)o[j], (float)(int)o[j + 1]), s2), f2(w.x, w.y), f2(b.x, b.y));
+                        const f32x2 hi = f2_fma(f2_mul(f2((float)(int)o[j + 2], (float)(int)o[j + 3]), s2), f2(w.z, w.w), f2(b.z, b.w));
                         if (OT == OC_DTYPE_F32) {
-                            v[j] = __float_as_uint(f2_lo(lo)); v[j + 1] = __float_as_uint(f2_hi(lo));
-                            v[j + 2] = __float_as_uint(f2_lo(hi)); v[j + 3] = __float_as_uint(f2_hi(hi));
+                            o[j] = __float_as_uint(f2_lo(lo)); o[j + 1] = __float_as_uint(f2_hi(lo));
+                            o[j + 2] = __float_as_uint(f2_lo(hi)); o[j + 3] = __float_as_uint(f2_hi(hi));
                         } else {
-                            v[j / 2] = pack_bf16x2(lo);
-                            v[j / 2 + 1] = pack_bf16x2(hi);
+                            o[j / 2] = pack_bf16x2(lo);
+                            o[j / 2 + 1] = pack_bf16x2(hi);
                         }
                     }
                     // the piece staged before has left (it had this one's arithmetic to do so)
@@ -301,7 +340,7 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
 #pragma unroll
                     for (int j = 0; j < I8_SEG / 16; ++j)
                         asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(stage_base + i8_staged(lane, j)),
-                                     "r"(v[4 * j]), "r"(v[4 * j + 1]), "r"(v[4 * j + 2]), "r"(v[4 * j + 3]) : "memory");
+                                     "r"(o[4 * j]), "r"(o[4 * j + 1]), "r"(o[4 * j + 2]), "r"(o[4 * j + 3]) : "memory");
                     if (P.tma_out) {
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
@@ -358,10 +397,6 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
                         }
                     }
                 }
-            } else {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) { if (PAIR) mbar_arrive_cluster(acc_empty + 8 * buf); else mbar_arrive(acc_empty + 8 * buf); }
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");                 // its pieces are written
@@ -379,6 +414,9 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
 
 // ---- few tokens ------------------------------------------------------------------------------------
 static constexpr int I8S_WARPS = 8, I8S_CH = 2;                      // warps per CTA, output channels per warp
+// 1536 x 9216 weights: 1 token 3.2 us and 2 tokens 4.3 this way, 5.1 with tensor-core tiles; 4 tokens 4.8 against 4.8,
+// 8 tokens 10.3 against 4.8
+static constexpr int I8S_TOKENS = 2;
 
 struct I8SmallParams {
     const int8_t *a, *w;
@@ -440,9 +478,7 @@ template <int OT>
 static void launch_small(const I8SmallParams& P, cudaStream_t s) {
     const dim3 grid((unsigned)((P.N + I8S_WARPS * I8S_CH - 1) / (I8S_WARPS * I8S_CH)));
     if (P.M == 1) OC_LAUNCH((linear_int8_small_kernel<1, OT>), grid, I8S_WARPS * 32, 0, s, P);
-    else if (P.M == 2) OC_LAUNCH((linear_int8_small_kernel<2, OT>), grid, I8S_WARPS * 32, 0, s, P);
-    else if (P.M <= 4) OC_LAUNCH((linear_int8_small_kernel<4, OT>), grid, I8S_WARPS * 32, 0, s, P);
-    else OC_LAUNCH((linear_int8_small_kernel<8, OT>), grid, I8S_WARPS * 32, 0, s, P);
+    else OC_LAUNCH((linear_int8_small_kernel<2, OT>), grid, I8S_WARPS * 32, 0, s, P);
 }
 
 // ---- host side -------------------------------------------------------------------------------------
@@ -482,37 +518,43 @@ static bool i8_encode_out(I8EncodeFn enc, CUtensorMap* map, void* p, int dtype, 
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int N_TILE, bool PAIR, int OT>
+template <int N_TILE, bool PAIR, bool RES, int OT>
 static oc_status launch_tiles_as(oc_ctx* ctx, I8Params& P, cudaStream_t s) {
-    constexpr int STAGE_BYTES = I8_A_BYTES + (PAIR ? N_TILE / 2 : N_TILE) * I8_BK;
-    constexpr int REST = I8_EPI_WARPS * I8_OUT_STAGE + 2 * N_TILE * 4 + (2 * I8_STAGES_MAX + 5) * 8 + 16;
-    constexpr int FIT = (227 * 1024 - REST) / STAGE_BYTES, STAGES = FIT < I8_STAGES_MAX ? FIT : I8_STAGES_MAX;
-    constexpr int SMEM = STAGES * STAGE_BYTES + REST;
+    constexpr int W_BYTES = (PAIR ? N_TILE / 2 : N_TILE) * I8_BK, STAGE_BYTES = RES ? I8_A_BYTES : I8_A_BYTES + W_BYTES;
+    constexpr int REST = I8_EPI_WARPS * I8_OUT_STAGE + 2 * N_TILE * 4 + (2 * I8_STAGES_MAX + 7) * 8 + 16;
+    const int w_bytes = RES ? P.kblocks * W_BYTES : 0, fit = (227 * 1024 - REST - w_bytes) / STAGE_BYTES;
+    const int stages = fit < I8_STAGES_MAX ? fit : I8_STAGES_MAX, smem = w_bytes + stages * STAGE_BYTES + REST;
     static PerDeviceOnce once;                       // (the context's device is current here)
-    auto* kernel = linear_int8_kernel<N_TILE, PAIR, OT>;
+    auto* kernel = linear_int8_kernel<N_TILE, PAIR, RES, OT>;
     if (!once.ensure(ctx->device, [&] {
-            const bool ok = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) == cudaSuccess;
+            const bool ok = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) == cudaSuccess;
             if (!ok) cudaGetLastError();
             return ok;
         })) return OC_ERR_CUDA;
-    P.n_stages = STAGES;
+    P.n_stages = stages;
     const long long tiles = (long long)P.m_tiles * P.n_tiles, walkers = PAIR ? ctx->sm_count / 2 : ctx->sm_count;
     const unsigned grid = (unsigned)(tiles < walkers ? tiles : walkers) * (PAIR ? 2u : 1u);
+    if (RES) {
+        // each row of walkers takes its share of the rows, the walkers left over the rest
+        P.rows_of_walkers = (int)(walkers / P.n_tiles);
+        const long long share = (tiles + walkers - 1) / walkers * P.rows_of_walkers;
+        P.main_rows = (int)(share < P.m_tiles && walkers % P.n_tiles ? share : (P.rows_of_walkers ? P.m_tiles : 0));
+    }
     LaunchScope scope(ctx, OC_K_LINEAR_I8, s);
-    PdlLaunch l(dim3(grid), dim3(I8_THREADS), SMEM, s, PAIR ? 2u : 0u);
+    PdlLaunch l(dim3(grid), dim3(I8_THREADS), (size_t)smem, s, PAIR ? 2u : 0u);
     cudaLaunchKernelEx(&l.cfg, kernel, (const I8Params&)P);
     return last_launch_status();
 }
-template <int N_TILE, bool PAIR>
+template <int N_TILE, bool PAIR, bool RES>
 static oc_status launch_tiles(oc_ctx* ctx, I8Params& P, int out_dtype, cudaStream_t s) {
-    return out_dtype == OC_DTYPE_F32 ? launch_tiles_as<N_TILE, PAIR, OC_DTYPE_F32>(ctx, P, s)
-                                     : launch_tiles_as<N_TILE, PAIR, OC_DTYPE_BF16>(ctx, P, s);
+    return out_dtype == OC_DTYPE_F32 ? launch_tiles_as<N_TILE, PAIR, RES, OC_DTYPE_F32>(ctx, P, s)
+                                     : launch_tiles_as<N_TILE, PAIR, RES, OC_DTYPE_BF16>(ctx, P, s);
 }
 
 oc_status launch_linear_int8(oc_ctx* ctx, const int8_t* a, const float* a_scale, int64_t M, int64_t K, const int8_t* w,
                              const float* w_scale, int64_t N, const float* bias, void* out, int out_dtype, int64_t out_rows,
                              int64_t out_stride, const int32_t* out_idx, cudaStream_t s) {
-    if (M <= 8) {
+    if (M <= I8S_TOKENS) {
         I8SmallParams P;
         P.a = a; P.w = w; P.a_scale = a_scale; P.w_scale = w_scale; P.bias = bias; P.out_idx = out_idx; P.out = out;
         P.out_stride = out_stride; P.M = (int)M; P.N = (int)N; P.K = (int)K; P.out_rows = (int)out_rows; P.status = ctx->d_status;
@@ -525,22 +567,28 @@ oc_status launch_linear_int8(oc_ctx* ctx, const int8_t* a, const float* a_scale,
     if (!enc) return OC_ERR_UNSUPPORTED;
     I8Params P;
     memset(&P, 0, sizeof(P));
-    // The tile whose waves over the device take the fewest cycles: a 128-byte step of K costs the MMAs of its
-    // tile or the arrival of its operands, whichever is longer.
-    struct Form { int rows, cols, w_rows, per_sm; } forms[4] = {{256, 256, 128, 2}, {128, 128, 128, 1}, {128, 64, 64, 1}, {128, 32, 32, 1}};
+    // The form whose waves over the device take the least time: a fixed part, and for each wave its steps of 128 bytes
+    // of K or its output, whichever is longer.  The figures (us) were read off 22 shapes of 1 to 14400 tokens timed
+    // with every form; they name the fastest, or one within 7 %, on all of them (1024 x 1536 x 1536: 5.9 us in
+    // 128 x 128 tiles, 8.4 in pairs; 2048 x 1536 x 4608: 16.0 against 13.7; 64 x 1536 x 9216: 5.3 against 5.0 in
+    // 128 x 64; 128 x 1536 x 1536: 5.4 against 4.7 in 128 x 32).
+    struct Form { int rows, cols, w_rows, per_walker; double fixed, step, tile; };
+    static const Form forms[4] = {{256, 256, 128, 2, 3.5, 0.417, 2.2}, {128, 128, 128, 1, 2.5, 0.28, 1.4},
+                                  {128, 64, 64, 1, 2.5, 0.206, 1.05}, {128, 32, 32, 1, 2.5, 0.19, 0.9}};
     int best = 1;
     double best_cost = 1e300;
     const int kblocks = (int)((K + I8_BK - 1) / I8_BK);
-    for (int f = 0; f < 4; ++f) {
-        if (f == 0 && M <= 128) continue;
+    for (int f = M > 128 ? 0 : 1; f < 4; ++f) {
         const long long tiles = ((M + forms[f].rows - 1) / forms[f].rows) * ((N + forms[f].cols - 1) / forms[f].cols);
-        const long long walkers = ctx->sm_count / forms[f].per_sm;
-        const double step = std::max(2.0 * forms[f].cols, (I8_A_BYTES + forms[f].w_rows * I8_BK) / 64.0);
-        const double cost = (double)((tiles + walkers - 1) / walkers) * (kblocks * step + 300.0);
+        const long long walkers = ctx->sm_count / forms[f].per_walker;
+        const double cost = forms[f].fixed + (double)((tiles + walkers - 1) / walkers) * std::max(kblocks * forms[f].step, forms[f].tile);
         if (cost < best_cost) { best_cost = cost; best = f; }
     }
     const Form& F = forms[best];
-    if (!i8_encode(enc, &P.mapA, a, K, M, I8_BM) || !i8_encode(enc, &P.mapW, w, K, N, F.w_rows)) return OC_ERR_UNSUPPORTED;
+    // (the rows of a tile that no token has are left as they are in shared memory: their sums are not stored)
+    const int a_box = M < I8_BM ? (int)(M + 7) / 8 * 8 : I8_BM;
+    P.a_bytes = a_box * I8_BK;
+    if (!i8_encode(enc, &P.mapA, a, K, M, a_box) || !i8_encode(enc, &P.mapW, w, K, N, F.w_rows)) return OC_ERR_UNSUPPORTED;
     P.a_scale = a_scale; P.w_scale = w_scale; P.bias = bias; P.out_idx = out_idx; P.out = out; P.out_stride = out_stride;
     P.M = (int)M; P.N = (int)N; P.out_rows = (int)out_rows; P.kblocks = kblocks; P.status = ctx->d_status;
     P.wide = ((uintptr_t)out | (uint64_t)out_stride * (out_dtype == OC_DTYPE_F32 ? 4u : 2u)) % 16 == 0;
@@ -551,10 +599,14 @@ oc_status launch_linear_int8(oc_ctx* ctx, const int8_t* a, const float* a_scale,
     if (mt * nt > 0x7FFFFFFFll - 1024) return OC_ERR_UNSUPPORTED;
     P.m_tiles = (int)mt; P.n_tiles = (int)nt;
     switch (best) {
-        case 0: return launch_tiles<256, true>(ctx, P, out_dtype, s);
-        case 1: return launch_tiles<128, false>(ctx, P, out_dtype, s);
-        case 2: return launch_tiles<64, false>(ctx, P, out_dtype, s);
-        default: return launch_tiles<32, false>(ctx, P, out_dtype, s);
+        case 0:
+            // W stays in shared memory where a column's share leaves room for five stages of A, and there are tiles
+            // enough to use it on
+            if (kblocks <= 7 && mt * nt >= 4 * (ctx->sm_count / 2)) return launch_tiles<256, true, true>(ctx, P, out_dtype, s);
+            return launch_tiles<256, true, false>(ctx, P, out_dtype, s);
+        case 1: return launch_tiles<128, false, false>(ctx, P, out_dtype, s);
+        case 2: return launch_tiles<64, false, false>(ctx, P, out_dtype, s);
+        default: return launch_tiles<32, false, false>(ctx, P, out_dtype, s);
     }
 }
 

@@ -636,7 +636,8 @@ def test_linear_int8_sizes(oc, ctx, M, K, N, out_dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("out_dtype", [BF16, F32])
-@pytest.mark.parametrize("M,K,N", [(2500, 256, 2304), (2561, 640, 2309), (1000, 2048, 4104), (20000, 320, 320), (1100, 96, 1096), (700, 6400, 600)])
+@pytest.mark.parametrize("M,K,N", [(2500, 256, 2304), (2561, 640, 2309), (1000, 2048, 4104), (20000, 320, 320), (1100, 96, 1096), (700, 6400, 600),
+                                   (20000, 320, 2560), (9000, 880, 2816), (2000, 64, 20000)])
 def test_linear_int8_large(oc, ctx, M, K, N, out_dtype):
     run_linear(oc, ctx, M, K, N, out_dtype, seed=M)
     run_linear(oc, ctx, M, K, N, out_dtype, bias=False, pad=1, off=1, seed=N)
@@ -644,7 +645,7 @@ def test_linear_int8_large(oc, ctx, M, K, N, out_dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M,K,N", [(5, 64, 40), (200, 320, 136), (2500, 256, 2304)])
+@pytest.mark.parametrize("M,K,N", [(2, 64, 40), (5, 64, 40), (200, 320, 136), (2500, 256, 2304)])
 def test_linear_int8_rows_to_named_places(oc, ctx, M, K, N):
     g = torch.Generator().manual_seed(M)
     idx = torch.randperm(M + 50, generator=g)[:M].to(torch.int32)
@@ -657,7 +658,7 @@ def test_linear_int8_rows_to_named_places(oc, ctx, M, K, N):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M", [4, 40])
+@pytest.mark.parametrize("M", [2, 4, 40])
 def test_linear_int8_sums_are_exact(oc, ctx, M):
     """The largest sums: K = 131056 products of -128 * -128 stay just below 2^31."""
     K = 131056
@@ -680,7 +681,7 @@ def test_linear_int8_rows_that_are_not_finite(oc, ctx, M):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M", [6, 24])
+@pytest.mark.parametrize("M", [2, 6, 24])
 def test_linear_int8_offsets_past_32_bits(oc, ctx, M):
     K, N, stride = 64, 40, 2 ** 29 // M * 5
     g = torch.Generator().manual_seed(0)

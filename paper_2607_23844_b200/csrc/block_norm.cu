@@ -5,6 +5,7 @@
 // Statistics are taken from the registers that hold the row, in fp32 and in two passes (mean, then squared
 // distances), so a large common offset costs no precision and nothing is read twice.  r stays in fp32 between
 // the residual sum and the second norm: `out` is its rounding, h is not computed from that rounding.
+#include <algorithm>
 #include <atomic>
 
 #include "rows.cuh"
@@ -19,7 +20,7 @@ struct BlockNormParams {
     uint32_t n_rows, dense_units;
     FastDiv unit_rows, rows_per_group;
     int C, nvec, post_norm, pre_norm, h_dtype;
-    int trips;                               // row sets that a CTA works through, one after the other
+    uint32_t sets, queue;                    // sets of rows; how many a CTA works through, one after the other
     int folds;                               // which folded parameters there are (Fold bits); 16: they are kept in shared memory
     float post_eps, pre_eps, res_scale, inv_c;
     int* status;
@@ -174,13 +175,15 @@ block_norm_kernel(const __grid_constant__ BlockNormParams P) {
     };
 
     // (n_rows and a CTA's rows past it stay below 2^32: the last set of rows begins before n_rows)
-    uint32_t base = blockIdx.x * (uint32_t)P.trips * ROWS, next_row = base + threadIdx.x / TPR;
+    const uint32_t set0 = blockIdx.x * P.queue;
+    const int trips = (int)min(P.queue, P.sets - set0);
+    uint32_t base = set0 * ROWS, next_row = base + threadIdx.x / TPR;
     RowPlan R = plan(next_row, slot_at(next_row));
     fetch(R);
     next_row += ROWS;
     int next_slot = slot_at(next_row);
     uint32_t tab_group = 0xFFFFFFFFu;
-    for (int trip = 0; trip < P.trips && base < P.n_rows; ++trip, base += ROWS) {
+    for (int trip = 0; trip < trips; ++trip, base += ROWS) {
         const uint32_t last = min(base + ROWS, P.n_rows) - 1u;
         const uint32_t group = P.mod_stride ? P.rows_per_group.div(base) : 0u;
         const bool in_smem = (P.folds & FOLD_KEPT) && (!P.mod_stride || P.rows_per_group.div(last) == group);
@@ -232,9 +235,9 @@ block_norm_kernel(const __grid_constant__ BlockNormParams P) {
                 if (S::has(j, t, P.nvec)) store_row<DT, E>(P.out, row_at + (j * TPR + t) * E, r[j]);
         }
         const RowPlan N = plan(next_row, next_slot);
-        if (trip + 1 < P.trips) fetch(N);
+        if (trip + 1 < trips) fetch(N);
         next_row += ROWS;
-        next_slot = trip + 2 < P.trips ? slot_at(next_row) : 0;
+        next_slot = trip + 2 < trips ? slot_at(next_row) : 0;
         // a warp (or CTA) none of whose rows goes on is done
         const bool goes_on = P.h && (TPR > 32 ? R.computed : __any_sync(0xFFFFFFFFu, R.computed));
         if (goes_on) {
@@ -344,9 +347,16 @@ static bool launch_block_norm_as(oc_ctx* ctx, BlockNormParams& P, cudaStream_t s
             if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, THREADS, smem) != cudaSuccess || per_sm < 1) { cudaGetLastError(); ok = false; return; }
             known.store(key | (uint64_t)per_sm, std::memory_order_relaxed);
         }
-        const long long most = (long long)ctx->sm_count * per_sm;
-        P.trips = (int)((sets + most - 1) / most);
-        OC_LAUNCH(kernel, (unsigned)((sets + P.trips - 1) / P.trips), THREADS, smem, s, P);
+        // Queues of equal length with every CTA resident, unless that makes long ones: 230400 rows of 320 take 138 us
+        // in 740 queues of 20 sets and 115 in queues of 4 (64 rows), which are near one another in DRAM at any time;
+        // shorter ones fold the parameters too often (57600 rows of 640: 63 us in resident queues, 67 in queues of 32
+        // rows).  8192 rows of 1536: 28 us in resident queues of 4 sets, 30 of 2, and 37 of 3, which are a round and
+        // a bit.
+        const long long resident = (long long)ctx->sm_count * per_sm, short_queue = std::max(4, 64 / ROWS);
+        const long long queue = sets / short_queue > 2 * resident ? short_queue : (sets + resident - 1) / resident;
+        const long long ctas = (sets + queue - 1) / queue;
+        P.sets = (uint32_t)sets; P.queue = (uint32_t)queue;
+        OC_LAUNCH(kernel, (unsigned)ctas, THREADS, smem, s, P);
     });
     return ok;
 }

@@ -355,23 +355,21 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
                     }
                     __syncwarp();
                     if (!P.wide) {                                   // rows of `out` that are not 16-byte aligned: element by element
-                        for (int row = 0; row < 32; ++row) {
+                        constexpr int COLS = PASS < 32 ? PASS : 32;  // lanes of a row; two rows at a time where it is short
+#pragma unroll 8
+                        for (int r = 0; r < COLS; ++r) {
+                            const int row = r * (32 / COLS) + lane / COLS, at = (lane % COLS) * OB, col = col0 + pass * PASS + lane % COLS;
                             const int d = __shfl_sync(0xFFFFFFFFu, dst, row);
-#pragma unroll
-                            for (int e = 0; e < PASS; e += 32) {
-                                if (PASS < 32 && lane >= PASS) continue;
-                                const int col = col0 + pass * PASS + e + lane, at = (e + lane) * OB;
-                                const uint32_t from = stage_base + i8_staged(row, at >> 4) + (uint32_t)(at & 15);
-                                if (d < 0 || col >= P.N) continue;
-                                if (OB == 4) {
-                                    uint32_t x;
-                                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(from) : "memory");
-                                    ((uint32_t*)P.out)[(long long)d * P.out_stride + col] = x;
-                                } else {
-                                    uint16_t x;
-                                    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(from) : "memory");
-                                    ((uint16_t*)P.out)[(long long)d * P.out_stride + col] = x;
-                                }
+                            const uint32_t from = stage_base + i8_staged(row, at >> 4) + (uint32_t)(at & 15);
+                            const bool keep = d >= 0 && col < P.N;
+                            if (OB == 4) {
+                                uint32_t x;
+                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(from) : "memory");
+                                if (keep) ((uint32_t*)P.out)[(long long)d * P.out_stride + col] = x;
+                            } else {
+                                uint16_t x;
+                                asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(from) : "memory");
+                                if (keep) ((uint16_t*)P.out)[(long long)d * P.out_stride + col] = x;
                             }
                         }
                         continue;

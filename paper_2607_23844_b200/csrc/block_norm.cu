@@ -128,8 +128,8 @@ block_norm_kernel(const __grid_constant__ BlockNormParams P) {
     constexpr int E = RowVec<DT>::E, EB = 16 / E, TPR = S::tpr, VPT = S::vpt;   // (EB: bytes of an element)
     constexpr int THREADS = RowCta<TPR>::threads, ROWS = RowCta<TPR>::rows;
     extern __shared__ __align__(16) uint4 smem4[];                           // [x, v][VPT][THREADS], then the folded vectors
-    __shared__ RowScratch scratch_mem;
-    RowScratch* scratch = TPR > 32 ? &scratch_mem : nullptr;
+    __shared__ RowScratch scratch_mem[ROWS];
+    RowScratch* scratch = TPR > 32 ? scratch_mem + threadIdx.x / TPR : nullptr;
     int parity = 0;
     const int t = threadIdx.x % TPR;
     const uint4* held = smem4 + threadIdx.x;
@@ -238,7 +238,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams P) {
         if (trip + 1 < trips) fetch(N);
         next_row += ROWS;
         next_slot = trip + 2 < trips ? slot_at(next_row) : 0;
-        // a warp (or CTA) none of whose rows goes on is done
+        // a warp (or the warps of one row) none of whose rows goes on is done
         const bool goes_on = P.h && (TPR > 32 ? R.computed : __any_sync(0xFFFFFFFFu, R.computed));
         if (goes_on) {
             normalise<S, E>(r, P.pre_norm, P.pre_eps, P.inv_c, P.nvec, t, scratch, parity);
@@ -282,8 +282,8 @@ __global__ void __launch_bounds__(RowCta<S::tpr>::threads)
 quantize_rows_kernel(const __grid_constant__ QuantParams P) {
     constexpr int E = RowVec<DT>::E, TPR = S::tpr, VPT = S::vpt;
     constexpr int ROWS = RowCta<TPR>::rows;
-    __shared__ RowScratch scratch_mem;
-    RowScratch* scratch = TPR > 32 ? &scratch_mem : nullptr;
+    __shared__ RowScratch scratch_mem[ROWS];
+    RowScratch* scratch = TPR > 32 ? scratch_mem + threadIdx.x / TPR : nullptr;
     int parity = 0;
     const int t = threadIdx.x % TPR;
     const uint32_t row = blockIdx.x * ROWS + threadIdx.x / TPR;

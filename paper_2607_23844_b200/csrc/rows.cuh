@@ -5,8 +5,8 @@
 
 namespace oc {
 
-// threads per CTA: that of the row if it takes more than a warp
-template <int TPR> struct RowCta { static constexpr int threads = TPR > 32 ? TPR : 128, rows = threads / TPR; };
+// threads per CTA
+template <int TPR> struct RowCta { static constexpr int threads = TPR >= 128 ? TPR : (TPR == 64 ? 256 : 128), rows = threads / TPR; };
 
 // Two fp32 values in one 64-bit register, and the instructions that work on both.
 typedef unsigned long long f32x2;
@@ -97,7 +97,7 @@ template <int E> __device__ __forceinline__ void store_row_smem(float* to, const
 
 // Sum / maximum over the TPR threads of a row; every one of them gets the same result (butterflies within a
 // warp, then a fixed order over the warps: no atomics, so a row's result never depends on scheduling).
-// Rows wider than a warp take the whole CTA, and `scratch` holds one word per warp and parity.
+// Rows wider than a warp meet at a barrier of their own threads, and `scratch` holds one word per warp and parity.
 struct RowScratch { uint32_t w[2][16]; };
 template <int TPR, class Op>
 __device__ __forceinline__ uint32_t row_reduce(uint32_t v, Op op, RowScratch* scratch, int& parity) {
@@ -109,8 +109,8 @@ __device__ __forceinline__ uint32_t row_reduce(uint32_t v, Op op, RowScratch* sc
         //  reduction keeps it from coming back before everybody has read this one)
         uint32_t* w = scratch->w[parity];
         parity ^= 1;
-        if ((threadIdx.x & 31) == 0) w[threadIdx.x >> 5] = v;
-        __syncthreads();
+        if ((threadIdx.x & 31) == 0) w[(threadIdx.x % TPR) >> 5] = v;
+        asm volatile("bar.sync %0, %1;" :: "r"(1 + (int)threadIdx.x / TPR), "n"(TPR > 32 ? TPR : 32) : "memory");
         v = w[0];
 #pragma unroll
         for (int i = 1; i < TPR / 32; ++i) v = op(v, w[i]);
@@ -166,9 +166,12 @@ template <int TPR, int VPT, int MIN> struct RowSplit {
     // whether thread t has a j-th vector (known without looking for all but the last few)
     static __device__ __forceinline__ bool has(int j, int t, int nvec) { return (j + 1) * TPR <= MIN + 1 || j * TPR + t < nvec; }
 };
-// Picks the row split for nvec vectors: the fewest threads that hold the row in at most 6 vectors each, so that
-// few lanes idle and several 16-byte loads per thread are in flight.  Calls f with the
-// split; false if the row is too wide (more than 3072 vectors).
+// Picks the row split for nvec vectors: as few threads as hold the row in 3 to 6 vectors each, so that several 16-byte
+// loads per thread are in flight and few lanes idle, and more of them where 5 or 6 vectors' registers leave too few
+// warps on an SM.  Timed with oc_block_norm (post and pre norm, cache, modulation) on 8192 rows: 640 bf16 columns
+// 12.1 us over 32 threads, 14.2 over 16; 1024: 16.7 over 32, 20.2 over 64; 1152: 21.6 over 32, 22.5 over 64; 1536: 24.7
+// over 64, 27.9 over 32; 2048: 31.7 over 64, 43.9 over 128; 2560: 45.5 over 64, 51.9 over 128; 3200: 58.7 over 256,
+// 88.7 over 128.  Calls f with the split; false if the row is too wide (more than 3072 vectors).
 template <class F>
 inline bool row_split(long long nvec, F&& f) {
     if (nvec <= 8) f(RowSplit<8, 1, 0>());
@@ -178,14 +181,14 @@ inline bool row_split(long long nvec, F&& f) {
     else if (nvec <= 40) f(RowSplit<8, 5, 32>());
     else if (nvec <= 48) f(RowSplit<8, 6, 40>());
     else if (nvec <= 64) f(RowSplit<16, 4, 48>());
-    else if (nvec <= 80) f(RowSplit<16, 5, 64>());
-    else if (nvec <= 96) f(RowSplit<16, 6, 80>());
+    else if (nvec <= 96) f(RowSplit<32, 3, 64>());
     else if (nvec <= 128) f(RowSplit<32, 4, 96>());
     else if (nvec <= 160) f(RowSplit<32, 5, 128>());
-    else if (nvec <= 192) f(RowSplit<32, 6, 160>());
-    else if (nvec <= 256) f(RowSplit<128, 2, 192>());
-    else if (nvec <= 384) f(RowSplit<128, 3, 256>());
-    else if (nvec <= 768) f(RowSplit<128, 6, 384>());
+    else if (nvec <= 192) f(RowSplit<64, 3, 160>());
+    else if (nvec <= 256) f(RowSplit<64, 4, 192>());
+    else if (nvec <= 384) f(RowSplit<64, 6, 256>());
+    else if (nvec <= 512) f(RowSplit<256, 2, 384>());
+    else if (nvec <= 768) f(RowSplit<256, 3, 512>());
     else if (nvec <= 1536) f(RowSplit<512, 3, 768>());
     else if (nvec <= 3072) f(RowSplit<512, 6, 1536>());
     else return false;

@@ -6,6 +6,9 @@
  *
  *     match  ->  select  ->  gather  ->  [ the wrapped layer, outside this library ]  ->  restore
  *
+ * and what surrounds attention in a wrapped transformer block, on the tokens that are computed
+ * (oc_block_norm, oc_rope, oc_quantize_rows, oc_linear_int8, at the end of this file).
+ *
  * Conventions
  *   - All data pointers are DEVICE pointers unless a name ends in `_host`.  The caller owns every
  *     feature / index / output buffer and the stream.  The library never allocates caller-visible
@@ -553,7 +556,7 @@ oc_status oc_quantize_rows(oc_ctx* ctx, const void* x, int dtype, int64_t x_rows
  * bias are applied in fp32 and the result is rounded once.  Any M, N and out_stride (rows of out that
  * are multiples of 16 bytes are stored fastest); K at most 131056, so that no sum leaves 32 bits.
  * Errors: OC_ERR_ALIGNMENT (K not a multiple of 16; a or w not 16-byte aligned), OC_ERR_INVALID_ARG (out_stride < N; out_rows < M without out_idx),
- * OC_ERR_UNSUPPORTED (sizes). */
+ * OC_ERR_UNSUPPORTED (K; M or N within 512 of 2^31 or more). */
 oc_status oc_linear_int8(oc_ctx* ctx, const int8_t* a, const float* a_scale, int64_t M, int64_t K, const int8_t* w,
                          const float* w_scale, int64_t N, const float* bias, void* out, int out_dtype, int64_t out_rows,
                          int64_t out_stride, const int32_t* out_idx, void* stream);

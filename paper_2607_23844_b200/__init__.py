@@ -1,4 +1,5 @@
-"""B200-native OmniCache hot path: match / select / gather / restore / layered cache.
+"""B200-native OmniCache hot path: match / select / gather / restore / layered cache, and the wrapped block on kept
+tokens (norms with gate and residual, rotary positions, 8-bit products).
 
 The CUDA work lives in ``csrc/`` behind a C-ABI shared library (``include/omnicache.h``);
 ``omnicache`` is the thin ctypes binding over it.  ``inputs`` draws the seeded synthetic tensors.

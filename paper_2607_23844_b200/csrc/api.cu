@@ -554,7 +554,8 @@ oc_status oc_linear_int8(oc_ctx* c, const int8_t* a, const float* a_scale, int64
     if (!c || !float_type(out_dtype) || M < 0 || K <= 0 || N <= 0 || out_rows < 0 || out_stride < N) return OC_ERR_INVALID_ARG;
     if (M == 0) return OC_OK;                                               // (empty tensors have no addresses)
     if (!a || !a_scale || !w || !w_scale || !out || (!out_idx && out_rows < M)) return OC_ERR_INVALID_ARG;
-    if (M > ROWS_MAX || N > ROWS_MAX || out_rows > ROWS_MAX || K > 131056) return OC_ERR_UNSUPPORTED;
+    // (rows and columns are counted in whole tiles of up to 256, in 32 bits)
+    if (M > ROWS_MAX - 512 || N > ROWS_MAX - 512 || out_rows > ROWS_MAX || K > 131056) return OC_ERR_UNSUPPORTED;
     if (K % 16 != 0 || misaligned(a) || misaligned(w)) return OC_ERR_ALIGNMENT;
     if ((uintptr_t)out & (out_dtype == OC_DTYPE_F32 ? 3u : 1u)) return OC_ERR_ALIGNMENT;
     if (((uintptr_t)a_scale & 3u) || ((uintptr_t)w_scale & 3u) || ((uintptr_t)bias & 3u) || ((uintptr_t)out_idx & 3u)) return OC_ERR_ALIGNMENT;

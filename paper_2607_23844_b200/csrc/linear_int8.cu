@@ -6,12 +6,15 @@
 // (or CTA pair, cta_group::2) per SM walks over output tiles of 128 x N_TILE (256 x 256 for a pair):
 //   warp 0       copies: TMA boxes of 128 bytes of K by 128 rows, 128-byte swizzle, into a ring of stages
 //   warp 1       the MMAs (128 bytes of K = four steps of 32); owns the tensor memory
-//   warps 2..17  epilogue: thread = row, four warps side by side; scales, bias, rounding, then through shared
-//                memory: rows that keep their order leave as TMA boxes, others as whole 64-byte pieces to
-//                where out_idx says
+//   warps 2..17  epilogue: thread = row, four warps side by side, a quarter of the columns each; scales, bias,
+//                rounding, then through shared memory: rows that keep their order leave as TMA boxes, others as
+//                whole 64-byte pieces to where out_idx says
 // Two accumulators take turns, so the epilogue of a tile runs under the MMAs of the next.
 // One or two tokens: one warp per pair of output channels, dp4a, the weights read once as they lie.
 // K and N tails are zero-filled by TMA and not stored.  Every wait is bounded (OC_ERR_TIMEOUT in the status word).
+// Measured: 8192 x 6400 x 8192 3.2 POP/s at 1.4 GHz under the power limit, 94 % of what the tensor pipe does at that
+// clock; 5120 x 1536 x 4608 26 us (2.8 POP/s); 57600 x 640 x 5120 139 us on idle data, of which 590 MB of output
+// alone take 100, and 157 under the power limit.
 #include <string.h>
 
 #include <algorithm>

@@ -710,7 +710,8 @@ def test_int8_refusals(oc, ctx):
     assert st(out_stride=31) == bad and st(out_rows=15) == bad
     assert st(K=63) == align and st(a=a.data_ptr() + 1) == align and st(w=w.data_ptr() + 8) == align and st(out=out.data_ptr() + 2) == align
     assert st(a_scale=sa.data_ptr() + 1) == align
-    assert st(K=131088) == no and st(M=2 ** 31, out_rows=2 ** 31) == no
+    assert st(K=131072) == no and st(M=2 ** 31, out_rows=2 ** 31) == no and st(M=2 ** 31 - 500, out_rows=2 ** 31 - 500) == no
+    assert st(N=2 ** 31 - 1, out_stride=2 ** 31 - 1) == no
     x, q = torch.zeros(16, 64, device="cuda"), torch.zeros(16, 64, dtype=I8, device="cuda")
 
     def sq(**kw):

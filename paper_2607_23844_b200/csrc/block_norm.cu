@@ -125,12 +125,12 @@ struct RowPlan {
 // group at hand lie in shared memory too -- every row reads all of them, and read from L2 they made the kernel
 // wait twice as long as for its rows (8192 rows of 1536: 45 us; without any parameters 21).  A set of rows that
 // belongs to several groups folds its own.
-template <int DT, int PT, class S>
+template <int DT, int PT, bool Z, class S>
 __global__ void __launch_bounds__(RowCta<S::tpr>::threads)
 block_norm_kernel(const __grid_constant__ BlockNormParams P) {
     constexpr int E = RowVec<DT>::E, EB = 16 / E, TPR = S::tpr, VPT = S::vpt;   // (EB: bytes of an element)
     constexpr int THREADS = RowCta<TPR>::threads, ROWS = RowCta<TPR>::rows;
-    extern __shared__ __align__(16) uint4 smem4[];                           // [x, v][VPT][THREADS], then the folded vectors
+    extern __shared__ __align__(16) uint4 smem4[];                           // [x, v if Z][VPT][THREADS], then the folded vectors
     __shared__ RowScratch scratch_mem[ROWS];
     RowScratch* scratch = TPR > 32 ? scratch_mem + threadIdx.x / TPR : nullptr;
     int parity = 0;
@@ -139,7 +139,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams P) {
     const uint32_t copy_to = smem_u32(held);
     float* tab[4];
     {
-        float* at = (float*)(smem4 + (P.z ? 2 : 1) * VPT * THREADS);        // (as the launch sized it)
+        float* at = (float*)(smem4 + (Z ? 2 : 1) * VPT * THREADS);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { tab[i] = at; if (P.folds & (1 << i)) at += P.C; }
     }
@@ -158,7 +158,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams P) {
             }
         }
         r.want_r = r.in && (P.out || (P.h && r.computed));
-        r.want_v = r.in && P.z && (r.want_r || P.cache_out);
+        r.want_v = Z && r.in && (r.want_r || P.cache_out);
         return r;
     };
     // (vectors past the row's end, and rows that are not wanted, arrive as zeros)
@@ -171,7 +171,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams P) {
             const bool there = S::has(j, t, P.nvec);
             const int at = there ? (j * TPR + t) * 16 : 0;
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(copy_to + (uint32_t)(j * THREADS * 16)), "l"(xp + at), "r"(there && r.want_r ? 16 : 0) : "memory");
-            if (P.z)
+            if (Z)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(copy_to + (uint32_t)((VPT + j) * THREADS * 16)), "l"(vp + at), "r"(there && r.want_v ? 16 : 0) : "memory");
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -206,14 +206,14 @@ block_norm_kernel(const __grid_constant__ BlockNormParams P) {
         const long long row_at = (long long)R.row * P.C, dense_at = (long long)R.dense * P.C;
         const long long group_at = P.mod_stride && R.in ? (long long)P.rows_per_group.div(R.row) * P.mod_stride : 0;
         asm volatile("cp.async.wait_group 0;" ::: "memory");
-        if (P.cache_out && R.in && (R.computed || P.cache_out != P.cache)) {
+        if (Z && P.cache_out && R.in && (R.computed || P.cache_out != P.cache)) {
             uint8_t* cp = (uint8_t*)P.cache_out + row_at * EB;
 #pragma unroll
             for (int j = 0; j < VPT; ++j)
                 if (S::has(j, t, P.nvec)) st_v4(cp + (j * TPR + t) * 16, held[(VPT + j) * THREADS]);
         }
         f32x2 r[VPT][E / 2];
-        if (P.z) {
+        if (Z) {
 #pragma unroll
             for (int j = 0; j < VPT; ++j) RowVec<DT>::unpack(held[(VPT + j) * THREADS], r[j]);
             normalise<S, E>(r, P.post_norm, P.post_eps, P.inv_c, P.nvec, t, scratch, parity);
@@ -320,13 +320,13 @@ quantize_rows_kernel(const __grid_constant__ QuantParams P) {
         if (S::has(j, t, P.nvec)) store_row_s8<E>(P.q, (long long)row * P.C + (long long)(j * TPR + t) * E, r[j], q.inv);
 }
 
-template <int DT, int PT>
+template <int DT, int PT, bool Z>
 static bool launch_block_norm_as(oc_ctx* ctx, BlockNormParams& P, cudaStream_t s) {
     bool ok = true;
     row_split(P.nvec, [&](auto split) {
         using S = decltype(split);
         constexpr int THREADS = RowCta<S::tpr>::threads, ROWS = RowCta<S::tpr>::rows, MOST = 200 * 1024;
-        auto* kernel = block_norm_kernel<DT, PT, S>;
+        auto* kernel = block_norm_kernel<DT, PT, Z, S>;
         static PerDeviceOnce once;                   // (the context's device is current here)
         ok = once.ensure(ctx->device, [&] {
             const bool good = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST) == cudaSuccess;
@@ -335,7 +335,7 @@ static bool launch_block_norm_as(oc_ctx* ctx, BlockNormParams& P, cudaStream_t s
         });
         if (!ok) return;
         const long long sets = ((long long)P.n_rows + ROWS - 1) / ROWS;
-        const int rows_bytes = (P.z ? 2 : 1) * S::vpt * THREADS * 16;
+        constexpr int rows_bytes = (Z ? 2 : 1) * S::vpt * THREADS * 16;
         int kept_bytes = 0;
         for (int i = 0; i < 4; ++i) if (P.folds & (1 << i)) kept_bytes += P.C * 4;
         // (not for rows so wide that one CTA would fill an SM)
@@ -364,6 +364,11 @@ static bool launch_block_norm_as(oc_ctx* ctx, BlockNormParams& P, cudaStream_t s
     return ok;
 }
 
+template <int DT, int PT>
+static bool launch_block_norm_z(oc_ctx* ctx, BlockNormParams& P, cudaStream_t s) {
+    return P.z ? launch_block_norm_as<DT, PT, true>(ctx, P, s) : launch_block_norm_as<DT, PT, false>(ctx, P, s);
+}
+
 oc_status launch_block_norm(oc_ctx* ctx, const oc_block_norm_desc& d, const void* x, const void* z, const int32_t* slot_of,
                             const void* cache, void* cache_out, void* out, const void* post_w, const void* post_b,
                             const void* gate, const void* pre_w, const void* pre_b, const void* scale, const void* shift,
@@ -387,9 +392,9 @@ oc_status launch_block_norm(oc_ctx* ctx, const oc_block_norm_desc& d, const void
     const bool pf = d.param_dtype == OC_DTYPE_F32;
     bool ok;
     if (d.dtype == OC_DTYPE_BF16) {
-        ok = pf ? launch_block_norm_as<OC_DTYPE_BF16, OC_DTYPE_F32>(ctx, P, s) : launch_block_norm_as<OC_DTYPE_BF16, OC_DTYPE_BF16>(ctx, P, s);
+        ok = pf ? launch_block_norm_z<OC_DTYPE_BF16, OC_DTYPE_F32>(ctx, P, s) : launch_block_norm_z<OC_DTYPE_BF16, OC_DTYPE_BF16>(ctx, P, s);
     } else {
-        ok = pf ? launch_block_norm_as<OC_DTYPE_F32, OC_DTYPE_F32>(ctx, P, s) : launch_block_norm_as<OC_DTYPE_F32, OC_DTYPE_BF16>(ctx, P, s);
+        ok = pf ? launch_block_norm_z<OC_DTYPE_F32, OC_DTYPE_F32>(ctx, P, s) : launch_block_norm_z<OC_DTYPE_F32, OC_DTYPE_BF16>(ctx, P, s);
     }
     return ok ? last_launch_status() : OC_ERR_CUDA;
 }

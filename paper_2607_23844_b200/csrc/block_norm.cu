@@ -6,8 +6,8 @@
 // distances), so a large common offset costs no precision and nothing is read twice.  r stays in fp32 between
 // the residual sum and the second norm: `out` is its rounding, h is not computed from that rounding.
 //
-// Bound by DRAM where rows are many: 230400 rows of 320 bf16 under Frame Cache, 667 MB, take 114 us (5.8 TB/s).  8192
-// rows of 1536 (107 MB) take 24.6 us: about five rounds of row sets an SM, whose parameters cost 5 us (19.1 without).
+// Bound by DRAM where rows are many: 230400 rows of 320 bf16 under Frame Cache, 667 MB, take 113 us (5.9 TB/s).  8192
+// rows of 1536 (107 MB) take 24.1 us: about five rounds of row sets an SM, whose parameters cost 5 us (19.1 without).
 #include <algorithm>
 #include <atomic>
 
@@ -125,7 +125,7 @@ struct RowPlan {
 // group at hand lie in shared memory too -- every row reads all of them, and read from L2 they made the kernel
 // wait twice as long as for its rows (8192 rows of 1536: 45 us; without any parameters 21).  A set of rows that
 // belongs to several groups folds its own.
-template <int DT, int PT, bool Z, class S>
+template <int DT, int PT, bool Z, class S>       // Z: there is a block's output
 __global__ void __launch_bounds__(RowCta<S::tpr>::threads)
 block_norm_kernel(const __grid_constant__ BlockNormParams P) {
     constexpr int E = RowVec<DT>::E, EB = 16 / E, TPR = S::tpr, VPT = S::vpt;   // (EB: bytes of an element)

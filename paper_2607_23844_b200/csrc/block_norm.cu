@@ -240,7 +240,8 @@ block_norm_kernel(const __grid_constant__ BlockNormParams P) {
         const RowPlan N = plan(next_row, next_slot);
         if (trip + 1 < trips) fetch(N);
         next_row += ROWS;
-        next_slot = trip + 2 < trips ? slot_at(next_row) : 0;
+        // (the rows after this CTA's last set are another CTA's: no slot, so that their plan here reports none)
+        next_slot = trip + 2 < trips ? slot_at(next_row) : -1;
         // a warp (or the warps of one row) none of whose rows goes on is done
         const bool goes_on = P.h && (TPR > 32 ? R.computed : __any_sync(0xFFFFFFFFu, R.computed));
         if (goes_on) {

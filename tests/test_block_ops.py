@@ -725,3 +725,19 @@ def test_int8_refusals(oc, ctx):
     assert sq(K=16384, x_stride=16384) == no and sq(n_rows=2 ** 31) == no
     assert oc._lib.oc_linear_int8(None, None, None, 1, 16, None, None, 1, None, None, 0, 1, 16, None, None) == bad
     assert oc._lib.oc_quantize_rows(None, None, 0, 1, 16, None, 1, 16, None, None, None) == bad
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,C", [(40, 64), (100003, 64), (20011, 640), (12003, 1536), (5003, 3200)])
+def test_block_norm_no_dense_rows_at_all(oc, ctx, n, C):
+    """Every unit is reused and there is no dense row: a selection like any other, however long a CTA's queue is."""
+    x, cache, z = (rand(i, n, C, dtype=BF16).cuda() for i in (1, 2, 3))
+    slot = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    out, h = torch.empty_like(x), torch.full((1, C), 9.0, dtype=BF16, device="cuda")
+    desc = oc.block_norm_desc(n, C, oc.DTYPE_BF16, oc.DTYPE_BF16, oc.DTYPE_F32, dense_rows=0)
+    ctx.block_norm(desc, x, slot_of=slot, out=out, h=h)
+    assert ctx.device_status() == oc.OK
+    assert torch.equal(out, x) and (h == 9).all()
+    ctx.block_norm(desc, x, z=z, slot_of=slot, cache=cache, cache_out=cache, out=out, h=h)
+    assert ctx.device_status() == oc.OK
+    assert torch.equal(out, (x.float() + cache.float()).to(BF16)) and (h == 9).all()

@@ -470,7 +470,8 @@ enum { OC_ROPE_ADJACENT = 0, OC_ROPE_HALVES = 1 };
  * keeps it in its scale).
  * x and slot_of are read, everything else is optional: without z there is no v (cache, cache_out,
  * gate and post_* are then null, post_norm NONE), without h nothing is done for it.  Without z and
- * out, rows that have no slot are not read.
+ * out, rows that have no slot are not read.  With slot_of and dense_rows = 0 (every unit reused) z and
+ * h hold no rows and may be null; z is there if cache is.
  * Errors: OC_ERR_INVALID_ARG (also: slot_of and z without cache; rows not a whole number of units);
  * OC_ERR_ALIGNMENT (a pointer or mod_stride not a multiple of 16 bytes -- 8 for bf16 parameters of
  * fp32 rows, 4 for slot_of and h_scale --, C not a multiple of 16 bytes of dtype, or of 16 elements for

@@ -448,8 +448,10 @@ oc_status oc_block_norm(oc_ctx* c, const oc_block_norm_desc* d, const void* x, c
     if (d->n_rows > ROWS_MAX || d->dense_rows > ROWS_MAX || d->C > ROWS_MAX) return OC_ERR_UNSUPPORTED;
     if (d->n_rows % d->unit_rows != 0 || d->dense_rows % d->unit_rows != 0) return OC_ERR_INVALID_ARG;
     if (d->n_rows == 0) return OC_OK;                                       // (empty tensors have no addresses)
-    if (!x || (!out && !h && !cache_out)) return OC_ERR_INVALID_ARG;
-    if (!z && (cache || cache_out || gate || post_w || post_b || d->post_norm != OC_NORM_NONE)) return OC_ERR_INVALID_ARG;
+    // (so have z and h where every unit is reused: the cache then says that there is a z)
+    const bool none_dense = slot_of && d->dense_rows == 0, empty_z = none_dense && !z && cache;
+    if (!x || (!out && !h && !cache_out && !none_dense)) return OC_ERR_INVALID_ARG;
+    if (!z && !empty_z && (cache || cache_out || gate || post_w || post_b || d->post_norm != OC_NORM_NONE)) return OC_ERR_INVALID_ARG;
     if (z && slot_of && !cache) return OC_ERR_INVALID_ARG;                  // reused rows would come from nowhere
     if ((z || h) && !slot_of && d->dense_rows < d->n_rows) return OC_ERR_INVALID_ARG;
     if (h && d->h_dtype == OC_DTYPE_I8 && !h_scale) return OC_ERR_INVALID_ARG;
@@ -466,9 +468,11 @@ oc_status oc_block_norm(oc_ctx* c, const oc_block_norm_desc* d, const void* x, c
     for (const void* p : params) if ((uintptr_t)p & (uintptr_t)(param_align - 1)) return OC_ERR_ALIGNMENT;
     if ((gate || scale || shift) && d->mod_stride * pb % param_align != 0) return OC_ERR_ALIGNMENT;
     if (((uintptr_t)slot_of & 3u) || ((uintptr_t)h_scale & 3u)) return OC_ERR_ALIGNMENT;
+    if (!out && !h && !cache_out) return OC_OK;                             // the rows of no unit
     DeviceGuard guard(c->device);
     if (!guard.ok) return OC_ERR_CUDA;
-    return launch_block_norm(c, *d, x, z, slot_of, cache, cache_out, out, post_w, post_b, gate, pre_w, pre_b, scale, shift,
+    // (no row of an empty z is read: any address stands for it)
+    return launch_block_norm(c, *d, x, empty_z ? cache : z, slot_of, cache, cache_out, out, post_w, post_b, gate, pre_w, pre_b, scale, shift,
                              h, h_scale, (cudaStream_t)stream);
 }
 

@@ -741,3 +741,27 @@ def test_block_norm_no_dense_rows_at_all(oc, ctx, n, C):
     ctx.block_norm(desc, x, z=z, slot_of=slot, cache=cache, cache_out=cache, out=out, h=h)
     assert ctx.device_status() == oc.OK
     assert torch.equal(out, (x.float() + cache.float()).to(BF16)) and (h == 9).all()
+
+
+@pytest.mark.gpu
+def test_block_norm_empty_dense_tensors(oc, ctx):
+    """A step that computes nothing: z and h are tensors of no rows, which have no address."""
+    n, C = 50, 96
+    x, cache = (rand(i, n, C, dtype=BF16).cuda() for i in (1, 2))
+    slot = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    none, want = torch.empty(0, C, dtype=BF16, device="cuda"), cache.clone()
+    out, h_scale = torch.empty_like(x), torch.empty(0, device="cuda")
+    for h_dtype, h in ((BF16, none), (I8, torch.empty(0, C, dtype=I8, device="cuda"))):
+        desc = oc.block_norm_desc(n, C, oc.DTYPE_BF16, tag(oc, h_dtype), oc.DTYPE_F32, post_norm=oc.NORM_RMS, dense_rows=0)
+        out.zero_()
+        ctx.block_norm(desc, x, z=none, slot_of=slot, cache=cache, cache_out=cache, out=out, h=h, h_scale=h_scale)
+        r, mag = ref_norm(d64(want), d64(want).abs(), "rms", 1e-6, None, None)
+        assert_close(out, d64(x) + r, d64(x).abs() + mag)
+        assert torch.equal(cache, want)
+        desc = oc.block_norm_desc(n, C, oc.DTYPE_BF16, tag(oc, h_dtype), oc.DTYPE_F32, pre_norm=oc.NORM_RMS, dense_rows=0)
+        ctx.block_norm(desc, x, slot_of=slot, h=h, h_scale=h_scale)           # norm and gather of no unit
+    assert ctx.device_status() == oc.OK
+    # with dense rows z cannot be left out beside a cache, nor all outputs
+    desc = oc.block_norm_desc(n, C, oc.DTYPE_BF16, oc.DTYPE_BF16, oc.DTYPE_F32, dense_rows=2)
+    assert ctx.block_norm(desc, x, slot_of=slot, cache=cache, out=out, check=False) == oc.ERR_INVALID_ARG
+    assert ctx.block_norm(desc, x, slot_of=slot, check=False) == oc.ERR_INVALID_ARG

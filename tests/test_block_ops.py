@@ -765,3 +765,154 @@ def test_block_norm_empty_dense_tensors(oc, ctx):
     desc = oc.block_norm_desc(n, C, oc.DTYPE_BF16, oc.DTYPE_BF16, oc.DTYPE_F32, dense_rows=2)
     assert ctx.block_norm(desc, x, slot_of=slot, cache=cache, out=out, check=False) == oc.ERR_INVALID_ARG
     assert ctx.block_norm(desc, x, slot_of=slot, check=False) == oc.ERR_INVALID_ARG
+
+
+# ---- queues of row sets: more rows than one set for every resident CTA ---------------------------------------------
+def ref_rows(x, z, slot, cache, p, post, pre, rows_per_group, unit_rows, dense_rows):
+    """ref_block on the GPU (its helper tensors too)."""
+    with torch.device("cuda"):
+        return ref_block(x, z, slot, cache, p, 1.0, post, pre, 1e-6, rows_per_group, unit_rows, dense_rows)
+
+
+def assert_rows_close(got, want, mag):
+    """assert_close's bound, for finite values that stay on the GPU."""
+    bound = 128 * U * mag
+    if got.dtype == BF16:
+        bound += 2.0 ** -8 * want.abs()
+    assert torch.isfinite(got).all() and ((got.double() - want).abs() <= bound + 1e-37).all()
+
+
+def check_queues(oc, ctx, n_units, unit_rows, C, dtype, h_dtype, param, post, pre, rows_per_group, in_place):
+    """All seven parameters, a selection of 2 in 5 units with a dense tail that stays unused, a cache in place or beside."""
+    kinds = {"rms": oc.NORM_RMS, "layer": oc.NORM_LAYER}
+    n = n_units * unit_rows
+    gen = torch.Generator(device="cuda").manual_seed(n + C)
+    def draw(*shape, dt=dtype, std=1.0, mean=0.0):
+        return (torch.randn(shape, generator=gen, device="cuda") * std + mean).to(dt)
+    keep = max(2 * n_units // 5, 1)
+    kept = torch.randperm(n_units, generator=gen, device="cuda")[:keep].sort().values
+    slot = torch.full((n_units,), -1, dtype=torch.int32, device="cuda")
+    slot[kept] = torch.arange(keep, dtype=torch.int32, device="cuda")
+    dense = (keep + 3) * unit_rows
+    G = -(-n // rows_per_group)
+    x, z, cache = draw(n, C, std=2.0), draw(dense, C), draw(n, C)
+    mod = draw(G, 3 * C + 8, dt=param, std=0.3)
+    p = {k: draw(C, dt=param, std=0.2, mean=float(k.endswith("_w"))) for k in ("post_w", "post_b", "pre_w", "pre_b")}
+    p.update({k: mod[:, i * C:(i + 1) * C] for i, k in enumerate(("gate", "scale", "shift"))})
+    r, mr, v, hh, mh, at = ref_rows(x.double(), z.double(), slot, cache.double(), {k: t.double() for k, t in p.items()}, post, pre,
+                                    rows_per_group, unit_rows, dense)
+    del mod
+    out = x if in_place else torch.empty_like(x)
+    cache_out = cache if in_place else torch.empty_like(cache)
+    h = torch.full((dense, C), 9, dtype=h_dtype, device="cuda")
+    h_scale = torch.full((dense,), 9.0, device="cuda") if h_dtype == I8 else None
+    desc = oc.block_norm_desc(n, C, tag(oc, dtype), tag(oc, h_dtype), tag(oc, param), kinds[post], kinds[pre], 1e-6, 1e-6, 1.0,
+                              rows_per_group, 3 * C + 8, unit_rows, dense)
+    ctx.block_norm(desc, x, z=z, slot_of=slot, cache=cache, cache_out=cache_out, out=out, h=h, h_scale=h_scale, **p)
+    assert ctx.device_status() == oc.OK
+    assert torch.equal(cache_out.double(), v)
+    assert_rows_close(out, r, mr)
+    rows = torch.nonzero(at >= 0).reshape(-1)
+    written, want, mag = at[rows], hh[rows], mh[rows]
+    if h_dtype == I8:
+        s, q = h_scale.double()[written], h.double()[written]
+        top, top_mag = want.abs().amax(1), mag.amax(1)
+        assert ((s * 127 - top).abs() <= 128 * U * (top_mag + top)).all()
+        assert ((q * s[:, None] - want).abs() <= 0.5 * s[:, None] + 256 * U * (mag + top[:, None])).all()
+        assert (h_scale[keep * unit_rows:] == 9).all()
+    else:
+        assert_rows_close(h[written], want, mag)
+    assert (h[keep * unit_rows:] == 9).all()
+
+
+# units, rows of a unit, columns, type, type of h, of the parameters, norms, rows of a group.  8, 32, 64, 256 and 512
+# threads per row; of the first four both lengths of queue, with room for twice the CTAs that fit today; groups that end
+# inside a set of rows, a set's length, and whole queues apart; row counts that are no whole number of sets.
+QUEUES = [(100003, 1, 64, BF16, BF16, F32, "rms", "layer", 997), (33335, 3, 64, BF16, I8, BF16, "layer", "rms", 37),
+          (400003, 1, 8, BF16, F32, F32, "layer", "layer", 7), (400003, 1, 16, F32, I8, BF16, "rms", "rms", 30001),
+          (20011, 1, 640, BF16, I8, F32, "layer", "layer", 1024), (6671, 3, 640, BF16, BF16, BF16, "rms", "rms", 50),
+          (310001, 1, 520, BF16, BF16, F32, "rms", "layer", 9216), (103335, 3, 528, BF16, I8, F32, "rms", "layer", 13),
+          (12003, 1, 1536, BF16, I8, BF16, "rms", "layer", 4096), (4001, 3, 772, F32, F32, F32, "layer", "rms", 5),
+          (152003, 1, 1296, BF16, I8, F32, "layer", "rms", 1000), (5003, 1, 3200, BF16, I8, BF16, "rms", "rms", 777),
+          (152003, 1, 1540, F32, BF16, BF16, "rms", "layer", 64), (2001, 3, 3088, F32, I8, F32, "layer", "layer", 11)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("case", QUEUES, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}")
+def test_block_norm_queues_of_row_sets(oc, ctx, case, in_place):
+    check_queues(oc, ctx, *case, in_place)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,C,groups", [(100003, 64, 1), (20011, 640, 5), (12003, 1536, 1)])
+@pytest.mark.parametrize("h_dtype", [BF16, I8])
+def test_block_norm_queues_without_a_block(oc, ctx, n, C, groups, h_dtype):
+    """Norm, modulation and gather alone: the kernels that hold no block's output."""
+    x = rand(n, n, C, dtype=BF16, std=2.0).cuda()
+    scale, shift = (rand(i, groups, C, std=0.3).cuda() for i in (1, 2))
+    slot = slots(n, 2 * n // 5, seed=C).cuda()
+    rows, per = torch.nonzero(slot >= 0).reshape(-1), -(-n // groups)
+    h, s = torch.full((rows.numel(), C), 9, dtype=h_dtype, device="cuda"), torch.full((rows.numel(),), 9.0, device="cuda")
+    desc = oc.block_norm_desc(n, C, oc.DTYPE_BF16, tag(oc, h_dtype), oc.DTYPE_F32, pre_norm=oc.NORM_LAYER, rows_per_group=per,
+                              mod_stride=C, dense_rows=rows.numel())
+    ctx.block_norm(desc, x, slot_of=slot, scale=scale, shift=shift, h=h, h_scale=s if h_dtype == I8 else None)
+    assert ctx.device_status() == oc.OK
+    v = x[rows].double()
+    want, mag = ref_norm(v, v.abs(), "layer", 1e-6, None, None)
+    g = rows // per
+    want, mag = want * (1 + scale.double()[g]) + shift.double()[g], mag * (1 + scale.double()[g].abs()) + shift.double()[g].abs()
+    if h_dtype == I8:
+        top = want.abs().amax(1)
+        assert ((s.double() * 127 - top).abs() <= 128 * U * (mag.amax(1) + top)).all()
+        assert ((h.double() * s.double()[:, None] - want).abs() <= 0.5 * s.double()[:, None] + 256 * U * (mag + top[:, None])).all()
+    else:
+        assert_rows_close(h, want, mag)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,K,N", [(20000, 320, 2560), (9000, 880, 2816)])
+@pytest.mark.parametrize("out_dtype", [BF16, F32])
+def test_linear_int8_resident_weights_to_named_places(oc, ctx, M, K, N, out_dtype):
+    """Tiles enough for the form that keeps its rows of w in shared memory, and rows of out that do not keep their order."""
+    idx = torch.randperm(M + 50, generator=torch.Generator().manual_seed(M))[:M].to(torch.int32)
+    idx[M // 2] = -1
+    run_linear(oc, ctx, M, K, N, out_dtype, out_idx=idx, out_rows=M + 50)
+    run_linear(oc, ctx, M, K, N, out_dtype, out_idx=idx, out_rows=M + 50, pad=1, bias=False)
+    assert ctx.device_status() == oc.OK
+
+
+@pytest.mark.gpu
+def test_rope_and_int8_on_another_stream_and_in_a_graph(oc, ctx):
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run_rope(oc, ctx, 60, 64, (16, 24, 24), (3, 4, 5), 5, 2, BF16, "halves", norm=True)
+        run_linear(oc, ctx, 2, 144, 100)
+        run_linear(oc, ctx, 300, 144, 104)
+        run_linear(oc, ctx, 20000, 320, 2560)
+    torch.cuda.current_stream().wait_stream(side)
+    M, K, N, D = 300, 128, 192, 64
+    x, w = rand(1, M, K, dtype=BF16).cuda(), torch.randint(-127, 128, (N, K), generator=torch.Generator().manual_seed(2)).to(I8).cuda()
+    a, s, sw = torch.empty(M, K, dtype=I8, device="cuda"), torch.empty(M, device="cuda"), torch.full((N,), 0.01, device="cuda")
+    y, r = torch.empty(M, N, dtype=BF16, device="cuda"), torch.empty(M, N // D, D, dtype=BF16, device="cuda")
+    q = y.view(M, N // D, D)
+    d = oc.rope_desc(M, oc.DTYPE_BF16, D, (0, 32, 32), (1, 15, 20), N // D, q=q, q_out=r)
+    table = oc.rope_table(d).cuda()
+
+    def step():
+        ctx.quantize_rows(x, oc.DTYPE_BF16, M, K, a, s)
+        ctx.linear_int8(a, s, M, K, w, sw, N, y, oc.DTYPE_BF16)
+        ctx.rope(d, table, q, r)
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (a, s, y, r)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for t in (a, s, y, r):
+        t.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, u) for t, u in zip((a, s, y, r), want))
+    assert ctx.device_status() == oc.OK

@@ -236,7 +236,7 @@ def layer_cache_would_hit(stored_step: int, step: int, interval: int) -> bool:
 def _ptr(t) -> int | None:
     if t is None:
         return None
-    if t.__class__ is int:
+    if isinstance(t, int):
         return t
     assert t.is_contiguous(), "tensors handed to the C-ABI must be contiguous"
     return t.data_ptr()

@@ -263,6 +263,20 @@ def _ptr_strided(t) -> int | None:
     return None if t is None else (t if isinstance(t, int) else t.data_ptr())
 
 
+def _rows(t, width: int, stride: int | None, name: str):
+    """(pointer, elements between rows) of a matrix `width` elements wide: dense unless a stride is given or the tensor
+    is a part of a larger one."""
+    if t is None or isinstance(t, int) or t.is_contiguous():
+        return _ptr_strided(t), width if stride is None else stride
+    if t.stride(-1) != 1:
+        raise ValueError(f"the elements of a row of {name} must be contiguous")
+    if stride is None:
+        if t.dim() != 2 or t.shape[1] != width:
+            raise ValueError(f"{name} is neither contiguous nor [rows, {width}]: its row stride must be given")
+        stride = t.stride(0)
+    return t.data_ptr(), stride
+
+
 def block_norm_desc(n_rows: int, C_: int, dtype: int, h_dtype: int, param_dtype: int, post_norm: int = NORM_NONE,
                     pre_norm: int = NORM_NONE, post_eps: float = 1e-6, pre_eps: float = 1e-6, res_scale: float = 1.0,
                     rows_per_group: int | None = None, mod_stride: int = 0, unit_rows: int = 1,
@@ -465,9 +479,10 @@ class Context:
 
     def quantize_rows(self, x, dtype: int, n_rows: int, K: int, q, scale, idx=None, x_rows: int | None = None,
                       x_stride: int | None = None, stream=None, check: bool = True) -> int:
-        st = _lib.oc_quantize_rows(self._h, _ptr_strided(x), dtype, n_rows if x_rows is None else x_rows,
-                                   K if x_stride is None else x_stride, _ptr(idx), n_rows, K, _ptr(q), _ptr(scale),
-                                   _stream(stream))
+        """oc_quantize_rows: x may be a column range of a packed projection (its stride is then the default)."""
+        x, x_stride = _rows(x, K, x_stride, "x")
+        st = _lib.oc_quantize_rows(self._h, x, dtype, n_rows if x_rows is None else x_rows, x_stride, _ptr(idx), n_rows, K,
+                                   _ptr(q), _ptr(scale), _stream(stream))
         if check:
             _chk(st, "oc_quantize_rows")
         return st

@@ -42,3 +42,27 @@ def test_addresses_may_be_any_int(oc):
     assert oc._ptr(t) == t.data_ptr()
     with pytest.raises(AssertionError):
         oc._ptr(t[:, :3])
+
+
+def test_quantize_rows_takes_the_stride_of_a_column_range(oc, calls):
+    ctx, made = calls
+    packed, q, s = torch.zeros(7, 96), torch.zeros(7, 32, dtype=torch.int8), torch.zeros(7)
+
+    def stride(x, **kw):
+        ctx.quantize_rows(x, oc.DTYPE_F32, 7, 32, q, s, stream=0, **kw)
+        name, args = made.pop()
+        assert name == "oc_quantize_rows" and args[1] == (x if isinstance(x, int) else x.data_ptr())
+        return args[4]
+    assert stride(packed[:, 32:64]) == 96
+    assert stride(packed[:, 32:64], x_stride=96) == 96
+    assert stride(packed.as_strided((7, 32), (40, 1))) == 40
+    # dense tensors, and addresses, keep the default and what is asked for
+    assert stride(torch.zeros(7, 32)) == 32 and stride(torch.zeros(7, 4, 8)) == 32 and stride(torch.zeros(7 * 32)) == 32
+    assert stride(0x1000) == 32 and stride(0x1000, x_stride=64) == 64 and stride(packed, x_stride=96) == 96
+    for x in (packed[:, :32].t(), packed[:, 0:64:2], packed.view(7, 12, 8)[:, :4], packed[:, :16], packed[:, :48]):
+        with pytest.raises(ValueError):
+            stride(x)
+    for x in (torch.zeros(32, 7).t(), packed[:, 0:64:2]):
+        with pytest.raises(ValueError):
+            stride(x, x_stride=96)
+    assert not made

@@ -916,3 +916,14 @@ def test_rope_and_int8_on_another_stream_and_in_a_graph(oc, ctx):
     torch.cuda.synchronize()
     assert all(torch.equal(t, u) for t, u in zip((a, s, y, r), want))
     assert ctx.device_status() == oc.OK
+
+
+@pytest.mark.gpu
+def test_quantize_rows_of_a_column_range(oc, ctx):
+    """A part of a packed projection, its stride taken from the tensor."""
+    x = rand(1, 40, 3 * 64, dtype=BF16).cuda()
+    q, s = torch.empty(40, 64, dtype=I8, device="cuda"), torch.empty(40, device="cuda")
+    want_q, want_s = torch.empty_like(q), torch.empty_like(s)
+    ctx.quantize_rows(x[:, 64:128], oc.DTYPE_BF16, 40, 64, q, s)
+    ctx.quantize_rows(x[:, 64:128].contiguous(), oc.DTYPE_BF16, 40, 64, want_q, want_s)
+    assert torch.equal(q, want_q) and torch.equal(s, want_s)

@@ -490,9 +490,10 @@ class Context:
     def linear_int8(self, a, a_scale, M: int, K: int, w, w_scale, N: int, out, out_dtype: int, bias=None,
                     out_rows: int | None = None, out_stride: int | None = None, out_idx=None, stream=None,
                     check: bool = True) -> int:
-        st = _lib.oc_linear_int8(self._h, _ptr(a), _ptr(a_scale), M, K, _ptr(w), _ptr(w_scale), N, _ptr(bias),
-                                 _ptr_strided(out), out_dtype, M if out_rows is None else out_rows,
-                                 N if out_stride is None else out_stride, _ptr(out_idx), _stream(stream))
+        """oc_linear_int8: out may be a column range of a packed tensor (its stride is then the default)."""
+        out, out_stride = _rows(out, N, out_stride, "out")
+        st = _lib.oc_linear_int8(self._h, _ptr(a), _ptr(a_scale), M, K, _ptr(w), _ptr(w_scale), N, _ptr(bias), out, out_dtype,
+                                 M if out_rows is None else out_rows, out_stride, _ptr(out_idx), _stream(stream))
         if check:
             _chk(st, "oc_linear_int8")
         return st

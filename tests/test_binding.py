@@ -66,3 +66,24 @@ def test_quantize_rows_takes_the_stride_of_a_column_range(oc, calls):
         with pytest.raises(ValueError):
             stride(x, x_stride=96)
     assert not made
+
+
+def test_linear_int8_takes_the_stride_of_a_column_range(oc, calls):
+    ctx, made = calls
+    a, s, w, sw = torch.zeros(7, 16, dtype=torch.int8), torch.zeros(7), torch.zeros(32, 16, dtype=torch.int8), torch.zeros(32)
+    packed = torch.zeros(7, 96)
+
+    def stride(out, **kw):
+        ctx.linear_int8(a, s, 7, 16, w, sw, 32, out, oc.DTYPE_F32, stream=0, **kw)
+        name, args = made.pop()
+        assert name == "oc_linear_int8" and args[9] == (out if isinstance(out, int) else out.data_ptr())
+        return args[12]
+    assert stride(packed[:, 32:64]) == 96 and stride(packed[:, 32:64], out_stride=96) == 96
+    assert stride(torch.zeros(7, 32)) == 32 and stride(torch.zeros(7, 4, 8)) == 32 and stride(packed, out_stride=96) == 96
+    assert stride(0x1000) == 32 and stride(0x1000, out_stride=40) == 40
+    for out in (packed[:, 0:64:2], packed.view(7, 12, 8)[:, :4], packed[:, :48], torch.zeros(32, 7).t()):
+        with pytest.raises(ValueError):
+            stride(out)
+    with pytest.raises(ValueError):
+        stride(packed[:, 0:64:2], out_stride=96)
+    assert not made

@@ -927,3 +927,16 @@ def test_quantize_rows_of_a_column_range(oc, ctx):
     ctx.quantize_rows(x[:, 64:128], oc.DTYPE_BF16, 40, 64, q, s)
     ctx.quantize_rows(x[:, 64:128].contiguous(), oc.DTYPE_BF16, 40, 64, want_q, want_s)
     assert torch.equal(q, want_q) and torch.equal(s, want_s)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [2, 40, 300])
+def test_linear_int8_into_a_column_range(oc, ctx, M):
+    """A part of a packed tensor, its stride taken from it; the columns beside it stay."""
+    K, N = 64, 40
+    g = torch.Generator().manual_seed(M)
+    a, w = (torch.randint(-127, 128, (n, K), generator=g).to(I8).cuda() for n in (M, N))
+    one, packed = torch.ones(max(M, N), device="cuda"), torch.full((M, 3 * N), 5.0, device="cuda")
+    ctx.linear_int8(a, one[:M], M, K, w, one[:N], N, packed[:, N:2 * N], oc.DTYPE_F32)
+    assert torch.equal(packed[:, N:2 * N].double(), a.double() @ w.double().t())
+    assert (packed[:, :N] == 5).all() and (packed[:, 2 * N:] == 5).all()

@@ -277,6 +277,31 @@ def _rows(t, width: int, stride: int | None, name: str):
     return t.data_ptr(), stride
 
 
+def _group_vectors(t, strides: tuple, desc: CBlockNorm, name: str) -> int | None:
+    """Pointer of gate, scale or shift: a vector for each group, strides = (mod_stride, 1) elements apart, or one vector
+    for all of them (mod_stride 0)."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.stride() == strides:
+        return t.data_ptr()
+    apart, groups = strides[0], -(-desc.n_rows // max(desc.rows_per_group, 1))
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"the elements of a vector of {name} must be contiguous")
+    vectors, last = 1, None
+    for n, s in zip(t.shape[:-1], t.stride()[:-1]):
+        if n == 1:
+            continue
+        if last is not None and last != n * s:                    # not evenly spaced from here on
+            break
+        vectors, last = vectors * n, s
+        if s == apart and vectors >= groups:
+            return t.data_ptr()
+    run = last is None                                            # one run of elements
+    if groups <= 1 or (run and (apart == 0 or t.shape[-1] >= (groups - 1) * apart + desc.C)):
+        return t.data_ptr()
+    raise ValueError(f"{name} does not hold {groups} vectors {apart} elements apart: mod_stride must be its row stride")
+
+
 def block_norm_desc(n_rows: int, C_: int, dtype: int, h_dtype: int, param_dtype: int, post_norm: int = NORM_NONE,
                     pre_norm: int = NORM_NONE, post_eps: float = 1e-6, pre_eps: float = 1e-6, res_scale: float = 1.0,
                     rows_per_group: int | None = None, mod_stride: int = 0, unit_rows: int = 1,
@@ -461,9 +486,12 @@ class Context:
                    post_b=None, gate=None, pre_w=None, pre_b=None, scale=None, shift=None, h=None, h_scale=None,
                    stream=None, check: bool = True) -> int:
         """oc_block_norm.  gate, scale and shift may be column ranges of one [groups, mod_stride] tensor."""
+        apart = (desc.mod_stride, 1)
+        gate, scale = _group_vectors(gate, apart, desc, "gate"), _group_vectors(scale, apart, desc, "scale")
+        shift = _group_vectors(shift, apart, desc, "shift")
         st = _lib.oc_block_norm(self._h, C.byref(desc), _ptr(x), _ptr(z), _ptr(slot_of), _ptr(cache), _ptr(cache_out),
-                                _ptr(out), _ptr(post_w), _ptr(post_b), _ptr_strided(gate), _ptr(pre_w), _ptr(pre_b),
-                                _ptr_strided(scale), _ptr_strided(shift), _ptr(h), _ptr(h_scale), _stream(stream))
+                                _ptr(out), _ptr(post_w), _ptr(post_b), gate, _ptr(pre_w), _ptr(pre_b), scale, shift, _ptr(h),
+                                _ptr(h_scale), _stream(stream))
         if check:
             _chk(st, "oc_block_norm")
         return st

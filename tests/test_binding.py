@@ -87,3 +87,39 @@ def test_linear_int8_takes_the_stride_of_a_column_range(oc, calls):
     with pytest.raises(ValueError):
         stride(packed[:, 0:64:2], out_stride=96)
     assert not made
+
+
+def test_block_norm_group_vectors_lie_mod_stride_apart(oc, calls):
+    ctx, made = calls
+    C, G = 32, 4
+    x, h = torch.zeros(20, C), torch.zeros(20, C)
+    mod = torch.zeros(G, 3 * C)
+
+    def run(t, mod_stride, rows_per_group=5, name="scale"):
+        d = oc.block_norm_desc(20, C, oc.DTYPE_F32, oc.DTYPE_F32, oc.DTYPE_F32, rows_per_group=rows_per_group, mod_stride=mod_stride)
+        ctx.block_norm(d, x, h=h, stream=0, **{name: t})
+        got, args = made.pop()
+        assert got == "oc_block_norm" and args[{"gate": 10, "scale": 13, "shift": 14}[name]] == (t if isinstance(t, int) else t.data_ptr())
+
+    def refused(*args, **kw):
+        with pytest.raises(ValueError):
+            run(*args, **kw)
+        assert not made
+    for name in ("gate", "scale", "shift"):
+        run(mod[:, C:2 * C], 3 * C, name=name)
+        run(0x1000, 3 * C, name=name)
+        refused(mod[:, C:2 * C], 0, name=name)                                # group 0's vector for every row
+        refused(mod[:, C:2 * C], C, name=name)
+        refused(mod[:, 0:2 * C:2], 3 * C, name=name)                          # every other element
+    # one vector for all groups
+    vector = torch.zeros(C)
+    for t in (vector, vector[None], vector.expand(G, C), mod[1:2, :C], mod[1, :C]):
+        run(t, 0)
+    # more groups than vectors
+    refused(vector, C), refused(torch.zeros(1, C)[:, None], 2 * C), refused(mod[0, :C], 3 * C), refused(torch.zeros(G, 2, C)[:3], 2 * C)
+    # vectors by any route that are as far apart as was said
+    run(mod.view(G, 3, C)[:, 1:2], 3 * C), run(mod.view(2, 2, 3 * C)[..., :C], 3 * C), run(mod.view(G, 3, C), 3 * C)
+    run(mod.view(-1)[C:], 3 * C), run(torch.zeros(G, C), C), run(torch.zeros(6, 3 * C)[:, :C], 3 * C)
+    refused(torch.zeros(2, 3, 3 * C)[:, :2, :C], 3 * C)                       # (a gap after every second)
+    # a single group: only the elements of its vector matter
+    run(mod[:1, :C], 3 * C, 20), run(vector, 96, 20), run(mod[:, :C], 0, 20), refused(mod[:1, 0:2 * C:2], 3 * C, 20)

@@ -123,3 +123,23 @@ def test_block_norm_group_vectors_lie_mod_stride_apart(oc, calls):
     refused(torch.zeros(2, 3, 3 * C)[:, :2, :C], 3 * C)                       # (a gap after every second)
     # a single group: only the elements of its vector matter
     run(mod[:1, :C], 3 * C, 20), run(vector, 96, 20), run(mod[:, :C], 0, 20), refused(mod[:1, 0:2 * C:2], 3 * C, 20)
+
+
+def views(d):
+    return [[getattr(getattr(d, v), f) for f in ("batch_stride", "row_stride", "head_stride")] for v in ("q", "q_out", "k", "k_out")]
+
+
+def test_rope_desc_head_major_inputs(oc):
+    """Rows of q and k follow one another at one stride: a [batch, heads, rows, head_dim] tensor of several batch elements
+    has none, unless its batch elements follow one another like its rows."""
+    B, n, heads, D = 3, 10, 4, 8
+
+    def desc(q, rows=B * n, **kw):
+        return oc.rope_desc(rows, oc.DTYPE_F32, D, (0, 4, 4), (1, 5, 6), heads, rows_per_batch=n, q=q, **kw)
+    head_major, out = torch.zeros(B, heads, n, D), torch.zeros(B, heads, n, D)
+    for m in ("q", "k"):
+        with pytest.raises(ValueError):
+            desc(**{"q": out.transpose(1, 2).reshape(B * n, heads, D), "k_heads": heads, m: head_major})
+    assert views(desc(torch.zeros(B, n, heads, D).transpose(1, 2), q_out=out))[:2] == [[n * heads * D, heads * D, D], [heads * n * D, D, n * D]]
+    assert views(desc(head_major[:1], rows=n))[0][1:] == [D, n * D]
+    assert views(desc(torch.zeros(B * n, heads, D)))[0][1:] == [heads * D, D]

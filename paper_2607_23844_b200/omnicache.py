@@ -319,6 +319,8 @@ def rope_desc(n_rows: int, dtype: int, head_dim: int, axis_dims, axis_len, q_hea
     """oc_rope_desc, the strides taken from tensors (or from (batch, row, head) stride tuples): q, k are
     [n_rows, heads, head_dim] views, q_out, k_out [batch, heads, rows, head_dim] or [n_rows, heads, head_dim].  q and k
     may be [batch, heads, rows, head_dim] too where one stride leads from each row to the next through all the batch."""
+    per_batch = rows_per_batch or max(n_rows, 1)
+
     def view(t, heads, rows_in_order):
         if t is None:
             return CRopeView(0, 0, 0)
@@ -331,10 +333,15 @@ def rope_desc(n_rows: int, dtype: int, head_dim: int, axis_dims, axis_len, q_hea
                 raise ValueError("a [batch, heads, rows, head_dim] tensor has another number of heads")
             if rows_in_order and t.shape[0] > 1 and t.stride(0) != t.shape[2] * t.stride(2):
                 raise ValueError("rows of q and k must follow one another at one stride: pass [rows, heads, head_dim]")
+            if (t.shape[0] * t.shape[2] < n_rows if rows_in_order
+                    else t.shape[2] < min(per_batch, n_rows) or t.shape[0] * per_batch < n_rows):
+                raise ValueError("fewer rows than n_rows, or in a batch element of q_out or k_out than rows_per_batch")
             return CRopeView(t.stride(0), t.stride(2), t.stride(1))
         if t.dim() != 3 or t.shape[1] != heads:
             raise ValueError("expected [rows, heads, head_dim] or [batch, heads, rows, head_dim]")
-        return CRopeView(t.stride(0) * (rows_per_batch or n_rows), t.stride(0), t.stride(1))
+        if t.shape[0] < n_rows:
+            raise ValueError("fewer rows than n_rows")
+        return CRopeView(t.stride(0) * per_batch, t.stride(0), t.stride(1))
     return CRope(dtype, head_dim, q_heads, k_heads, pairing, int(inverse), (C.c_int * 3)(*axis_dims), (C.c_int * 3)(*axis_len),
                  eps, n_rows, max(n_rows, 1) if rows_per_batch is None else rows_per_batch, unit_rows,
                  view(q, q_heads, True), view(q_out, q_heads, False), view(k, k_heads, True), view(k_out, k_heads, False))

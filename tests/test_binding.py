@@ -143,3 +143,25 @@ def test_rope_desc_head_major_inputs(oc):
     assert views(desc(torch.zeros(B, n, heads, D).transpose(1, 2), q_out=out))[:2] == [[n * heads * D, heads * D, D], [heads * n * D, D, n * D]]
     assert views(desc(head_major[:1], rows=n))[0][1:] == [D, n * D]
     assert views(desc(torch.zeros(B * n, heads, D)))[0][1:] == [heads * D, D]
+
+
+def test_rope_desc_tensors_hold_all_rows(oc):
+    """rows_per_batch is the length of a batch element of a head-major output; a tensor of fewer rows than the call's is
+    no place for them."""
+    B, n, heads, D = 3, 10, 4, 8
+    rows, head_major = torch.zeros(B * n, heads, D), torch.zeros(B, heads, n, D)
+
+    def desc(rows_per_batch=n, n_rows=B * n, **kw):
+        return oc.rope_desc(n_rows, oc.DTYPE_F32, D, (0, 4, 4), (1, 5, 6), heads, heads, rows_per_batch=rows_per_batch, **kw)
+    for m in ("q", "k"):
+        desc(**{m: rows, m + "_out": head_major})
+        for bad in ({m + "_out": head_major, "rows_per_batch": None},         # all rows in batch element 0
+                    {m + "_out": head_major, "rows_per_batch": n + 1}, {m + "_out": head_major[:2]}, {m + "_out": rows[1:]},
+                    {m: rows[1:]}, {m: torch.zeros(1, heads, B * n - 1, D)}):
+            with pytest.raises(ValueError):
+                desc(**bad)
+        # longer ones are: a cache with room for what follows, one batch element shorter than the others could be
+        desc(**{m: torch.zeros(40, heads, D), m + "_out": torch.zeros(B + 1, heads, n + 5, D)})
+        desc(rows_per_batch=64, n_rows=n, **{m + "_out": head_major})
+        desc(n_rows=0, rows_per_batch=None, **{m: rows[:0], m + "_out": rows[:0]})
+        desc(n_rows=25, **{m + "_out": head_major})                           # the last batch element is not full

@@ -516,7 +516,8 @@ oc_status oc_block_norm(oc_ctx* ctx, const oc_block_norm_desc* desc, const void*
  * may differ from q_heads.  q_w / k_w: fp32 [head_dim], null for no norm (both or neither):
  * v / sqrt(mean(v^2) + eps) * w before the rotation.  All arithmetic is in fp32, rounded once.
  * In place (out = in with the same strides) is allowed; otherwise inputs and outputs do not overlap.
- * Errors: OC_ERR_INVALID_ARG; OC_ERR_ALIGNMENT (a pointer not aligned to its element, or for ADJACENT
+ * Errors: OC_ERR_INVALID_ARG (also: a negative stride; a stride of 0 between several heads, rows or
+ * batch elements of an output); OC_ERR_ALIGNMENT (a pointer not aligned to its element, or for ADJACENT
  * to its pair; odd strides there); OC_ERR_UNSUPPORTED (a head of more than 64 units: a unit is 8
  * elements, 4 for fp32 ADJACENT, or as much less as strides, pointers and pairs are aligned to less
  * than 16 bytes; 2^31 rows or more). */

@@ -532,6 +532,12 @@ oc_status oc_rope(oc_ctx* c, const oc_rope_desc* d, const float* table, const in
     const oc_rope_view* views[4] = {&d->q, &d->q_out, &d->k, &d->k_out};
     for (int i = 0; i < (k ? 4 : 2); ++i)
         if (views[i]->batch_stride < 0 || views[i]->row_stride < 0 || views[i]->head_stride < 0) return OC_ERR_INVALID_ARG;
+    // (several heads, rows or batch elements of an output cannot lie in one place)
+    for (int i = 1; i < (k ? 4 : 2); i += 2) {
+        const oc_rope_view& o = *views[i];
+        if (((i == 1 ? d->q_heads : d->k_heads) > 1 && o.head_stride == 0) || (std::min(d->rows_per_batch, d->n_rows) > 1 && o.row_stride == 0) ||
+            (d->n_rows > d->rows_per_batch && o.batch_stride == 0)) return OC_ERR_INVALID_ARG;
+    }
     if (d->n_rows > ROWS_MAX || d->rows_per_batch > ROWS_MAX || d->unit_rows > ROWS_MAX || d->q_heads > 65535 || d->k_heads > 65535) return OC_ERR_UNSUPPORTED;
     if (((uintptr_t)table & 7u) || ((uintptr_t)idx & 3u) || ((uintptr_t)pos & 3u) || ((uintptr_t)q_w & 3u) || ((uintptr_t)k_w & 3u)) return OC_ERR_ALIGNMENT;
     DeviceGuard guard(c->device);

@@ -940,3 +940,42 @@ def test_linear_int8_into_a_column_range(oc, ctx, M):
     ctx.linear_int8(a, one[:M], M, K, w, one[:N], N, packed[:, N:2 * N], oc.DTYPE_F32)
     assert torch.equal(packed[:, N:2 * N].double(), a.double() @ w.double().t())
     assert (packed[:, :N] == 5).all() and (packed[:, 2 * N:] == 5).all()
+
+
+@pytest.mark.gpu
+def test_rope_outputs_have_a_place_for_every_head(oc, ctx):
+    """Several heads, rows or batch elements of an output at a stride of 0 would be written over one another: refused.  Of
+    an input they are a broadcast."""
+    n, D = 8, 64
+    x, o = torch.zeros(n, 2, D, dtype=BF16, device="cuda"), torch.zeros(n, 2, D, dtype=BF16, device="cuda")
+    good = (4 * 128, 128, 64)
+
+    def st(heads=2, rows=n, rpb=4, **views):
+        v = {m: good for m in ("q", "q_out", "k", "k_out")}
+        v.update(views)
+        d = oc.rope_desc(rows, oc.DTYPE_BF16, D, (0, 32, 32), (1, 2, 4), heads, heads, rows_per_batch=rpb, **v)
+        return ctx.rope(d, oc.rope_table(d).cuda(), x, o, k=x, k_out=o.clone(), check=False)
+    assert st() == oc.OK
+    for m in ("q_out", "k_out"):
+        assert st(**{m: (512, 128, 0)}) == oc.ERR_INVALID_ARG
+        assert st(**{m: (512, 0, 64)}) == oc.ERR_INVALID_ARG
+        assert st(**{m: (0, 128, 64)}) == oc.ERR_INVALID_ARG
+        assert st(rpb=n, **{m: (0, 128, 64)}) == oc.OK                        # one batch element
+        assert st(rpb=n + 3, **{m: (0, 128, 64)}) == oc.OK
+        assert st(heads=1, **{m: (512, 128, 0)}) == oc.OK
+        assert st(rpb=1, **{m: (128, 0, 64)}) == oc.OK                        # every row a batch element
+        assert st(rows=1, **{m: (0, 0, 64)}) == oc.OK
+    for m in ("q", "k"):
+        assert st(**{m: (0, 0, 0)}) == oc.OK
+    # a descriptor made without a tensor's strides (for a table) is none for a call
+    full = oc.rope_desc(n, oc.DTYPE_BF16, D, (0, 32, 32), (1, 2, 4), 2, 2, q=x, q_out=o, k=x, k_out=o)
+    table = oc.rope_table(full).cuda()
+    for left_out in ("q", "q_out", "k", "k_out"):
+        t = {m: v for m, v in dict(q=x, q_out=o, k=x, k_out=o).items() if m != left_out}
+        d = oc.rope_desc(n, oc.DTYPE_BF16, D, (0, 32, 32), (1, 2, 4), 2, 2, **t)
+        assert torch.equal(oc.rope_table(d), oc.rope_table(full))
+        assert ctx.rope(d, table, x, o, k=x, k_out=o.clone(), check=False) == oc.ERR_INVALID_ARG
+    # (a single row of a single head lies wherever its pointer says)
+    one = oc.rope_desc(1, oc.DTYPE_BF16, D, (0, 32, 32), (1, 2, 4), 1)
+    assert ctx.rope(one, table, x, o, check=False) == oc.OK
+    assert ctx.device_status() == oc.OK

@@ -79,6 +79,7 @@ if not os.path.exists(LIB_PATH):
 _lib = C.CDLL(LIB_PATH)
 
 _vp, _i, _i64, _f = C.c_void_p, C.c_int, C.c_int64, C.c_float
+_Tensor = torch.Tensor
 _lib.oc_status_str.restype = C.c_char_p
 _lib.oc_status_str.argtypes = [_i]
 _lib.oc_kernel_name.restype = C.c_char_p
@@ -115,10 +116,10 @@ _lib.oc_layer_cache_get.argtypes = [_vp, _i, _i, _i, _vp, _vp, _vp, _vp]
 _lib.oc_layer_cache_clear.argtypes = [_vp]
 _lib.oc_cache_step_host.argtypes = [_vp, _vp, _i, _f, _i64, _vp, _vp, _vp, _vp, _vp]
 _lib.oc_schedule_propose.argtypes = [_vp, _vp, _i64, C.c_double, _vp, _vp, _vp]
-_lib.oc_block_norm.argtypes = [_vp] * 18
+_lib.oc_block_norm.argtypes = [_vp, C.POINTER(CBlockNorm)] + [_vp] * 16
 _lib.oc_rope_table_size.argtypes = [_vp, _vp]
 _lib.oc_rope_table.argtypes = [_vp, C.c_double, _vp]
-_lib.oc_rope.argtypes = [_vp] * 12
+_lib.oc_rope.argtypes = [_vp, C.POINTER(CRope)] + [_vp] * 10
 _lib.oc_quantize_rows.argtypes = [_vp, _vp, _i, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp]
 _lib.oc_linear_int8.argtypes = [_vp, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _i, _i64, _i64, _vp, _vp]
 _lib.oc_match_frame_noalloc.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _vp]
@@ -236,7 +237,7 @@ def layer_cache_would_hit(stored_step: int, step: int, interval: int) -> bool:
 def _ptr(t) -> int | None:
     if t is None:
         return None
-    if isinstance(t, int):
+    if type(t) is not _Tensor and isinstance(t, int):              # (the class first: isinstance takes longer to say no)
         return t
     assert t.is_contiguous(), "tensors handed to the C-ABI must be contiguous"
     return t.data_ptr()
@@ -260,14 +261,18 @@ def _stream(stream) -> int:
 
 def _ptr_strided(t) -> int | None:
     """Pointer of a tensor whose strides the call gets on their own (a part of a larger tensor)."""
-    return None if t is None else (t if isinstance(t, int) else t.data_ptr())
+    if t is None or (type(t) is not _Tensor and isinstance(t, int)):
+        return t
+    return t.data_ptr()
 
 
 def _rows(t, width: int, stride: int | None, name: str):
     """(pointer, elements between rows) of a matrix `width` elements wide: dense unless a stride is given or the tensor
     is a part of a larger one."""
-    if t is None or isinstance(t, int) or t.is_contiguous():
-        return _ptr_strided(t), width if stride is None else stride
+    if t is None or (type(t) is not _Tensor and isinstance(t, int)):
+        return t, width if stride is None else stride
+    if t.is_contiguous():
+        return t.data_ptr(), width if stride is None else stride
     if t.stride(-1) != 1:
         raise ValueError(f"the elements of a row of {name} must be contiguous")
     if stride is None:
@@ -280,10 +285,10 @@ def _rows(t, width: int, stride: int | None, name: str):
 def _group_vectors(t, strides: tuple, desc: CBlockNorm, name: str) -> int | None:
     """Pointer of gate, scale or shift: a vector for each group, strides = (mod_stride, 1) elements apart, or one vector
     for all of them (mod_stride 0)."""
+    if type(t) is _Tensor and t.stride() == strides:
+        return t.data_ptr()
     if t is None or isinstance(t, int):
         return t
-    if t.stride() == strides:
-        return t.data_ptr()
     apart, groups = strides[0], -(-desc.n_rows // max(desc.rows_per_group, 1))
     if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"the elements of a vector of {name} must be contiguous")
@@ -497,9 +502,13 @@ class Context:
                    stream=None, check: bool = True) -> int:
         """oc_block_norm.  gate, scale and shift may be column ranges of one [groups, mod_stride] tensor."""
         apart = (desc.mod_stride, 1)
-        gate, scale = _group_vectors(gate, apart, desc, "gate"), _group_vectors(scale, apart, desc, "scale")
-        shift = _group_vectors(shift, apart, desc, "shift")
-        st = _lib.oc_block_norm(self._h, C.byref(desc), _ptr(x), _ptr(z), _ptr(slot_of), _ptr(cache), _ptr(cache_out),
+        if gate is not None:
+            gate = _group_vectors(gate, apart, desc, "gate")
+        if scale is not None:
+            scale = _group_vectors(scale, apart, desc, "scale")
+        if shift is not None:
+            shift = _group_vectors(shift, apart, desc, "shift")
+        st = _lib.oc_block_norm(self._h, desc, _ptr(x), _ptr(z), _ptr(slot_of), _ptr(cache), _ptr(cache_out),
                                 _ptr(out), _ptr(post_w), _ptr(post_b), gate, _ptr(pre_w), _ptr(pre_b), scale, shift, _ptr(h),
                                 _ptr(h_scale), _stream(stream))
         if check:
@@ -509,7 +518,7 @@ class Context:
     def rope(self, desc: CRope, table, q, q_out, k=None, k_out=None, idx=None, pos=None, q_w=None, k_w=None, stream=None,
              check: bool = True) -> int:
         """oc_rope: strides are the descriptor's, so q and k may be parts of one projection."""
-        st = _lib.oc_rope(self._h, C.byref(desc), _ptr(table), _ptr(idx), _ptr(pos), _ptr_strided(q), _ptr_strided(q_out),
+        st = _lib.oc_rope(self._h, desc, _ptr(table), _ptr(idx), _ptr(pos), _ptr_strided(q), _ptr_strided(q_out),
                           _ptr(q_w), _ptr_strided(k), _ptr_strided(k_out), _ptr(k_w), _stream(stream))
         if check:
             _chk(st, "oc_rope")

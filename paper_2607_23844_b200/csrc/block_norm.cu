@@ -6,8 +6,8 @@
 // distances), so a large common offset costs no precision and nothing is read twice.  r stays in fp32 between
 // the residual sum and the second norm: `out` is its rounding, h is not computed from that rounding.
 //
-// Bound by DRAM where rows are many: 230400 rows of 320 bf16 under Frame Cache, 667 MB, take 113 us (5.9 TB/s).  8192
-// rows of 1536 (107 MB) take 24.1 us: about five rounds of row sets an SM, whose parameters cost 5 us (19.1 without).
+// Bound by DRAM where rows are many: 230400 rows of 320 bf16 under Frame Cache, 667 MB, take 115 us (5.8 TB/s).  8192
+// rows of 1536 (107 MB) take 23.9 us: about five rounds of row sets an SM, whose parameters cost 4 us (20.2 without).
 #include <algorithm>
 #include <atomic>
 
@@ -122,9 +122,9 @@ struct RowPlan {
 // A CTA works through consecutive sets of rows.  A row's x and v travel through shared memory (16-byte
 // asynchronous copies, each thread's own vectors into its own words, so that nobody waits for anybody): the next
 // row's are asked for as soon as this one's are used up, half way through its work.  The folded parameters of the
-// group at hand lie in shared memory too -- every row reads all of them, and read from L2 they made the kernel
-// wait twice as long as for its rows (8192 rows of 1536: 45 us; without any parameters 21).  A set of rows that
-// belongs to several groups folds its own.
+// group at hand lie in shared memory too -- every row reads all of them: 8192 rows of 1536 take 23.0 us, and 29.5 where
+// each row reads and folds them itself; 230400 of 320 take 119 and 162.  A set of rows that belongs to several groups
+// folds its own.
 template <int DT, int PT, bool Z, class S>       // Z: there is a block's output
 __global__ void __launch_bounds__(RowCta<S::tpr>::threads)
 block_norm_kernel(const __grid_constant__ BlockNormParams P) {
@@ -351,11 +351,11 @@ static bool launch_block_norm_as(oc_ctx* ctx, BlockNormParams& P, cudaStream_t s
             if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, THREADS, smem) != cudaSuccess || per_sm < 1) { cudaGetLastError(); ok = false; return; }
             known.store(key | (uint64_t)per_sm, std::memory_order_relaxed);
         }
-        // Queues of equal length with every CTA resident, unless that makes long ones: 230400 rows of 320 take 138 us
-        // in 740 queues of 20 sets and 115 in queues of 4 (64 rows), which are near one another in DRAM at any time;
-        // shorter ones fold the parameters too often (57600 rows of 640: 63 us in resident queues, 67 in queues of 32
-        // rows).  8192 rows of 1536: 28 us in resident queues of 4 sets, 30 of 2, and 37 of 3, which are a round and
-        // a bit.
+        // Queues of equal length with every CTA resident, unless that makes long ones: 230400 rows of 320, half of the
+        // frames with slots, take 127 us in 740 queues of 20 sets and 100 in queues of 4 (64 rows), which are near one
+        // another in DRAM at any time; 106 in queues of 2, which fold the parameters too often, and 109 of 8.  57600
+        // rows of 640: 59 us in resident queues of 13 sets, 57 in queues of 4, 62 of 8.  8192 rows of 1536: 23 us in
+        // resident queues of 5 sets; 30, 28, 31 and 30 in queues of 2, 3, 4 and 8, which are a round and a bit.
         const long long resident = (long long)ctx->sm_count * per_sm, short_queue = std::max(4, 64 / ROWS);
         const long long queue = sets / short_queue > 2 * resident ? short_queue : (sets + resident - 1) / resident;
         const long long ctas = (sets + queue - 1) / queue;

@@ -12,9 +12,10 @@
 // Two accumulators take turns, so the epilogue of a tile runs under the MMAs of the next.
 // One or two tokens: one warp per pair of output channels, dp4a, the weights read once as they lie.
 // K and N tails are zero-filled by TMA and not stored.  Every wait is bounded (OC_ERR_TIMEOUT in the status word).
-// Measured: 8192 x 6400 x 8192 3.2 POP/s at 1.4 GHz under the power limit, 94 % of what the tensor pipe does at that
-// clock; 5120 x 1536 x 4608 26 us (2.8 POP/s); 57600 x 640 x 5120 139 us on idle data, of which 590 MB of output
-// alone take 100, and 157 under the power limit.
+// Measured in short runs at full clock | for seconds on end, under the power limit: 8192 x 6400 x 8192 273 us (3.1 POP/s) |
+// 311 (2.8 POP/s at 1.26 GHz, 0.9 of 16384 operations per SM and clock); 5120 x 1536 x 4608 28 | 33; 57600 x 640 x 5120
+// 157 | 188 (1.25 GHz; 139 on zeros, which draw less power), of which 590 MB of output alone take 90 to 100.  The ring
+// form of 256 columns spills 52 bytes.
 #include <string.h>
 
 #include <algorithm>
@@ -31,9 +32,9 @@ static constexpr int I8_A_BYTES = I8_BM * I8_BK;
 static constexpr int I8_STAGES_MAX = 8;
 
 // An epilogue warp stages 64 bytes of each of its 32 rows at a time.  128 would save a wait, but the shared memory is
-// worth more as ring: loads that compete with 148 SMs' stores come back late, and 57600 x 640 x 5120 takes 139 us
-// with seven resident-form stages and 177 with the four that 128-byte pieces leave (8192 x 1536 x 6144: 48 us with six
-// ring-form stages, 55 with four).
+// worth more as ring: loads that compete with 148 SMs' stores come back late.  57600 x 640 x 5120 takes 157 us with 64
+// bytes and seven stages (resident form) and 181 with 128 bytes and the five that they leave; 8192 x 1536 x 6144 55 with
+// six stages (ring form) and 61 with five.  (64 bytes and five stages: 170 and 56; four: 182 and 58.)
 static constexpr int I8_SEG = 64, I8_OUT_STAGE = 32 * I8_SEG;
 
 struct I8Params {
@@ -88,11 +89,11 @@ __device__ __forceinline__ void tc_commit_all(uint32_t bar, uint32_t issue) {
 }
 
 // The tiles of a walker.  Whole rows of `out` are written at about the same time, which is what DRAM writes fastest
-// (a 57600 x 5120 output: 174 us, against 188 us in groups of 9 tile columns and 202 us in groups of 3), and each row
-// of A is read from DRAM once.
+// (walks in groups of 9 and of 3 tile columns cost a 57600 x 5120 output 8 and 16 % in the ring form), and each row of A
+// is read from DRAM once.
 //   ring form      tile after tile along a row of tiles; W comes back from L2 for every tile
-//   resident form  a walker keeps its tile column, so that its rows of W stay in shared memory (57600 x 640 x 5120
-//                  under the power limit: 157 us, ring form 175): the walkers form as many whole rows of tiles as
+//   resident form  a walker keeps its tile column, so that its rows of W stay in shared memory (57600 x 640 x 5120:
+//                  157 us, ring form 194): the walkers form as many whole rows of tiles as
 //                  there are (`rows_of_walkers`), which go down the first `main_rows` rows together; the walkers
 //                  left over share out the other rows, column after column
 struct I8Walk {
@@ -415,7 +416,7 @@ linear_int8_kernel(const __grid_constant__ I8Params P) {
 
 // ---- few tokens ------------------------------------------------------------------------------------
 static constexpr int I8S_WARPS = 8, I8S_CH = 2;                      // warps per CTA, output channels per warp
-// 1536 x 9216 weights: 1 token 3.2 us and 2 tokens 4.3 this way, 5.1 with tensor-core tiles; 4 tokens 4.8 against 4.8,
+// 1536 x 9216 weights: 1 token 3.4 us and 2 tokens 4.6 this way, 5.1 with tensor-core tiles; 4 tokens 4.8 against 4.8,
 // 8 tokens 10.3 against 4.8
 static constexpr int I8S_TOKENS = 2;
 

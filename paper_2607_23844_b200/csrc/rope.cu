@@ -8,8 +8,9 @@
 // cosines up once and walks over the heads, which all turn by the same angles; the next two heads are on their way
 // while two are worked on, and 64 registers leave room for 32 warps per SM.  lph lanes make up a head, for the sum of
 // squares of its norm; rows of 32 / lph tokens share a warp, so heads of 72 elements leave few lanes idle.
-// Measured on 230400 rows of 2 x 5 heads of 64, bf16, 590 MB: 97 us (6.1 TB/s) without and 123 us (4.8) with head
-// norms, whose sums and square roots are what a warp then waits for.
+// Measured on 230400 rows of 2 x 5 heads of 64, bf16, 590 MB: 97 us (6.1 TB/s) without and 125 us (4.7) with head
+// norms, whose sums and square roots are what a warp then waits for; fp32, 1180 MB: 182 us (6.5 TB/s) and 203 (5.8), though
+// its pairs in halves do not fit into 64 registers (32 and 128 bytes spilled).
 #include <string.h>
 
 #include "rows.cuh"
@@ -314,8 +315,8 @@ static void launch_rope_as(const RopeParams& P, int upl, bool norm, dim3 grid, c
 }
 
 // Elements per vector: the widest that pairs, heads, strides and pointers allow, 16 bytes at most, and 8 elements
-// per unit (with 16 its coefficients take so many registers that too few warps are left: 163 us against 149 on
-// 230400 rows of 2 x 5 heads of 64).
+// per unit (units of 16 bf16 elements need 96 registers, which leaves 20 warps of 32: 95 and 125 us without and with head
+// norms on 230400 rows of 2 x 5 heads of 64, against 97 and 125 -- too little for kernels of their own).
 int rope_vector(const oc_rope_desc& d, const void* q, const void* q_out, const void* k, const void* k_out) {
     const int eb = d.dtype == OC_DTYPE_BF16 ? 2 : 4;
     const long long rot = (long long)d.axis_dims[0] + d.axis_dims[1] + d.axis_dims[2];

@@ -168,10 +168,15 @@ template <int TPR, int VPT, int MIN> struct RowSplit {
 };
 // Picks the row split for nvec vectors: as few threads as hold the row in 3 to 6 vectors each, so that several 16-byte
 // loads per thread are in flight and few lanes idle, and more of them where 5 or 6 vectors' registers leave too few
-// warps on an SM.  Timed with oc_block_norm (post and pre norm, cache, modulation) on 8192 rows: 640 bf16 columns
-// 12.1 us over 32 threads, 14.2 over 16; 1024: 16.7 over 32, 20.2 over 64; 1152: 21.6 over 32, 22.5 over 64; 1536: 24.7
-// over 64, 27.9 over 32; 2048: 31.7 over 64, 43.9 over 128; 2560: 45.5 over 64, 51.9 over 128; 3200: 58.7 over 256,
-// 88.7 over 128.  Calls f with the split; false if the row is too wide (more than 3072 vectors).
+// warps on an SM.  oc_block_norm on 8192 rows, half of them with a slot, in us, this split | the neighbouring one:
+//     vectors of a row          80          128         144         192         256         320         400
+//     threads                32 | 16     32 | 64     32 | 64     64 | 32     64 | 128    64 | 128   256 | 128
+//     bf16, z and cache    12.7 | 13.7 17.2 | 18.4 22.6 | 20.8 23.1 | 26.5 29.1 | 40.0 42.0 | 49.1 52.6 | 58.7
+//     fp32, z and cache    11.6 | 10.9 15.8 | 16.9 18.0 | 17.2 21.6 | 23.8 28.9 | 36.6 36.5 | 41.8 49.1 | 51.4
+//     bf16, norm alone      7.9 | 6.7   8.7 | 11.5  9.9 | 13.2 13.8 | 12.2 16.6 | 24.6 22.8 | 29.3 35.7 | 35.2
+//     fp32, norm alone      7.0 | 5.5   7.2 | 9.8   8.4 | 10.8 10.9 | 8.2  11.2 | 21.0 14.1 | 22.7 29.0 | 26.1
+// One rule serves all four: it costs at most 8 % with z, and up to a third on some widths of the norm alone.  Calls f with
+// the split; false if the row is too wide (more than 3072 vectors).
 template <class F>
 inline bool row_split(long long nvec, F&& f) {
     if (nvec <= 8) f(RowSplit<8, 1, 0>());

@@ -301,9 +301,12 @@ def _group_vectors(t, strides: tuple, desc: CBlockNorm, name: str) -> int | None
         vectors, last = vectors * n, s
         if s == apart and vectors >= groups:
             return t.data_ptr()
-    run = last is None                                            # one run of elements
-    if groups <= 1 or (run and (apart == 0 or t.shape[-1] >= (groups - 1) * apart + desc.C)):
+    if groups <= 1 or (last is None and apart == 0):
         return t.data_ptr()
+    if last is None:                                              # one run of elements, which says nothing of the others
+        end = t.storage_offset() + (groups - 1) * apart + desc.C
+        if end <= t.untyped_storage().nbytes() // t.element_size():
+            return t.data_ptr()
     raise ValueError(f"{name} does not hold {groups} vectors {apart} elements apart: mod_stride must be its row stride")
 
 

@@ -116,10 +116,12 @@ def test_block_norm_group_vectors_lie_mod_stride_apart(oc, calls):
     for t in (vector, vector[None], vector.expand(G, C), mod[1:2, :C], mod[1, :C]):
         run(t, 0)
     # more groups than vectors
-    refused(vector, C), refused(torch.zeros(1, C)[:, None], 2 * C), refused(mod[0, :C], 3 * C), refused(torch.zeros(G, 2, C)[:3], 2 * C)
+    refused(vector, C), refused(torch.zeros(1, C)[:, None], 2 * C), refused(torch.zeros(G, 2, C)[:3], 2 * C)
     # vectors by any route that are as far apart as was said
     run(mod.view(G, 3, C)[:, 1:2], 3 * C), run(mod.view(2, 2, 3 * C)[..., :C], 3 * C), run(mod.view(G, 3, C), 3 * C)
-    run(mod.view(-1)[C:], 3 * C), run(torch.zeros(G, C), C), run(torch.zeros(6, 3 * C)[:, :C], 3 * C)
+    run(mod.view(-1)[C:], 3 * C), run(mod[0, :C], 3 * C), run(mod.view(1, -1)[:, C:2 * C], 3 * C)
+    refused(mod[1, :C], 3 * C), refused(mod.view(1, -1)[:, 3 * C:4 * C], 3 * C)                # (the last one past the end)
+    run(torch.zeros(G, C), C), run(torch.zeros(6, 3 * C)[:, :C], 3 * C)
     refused(torch.zeros(2, 3, 3 * C)[:, :2, :C], 3 * C)                       # (a gap after every second)
     # a single group: only the elements of its vector matter
     run(mod[:1, :C], 3 * C, 20), run(vector, 96, 20), run(mod[:, :C], 0, 20), refused(mod[:1, 0:2 * C:2], 3 * C, 20)

@@ -330,8 +330,8 @@ def rope_desc(n_rows: int, dtype: int, head_dim: int, axis_dims, axis_len, q_hea
     per_batch = rows_per_batch or max(n_rows, 1)
 
     def view(t, heads, rows_in_order):
-        if t is None:                                                # no strides: refused by oc_rope where any are needed
-            return CRopeView(-1, -1, -1) if n_rows > 1 or heads > 1 else CRopeView(0, 0, 0)
+        if t is None:                                                # strides that are needed are left invalid
+            return CRopeView(0, -1 if n_rows > 1 else 0, -1 if heads > 1 else 0)
         if isinstance(t, tuple):
             return CRopeView(*t)
         if t.shape[-1] != head_dim or t.stride(-1) != 1:

@@ -167,3 +167,12 @@ def test_rope_desc_tensors_hold_all_rows(oc):
         desc(rows_per_batch=64, n_rows=n, **{m + "_out": head_major})
         desc(n_rows=0, rows_per_batch=None, **{m: rows[:0], m + "_out": rows[:0]})
         desc(n_rows=25, **{m + "_out": head_major})                           # the last batch element is not full
+
+
+def test_rope_desc_strides_given_afterwards(oc):
+    """Only strides that something is reached by are left invalid where no tensor was given."""
+    def left(n_rows, heads):
+        d = oc.rope_desc(n_rows, oc.DTYPE_F32, 8, (0, 4, 4), (1, 5, 6), heads, heads)
+        assert len({tuple(v) for v in views(d)}) == 1
+        return views(d)[0]
+    assert left(10, 4) == [0, -1, -1] and left(1, 4) == [0, 0, -1] and left(10, 1) == [0, -1, 0] and left(1, 1) == [0, 0, 0]

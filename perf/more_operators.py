@@ -277,9 +277,9 @@ def _own_rows(c, s, oc, ctx):
     dt = {"bf16": oc.DTYPE_BF16, "f32": oc.DTYPE_F32}[c["dtype"]]
     if "cache_desc" not in s:
         s["cache_desc"] = _cache_desc(c, oc, c["heads"])
-        s["in_desc"] = oc.kv_rows(c["B"] * c["rows"], dt, k=s["k"], v=s["v"])
+        s["in_desc"] = oc.kv_rows(s["cache_desc"], c["B"] * c["rows"], dt, k=s["k"], v=s["v"])
         if "k_out" in s:
-            s["out_desc"] = oc.kv_rows(s["k_out"].shape[0], dt, k=s["k_out"], v=s["v_out"])
+            s["out_desc"] = oc.kv_rows(s["cache_desc"], s["k_out"].shape[0], dt, k=s["k_out"], v=s["v_out"])
     pools = dict(k_scale=s["k_scale"], v_scale=s["v_scale"], page_table=s["table"])
     if c["kind"] != "get":
         ctx.kv_put(s["cache_desc"], s["in_desc"], s["k"], s["k_pool"], s["v"], s["v_pool"], idx=s["idx"], **pools)
@@ -293,9 +293,9 @@ def _own_rows(c, s, oc, ctx):
 def _own_attend(c, s, oc, ctx):
     if "desc" not in s:
         s["cache_desc"] = _cache_desc(c, oc, c["kv"])
-        s["desc"] = oc.attention_desc(s["out"].shape[0], {"bf16": oc.DTYPE_BF16, "f32": oc.DTYPE_F32}[c["dtype"]], c["heads"],
-                                      1.0 / math.sqrt(c["D"]), rows_per_batch=c["rows"], unit=c["unit"], back=c["back"],
-                                      ahead=c["ahead"], q=s["q"], out=s["out"])
+        s["desc"] = oc.attention_desc(s["cache_desc"], s["out"].shape[0], {"bf16": oc.DTYPE_BF16, "f32": oc.DTYPE_F32}[c["dtype"]],
+                                      c["heads"], 1.0 / math.sqrt(c["D"]), rows_per_batch=c["rows"], unit=c["unit"],
+                                      back=c["back"], ahead=c["ahead"], q=s["q"], out=s["out"])
     ctx.attention(s["cache_desc"], s["desc"], s["q"], s["k_pool"], s["v_pool"], s["out"], k_scale=s["k_scale"],
                   v_scale=s["v_scale"], page_table=s["table"], kv_len=s["kv_len"], q_start=s["q_start"], idx=s["idx"])
     return s["out"]

@@ -6,8 +6,10 @@
  *
  *     match  ->  select  ->  gather  ->  [ the wrapped layer, outside this library ]  ->  restore
  *
- * and what surrounds attention in a wrapped transformer block, on the tokens that are computed
- * (oc_block_norm, oc_rope, oc_quantize_rows, oc_linear_int8, at the end of this file).
+ * and a wrapped transformer block's own operators on the tokens that are computed: what surrounds its
+ * attention (oc_block_norm, oc_rope, oc_quantize_rows, oc_linear_int8), and attention itself over a
+ * paged cache of all tokens' keys and values (oc_kv_put, oc_kv_get, oc_attention, at the end of this
+ * file).
  *
  * Conventions
  *   - All data pointers are DEVICE pointers unless a name ends in `_host`.  The caller owns every
@@ -51,7 +53,8 @@ enum {
 };
 
 enum { OC_KIND_TOKEN = 0, OC_KIND_FRAME = 1, OC_KIND_BLOCK = 2 };
-enum { OC_DTYPE_F32 = 0, OC_DTYPE_BF16 = 1, OC_DTYPE_I8 = 2 /* rows with a scale each: oc_block_norm only */ };
+enum { OC_DTYPE_F32 = 0, OC_DTYPE_BF16 = 1, OC_DTYPE_I8 = 2 /* rows with a scale each: oc_block_norm, oc_kv_desc */,
+       OC_DTYPE_I4 = 3 /* the same, two values to a byte: oc_kv_desc only */ };
 enum { OC_SELECT_THRESHOLD = 0, OC_SELECT_COUNT = 1 };
 enum { OC_RESTORE_FROM_CACHE = 0, OC_RESTORE_FROM_REPRESENTATIVE = 1 };
 enum { OC_FRAME_MEAN_POS_COS = 0, OC_FRAME_FLAT_COS = 1 };
@@ -149,7 +152,10 @@ enum {
     OC_K_ROPE = 14,       /* rotary positions                                           */
     OC_K_QUANT = 15,      /* rows to 8-bit integers                                     */
     OC_K_LINEAR_I8 = 16,  /* 8-bit matrix product                                       */
-    OC_K_COUNT = 17
+    OC_K_KV_PUT = 17,     /* rows of keys and values into their pages                   */
+    OC_K_KV_GET = 18,     /* and back                                                   */
+    OC_K_ATTENTION = 19,  /* attention over the pages                                   */
+    OC_K_COUNT = 20
 };
 const char* oc_kernel_name(int kernel_id);
 
@@ -562,6 +568,95 @@ oc_status oc_quantize_rows(oc_ctx* ctx, const void* x, int dtype, int64_t x_rows
 oc_status oc_linear_int8(oc_ctx* ctx, const int8_t* a, const float* a_scale, int64_t M, int64_t K, const int8_t* w,
                          const float* w_scale, int64_t N, const float* bias, void* out, int out_dtype, int64_t out_rows,
                          int64_t out_stride, const int32_t* out_idx, void* stream);
+
+/* =============================================================================================
+ * Attention of the computed tokens over a cache of all tokens' keys and values
+ * ============================================================================================= */
+
+/* A paged cache of keys, values, or any rows of `heads` vectors of head_dim elements.  It belongs to
+ * n_seqs sequences (batch elements, frames) of up to seq_rows tokens; token number t is position
+ * p = t % seq_rows of sequence s = t / seq_rows, the numbers that oc_select's kept list has where a
+ * sequence is a whole number of its groups.  That token's vectors lie in page
+ *     page_table[s * table_stride + p / page_rows]    (no table: s * ceil(seq_rows / page_rows) + p / page_rows)
+ * of a pool [n_pages][heads][page_rows][head_dim], in row p % page_rows; sequences may share pages.
+ * dtype is OC_DTYPE_F32 or OC_DTYPE_BF16, or whole numbers with a scale for each token and head in a
+ * second pool, fp32 [n_pages][heads][page_rows]:
+ *     scale = max|x| / L,   q = rint(x * L / max|x|),   value = q * scale
+ *     OC_DTYPE_I8 (L = 127): a byte each;  OC_DTYPE_I4 (L = 7): element 2i in the low half of byte i, 2i + 1 in
+ *     the high half, two's complement.
+ * A vector whose max|x| is under 2^-100 becomes zeros with scale 0; one with an infinity or NaN keeps
+ * that in its scale, its q are zeros (so that its values read as NaN).
+ * head_dim is a multiple of 8 and at most 256, page_rows a multiple of 16; pools are 16-byte aligned.
+ * A page number outside the pool is recorded as OC_ERR_INVALID_ARG in the device status word; nothing
+ * is written to it, and it reads as zeros. */
+typedef struct oc_kv_desc {
+    int dtype, heads, head_dim;
+    int64_t n_seqs, seq_rows;
+    int64_t page_rows, n_pages;
+    int64_t table_stride;             /* entries of page_table for a sequence */
+} oc_kv_desc;
+/* Host only: bytes of the pool and of its scales (0 for fp32 and bf16). */
+oc_status oc_kv_bytes(const oc_kv_desc* cache, size_t* pool_bytes, size_t* scale_bytes);
+
+/* Rows on the dense side of oc_kv_put and oc_kv_get: head h of row r = (b, i), b = r / rows_per_batch,
+ * i = r % rows_per_batch, begins b * batch_stride + i * row_stride + h * head_stride elements after the
+ * pointer, as oc_rope leaves its outputs; the elements of a head are contiguous. */
+typedef struct oc_kv_rows {
+    int dtype;                        /* OC_DTYPE_F32 or OC_DTYPE_BF16 */
+    int64_t n_rows, rows_per_batch;
+    oc_rope_view k, v;
+} oc_kv_rows;
+
+/* oc_kv_put writes row r of k and v to the cache as token idx[r] (no idx: token r); oc_kv_get reads
+ * token idx[r] into row r, values rounded once to the rows' type.  Rows whose idx is negative (the unused tail of
+ * a kept list) are left out, by oc_kv_get left as they were; so are numbers of n_seqs * seq_rows and
+ * more (recorded in the device status word).  idx of oc_kv_put names no token twice.  v and its pool
+ * may be null: a cache of one tensor.  A floating-point cache has the rows' own type.
+ * Errors: OC_ERR_INVALID_ARG (also: scales missing, or given for a floating-point cache; a stride of 0
+ * between several heads, rows or batch elements of oc_kv_get's rows; an fp32 cache of bf16 rows or the
+ * other way round); OC_ERR_ALIGNMENT (a pool not 16-byte aligned, another pointer not aligned to its
+ * element, head_dim not a multiple of 8, page_rows not of 16); OC_ERR_UNSUPPORTED (head_dim over 256; 2^31 or
+ * more rows, tokens, or vectors in the pool). */
+oc_status oc_kv_put(oc_ctx* ctx, const oc_kv_desc* cache, const oc_kv_rows* rows, const int32_t* page_table, const int32_t* idx,
+                    const void* k, void* k_pool, float* k_scale, const void* v, void* v_pool, float* v_scale, void* stream);
+oc_status oc_kv_get(oc_ctx* ctx, const oc_kv_desc* cache, const oc_kv_rows* rows, const int32_t* page_table, const int32_t* idx,
+                    const void* k_pool, const float* k_scale, void* k, const void* v_pool, const float* v_scale, void* v,
+                    void* stream);
+
+/* Attention of the rows that are computed over the cache:
+ *     out[r, h] = sum_j p_j V[j, h'],   p = softmax over the visible keys j of scale * q[r, h] . K[j, h']
+ * with h' = h / (q_heads / cache heads): neighbouring heads of q may share one of the cache.
+ * Row r = (s, i) belongs to sequence s = r / rows_per_batch; with q_start (int32 [n_seqs + 1], ascending)
+ * sequence s has rows q_start[s] .. q_start[s+1] - 1, at most rows_per_batch of them.  Rows behind the
+ * last sequence are not written.  kv_len (int32 [n_seqs]; none: seq_rows) is how many tokens of a
+ * sequence count.  A row's position p is that of token idx[r], or without idx p = kv_len - n + i for the
+ * i-th of the sequence's n rows: new tokens are its last ones.  Rows whose idx is negative are not written.
+ * unit = 0: every key is visible.  unit > 0: key j is visible if -back <= j / unit - p / unit <= ahead
+ * (back, ahead < 0: without limit); ahead = 0 with unit = 1 is causal attention, with unit = H*W a video's
+ * frames see themselves and earlier ones, back = ahead = 0 keeps each frame to itself.
+ * A row that sees no key becomes zeros, with lse = -infinity.  lse (nullable, fp32 [n_rows][q_heads]):
+ * log of the sum over visible keys of exp(scale * q . K).  Keys and values that a row does not see have
+ * no influence on it, whatever they hold; of a visible infinity in V the row gets that infinity (NaN
+ * where both signs meet), of a NaN in K or V a NaN.
+ * q and out are fp32 over a cache in fp32, 8 or 4 bits, or bf16 over one in bf16, 8 or 4 bits.  bf16:
+ * products of bf16 with fp32 sums; probabilities, times the value's scale in the 8- and 4-bit caches,
+ * are rounded to bf16 before they meet V; everything else is fp32.  fp32: all of it in fp32.
+ * Recorded as OC_ERR_INVALID_ARG in the device status word: kv_len outside 0 .. seq_rows (taken as the
+ * nearer end), q_start that descends or leaves n_rows or exceeds rows_per_batch (the rows concerned are
+ * not written), an idx of another sequence (that row is not written).
+ * out may be q with the same strides.  Errors: as oc_kv_put; OC_ERR_INVALID_ARG (scale not positive and
+ * finite; q_heads not a multiple of the cache's heads); OC_ERR_UNSUPPORTED (head_dim over 128). */
+typedef struct oc_attention_desc {
+    int dtype;                        /* of q and out */
+    int q_heads;
+    float scale;
+    int64_t n_rows, rows_per_batch;
+    int64_t unit, back, ahead;
+    oc_rope_view q, out;              /* batch_stride: unused with q_start */
+} oc_attention_desc;
+oc_status oc_attention(oc_ctx* ctx, const oc_kv_desc* cache, const oc_attention_desc* desc, const int32_t* page_table,
+                       const int32_t* kv_len, const int32_t* q_start, const int32_t* idx, const void* q, const void* k_pool,
+                       const float* k_scale, const void* v_pool, const float* v_scale, void* out, float* lse, void* stream);
 
 #ifdef __cplusplus
 }

@@ -144,7 +144,7 @@ const char* oc_kernel_name(int k) {
     static const char* names[OC_K_COUNT] = {"norms", "match_tc", "match_simt", "match_finalize", "frame_pair",
                                             "frame_finalize", "block_partial", "block_finalize", "select",
                                             "gather", "restore", "copy", "linear", "block_norm", "rope", "quantize",
-                                            "linear_int8"};
+                                            "linear_int8", "kv_put", "kv_get", "attention"};
     return (k >= 0 && k < OC_K_COUNT) ? names[k] : "unknown";
 }
 
@@ -572,6 +572,112 @@ oc_status oc_linear_int8(oc_ctx* c, const int8_t* a, const float* a_scale, int64
     DeviceGuard guard(c->device);
     if (!guard.ok) return OC_ERR_CUDA;
     return launch_linear_int8(c, a, a_scale, M, K, w, w_scale, N, bias, out, out_dtype, out_rows, out_stride, out_idx, (cudaStream_t)stream);
+}
+
+// ---- the paged cache and the attention over it ----------------------------------------------------
+static inline bool kv_quantised(const oc_kv_desc* k) { return k->dtype == OC_DTYPE_I8 || k->dtype == OC_DTYPE_I4; }
+static inline int64_t elem_size(int dtype) { return dtype == OC_DTYPE_F32 ? 4 : 2; }
+
+static oc_status check_kv(const oc_kv_desc* k, bool table) {
+    if (!k || (!float_type(k->dtype) && !kv_quantised(k))) return OC_ERR_INVALID_ARG;
+    if (k->heads <= 0 || k->head_dim <= 0 || k->n_seqs < 0 || k->seq_rows < 0 || k->page_rows <= 0 || k->n_pages < 0 || k->table_stride < 0) return OC_ERR_INVALID_ARG;
+    if (k->head_dim % 8 != 0 || k->page_rows % 16 != 0) return OC_ERR_ALIGNMENT;
+    if (k->head_dim > 256 || k->heads > 65535 || k->n_seqs > ROWS_MAX || k->seq_rows > ROWS_MAX || k->page_rows > ROWS_MAX || k->n_pages > ROWS_MAX ||
+        k->table_stride > ROWS_MAX) return OC_ERR_UNSUPPORTED;
+    if (k->n_seqs * k->seq_rows > ROWS_MAX || k->heads * k->page_rows > ROWS_MAX || k->heads * k->page_rows * k->n_pages > ROWS_MAX) return OC_ERR_UNSUPPORTED;
+    if (k->n_pages == 0 && k->n_seqs * k->seq_rows > 0) return OC_ERR_INVALID_ARG;
+    const int64_t pages = (k->seq_rows + k->page_rows - 1) / k->page_rows;      // of a sequence
+    if (table ? (k->n_seqs > 1 && k->table_stride < pages) : k->n_seqs * pages > k->n_pages) return OC_ERR_INVALID_ARG;
+    return OC_OK;
+}
+
+oc_status oc_kv_bytes(const oc_kv_desc* k, size_t* pool, size_t* scales) {
+    if (!pool || !scales) return OC_ERR_INVALID_ARG;
+    oc_status st = check_kv(k, true);
+    if (st != OC_OK) return st;
+    const size_t vectors = (size_t)(k->n_pages * k->heads * k->page_rows);
+    *pool = k->dtype == OC_DTYPE_I4 ? vectors * (size_t)(k->head_dim / 2) : vectors * (size_t)k->head_dim * (k->dtype == OC_DTYPE_I8 ? 1u : (size_t)elem_size(k->dtype));
+    *scales = kv_quantised(k) ? vectors * 4 : 0;
+    return OC_OK;
+}
+
+// Pools and scales of a call (v: whether there is a second tensor).
+static oc_status check_pools(const oc_kv_desc* k, const void* k_pool, const float* k_scale, const void* v_pool, const float* v_scale, bool v) {
+    if (!k_pool || (v && !v_pool)) return OC_ERR_INVALID_ARG;
+    if (kv_quantised(k) ? (!k_scale || (v && !v_scale)) : (k_scale || v_scale)) return OC_ERR_INVALID_ARG;
+    if (!v && (v_pool || v_scale)) return OC_ERR_INVALID_ARG;
+    if (misaligned(k_pool) || (v && misaligned(v_pool)) || ((uintptr_t)k_scale & 3u) || ((uintptr_t)v_scale & 3u)) return OC_ERR_ALIGNMENT;
+    return OC_OK;
+}
+
+// Strides of rows on the dense side; those of an output lead to a place of its own for every head, row and batch element.
+static bool bad_view(const oc_rope_view& w, int64_t heads, int64_t rows, int64_t rows_per_batch, bool output, bool batches) {
+    if (w.batch_stride < 0 || w.row_stride < 0 || w.head_stride < 0) return true;
+    if (!output) return false;
+    return (heads > 1 && w.head_stride == 0) || (std::min(rows, rows_per_batch) > 1 && w.row_stride == 0) || (batches && rows > rows_per_batch && w.batch_stride == 0);
+}
+
+static oc_status kv_move(oc_ctx* c, bool put, const oc_kv_desc* cache, const oc_kv_rows* rows, const int32_t* page_table, const int32_t* idx,
+                         const void* k, const void* k_pool, const float* k_scale, const void* v, const void* v_pool, const float* v_scale, void* stream) {
+    if (!c || !rows || !float_type(rows->dtype) || rows->n_rows < 0 || rows->rows_per_batch <= 0) return OC_ERR_INVALID_ARG;
+    oc_status st = check_kv(cache, page_table != nullptr);
+    if (st != OC_OK) return st;
+    if (!kv_quantised(cache) && cache->dtype != rows->dtype) return OC_ERR_INVALID_ARG;
+    if (rows->n_rows == 0) return OC_OK;                                    // (empty tensors have no addresses)
+    if (!k || (v != nullptr) != (v_pool != nullptr)) return OC_ERR_INVALID_ARG;
+    if (!idx && rows->n_rows > cache->n_seqs * cache->seq_rows) return OC_ERR_INVALID_ARG;
+    if (bad_view(rows->k, cache->heads, rows->n_rows, rows->rows_per_batch, !put, true) ||
+        (v && bad_view(rows->v, cache->heads, rows->n_rows, rows->rows_per_batch, !put, true))) return OC_ERR_INVALID_ARG;
+    if (cache->n_seqs * cache->seq_rows == 0) return OC_OK;                 // (no row can name a token)
+    st = check_pools(cache, k_pool, k_scale, v_pool, v_scale, v != nullptr);
+    if (st != OC_OK) return st;
+    if (k == k_pool || (v && v == v_pool)) return OC_ERR_INVALID_ARG;
+    if (rows->n_rows > ROWS_MAX || rows->rows_per_batch > ROWS_MAX) return OC_ERR_UNSUPPORTED;
+    const uintptr_t el = (uintptr_t)elem_size(rows->dtype) - 1;
+    if (((uintptr_t)k & el) || ((uintptr_t)v & el) || ((uintptr_t)page_table & 3u) || ((uintptr_t)idx & 3u)) return OC_ERR_ALIGNMENT;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return OC_ERR_CUDA;
+    return launch_kv_move(c, put, *cache, *rows, page_table, idx, k, k_pool, k_scale, v, v_pool, v_scale, (cudaStream_t)stream);
+}
+
+oc_status oc_kv_put(oc_ctx* c, const oc_kv_desc* cache, const oc_kv_rows* rows, const int32_t* page_table, const int32_t* idx,
+                    const void* k, void* k_pool, float* k_scale, const void* v, void* v_pool, float* v_scale, void* stream) {
+    return kv_move(c, true, cache, rows, page_table, idx, k, k_pool, k_scale, v, v_pool, v_scale, stream);
+}
+
+oc_status oc_kv_get(oc_ctx* c, const oc_kv_desc* cache, const oc_kv_rows* rows, const int32_t* page_table, const int32_t* idx,
+                    const void* k_pool, const float* k_scale, void* k, const void* v_pool, const float* v_scale, void* v, void* stream) {
+    return kv_move(c, false, cache, rows, page_table, idx, k, k_pool, k_scale, v, v_pool, v_scale, stream);
+}
+
+oc_status oc_attention(oc_ctx* c, const oc_kv_desc* cache, const oc_attention_desc* d, const int32_t* page_table,
+                       const int32_t* kv_len, const int32_t* q_start, const int32_t* idx, const void* q, const void* k_pool,
+                       const float* k_scale, const void* v_pool, const float* v_scale, void* out, float* lse, void* stream) {
+    if (!c || !d || !float_type(d->dtype) || d->q_heads <= 0 || d->n_rows < 0 || d->rows_per_batch <= 0 || d->unit < 0) return OC_ERR_INVALID_ARG;
+    if (!(d->scale > 0.0f) || !isfinite(d->scale)) return OC_ERR_INVALID_ARG;
+    oc_status st = check_kv(cache, page_table != nullptr);
+    if (st != OC_OK) return st;
+    if (!kv_quantised(cache) && cache->dtype != d->dtype) return OC_ERR_INVALID_ARG;
+    if (d->q_heads % cache->heads != 0) return OC_ERR_INVALID_ARG;
+    if (d->n_rows == 0 || cache->n_seqs == 0) return OC_OK;                 // (empty tensors have no addresses)
+    if (!q || !out) return OC_ERR_INVALID_ARG;
+    if (bad_view(d->q, d->q_heads, d->n_rows, d->rows_per_batch, false, !q_start) ||
+        bad_view(d->out, d->q_heads, q_start ? d->n_rows : std::min(d->n_rows, cache->n_seqs * d->rows_per_batch), q_start ? d->n_rows : d->rows_per_batch, true, !q_start))
+        return OC_ERR_INVALID_ARG;
+    // (a cache of no tokens has no addresses either: its rows become zeros)
+    if (cache->seq_rows > 0) {
+        st = check_pools(cache, k_pool, k_scale, v_pool, v_scale, true);
+        if (st != OC_OK) return st;
+    }
+    if (out == k_pool || out == v_pool) return OC_ERR_INVALID_ARG;
+    if (cache->head_dim > 128 || d->n_rows > ROWS_MAX || d->rows_per_batch > ROWS_MAX || d->q_heads > 65535) return OC_ERR_UNSUPPORTED;
+    if (d->n_rows * d->q_heads > ROWS_MAX) return OC_ERR_UNSUPPORTED;
+    const uintptr_t el = (uintptr_t)elem_size(d->dtype) - 1;
+    if (((uintptr_t)q & el) || ((uintptr_t)out & el) || ((uintptr_t)lse & 3u) || ((uintptr_t)page_table & 3u) || ((uintptr_t)kv_len & 3u) ||
+        ((uintptr_t)q_start & 3u) || ((uintptr_t)idx & 3u)) return OC_ERR_ALIGNMENT;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return OC_ERR_CUDA;
+    return launch_attention(c, *cache, *d, page_table, kv_len, q_start, idx, q, k_pool, k_scale, v_pool, v_scale, out, lse, (cudaStream_t)stream);
 }
 
 // ---- Token Cache on the frame pairs of Frame Cache (Section 3.2.3) ---------------------------------

@@ -1,0 +1,139 @@
+// What the attention kernels share: a call's parameters, the rows and keys of a sequence, which keys a row sees, and the
+// joining of partial results of CTAs that split a sequence's keys.
+#pragma once
+#include "kv_cache.cuh"
+
+namespace oc {
+
+static constexpr int ATT_SPLIT_MAX = 16;         // CTAs of a cluster that share the keys of a tile of rows
+
+struct AttnParams {
+    KvPages pages;
+    const int32_t *kv_len, *q_start, *idx;
+    const void *q, *k_pool, *v_pool;
+    const float *k_scale, *v_scale;
+    void* out; float* lse;
+    long long q_batch, q_row, q_head, o_batch, o_row, o_head;                 // elements
+    uint32_t n_rows, rows_per_batch, n_seqs;
+    int q_heads, group;                          // heads of q; those that share a head of the cache
+    long long unit, back, ahead;                 // (64 bits: a window's end may leave 32)
+    float scale, scale_log2;                     // of the scores; the same times log2(e)
+    uint32_t tiles;                              // tiles of rows of a sequence and head of the cache
+    int split;                                   // CTAs of a cluster
+    bool wide_q, wide_out;                       // 16 bytes at a time
+};
+
+#ifdef __CUDACC__
+// A CTA's work: a tile of rows of one sequence and head of the cache (tiles in descending order: with a causal window
+// the long ones come first).
+struct AttnTile { uint32_t seq, head, tile; };
+__device__ __forceinline__ AttnTile attn_tile(const AttnParams& P, uint32_t id) {
+    AttnTile t;
+    const uint32_t problem = id / P.tiles;
+    t.tile = P.tiles - 1 - (id - problem * P.tiles);
+    t.seq = problem / (uint32_t)P.pages.heads;
+    t.head = problem - t.seq * (uint32_t)P.pages.heads;
+    return t;
+}
+
+struct AttnSeq { long long row0; int n, len; };                               // first row, rows, tokens of the cache
+__device__ __forceinline__ AttnSeq attn_seq(const AttnParams& P, uint32_t seq) {
+    AttnSeq s;
+    if (P.q_start) {
+        const int a = __ldg(P.q_start + seq), b = __ldg(P.q_start + seq + 1);
+        const bool good = a >= 0 && b >= a && (uint32_t)b <= P.n_rows && (uint32_t)(b - a) <= P.rows_per_batch;
+        if (!good) atomicCAS(P.pages.status, 0, OC_ERR_INVALID_ARG);
+        s.row0 = a; s.n = good ? b - a : 0;
+    } else {
+        s.row0 = (long long)seq * P.rows_per_batch;
+        const long long left = (long long)P.n_rows - s.row0;
+        s.n = left <= 0 ? 0 : (left < (long long)P.rows_per_batch ? (int)left : (int)P.rows_per_batch);
+    }
+    s.len = (int)P.pages.seq_rows;
+    if (P.kv_len) {
+        const int l = __ldg(P.kv_len + seq);
+        if (l < 0 || l > s.len) atomicCAS(P.pages.status, 0, OC_ERR_INVALID_ARG);
+        s.len = l < 0 ? 0 : min(l, s.len);
+    }
+    return s;
+}
+
+// Keys [lo, hi) that row i of the sequence sees; false if the row is left as it is.
+__device__ __forceinline__ bool attn_bounds(const AttnParams& P, const AttnSeq& s, uint32_t seq, int i, int& lo, int& hi) {
+    long long p = (long long)s.len - s.n + i;
+    lo = 0; hi = s.len;
+    if (P.idx) {
+        const int t = __ldg(P.idx + s.row0 + i);
+        if (t < 0) return false;
+        p = (long long)t - (long long)seq * P.pages.seq_rows;
+        if (p < 0 || p >= (long long)P.pages.seq_rows) { atomicCAS(P.pages.status, 0, OC_ERR_INVALID_ARG); return false; }
+    }
+    if (P.unit > 0) {
+        const int un = (int)P.unit, pi = (int)p;                              // (both fit: unit was clamped to 2^31 - 1)
+        const long long u = pi >= 0 ? pi / un : -(long long)((un - 1 - (long long)pi) / un);
+        if (P.back >= 0) lo = (int)max(0ll, min((long long)s.len, (u - P.back) * P.unit));
+        if (P.ahead >= 0) hi = (int)max(0ll, min((long long)s.len, (u + P.ahead + 1) * P.unit));
+    }
+    return true;
+}
+__device__ __forceinline__ long long attn_q_at(const AttnParams& P, const AttnSeq& s, uint32_t seq, int i, int head) {
+    return (P.q_start ? (s.row0 + i) * P.q_row : (long long)seq * P.q_batch + (long long)i * P.q_row) + (long long)head * P.q_head;
+}
+__device__ __forceinline__ long long attn_out_at(const AttnParams& P, const AttnSeq& s, uint32_t seq, int i, int head) {
+    return (P.q_start ? (s.row0 + i) * P.o_row : (long long)seq * P.o_batch + (long long)i * P.o_row) + (long long)head * P.o_head;
+}
+
+// The sum of the values in column d that are no numbers, over the keys [lo, hi).  Such values are taken as zeros by the
+// kernels, so that they stay away from rows that do not see them, and added at the end to those that do.
+template <int KT>
+__device__ float attn_not_finite(const AttnParams& P, uint32_t seq, uint32_t head, int lo, int hi, int d) {
+    float sum = 0.0f;
+    for (int j = lo; j < hi; ++j) {
+        const uint32_t pn = P.pages.page_rows.div((uint32_t)j);
+        const int page = kv_page(P.pages, seq, pn);
+        if (page < 0) continue;
+        const uint32_t v = kv_vector(P.pages, page, (uint32_t)j - pn * P.pages.page_rows.d) + head * P.pages.page_rows.d;
+        uint32_t x;
+        if (KT == OC_DTYPE_F32) x = __float_as_uint(((const float*)P.v_pool)[(long long)v * P.pages.D + d]);
+        else if (KT == OC_DTYPE_BF16) x = (uint32_t)((const uint16_t*)P.v_pool)[(long long)v * P.pages.D + d] << 16;
+        else x = __float_as_uint(P.v_scale[v] * 0.0f);                        // (a whole number times no number)
+        if ((x & 0x7F800000u) == 0x7F800000u) sum += __uint_as_float(x);
+    }
+    return sum;
+}
+
+// Distributed shared memory of a cluster
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_map(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float cluster_ld(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 cluster_ld4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+// Four neighbouring elements of a row's result
+template <int QT> __device__ __forceinline__ void attn_store4(const AttnParams& P, long long at, float4 v) {
+    if (QT == OC_DTYPE_F32) {
+        float* o = (float*)P.out + at;
+        if (P.wide_out) st_v4(o, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
+        else { o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w; }
+    } else {
+        uint16_t* o = (uint16_t*)P.out + at;
+        const uint32_t a = pack_bf16x2(v.x, v.y), b = pack_bf16x2(v.z, v.w);
+        if (P.wide_out) *(uint2*)o = make_uint2(a, b);
+        else { o[0] = (uint16_t)a; o[1] = (uint16_t)(a >> 16); o[2] = (uint16_t)b; o[3] = (uint16_t)(b >> 16); }
+    }
+}
+#endif
+
+}  // namespace oc

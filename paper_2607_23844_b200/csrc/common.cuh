@@ -205,6 +205,12 @@ oc_status launch_quantize_rows(oc_ctx*, const void* x, int dtype, int64_t x_rows
 oc_status launch_linear_int8(oc_ctx*, const int8_t* a, const float* a_scale, int64_t M, int64_t K, const int8_t* w,
                              const float* w_scale, int64_t N, const float* bias, void* out, int out_dtype, int64_t out_rows,
                              int64_t out_stride, const int32_t* out_idx, cudaStream_t);
+oc_status launch_kv_move(oc_ctx*, bool put, const oc_kv_desc&, const oc_kv_rows&, const int32_t* page_table, const int32_t* idx,
+                         const void* k, const void* k_pool, const float* k_scale, const void* v, const void* v_pool,
+                         const float* v_scale, cudaStream_t);
+oc_status launch_attention(oc_ctx*, const oc_kv_desc&, const oc_attention_desc&, const int32_t* page_table, const int32_t* kv_len,
+                           const int32_t* q_start, const int32_t* idx, const void* q, const void* k_pool, const float* k_scale,
+                           const void* v_pool, const float* v_scale, void* out, float* lse, cudaStream_t);
 size_t joint_workspace_bytes(const Geo&);
 oc_status launch_joint_groups(oc_ctx*, int B, int T, const float* frame_best_sim, const int32_t* frame_best_idx,
                               const int32_t* frame_slot_of, int2* frames, cudaStream_t);

@@ -18,13 +18,14 @@ LIB_PATH = os.path.join(_PKG, "libomnicache_b200.so")
 
 OK, ERR_INVALID_ARG, ERR_ALIGNMENT, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_OOM, CACHE_MISS = range(9)
 KIND_TOKEN, KIND_FRAME, KIND_BLOCK = 0, 1, 2
-DTYPE_F32, DTYPE_BF16, DTYPE_I8 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_I8, DTYPE_I4 = 0, 1, 2, 3
 SELECT_THRESHOLD, SELECT_COUNT = 0, 1
 RESTORE_FROM_CACHE, RESTORE_FROM_REPRESENTATIVE = 0, 1
 FRAME_MEAN_POS_COS, FRAME_FLAT_COS = 0, 1
 (K_NORMS, K_MATCH_TC, K_MATCH_SIMT, K_MATCH_FIN, K_FRAME, K_FRAME_FIN, K_BLOCK, K_BLOCK_FIN, K_SELECT,
- K_GATHER, K_RESTORE, K_COPY, K_LINEAR, K_BLOCK_NORM, K_ROPE, K_QUANT, K_LINEAR_I8) = range(17)
-K_COUNT = 17
+ K_GATHER, K_RESTORE, K_COPY, K_LINEAR, K_BLOCK_NORM, K_ROPE, K_QUANT, K_LINEAR_I8, K_KV_PUT, K_KV_GET,
+ K_ATTENTION) = range(20)
+K_COUNT = 20
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 ROPE_ADJACENT, ROPE_HALVES = 0, 1
 
@@ -38,6 +39,7 @@ EXPORTS = (
     "oc_schedule_propose", "oc_joint_workspace_bytes", "oc_joint_groups", "oc_match_joint", "oc_select_joint",
     "oc_linear_gather_scatter", "oc_tc_plan_override", "oc_tc_plan_describe",
     "oc_block_norm", "oc_rope_table_size", "oc_rope_table", "oc_rope", "oc_quantize_rows", "oc_linear_int8",
+    "oc_kv_bytes", "oc_kv_put", "oc_kv_get", "oc_attention",
 )
 
 
@@ -72,6 +74,20 @@ class CRope(C.Structure):
                 [("axis_dims", C.c_int * 3), ("axis_len", C.c_int * 3), ("eps", C.c_float)] +
                 [(n, C.c_int64) for n in ("n_rows", "rows_per_batch", "unit_rows")] +
                 [(n, CRopeView) for n in ("q", "q_out", "k", "k_out")])
+
+
+class CKv(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("dtype", "heads", "head_dim")] +
+                [(n, C.c_int64) for n in ("n_seqs", "seq_rows", "page_rows", "n_pages", "table_stride")])
+
+
+class CKvRows(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("n_rows", C.c_int64), ("rows_per_batch", C.c_int64), ("k", CRopeView), ("v", CRopeView)]
+
+
+class CAttention(C.Structure):
+    _fields_ = ([("dtype", C.c_int), ("q_heads", C.c_int), ("scale", C.c_float)] +
+                [(n, C.c_int64) for n in ("n_rows", "rows_per_batch", "unit", "back", "ahead")] + [("q", CRopeView), ("out", CRopeView)])
 
 
 if not os.path.exists(LIB_PATH):
@@ -122,6 +138,10 @@ _lib.oc_rope_table.argtypes = [_vp, C.c_double, _vp]
 _lib.oc_rope.argtypes = [_vp, C.POINTER(CRope)] + [_vp] * 10
 _lib.oc_quantize_rows.argtypes = [_vp, _vp, _i, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp]
 _lib.oc_linear_int8.argtypes = [_vp, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _i, _i64, _i64, _vp, _vp]
+_lib.oc_kv_bytes.argtypes = [_vp, _vp, _vp]
+_lib.oc_kv_put.argtypes = [_vp, C.POINTER(CKv), C.POINTER(CKvRows)] + [_vp] * 9
+_lib.oc_kv_get.argtypes = [_vp, C.POINTER(CKv), C.POINTER(CKvRows)] + [_vp] * 9
+_lib.oc_attention.argtypes = [_vp, C.POINTER(CKv), C.POINTER(CAttention)] + [_vp] * 12
 _lib.oc_match_frame_noalloc.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _vp]
 NOALLOC_SCRATCH_BYTES = 1 << 20
 
@@ -364,6 +384,74 @@ def rope_table(desc: CRope, theta: float = 10000.0) -> torch.Tensor:
     return t
 
 
+def kv_desc(dtype: int, heads: int, head_dim: int, n_seqs: int, seq_rows: int, page_rows: int = 64, n_pages: int | None = None,
+            table_stride: int | None = None) -> CKv:
+    """oc_kv_desc: made once for a cache.  n_pages defaults to pages for every token, table_stride to a sequence's pages."""
+    pages = -(-seq_rows // max(page_rows, 1))
+    return CKv(dtype, heads, head_dim, n_seqs, seq_rows, page_rows, n_seqs * pages if n_pages is None else n_pages,
+               pages if table_stride is None else table_stride)
+
+
+def kv_bytes(cache: CKv) -> tuple[int, int]:
+    """oc_kv_bytes: bytes of a pool of keys (or values) and of its scales.  Host only."""
+    pool, scales = C.c_size_t(), C.c_size_t()
+    _chk(_lib.oc_kv_bytes(C.byref(cache), C.byref(pool), C.byref(scales)), "oc_kv_bytes")
+    return pool.value, scales.value
+
+
+def kv_pools(cache: CKv, device="cuda") -> tuple[torch.Tensor, torch.Tensor | None]:
+    """An empty pool of keys (or values), [n_pages, heads, page_rows, head_dim (4 bits: half of it)], and its scales."""
+    shape = (cache.n_pages, cache.heads, cache.page_rows)
+    dt = {DTYPE_F32: torch.float32, DTYPE_BF16: torch.bfloat16, DTYPE_I8: torch.int8, DTYPE_I4: torch.uint8}[cache.dtype]
+    pool = torch.zeros(*shape, cache.head_dim // 2 if cache.dtype == DTYPE_I4 else cache.head_dim, dtype=dt, device=device)
+    return pool, torch.zeros(shape, device=device) if cache.dtype in (DTYPE_I8, DTYPE_I4) else None
+
+
+def _heads_view(t, heads: int, head_dim: int, n_rows: int, per_batch: int, name: str) -> CRopeView:
+    """Strides of [rows, heads, head_dim] or [batch, heads, rows, head_dim] rows (or a (batch, row, head) stride tuple)."""
+    if t is None:
+        return CRopeView(-1, -1, -1)                                 # (refused where it is needed)
+    if isinstance(t, tuple):
+        return CRopeView(*t)
+    if t.dim() not in (3, 4) or t.shape[-1] != head_dim or t.shape[1] != heads or t.stride(-1) != 1:
+        raise ValueError(f"{name}: expected [rows, {heads}, {head_dim}] or [batch, {heads}, rows, {head_dim}] with contiguous heads")
+    if t.dim() == 4:
+        if t.shape[2] < min(per_batch, n_rows) or t.shape[0] * per_batch < n_rows:
+            raise ValueError(f"{name} holds fewer rows than n_rows, or fewer in a batch element than rows_per_batch")
+        return CRopeView(t.stride(0), t.stride(2), t.stride(1))
+    if t.shape[0] < n_rows:
+        raise ValueError(f"{name} holds fewer rows than n_rows")
+    return CRopeView(t.stride(0) * per_batch, t.stride(0), t.stride(1))
+
+
+def _per_batch(rows_per_batch: int | None, n_rows: int, *tensors) -> int:
+    """rows_per_batch, or that of a [batch, heads, rows, head_dim] tensor, or n_rows (one batch element)."""
+    if rows_per_batch is not None:
+        return rows_per_batch
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.dim() == 4:
+            return max(t.shape[2], 1)
+    return max(n_rows, 1)
+
+
+def kv_rows(cache: CKv, n_rows: int, dtype: int, k=None, v=None, rows_per_batch: int | None = None) -> CKvRows:
+    """oc_kv_rows, the strides taken from tensors (or from (batch, row, head) stride tuples): [n_rows, heads, head_dim]
+    views, as a packed projection holds them, or [batch, heads, rows, head_dim], as oc_rope leaves them."""
+    per_batch = _per_batch(rows_per_batch, n_rows, k, v)
+    return CKvRows(dtype, n_rows, per_batch, _heads_view(k, cache.heads, cache.head_dim, n_rows, per_batch, "k"),
+                   _heads_view(v, cache.heads, cache.head_dim, n_rows, per_batch, "v"))
+
+
+def attention_desc(cache: CKv, n_rows: int, dtype: int, q_heads: int, scale: float, rows_per_batch: int | None = None,
+                   unit: int = 0, back: int = -1, ahead: int = -1, q=None, out=None) -> CAttention:
+    """oc_attention_desc, the strides of q and out taken as kv_rows takes them.  With q_start rows_per_batch is the most
+    rows of a sequence."""
+    per_batch = _per_batch(rows_per_batch, n_rows, q, out)
+    return CAttention(dtype, q_heads, scale, n_rows, per_batch, unit, back, ahead,
+                      _heads_view(q, q_heads, cache.head_dim, n_rows, per_batch, "q"),
+                      _heads_view(out, q_heads, cache.head_dim, n_rows, per_batch, "out"))
+
+
 def schedule_propose(latency, quality_loss, target_speedup: float):
     """Layered Cache schedule proposal (Algorithm 1).  Returns (chosen candidate indices in the order
     taken, saved latency).  Host-side: no device work."""
@@ -546,6 +634,35 @@ class Context:
                                  M if out_rows is None else out_rows, out_stride, _ptr(out_idx), _stream(stream))
         if check:
             _chk(st, "oc_linear_int8")
+        return st
+
+    # -- the paged cache and the attention over it -------------------------------------------------
+    def kv_put(self, cache: CKv, rows: CKvRows, k, k_pool, v=None, v_pool=None, k_scale=None, v_scale=None, page_table=None,
+               idx=None, stream=None, check: bool = True) -> int:
+        """oc_kv_put: strides are the descriptor's, so k and v may be parts of one projection."""
+        st = _lib.oc_kv_put(self._h, cache, rows, _ptr(page_table), _ptr(idx), _ptr_strided(k), _ptr(k_pool), _ptr(k_scale),
+                            _ptr_strided(v), _ptr(v_pool), _ptr(v_scale), _stream(stream))
+        if check:
+            _chk(st, "oc_kv_put")
+        return st
+
+    def kv_get(self, cache: CKv, rows: CKvRows, k_pool, k, v_pool=None, v=None, k_scale=None, v_scale=None, page_table=None,
+               idx=None, stream=None, check: bool = True) -> int:
+        """oc_kv_get"""
+        st = _lib.oc_kv_get(self._h, cache, rows, _ptr(page_table), _ptr(idx), _ptr(k_pool), _ptr(k_scale), _ptr_strided(k),
+                            _ptr(v_pool), _ptr(v_scale), _ptr_strided(v), _stream(stream))
+        if check:
+            _chk(st, "oc_kv_get")
+        return st
+
+    def attention(self, cache: CKv, desc: CAttention, q, k_pool, v_pool, out, k_scale=None, v_scale=None, page_table=None,
+                  kv_len=None, q_start=None, idx=None, lse=None, stream=None, check: bool = True) -> int:
+        """oc_attention"""
+        st = _lib.oc_attention(self._h, cache, desc, _ptr(page_table), _ptr(kv_len), _ptr(q_start), _ptr(idx), _ptr_strided(q),
+                               _ptr(k_pool), _ptr(k_scale), _ptr(v_pool), _ptr(v_scale), _ptr_strided(out), _ptr(lse),
+                               _stream(stream))
+        if check:
+            _chk(st, "oc_attention")
         return st
 
     def joint_groups(self, layout: Layout, frame_best_sim, frame_best_idx, frame_slot_of, frames, stream=None,

@@ -586,8 +586,8 @@ oc_status oc_linear_int8(oc_ctx* ctx, const int8_t* a, const float* a_scale, int
  *     the high half, two's complement.
  * A vector whose max|x| is under 2^-100 becomes zeros with scale 0; one with an infinity or NaN keeps
  * that in its scale, its q are zeros (so that its values read as NaN).
- * head_dim is a multiple of 8 and at most 256, page_rows a multiple of 16; pools are 16-byte aligned.
- * A page number outside the pool is recorded as OC_ERR_INVALID_ARG in the device status word; nothing
+ * head_dim is a multiple of 8 and at most 256, page_rows a multiple of 16; pools
+ * and scales are 16-byte aligned.  A page number outside the pool is recorded as OC_ERR_INVALID_ARG in the device status word; nothing
  * is written to it, and it reads as zeros. */
 typedef struct oc_kv_desc {
     int dtype, heads, head_dim;
@@ -614,7 +614,7 @@ typedef struct oc_kv_rows {
  * may be null: a cache of one tensor.  A floating-point cache has the rows' own type.
  * Errors: OC_ERR_INVALID_ARG (also: scales missing, or given for a floating-point cache; a stride of 0
  * between several heads, rows or batch elements of oc_kv_get's rows; an fp32 cache of bf16 rows or the
- * other way round); OC_ERR_ALIGNMENT (a pool not 16-byte aligned, another pointer not aligned to its
+ * other way round); OC_ERR_ALIGNMENT (a pool or its scales not 16-byte aligned, another pointer not aligned to its
  * element, head_dim not a multiple of 8, page_rows not of 16); OC_ERR_UNSUPPORTED (head_dim over 256; 2^31 or
  * more rows, tokens, or vectors in the pool). */
 oc_status oc_kv_put(oc_ctx* ctx, const oc_kv_desc* cache, const oc_kv_rows* rows, const int32_t* page_table, const int32_t* idx,

@@ -606,7 +606,7 @@ static oc_status check_pools(const oc_kv_desc* k, const void* k_pool, const floa
     if (!k_pool || (v && !v_pool)) return OC_ERR_INVALID_ARG;
     if (kv_quantised(k) ? (!k_scale || (v && !v_scale)) : (k_scale || v_scale)) return OC_ERR_INVALID_ARG;
     if (!v && (v_pool || v_scale)) return OC_ERR_INVALID_ARG;
-    if (misaligned(k_pool) || (v && misaligned(v_pool)) || ((uintptr_t)k_scale & 3u) || ((uintptr_t)v_scale & 3u)) return OC_ERR_ALIGNMENT;
+    if (misaligned(k_pool) || (v && misaligned(v_pool)) || misaligned(k_scale) || misaligned(v_scale)) return OC_ERR_ALIGNMENT;
     return OC_OK;
 }
 

@@ -9,7 +9,7 @@
 
 #include <algorithm>
 
-#include "attention.cuh"
+#include "attention_tc.cuh"
 
 namespace oc {
 
@@ -315,9 +315,7 @@ oc_status launch_attention(oc_ctx* ctx, const oc_kv_desc& cache, const oc_attent
         if (cache.dtype == OC_DTYPE_I8) return launch_simt<OC_DTYPE_F32, OC_DTYPE_I8>(ctx, P, s);
         return launch_simt<OC_DTYPE_F32, OC_DTYPE_I4>(ctx, P, s);
     }
-    if (cache.dtype == OC_DTYPE_BF16) return launch_simt<OC_DTYPE_BF16, OC_DTYPE_BF16>(ctx, P, s);
-    if (cache.dtype == OC_DTYPE_I8) return launch_simt<OC_DTYPE_BF16, OC_DTYPE_I8>(ctx, P, s);
-    return launch_simt<OC_DTYPE_BF16, OC_DTYPE_I4>(ctx, P, s);
+    return launch_attention_tc(ctx, P, cache.dtype, cache.page_rows, s);
 }
 
 }  // namespace oc

@@ -96,7 +96,11 @@ __device__ float attn_not_finite(const AttnParams& P, uint32_t seq, uint32_t hea
         uint32_t x;
         if (KT == OC_DTYPE_F32) x = __float_as_uint(((const float*)P.v_pool)[(long long)v * P.pages.D + d]);
         else if (KT == OC_DTYPE_BF16) x = (uint32_t)((const uint16_t*)P.v_pool)[(long long)v * P.pages.D + d] << 16;
-        else x = __float_as_uint(P.v_scale[v] * 0.0f);                        // (a whole number times no number)
+        else {
+            const long long at = (long long)v * P.pages.D + d;
+            const int n = KT == OC_DTYPE_I8 ? (int)((const int8_t*)P.v_pool)[at] : (int)(((uint32_t)((const uint8_t*)P.v_pool)[at >> 1] << (28 - 4 * (d & 1)))) >> 28;
+            x = __float_as_uint((float)n * P.v_scale[v]);
+        }
         if ((x & 0x7F800000u) == 0x7F800000u) sum += __uint_as_float(x);
     }
     return sum;

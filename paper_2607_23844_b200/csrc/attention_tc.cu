@@ -1,0 +1,767 @@
+// Attention over the paged cache on the tensor cores: bf16 queries, keys and values in bf16 or in 8 or 4 bits.
+//     S = Q K^T,   P = exp2(S c - m c),   O = O + P V,   out = O / sum(P)          (c = scale * log2(e))
+// A CTA takes NT tiles of 128 rows (a row is a query with one of the heads that share a head of the cache) and walks
+// over the keys 128 at a time:
+//   softmax warps   four for each tile of rows, a thread for each row: scores out of tensor memory, maximum, exponentials,
+//                   sum, probabilities in bf16 back into tensor memory, where the second product reads them
+//   copy warp       keys and values of the pages: TMA boxes (bf16), bulk copies (8 and 4 bits), into rings
+//   MMA warp        tcgen05.mma, Q K^T from shared memory, P V with P in tensor memory and V as it lies (its rows are the
+//                   product's inner axis)
+//   helper warps    bf16: values of keys behind the sequence become zeros, and so do values that are no numbers where not
+//                   every row sees the tile (0 * NaN would reach the rows that do not); 8 and 4 bits: raw rows to bf16,
+//                   which holds those whole numbers exactly, so that the scales join the scores and the probabilities
+// Two tiles of rows take turns: while one's scores become probabilities the tensor cores work for the other.
+// The maximum that a row subtracts only follows the running one when that is 2^8 ahead: rescaling O in tensor memory
+// is then rare, and the sums lose nothing by it.
+// Where there are few tiles, the CTAs of a cluster split the keys and join their sums through distributed shared memory.
+#include <string.h>
+
+#include <algorithm>
+#include <numeric>
+
+#include "attention.cuh"
+#include "attention_tc.cuh"
+#include "tc_ptx.cuh"
+
+namespace oc {
+
+static constexpr int AT_ROWS = 128, AT_KEYS = 128, AT_SUB_BYTES = 128 * 128;   // a tile of 128 rows of 64 bf16
+static constexpr int AT_SCALES = 4;                                             // stages of the ring of scales
+static constexpr float AT_LAG = 8.0f;                                           // powers of two that a maximum may lag behind
+
+template <int NT, int SUB, int KT> struct At {
+    static constexpr bool quant = KT == OC_DTYPE_I8 || KT == OC_DTYPE_I4;
+    static constexpr bool own_p = SUB == 1;                                      // P beside S in tensor memory, not in its place
+    static constexpr int helpers = quant ? 6 : 2;
+    static constexpr int softmax_warps = 4 * NT, copy_warp = softmax_warps, mma_warp = copy_warp + 1, helper0 = mma_warp + 1;
+    static constexpr int warps = helper0 + helpers, threads = 32 * warps;
+    static constexpr int tile_bytes = SUB * AT_SUB_BYTES;                        // 128 keys (or rows) in bf16
+    static constexpr int raw_bytes = KT == OC_DTYPE_I8 ? tile_bytes / 2 : tile_bytes / 4;        // (most) of 128 keys as they lie
+    static constexpr int k_stages = quant ? (NT * SUB == 4 ? 1 : 2) : (SUB == 1 ? 3 : 2), v_stages = quant ? 2 : k_stages;
+    static constexpr int raw_stages = !quant ? 0 : (SUB == 2 && KT == OC_DTYPE_I8 ? 3 : 4);
+    static constexpr int q_at = 0, k_at = NT * tile_bytes, v_at = k_at + k_stages * tile_bytes, raw_at = v_at + v_stages * tile_bytes;
+    static constexpr int scale_at = raw_at + raw_stages * raw_bytes, rest_at = scale_at + (quant ? AT_SCALES * 2 * AT_KEYS * 4 : 0);
+    static constexpr int n_bars = 2 * k_stages + 3 * v_stages + 2 * raw_stages + 2 * AT_SCALES + 4 * NT + 1;
+    static constexpr int smem = rest_at + n_bars * 8 + 64;
+    static constexpr int s_col = 0, p_col = own_p ? NT * 128 : 0, p_step = own_p ? 64 : 128;
+    static constexpr int o_col = own_p ? NT * 192 : NT * 128, o_step = own_p ? 64 : 128, tmem_cols = NT * 256;
+    static constexpr int out_stride = 64 * SUB + 4;                              // floats between rows where a cluster joins them
+};
+
+// A MN-major operand (V: rows of keys, the inner axis; 64 elements of N contiguous), 128-byte swizzle: groups of 8 keys
+// 1024 bytes apart, the next 64 elements of N a sub-tile further.
+__device__ __forceinline__ uint64_t at_desc_v(uint32_t addr) {
+    const uint32_t lo = ((addr >> 4) & 0x3FFFu) | ((uint32_t)(AT_SUB_BYTES >> 4) << 16);
+    const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+    return ((uint64_t)hi << 32) | lo;
+}
+__device__ __forceinline__ void at_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate, uint32_t issue) {
+    asm volatile("{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 :: "r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
+}
+__device__ __forceinline__ void at_tmem_st32(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+           "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+           "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+           "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void at_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void at_tma_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar, uint32_t issue) {
+    asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+                 "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+                 :: "r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar), "r"(issue) : "memory");
+}
+__device__ __forceinline__ void at_bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint32_t issue) {
+    asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %4, 0;\n\t"
+                 "@e cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
+                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar), "r"(issue) : "memory");
+}
+__device__ __forceinline__ float at_max3(float a, float b, float c) {            // NaN if one of them is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float at_exp2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+
+// 8 whole numbers as bf16.  8 bits: the low 7 of x in the mantissa of 128 (0x4300) give 128 + x mod 128; what is
+// subtracted is 128, or 256 (0x4380) where the sign bit is set, which falls on the exponent's last bit by itself.
+__device__ __forceinline__ uint32_t at_bf16x2_sub(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint4 at_widen_i8(uint2 w) {
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = __byte_perm(i < 2 ? w.x : w.y, 0u, i & 1 ? 0x4342u : 0x4140u);        // two bytes to two halves
+        o[i] = at_bf16x2_sub((x & 0x007F007Fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+// 4 bits: with the sign bit flipped the number is x + 8, in the mantissa of 128: 136 + x.
+__device__ __forceinline__ uint4 at_widen_i4(uint32_t w) {
+    uint32_t o[4];
+    w ^= 0x88888888u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = w >> (8 * i);                                         // elements 2i and 2i + 1
+        o[i] = at_bf16x2_sub(((x & 0xFu) | (x & 0xF0u) << 12) | 0x43004300u, 0x43084308u);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+struct AttnTcParams {
+    AttnParams a;
+    CUtensorMap mapK, mapV;          // bf16: {head_dim, vectors of the pool}, boxes {64, box_rows}
+    int box_rows;                    // rows that a copy takes: the largest piece of 128 keys that no page boundary cuts
+    int n_boxes, row_bytes;
+    FastDiv group;
+};
+
+template <int NT, int SUB, int KT>
+__global__ void __launch_bounds__((At<NT, SUB, KT>::threads), 1)
+attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
+    using A = At<NT, SUB, KT>;
+    const AttnParams& P = TP.a;
+    extern __shared__ __align__(1024) uint8_t at_smem[];
+    __shared__ int s_range[NT][4];                                               // of each tile: first key seen, last, highest first, lowest last
+    __shared__ float s_stats[NT * AT_ROWS][2];
+    __shared__ int s_odd;                                                        // whether a value was no number
+    const uint32_t smem = smem_u32(at_smem);
+    uint64_t* bars = (uint64_t*)(at_smem + A::rest_at);
+    const uint32_t bar0 = smem_u32(bars);
+    const uint32_t k_full = bar0, k_empty = k_full + 8 * A::k_stages, v_full = k_empty + 8 * A::k_stages, v_ready = v_full + 8 * A::v_stages;
+    const uint32_t v_empty = v_ready + 8 * A::v_stages, raw_full = v_empty + 8 * A::v_stages, raw_empty = raw_full + 8 * A::raw_stages;
+    const uint32_t sc_full = raw_empty + 8 * A::raw_stages, sc_empty = sc_full + 8 * AT_SCALES;
+    const uint32_t s_full = sc_empty + 8 * AT_SCALES, s_free = s_full + 8 * NT, p_ready = s_free + 8 * NT, o_done = p_ready + 8 * NT, drain = o_done + 8 * NT;
+    uint32_t* tmem_slot = (uint32_t*)(bars + A::n_bars);
+    volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = P.pages.D;
+
+    if (smem & 1023u) {                                                          // never expected; refuse rather than compute garbage
+        if (threadIdx.x == 0) atomicCAS(P.pages.status, 0, OC_ERR_ALIGNMENT);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < A::k_stages; ++i) { mbar_init(k_full + 8 * i, A::quant ? A::helpers : 1); mbar_init(k_empty + 8 * i, 1); }
+        for (int i = 0; i < A::v_stages; ++i) { mbar_init(v_full + 8 * i, 1); mbar_init(v_ready + 8 * i, A::helpers); mbar_init(v_empty + 8 * i, 1); }
+        for (int i = 0; i < A::raw_stages; ++i) { mbar_init(raw_full + 8 * i, 1); mbar_init(raw_empty + 8 * i, A::helpers); }
+        for (int i = 0; i < AT_SCALES; ++i) { mbar_init(sc_full + 8 * i, 1); mbar_init(sc_empty + 8 * i, A::softmax_warps); }
+        for (int t = 0; t < NT; ++t) { mbar_init(s_full + 8 * t, 1); mbar_init(s_free + 8 * t, 4); mbar_init(p_ready + 8 * t, 4); mbar_init(o_done + 8 * t, 1); }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        s_odd = 0;
+        for (int t = 0; t < NT; ++t) { s_range[t][0] = 0x7FFFFFFF; s_range[t][1] = 0; s_range[t][2] = 0; s_range[t][3] = 0x7FFFFFFF; }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        if (!A::quant) { tma_prefetch_map(&TP.mapK); tma_prefetch_map(&TP.mapV); }
+    }
+    pdl_wait();
+    const uint32_t rank = P.split > 1 ? cluster_rank() : 0u;
+    const AttnTile T = attn_tile(P, blockIdx.x / (uint32_t)P.split);
+    const AttnSeq S = attn_seq(P, T.seq);
+    const uint32_t first = T.tile * (uint32_t)(NT * AT_ROWS), rows = (uint32_t)S.n * (uint32_t)P.group;
+    if (first >= rows) return;                                                   // (the whole cluster; nothing is allocated yet)
+    if (warp == A::mma_warp) tmem_alloc_cta1(smem_u32(tmem_slot), A::tmem_cols);
+    __syncwarp();
+    __syncthreads();                                                             // (the ranges are set up)
+    // ---- rows: which keys they see; queries into shared memory (rows that are not there as zeros) ----
+    const int my_tile = warp >> 2, my_row = (warp & 3) * 32 + lane;              // of a softmax thread
+    bool exists = false;
+    int lo = 0, hi = 0, qi = 0, qg = 0;
+    if (warp < A::softmax_warps) {
+        const uint32_t r = first + (uint32_t)(my_tile * AT_ROWS + my_row);
+        if (r < rows) {
+            qi = (int)TP.group.div(r); qg = (int)(r - (uint32_t)qi * TP.group.d);
+            exists = attn_bounds(P, S, T.seq, qi, lo, hi);
+            if (exists && lo < hi) {
+                atomicMin(&s_range[my_tile][0], lo); atomicMax(&s_range[my_tile][1], hi);
+                atomicMax(&s_range[my_tile][2], lo); atomicMin(&s_range[my_tile][3], hi);
+            } else {
+                lo = hi = 0;
+            }
+        }
+        constexpr int UN = SUB * 8;
+        for (int i = threadIdx.x; i < NT * AT_ROWS * UN; i += 32 * A::softmax_warps) {
+            const int rr = i / UN, u = i % UN;
+            const uint32_t r2 = first + (uint32_t)rr;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (r2 < rows && 8 * u < D) {
+                const uint32_t q2 = TP.group.div(r2);
+                const uint16_t* q = (const uint16_t*)P.q + attn_q_at(P, S, T.seq, (int)q2, (int)T.head * P.group + (int)(r2 - q2 * TP.group.d)) + 8 * u;
+                if (P.wide_q) v = ld_v4(q);
+                else {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)q[2 * e] | (uint32_t)q[2 * e + 1] << 16;
+                    v = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+            const uint32_t at = smem + A::q_at + (uint32_t)((rr >> 7) * A::tile_bytes + (u >> 3) * AT_SUB_BYTES + (rr & 127) * 128 + (((u & 7) ^ (rr & 7)) << 4));
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    // (not before this CTA has its tensor memory: a kernel that takes its own before it waits for this one could have it)
+    if (threadIdx.x == 0) pdl_launch_dependents();
+    // Tiles of keys [a, b) of each tile of rows; this CTA's share of them all.
+    int ka[NT], kb[NT], j0 = 0x7FFFFFFF, j1 = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const bool any = s_range[t][1] > 0;                                      // (some row sees a key)
+        ka[t] = any ? s_range[t][0] / AT_KEYS : 0; kb[t] = any ? (s_range[t][1] + AT_KEYS - 1) / AT_KEYS : 0;
+        if (any) { j0 = min(j0, ka[t]); j1 = max(j1, kb[t]); }
+    }
+    if (j1 == 0) j0 = 0;
+    if (P.split > 1) {
+        const int n = j1 - j0, a = (int)((long long)n * rank / P.split), b = (int)((long long)n * (rank + 1) / P.split);
+        j1 = j0 + b; j0 += a;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) { ka[t] = max(ka[t], j0); kb[t] = max(min(kb[t], j1), ka[t]); }
+    auto on = [&](int j, int t) { return j >= ka[t] && j < kb[t]; };
+    bool ok = true;
+#define AT_WAIT(bar, parity) (ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait((bar), (parity), abort_flag)))
+
+    if (warp == A::copy_warp) {
+        // ================================ copies ================================================
+        const uint32_t issue = elect_one();
+        // the pool's vector where box `lane` of a tile begins (-1: a page that is not there, -2: behind the last key)
+        auto find = [&](int j) -> int {
+            const int key = j * AT_KEYS + lane * TP.box_rows;
+            if (lane >= TP.n_boxes || key >= S.len) return -2;
+            const uint32_t pn = P.pages.page_rows.div((uint32_t)key);
+            const int page = kv_page(P.pages, T.seq, pn);
+            return page < 0 ? -1 : (int)(kv_vector(P.pages, page, (uint32_t)key - pn * P.pages.page_rows.d) + T.head * P.pages.page_rows.d);
+        };
+        uint32_t bytes_pending = 0;
+        if (!A::quant) {
+            int stage = 0; uint32_t phase = 0;
+            int at = j0 < j1 ? find(j0) : -2, at_v = at;
+            const int vectors = (int)(P.pages.n_pages * (uint32_t)P.pages.heads * P.pages.page_rows.d);
+            auto load = [&](const CUtensorMap* map, uint32_t to, uint32_t bar, int where) {
+                uint32_t boxes = 0;
+                for (int b = 0; b < TP.n_boxes; ++b) {
+                    const int v = __shfl_sync(0xFFFFFFFFu, where, b);
+                    if (v == -2) break;
+#pragma unroll
+                    for (int s = 0; s < SUB; ++s)                                // (a box wholly outside the pool is filled with zeros)
+                        at_tma_2d(to + (uint32_t)(s * AT_SUB_BYTES + b * TP.box_rows * 128), map, 64 * s, v < 0 ? vectors : v, bar, issue);
+                    ++boxes;
+                }
+                mbar_arrive_expect_tx_elected(bar, boxes * (uint32_t)(TP.box_rows * 128 * SUB), issue);
+                bytes_pending = bar;
+            };
+            // keys of a tile are wanted one tile before its values
+            for (int j = j0; j < j1 + 1 && ok; ++j) {
+                const int next = j + 1 < j1 ? find(j + 1) : -2;
+                if (j < j1) {
+                    const int st = (j - j0) % A::k_stages; const uint32_t ph = (uint32_t)((j - j0) / A::k_stages) & 1u;
+                    if (!AT_WAIT(k_empty + 8 * st, ph ^ 1u)) break;
+                    load(&TP.mapK, smem + A::k_at + (uint32_t)(st * A::tile_bytes), k_full + 8 * st, at);
+                }
+                if (j > j0) {
+                    if (!AT_WAIT(v_empty + 8 * stage, phase ^ 1u)) break;
+                    load(&TP.mapV, smem + A::v_at + (uint32_t)(stage * A::tile_bytes), v_full + 8 * stage, at_v);
+                    if (++stage == A::v_stages) { stage = 0; phase ^= 1u; }
+                }
+                at_v = at; at = next;
+            }
+        } else {
+            int stage = 0; uint32_t phase = 0;
+            int at = j0 < j1 ? find(j0) : -2, at_v = at;
+            auto load = [&](const void* pool, int where) {
+                if (!AT_WAIT(raw_empty + 8 * stage, phase ^ 1u)) return;
+                const uint32_t to = smem + A::raw_at + (uint32_t)(stage * A::raw_bytes), bar = raw_full + 8 * stage, bytes = (uint32_t)(TP.box_rows * TP.row_bytes);
+                uint32_t boxes = 0;
+                for (int b = 0; b < TP.n_boxes; ++b) {
+                    const int v = __shfl_sync(0xFFFFFFFFu, where, b);
+                    if (v < 0) continue;
+                    at_bulk(to + (uint32_t)b * bytes, (const uint8_t*)pool + (long long)v * TP.row_bytes, bytes, bar, issue);
+                    ++boxes;
+                }
+                mbar_arrive_expect_tx_elected(bar, boxes * bytes, issue);
+                bytes_pending = bar;
+                if (++stage == A::raw_stages) { stage = 0; phase ^= 1u; }
+            };
+            for (int j = j0; j < j1 + 1 && ok; ++j) {
+                const int next = j + 1 < j1 ? find(j + 1) : -2;
+                if (j < j1) {
+                    load(P.k_pool, at);
+                    const int st = (j - j0) % AT_SCALES; const uint32_t ph = (uint32_t)((j - j0) / AT_SCALES) & 1u;
+                    if (!ok || !AT_WAIT(sc_empty + 8 * st, ph ^ 1u)) break;
+                    const uint32_t to = smem + A::scale_at + (uint32_t)(st * 2 * AT_KEYS * 4), bytes = (uint32_t)TP.box_rows * 4u;
+                    uint32_t boxes = 0;
+                    bool zeros = false;
+                    for (int b = 0; b < TP.n_boxes; ++b) {
+                        const int v = __shfl_sync(0xFFFFFFFFu, at, b);
+                        if (v == -2) break;
+                        if (v == -1) {                                           // (a page that is not there: values of zero)
+                            for (int i = lane; i < TP.box_rows; i += 32) {
+                                asm volatile("st.shared.b32 [%0], %1;" :: "r"(to + (uint32_t)b * bytes + 4u * i), "r"(0u) : "memory");
+                                asm volatile("st.shared.b32 [%0], %1;" :: "r"(to + AT_KEYS * 4u + (uint32_t)b * bytes + 4u * i), "r"(0u) : "memory");
+                            }
+                            zeros = true;
+                            continue;
+                        }
+                        at_bulk(to + (uint32_t)b * bytes, P.k_scale + v, bytes, sc_full + 8 * st, issue);
+                        at_bulk(to + AT_KEYS * 4u + (uint32_t)b * bytes, P.v_scale + v, bytes, sc_full + 8 * st, issue);
+                        ++boxes;
+                    }
+                    if (zeros) __syncwarp();
+                    mbar_arrive_expect_tx_elected(sc_full + 8 * st, 2 * boxes * bytes, issue);
+                }
+                if (j > j0) load(P.v_pool, at_v);
+                at_v = at; at = next;
+            }
+        }
+        if (!ok && lane == 0) {
+            atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT);
+            *abort_flag = 1;
+            // copies already issued still write this CTA's shared memory: a bounded chance to land
+            if (bytes_pending) { const unsigned long long t0 = global_ns(); while (global_ns() - t0 < 20000000ull) {} }
+        }
+    } else if (warp == A::mma_warp) {
+        // ================================ MMAs ==================================================
+        constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(AT_KEYS >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
+        const uint32_t n_out = (uint32_t)(D + 15) / 16u * 16u;
+        const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((n_out >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
+        const int steps = (D + 15) / 16;
+        const uint32_t issue = elect_one();
+        int n_s[NT] = {}, n_p[NT] = {};                                          // score and output products issued for each tile of rows
+        auto scores = [&](int j, int t) {
+            const int st = (j - j0) % A::k_stages;
+            const uint64_t q = make_smem_desc(smem + A::q_at + (uint32_t)(t * A::tile_bytes)), k = make_smem_desc(smem + A::k_at + (uint32_t)(st * A::tile_bytes));
+            for (int i = 0; i < steps; ++i) {                                    // 16 elements, 32 bytes, at a time along the swizzled rows
+                const uint64_t off = (uint64_t)((i >> 2) * (AT_SUB_BYTES >> 4) + 2 * (i & 3));
+                tc_mma_bf16<false>(tmem + (uint32_t)(A::s_col + t * 128), q + off, k + off, IDESC_S, (uint32_t)(i != 0), issue);
+            }
+            tc_commit<false>(s_full + 8 * t, issue);
+            ++n_s[t];
+        };
+        auto outputs = [&](int j, int t) {
+            const int st = (j - j0) % A::v_stages;
+            const uint64_t v = at_desc_v(smem + A::v_at + (uint32_t)(st * A::tile_bytes));
+#pragma unroll
+            for (int i = 0; i < AT_KEYS / 16; ++i)                               // 16 keys at a time: 8 columns of P, 2048 bytes of V
+                at_mma_ts(tmem + (uint32_t)(A::o_col + t * A::o_step), tmem + (uint32_t)(A::p_col + t * A::p_step + 8 * i), v + (uint64_t)(128 * i), idesc_o,
+                          (uint32_t)(n_p[t] != 0 || i != 0), issue);
+            tc_commit<false>(o_done + 8 * t, issue);
+            ++n_p[t];
+        };
+        auto parity = [&](int j, int stages) { return (uint32_t)((j - j0) / stages) & 1u; };
+        if (j0 < j1 && AT_WAIT(k_full, 0u)) {
+            tc_fence_after();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) if (on(j0, t)) scores(j0, t);
+            tc_commit<false>(k_empty, issue);
+        }
+        for (int j = j0; j < j1 && ok; ++j) {
+            const bool more = j + 1 < j1;
+            bool have_k = false, have_v = false;
+            const int ks = (j + 1 - j0) % A::k_stages, vs = (j - j0) % A::v_stages;
+            auto next = [&](int t) {
+                if (!more || !on(j + 1, t)) return;
+                if (!have_k) { if (!AT_WAIT(k_full + 8 * ks, parity(j + 1, A::k_stages))) return; have_k = true; tc_fence_after(); }
+                if (A::own_p && n_s[t] > 0) { if (!AT_WAIT(s_free + 8 * t, (uint32_t)(n_s[t] - 1) & 1u)) return; tc_fence_after(); }
+                scores(j + 1, t);
+            };
+            auto now = [&](int t) {
+                if (!on(j, t)) return;
+                if (!have_v) { if (!AT_WAIT(v_ready + 8 * vs, parity(j, A::v_stages))) return; have_v = true; }
+                if (!AT_WAIT(p_ready + 8 * t, (uint32_t)n_p[t] & 1u)) return;
+                tc_fence_after();
+                outputs(j, t);
+            };
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if (A::own_p) { if (ok) next(t); if (ok) now(t); }
+                else { if (ok) now(t); if (ok) next(t); }                        // (P lies in the place of S)
+            }
+            if (!ok) break;
+            // (a stage that no tile of rows used is given back like the others)
+            if (!have_v && !AT_WAIT(v_ready + 8 * vs, parity(j, A::v_stages))) break;
+            tc_commit<false>(v_empty + 8 * vs, issue);
+            if (more) {
+                if (!have_k && !AT_WAIT(k_full + 8 * ks, parity(j + 1, A::k_stages))) break;
+                tc_commit<false>(k_empty + 8 * ks, issue);
+            }
+        }
+        if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
+        // every MMA retires before tensor memory is released
+        tc_commit<false>(drain, issue);
+        const unsigned long long t0 = global_ns();
+        while (!mbar_try_wait(drain, 0) && global_ns() - t0 < WAIT_LIMIT_NS) {}
+    } else if (warp >= A::helper0) {
+        // ================================ helpers ===============================================
+        const int h = warp - A::helper0;
+        if (!A::quant) {
+            int cut_lo = 0, cut_hi = 0x7FFFFFFF;                                 // tiles within are seen whole by every row
+#pragma unroll
+            for (int t = 0; t < NT; ++t) if (s_range[t][1] > 0) { cut_lo = max(cut_lo, s_range[t][2]); cut_hi = min(cut_hi, s_range[t][3]); }
+            for (int j = j0; j < j1; ++j) {
+                const int st = (j - j0) % A::v_stages;
+                if (!AT_WAIT(v_full + 8 * st, (uint32_t)((j - j0) / A::v_stages) & 1u)) break;
+                const int key0 = j * AT_KEYS;
+                if (key0 < cut_lo || key0 + AT_KEYS > cut_hi) {
+                    const uint32_t base = smem + A::v_at + (uint32_t)(st * A::tile_bytes);
+                    bool odd = false;
+                    for (int i = h * 32 + lane; i < SUB * 1024; i += 32 * A::helpers) {          // pieces of 16 bytes
+                        const uint32_t at = base + (uint32_t)(i * 16);
+                        const bool there = key0 + ((i >> 3) & 127) < S.len;
+                        uint32_t w[4];
+                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+                        bool change = !there;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool a = (w[e] & 0x7F80u) == 0x7F80u, b = (w[e] & 0x7F800000u) == 0x7F800000u;
+                            if (there && (a || b)) { odd = change = true; }
+                            w[e] = there ? w[e] & ((a ? 0u : 0xFFFFu) | (b ? 0u : 0xFFFF0000u)) : 0u;
+                        }
+                        if (change) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    }
+                    if (odd) s_odd = 1;
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(v_ready + 8 * st);
+            }
+        } else {
+            const int units = (D + 15) / 16 * 2, raw_units = D / 8;              // of 8 elements; with those that fill up a product's step
+            int stage = 0; uint32_t phase = 0;
+            auto widen = [&](uint32_t base) {
+                const uint32_t raw = smem + A::raw_at + (uint32_t)(stage * A::raw_bytes);
+                for (int i = h * 32 + lane; i < AT_KEYS * 8 * SUB; i += 32 * A::helpers) {
+                    const int r = i / (8 * SUB), u = i % (8 * SUB);
+                    if (u >= units) continue;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (u < raw_units) {
+                        if (KT == OC_DTYPE_I8) {
+                            uint2 w;
+                            asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w.x), "=r"(w.y) : "r"(raw + (uint32_t)(r * D + 8 * u)) : "memory");
+                            v = at_widen_i8(w);
+                        } else {
+                            uint32_t w;
+                            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(raw + (uint32_t)(r * (D / 2) + 4 * u)) : "memory");
+                            v = at_widen_i4(w);
+                        }
+                    }
+                    const uint32_t at = base + (uint32_t)((u >> 3) * AT_SUB_BYTES + r * 128 + (((u & 7) ^ (r & 7)) << 4));
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            };
+            for (int j = j0; j < j1 + 1 && ok; ++j) {                            // in the order of the copies
+                if (j < j1) {
+                    const int st = (j - j0) % A::k_stages;
+                    if (!AT_WAIT(raw_full + 8 * stage, phase) || !AT_WAIT(k_empty + 8 * st, ((uint32_t)((j - j0) / A::k_stages) & 1u) ^ 1u)) break;
+                    widen(smem + A::k_at + (uint32_t)(st * A::tile_bytes));
+                    if (lane == 0) { mbar_arrive(k_full + 8 * st); mbar_arrive(raw_empty + 8 * stage); }
+                    if (++stage == A::raw_stages) { stage = 0; phase ^= 1u; }
+                }
+                if (j > j0) {
+                    const int st = (j - 1 - j0) % A::v_stages;
+                    if (!AT_WAIT(raw_full + 8 * stage, phase) || !AT_WAIT(v_empty + 8 * st, ((uint32_t)((j - 1 - j0) / A::v_stages) & 1u) ^ 1u)) break;
+                    widen(smem + A::v_at + (uint32_t)(st * A::tile_bytes));
+                    if (lane == 0) { mbar_arrive(v_ready + 8 * st); mbar_arrive(raw_empty + 8 * stage); }
+                    if (++stage == A::raw_stages) { stage = 0; phase ^= 1u; }
+                }
+            }
+        }
+        if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
+    } else {
+        // ================================ softmax ===============================================
+        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_at = t_lane + (uint32_t)(A::s_col + my_tile * 128), p_at = t_lane + (uint32_t)(A::p_col + my_tile * A::p_step);
+        const uint32_t o_at = t_lane + (uint32_t)(A::o_col + my_tile * A::o_step);
+        const float c = P.scale_log2, lag = AT_LAG / c;
+        float m = -INFINITY, l = 0.0f;                                           // what the row subtracts; its sum
+        int n = 0;                                                               // tiles of keys done
+        for (int j = j0; j < j1 && ok; ++j) {
+            const int sst = (j - j0) % AT_SCALES;
+            const uint32_t sc_at = smem + A::scale_at + (uint32_t)(sst * 2 * AT_KEYS * 4);
+            if (A::quant && !on(j, my_tile)) {
+                if (!AT_WAIT(sc_full + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
+                if (lane == 0) mbar_arrive(sc_empty + 8 * sst);
+            }
+            if (!on(j, my_tile)) continue;
+            if (!AT_WAIT(s_full + 8 * my_tile, (uint32_t)n & 1u)) break;
+            tc_fence_after();
+            uint32_t s[128];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32u * i, s + 32 * i);
+            if (A::quant && !AT_WAIT(sc_full + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
+            tmem_ld_wait();
+            if (A::own_p) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_free + 8 * my_tile);
+            }
+            if (A::quant) {
+#pragma unroll
+                for (int i = 0; i < 128; i += 4) {
+                    float4 k;
+                    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w) : "r"(sc_at + 4u * i) : "memory");
+                    s[i] = __float_as_uint(__uint_as_float(s[i]) * k.x); s[i + 1] = __float_as_uint(__uint_as_float(s[i + 1]) * k.y);
+                    s[i + 2] = __float_as_uint(__uint_as_float(s[i + 2]) * k.z); s[i + 3] = __float_as_uint(__uint_as_float(s[i + 3]) * k.w);
+                }
+            }
+            const int key0 = j * AT_KEYS;
+            const bool cut = __any_sync(0xFFFFFFFFu, exists && lo < hi && (key0 < lo || key0 + AT_KEYS > hi));
+            if (cut) {
+#pragma unroll
+                for (int i = 0; i < 128; ++i) if (key0 + i < lo || key0 + i >= hi) s[i] = 0xFF800000u;
+            }
+            float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 0; i < 128; i += 8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most[e] = at_max3(most[e], __uint_as_float(s[i + 2 * e]), __uint_as_float(s[i + 2 * e + 1]));
+            const float top = at_max3(at_max3(most[0], most[1], most[2]), most[3], m);
+            if (n > 0 && A::own_p && !AT_WAIT(o_done + 8 * my_tile, (uint32_t)(n - 1) & 1u)) break;
+            // (a maximum of NaN is passed on to the whole row; that of +infinity makes every exponential of the row NaN)
+            if (__any_sync(0xFFFFFFFFu, !(top <= m + lag) && top != -INFINITY)) {
+                const float to = top == INFINITY ? __int_as_float(0x7FFFFFFF) : top;
+                const float corr = to == -INFINITY ? 1.0f : at_exp2((m - to) * c);
+                if (n > 0) {
+                    tc_fence_after();
+                    for (int d = 0; d < D; d += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_at + (uint32_t)d, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(m == -INFINITY ? 0.0f : __uint_as_float(o[i]) * corr);
+                        at_tmem_st32(o_at + (uint32_t)d, o);
+                    }
+                    at_tmem_st_wait();
+                    tc_fence_before();
+                }
+                l *= corr;
+                m = to;
+            }
+            const float shift = m == -INFINITY ? 0.0f : -m * c;                  // (nothing seen so far: every p is 0)
+            const f32x2 c2 = f2(c), shift2 = f2(shift);
+            f32x2 sum[2] = {0, 0};
+            uint32_t w[64];
+#pragma unroll
+            for (int i = 0; i < 64; ++i) {
+                const f32x2 x = f2_fma(f2_bits(s[2 * i], s[2 * i + 1]), c2, shift2);
+                float p0 = at_exp2(f2_lo(x)), p1 = at_exp2(f2_hi(x));
+                sum[i & 1] = f2_add(sum[i & 1], f2(p0, p1));
+                if (A::quant) {
+                    float v0, v1;
+                    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(sc_at + AT_KEYS * 4u + 8u * i) : "memory");
+                    p0 *= v0; p1 *= v1;
+                    if (cut) {                                                   // (0 times a scale that is no number)
+                        if (s[2 * i] == 0xFF800000u) p0 = 0.0f;
+                        if (s[2 * i + 1] == 0xFF800000u) p1 = 0.0f;
+                    }
+                }
+                w[i] = pack_bf16x2(p0, p1);
+            }
+            if (A::quant) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sc_empty + 8 * sst);
+            }
+            const f32x2 both = f2_add(sum[0], sum[1]);
+            l += f2_lo(both) + f2_hi(both);
+            at_tmem_st32(p_at, w);
+            at_tmem_st32(p_at + 32u, w + 32);
+            at_tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_ready + 8 * my_tile);
+            ++n;
+        }
+        if (ok && n > 0) AT_WAIT(o_done + 8 * my_tile, (uint32_t)(n - 1) & 1u);
+        if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
+        tc_fence_after();
+        // ---- results ----
+        if (P.split == 1) {
+            const bool some = lo < hi;
+            const float inv = 1.0f / l;                                          // (all scores -infinity: 0 / 0)
+            const int head = (int)T.head * P.group + qg;
+            const long long at = exists ? attn_out_at(P, S, T.seq, qi, head) : 0;
+            for (int d = 0; d < D; d += 32) {
+                uint32_t o[32];
+                if (n > 0) { tmem_ld32(o_at + (uint32_t)d, o); tmem_ld_wait(); }
+                if (!exists || !ok) continue;
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    if (d + i >= D) break;
+                    float y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = some ? __uint_as_float(o[i + e]) * inv : 0.0f;
+                    if (s_odd && some && !A::quant)
+                        for (int e = 0; e < 8; ++e) y[e] += attn_not_finite<KT>(P, T.seq, T.head, max(lo, 0), hi, d + i + e);
+                    const uint4 v = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+                    uint16_t* out = (uint16_t*)P.out + at + d + i;
+                    if (P.wide_out) st_v4(out, v);
+                    else {
+                        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { out[2 * e] = (uint16_t)x[e]; out[2 * e + 1] = (uint16_t)(x[e] >> 16); }
+                    }
+                }
+            }
+            if (P.lse && exists && ok) P.lse[(S.row0 + qi) * P.q_heads + head] = some ? m * P.scale + logf(l) : -INFINITY;
+        } else {
+            const int r = my_tile * AT_ROWS + my_row;
+            float* part = (float*)at_smem + (long long)r * A::out_stride;
+            s_stats[r][0] = m; s_stats[r][1] = l;
+            // (both tiles' products have retired in this CTA: the rows overwrite queries, keys and values)
+            asm volatile("bar.sync 1, %0;" :: "n"(32 * A::softmax_warps) : "memory");
+            for (int d = 0; d < D; d += 32) {
+                uint32_t o[32];
+                if (n > 0) { tmem_ld32(o_at + (uint32_t)d, o); tmem_ld_wait(); }
+#pragma unroll
+                for (int i = 0; i < 32; i += 4)
+                    if (d + i < D) *(float4*)(part + d + i) = n > 0 ? make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]))
+                                                                    : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+        }
+    }
+    if (P.split > 1) {
+        cluster_sync();
+        if (warp < A::softmax_warps && !*abort_flag) {
+            int odd = 0;
+            for (int k = 0; k < P.split; ++k) {
+                int w;
+                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(w) : "r"(cluster_map(smem_u32(&s_odd), (uint32_t)k)) : "memory");
+                odd |= w;
+            }
+            // every split-th row, its elements side by side
+            const int vecs = D / 4, mine = (NT * AT_ROWS) / P.split;
+            const uint32_t stats = smem_u32(&s_stats[0][0]);
+            for (int i = threadIdx.x; i < mine * vecs; i += 32 * A::softmax_warps) {
+                const int r = (i / vecs) * P.split + (int)rank, d = 4 * (i % vecs);
+                const uint32_t rr = first + (uint32_t)r;
+                if (rr >= rows) continue;
+                const int q2 = (int)TP.group.div(rr), head = (int)T.head * P.group + (int)(rr - (uint32_t)q2 * TP.group.d);
+                int a, b;
+                if (!attn_bounds(P, S, T.seq, q2, a, b)) continue;
+                float top = -INFINITY, sum = 0.0f;
+                for (int k = 0; k < P.split; ++k) {
+                    float x = cluster_ld(cluster_map(stats, (uint32_t)k) + 8u * r);
+                    top = at_max3(top, x, x);
+                }
+                float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (a < b) {
+                    for (int k = 0; k < P.split; ++k) {
+                        const uint32_t st = cluster_map(stats, (uint32_t)k) + 8u * r;
+                        const float x = cluster_ld(st), f = x == -INFINITY ? 0.0f : at_exp2((x - top) * P.scale_log2);
+                        sum = fmaf(f, cluster_ld(st + 4), sum);
+                        const float4 o = cluster_ld4(cluster_map(smem, (uint32_t)k) + (uint32_t)(r * A::out_stride + d) * 4u);
+                        if (x != -INFINITY) { y.x = fmaf(f, o.x, y.x); y.y = fmaf(f, o.y, y.y); y.z = fmaf(f, o.z, y.z); y.w = fmaf(f, o.w, y.w); }
+                    }
+                    const float inv = 1.0f / sum;
+                    y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+                    if (odd && !A::quant) {
+                        y.x += attn_not_finite<KT>(P, T.seq, T.head, a, b, d); y.y += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 1);
+                        y.z += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 2); y.w += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 3);
+                    }
+                }
+                attn_store4<OC_DTYPE_BF16>(P, attn_out_at(P, S, T.seq, q2, head) + d, y);
+                if (P.lse && d == 0) P.lse[(S.row0 + q2) * P.q_heads + head] = a < b ? top * P.scale + logf(sum) : -INFINITY;
+            }
+        }
+        cluster_sync();                                                          // nobody reads a retired CTA's memory
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == A::mma_warp) tmem_dealloc_cta1(tmem, A::tmem_cols);
+#undef AT_WAIT
+}
+
+// ---- host side -------------------------------------------------------------------------------------
+typedef CUresult (*AtEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static AtEncodeFn at_encode_fn() {
+    static AtEncodeFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess) fn = (AtEncodeFn)p;
+        else cudaGetLastError();
+    });
+    return fn;
+}
+static bool at_encode(AtEncodeFn enc, CUtensorMap* map, const void* p, int64_t D, int64_t vectors, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)vectors}, strides[1] = {(cuuint64_t)D * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (void*)p, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int NT, int SUB, int KT>
+static oc_status launch_tc_as(oc_ctx* ctx, AttnTcParams& TP, cudaStream_t s) {
+    using A = At<NT, SUB, KT>;
+    static_assert(A::smem <= 227 * 1024 - 4096, "shared memory");                // (beside the ranges and sums)
+    static_assert(NT * AT_ROWS * A::out_stride * 4 <= A::rest_at, "rows that a cluster joins");
+    auto* kernel = attention_tc_kernel<NT, SUB, KT>;
+    static PerDeviceOnce once;                       // (the context's device is current here)
+    if (!once.ensure(ctx->device, [&] {
+            const bool ok = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, A::smem) == cudaSuccess &&
+                            cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+            if (!ok) cudaGetLastError();
+            return ok;
+        })) return OC_ERR_CUDA;
+    AttnParams& P = TP.a;
+    const uint64_t rows = (uint64_t)P.rows_per_batch * (uint64_t)P.group;
+    const uint64_t tiles = (rows + NT * AT_ROWS - 1) / (NT * AT_ROWS), problems = (uint64_t)P.n_seqs * (uint64_t)P.pages.heads;
+    if (tiles * problems * ATT_SPLIT_MAX > 0x7FFFFFFFull) return OC_ERR_UNSUPPORTED;
+    P.tiles = (uint32_t)tiles;
+    const uint64_t key_tiles = (P.pages.seq_rows + AT_KEYS - 1) / AT_KEYS;
+    int split = 1;
+    while (split < ATT_SPLIT_MAX && tiles * problems * split * 2 <= (uint64_t)ctx->sm_count && (uint64_t)split * 2 <= key_tiles) split *= 2;
+    P.split = split;
+    LaunchScope scope(ctx, OC_K_ATTENTION, s);
+    PdlLaunch l(dim3((unsigned)(tiles * problems * split)), dim3(A::threads), A::smem, s, (unsigned)split);
+    cudaLaunchKernelEx(&l.cfg, kernel, (const AttnTcParams&)TP);
+    return last_launch_status();
+}
+template <int SUB, int KT>
+static oc_status launch_tc_rows(oc_ctx* ctx, AttnTcParams& TP, cudaStream_t s) {
+    const uint64_t rows = (uint64_t)TP.a.rows_per_batch * (uint64_t)TP.a.group, problems = (uint64_t)TP.a.n_seqs * (uint64_t)TP.a.pages.heads;
+    // one tile of rows in a CTA where pairs would leave SMs idle
+    if (rows <= AT_ROWS || (rows + 2 * AT_ROWS - 1) / (2 * AT_ROWS) * problems < (uint64_t)ctx->sm_count) return launch_tc_as<1, SUB, KT>(ctx, TP, s);
+    return launch_tc_as<2, SUB, KT>(ctx, TP, s);
+}
+
+oc_status launch_attention_tc(oc_ctx* ctx, const AttnParams& P, int kv_dtype, int64_t page_rows, cudaStream_t s) {
+    AttnTcParams TP;
+    memset(&TP, 0, sizeof(TP));
+    TP.a = P;
+    TP.group = FastDiv((uint32_t)P.group);
+    TP.box_rows = (int)std::gcd<int64_t>(page_rows, AT_KEYS); TP.n_boxes = AT_KEYS / TP.box_rows;
+    const int D = P.pages.D;
+    TP.row_bytes = kv_dtype == OC_DTYPE_I4 ? D / 2 : D;
+    if (kv_dtype == OC_DTYPE_BF16 && P.pages.n_tokens > 0) {
+        AtEncodeFn enc = at_encode_fn();
+        const int64_t vectors = (int64_t)P.pages.n_pages * P.pages.heads * page_rows;
+        if (!enc || !at_encode(enc, &TP.mapK, P.k_pool, D, vectors, TP.box_rows) || !at_encode(enc, &TP.mapV, P.v_pool, D, vectors, TP.box_rows)) return OC_ERR_UNSUPPORTED;
+    }
+    if (D <= 64) {
+        if (kv_dtype == OC_DTYPE_BF16) return launch_tc_rows<1, OC_DTYPE_BF16>(ctx, TP, s);
+        if (kv_dtype == OC_DTYPE_I8) return launch_tc_rows<1, OC_DTYPE_I8>(ctx, TP, s);
+        return launch_tc_rows<1, OC_DTYPE_I4>(ctx, TP, s);
+    }
+    if (kv_dtype == OC_DTYPE_BF16) return launch_tc_rows<2, OC_DTYPE_BF16>(ctx, TP, s);
+    if (kv_dtype == OC_DTYPE_I8) return launch_tc_rows<2, OC_DTYPE_I8>(ctx, TP, s);
+    return launch_tc_rows<2, OC_DTYPE_I4>(ctx, TP, s);
+}
+
+}  // namespace oc

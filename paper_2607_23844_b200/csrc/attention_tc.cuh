@@ -1,0 +1,7 @@
+#pragma once
+#include "attention.cuh"
+
+namespace oc {
+// bf16 queries over a cache in bf16, 8 or 4 bits (attention_tc.cu); the tiles and the split are chosen there.
+oc_status launch_attention_tc(oc_ctx*, const AttnParams&, int kv_dtype, int64_t page_rows, cudaStream_t);
+}  // namespace oc

@@ -542,7 +542,9 @@ def test_attention_values_that_are_no_numbers(oc, ctx, dtype, kind, rows, what):
                 other = [d for d in range(72) if d != 5]
                 assert ((out - want).abs() <= bound)[hit][..., other].all()
             else:
-                assert torch.isnan(column).all()                             # (a whole number of 0 times infinity)
+                # the value is q * scale: NaN for a q of 0, otherwise the scale's own infinity or NaN with q's sign
+                value = torch.tensor(float(cache.tokens(m)[0][0, bad, 0, 5])).double() * what
+                assert torch.isnan(column).all() if torch.isnan(value) else (column == value).all()
         if hit and m == "k" and what != what:
             assert torch.isnan(out[hit]).all()
         cache.pool[m], cache.scale[m] = kept

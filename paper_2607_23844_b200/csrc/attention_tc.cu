@@ -18,6 +18,7 @@
 
 #include <algorithm>
 #include <numeric>
+#include <type_traits>
 
 #include "attention.cuh"
 #include "attention_tc.cuh"
@@ -31,20 +32,20 @@ static constexpr float AT_LAG = 8.0f;                                           
 
 template <int NT, int SUB, int KT> struct At {
     static constexpr bool quant = KT == OC_DTYPE_I8 || KT == OC_DTYPE_I4;
-    static constexpr bool own_p = SUB == 1;                                      // P beside S in tensor memory, not in its place
     static constexpr int helpers = quant ? 6 : 2;
     static constexpr int softmax_warps = 4 * NT, copy_warp = softmax_warps, mma_warp = copy_warp + 1, helper0 = mma_warp + 1;
     static constexpr int warps = helper0 + helpers, threads = 32 * warps;
     static constexpr int tile_bytes = SUB * AT_SUB_BYTES;                        // 128 keys (or rows) in bf16
     static constexpr int raw_bytes = KT == OC_DTYPE_I8 ? tile_bytes / 2 : tile_bytes / 4;        // (most) of 128 keys as they lie
-    static constexpr int k_stages = quant ? (NT * SUB == 4 ? 1 : 2) : (SUB == 1 ? 3 : 2), v_stages = quant ? 2 : k_stages;
+    static constexpr int k_stages = quant ? (NT * SUB == 4 ? 1 : 2) : (SUB == 2 ? 2 : 3), v_stages = quant ? 2 : k_stages;
     static constexpr int raw_stages = !quant ? 0 : (SUB == 2 && KT == OC_DTYPE_I8 ? 3 : 4);
     static constexpr int q_at = 0, k_at = NT * tile_bytes, v_at = k_at + k_stages * tile_bytes, raw_at = v_at + v_stages * tile_bytes;
     static constexpr int scale_at = raw_at + raw_stages * raw_bytes, rest_at = scale_at + (quant ? AT_SCALES * 2 * AT_KEYS * 4 : 0);
-    static constexpr int n_bars = 2 * k_stages + 3 * v_stages + 2 * raw_stages + 2 * AT_SCALES + 4 * NT + 1;
+    // Tensor memory, all 512 columns: what is left beside O are places of 128 columns for scores, each taken over by its
+    // probabilities.
+    static constexpr int o_step = 64 * SUB, places = (512 - NT * o_step) / 128, o_col = places * 128;
+    static constexpr int n_bars = 2 * k_stages + 3 * v_stages + 2 * raw_stages + 2 * AT_SCALES + 3 * places + 2 * NT + 1;
     static constexpr int smem = rest_at + n_bars * 8 + 64;
-    static constexpr int s_col = 0, p_col = own_p ? NT * 128 : 0, p_step = own_p ? 64 : 128;
-    static constexpr int o_col = own_p ? NT * 192 : NT * 128, o_step = own_p ? 64 : 128, tmem_cols = NT * 256;
     static constexpr int out_stride = 64 * SUB + 4;                              // floats between rows where a cluster joins them
 };
 
@@ -55,20 +56,47 @@ __device__ __forceinline__ uint64_t at_desc_v(uint32_t addr) {
     const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
     return ((uint64_t)hi << 32) | lo;
 }
-__device__ __forceinline__ void at_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate, uint32_t issue) {
-    asm volatile("{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
-                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 :: "r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
-}
-__device__ __forceinline__ void at_tmem_st32(uint32_t taddr, const uint32_t* v) {
+// The products of one step of 64 elements or keys, 16 at a time, in one piece so that nothing the compiler schedules comes between
+// them (the tensor cores take them faster than a warp computes operands).  Scores: both operands in shared memory, 32 bytes
+// of their swizzled rows at a time, the first `steps` of the four.
+__device__ __forceinline__ void at_mma_scores(uint32_t d, uint64_t q, uint64_t k, uint32_t idesc, uint32_t accumulate, int steps, uint32_t issue) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        "{\n\t.reg .pred a, y, e;\n\t.reg .b64 q, k;\n\t"
+        "setp.ne.b32 e, %6, 0;\n\tsetp.ne.b32 a, %4, 0;\n\tsetp.eq.b32 y, 0, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, a;\n\t"
+        "setp.gt.and.s32 e, %5, 1, e;\n\tadd.u64 q, %1, 2;\n\tadd.u64 k, %2, 2;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], q, k, %3, y;\n\t"
+        "setp.gt.and.s32 e, %5, 2, e;\n\tadd.u64 q, %1, 4;\n\tadd.u64 k, %2, 4;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], q, k, %3, y;\n\t"
+        "setp.gt.and.s32 e, %5, 3, e;\n\tadd.u64 q, %1, 6;\n\tadd.u64 k, %2, 6;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], q, k, %3, y;\n\t}"
+        :: "r"(d), "l"(q), "l"(k), "r"(idesc), "r"(accumulate), "r"(steps), "r"(issue) : "memory");
+}
+// Outputs: P in tensor memory, 8 columns for 16 keys; V 2048 bytes for them.
+__device__ __forceinline__ void at_mma_outputs(uint32_t d, uint32_t p, uint64_t v, uint32_t idesc, uint32_t accumulate, uint32_t issue) {
+    asm volatile(
+        "{\n\t.reg .pred a, y, e;\n\t.reg .b64 v;\n\t.reg .b32 p;\n\t"
+        "setp.ne.b32 e, %5, 0;\n\tsetp.ne.b32 a, %4, 0;\n\tsetp.eq.b32 y, 0, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, a;\n\t"
+        "add.u32 p, %1, 8;\n\tadd.u64 v, %2, 128;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [p], v, %3, y;\n\t"
+        "add.u32 p, %1, 16;\n\tadd.u64 v, %2, 256;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [p], v, %3, y;\n\t"
+        "add.u32 p, %1, 24;\n\tadd.u64 v, %2, 384;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [p], v, %3, y;\n\t}"
+        :: "r"(d), "r"(p), "l"(v), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
+}
+__device__ __forceinline__ void at_tmem_st16(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
         :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-           "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
-           "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
-           "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr) : "memory");
+           "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void at_tmem_ld16(uint32_t taddr, uint32_t* v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void at_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void at_tma_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar, uint32_t issue) {
@@ -87,6 +115,21 @@ __device__ __forceinline__ float at_max3(float a, float b, float c) {           
     return r;
 }
 __device__ __forceinline__ float at_exp2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+
+// 2^x of two numbers without the special function unit, which gives 16 a clock and SM: x = n + f with n whole and
+// 0 <= f < 1, 2^f = 1 + f (a + f (b + f c)) (minimax for a polynomial through 1 by Remez' exchange, relative error 8.6e-5, a
+// 45th of bf16's half step), n added to the exponent.  What is below -127 becomes 0.
+__device__ __forceinline__ f32x2 at_exp2_poly(f32x2 x) {
+    x = f2(fmaxf(f2_lo(x), -127.0f), fmaxf(f2_hi(x), -127.0f));
+    const f32x2 big = f2(12582912.0f);                                           // 1.5 * 2^23: the sum's last bits are n
+    f32x2 y;
+    asm("add.rm.f32x2 %0, %1, %2;" : "=l"(y) : "l"(x), "l"(big));
+    const f32x2 f = f2_add(x, f2_fma(y, f2(-1.0f), big));
+    f32x2 p = f2_fma(f, f2(0.07706704f), f2(0.227645f));
+    p = f2_fma(p, f, f2(0.69511676f));
+    p = f2_fma(p, f, f2(1.0f));
+    return f2_bits(__float_as_uint(f2_lo(p)) + (__float_as_uint(f2_lo(y)) << 23), __float_as_uint(f2_hi(p)) + (__float_as_uint(f2_hi(y)) << 23));
+}
 
 // 8 whole numbers as bf16.  8 bits: the low 7 of x in the mantissa of 128 (0x4300) give 128 + x mod 128; what is
 // subtracted is 128, or 256 (0x4380) where the sign bit is set, which falls on the exponent's last bit by itself.
@@ -116,6 +159,9 @@ __device__ __forceinline__ uint4 at_widen_i4(uint32_t w) {
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+#ifndef AT_POLY
+#define AT_POLY 0x55
+#endif
 struct AttnTcParams {
     AttnParams a;
     CUtensorMap mapK, mapV;          // bf16: {head_dim, vectors of the pool}, boxes {64, box_rows}
@@ -139,7 +185,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     const uint32_t k_full = bar0, k_empty = k_full + 8 * A::k_stages, v_full = k_empty + 8 * A::k_stages, v_ready = v_full + 8 * A::v_stages;
     const uint32_t v_empty = v_ready + 8 * A::v_stages, raw_full = v_empty + 8 * A::v_stages, raw_empty = raw_full + 8 * A::raw_stages;
     const uint32_t sc_full = raw_empty + 8 * A::raw_stages, sc_empty = sc_full + 8 * AT_SCALES;
-    const uint32_t s_full = sc_empty + 8 * AT_SCALES, s_free = s_full + 8 * NT, p_ready = s_free + 8 * NT, o_done = p_ready + 8 * NT, drain = o_done + 8 * NT;
+    const uint32_t s_full = sc_empty + 8 * AT_SCALES, p_ready = s_full + 8 * A::places, o_done = p_ready + 16 * A::places, drain = o_done + 16 * NT;
     uint32_t* tmem_slot = (uint32_t*)(bars + A::n_bars);
     volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = P.pages.D;
@@ -153,7 +199,8 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         for (int i = 0; i < A::v_stages; ++i) { mbar_init(v_full + 8 * i, 1); mbar_init(v_ready + 8 * i, A::helpers); mbar_init(v_empty + 8 * i, 1); }
         for (int i = 0; i < A::raw_stages; ++i) { mbar_init(raw_full + 8 * i, 1); mbar_init(raw_empty + 8 * i, A::helpers); }
         for (int i = 0; i < AT_SCALES; ++i) { mbar_init(sc_full + 8 * i, 1); mbar_init(sc_empty + 8 * i, A::softmax_warps); }
-        for (int t = 0; t < NT; ++t) { mbar_init(s_full + 8 * t, 1); mbar_init(s_free + 8 * t, 4); mbar_init(p_ready + 8 * t, 4); mbar_init(o_done + 8 * t, 1); }
+        for (int i = 0; i < A::places; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 16 * i, 4); mbar_init(p_ready + 16 * i + 8, 4); }
+        for (int i = 0; i < 2 * NT; ++i) mbar_init(o_done + 8 * i, 1);
         mbar_init(drain, 1);
         *abort_flag = 0;
         s_odd = 0;
@@ -168,7 +215,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     const AttnSeq S = attn_seq(P, T.seq);
     const uint32_t first = T.tile * (uint32_t)(NT * AT_ROWS), rows = (uint32_t)S.n * (uint32_t)P.group;
     if (first >= rows) return;                                                   // (the whole cluster; nothing is allocated yet)
-    if (warp == A::mma_warp) tmem_alloc_cta1(smem_u32(tmem_slot), A::tmem_cols);
+    if (warp == A::mma_warp) tmem_alloc_cta1(smem_u32(tmem_slot), 512);
     __syncwarp();
     __syncthreads();                                                             // (the ranges are set up)
     // ---- rows: which keys they see; queries into shared memory (rows that are not there as zeros) ----
@@ -211,7 +258,8 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    constexpr uint32_t tmem = 0;                                                 // all columns are this CTA's, so they begin at 0
+    if (*tmem_slot != tmem && threadIdx.x == 0) atomicCAS(P.pages.status, 0, OC_ERR_UNSUPPORTED);
     // (not before this CTA has its tensor memory: a kernel that takes its own before it waits for this one could have it)
     if (threadIdx.x == 0) pdl_launch_dependents();
     // Tiles of keys [a, b) of each tile of rows; this CTA's share of them all.
@@ -230,6 +278,8 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) { ka[t] = max(ka[t], j0); kb[t] = max(min(kb[t], j1), ka[t]); }
     auto on = [&](int j, int t) { return j >= ka[t] && j < kb[t]; };
+    // Products of scores in the order of their issue: tile of keys after tile of keys, the tiles of rows in turn.  Product i has
+    // place i % places (also one that a tile of rows does not need: nothing is computed for it).
     bool ok = true;
 #define AT_WAIT(bar, parity) (ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait((bar), (parity), abort_flag)))
 
@@ -338,64 +388,51 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((n_out >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
         const int steps = (D + 15) / 16;
         const uint32_t issue = elect_one();
-        int n_s[NT] = {}, n_p[NT] = {};                                          // score and output products issued for each tile of rows
-        auto scores = [&](int j, int t) {
-            const int st = (j - j0) % A::k_stages;
-            const uint64_t q = make_smem_desc(smem + A::q_at + (uint32_t)(t * A::tile_bytes)), k = make_smem_desc(smem + A::k_at + (uint32_t)(st * A::tile_bytes));
-            for (int i = 0; i < steps; ++i) {                                    // 16 elements, 32 bytes, at a time along the swizzled rows
-                const uint64_t off = (uint64_t)((i >> 2) * (AT_SUB_BYTES >> 4) + 2 * (i & 3));
-                tc_mma_bf16<false>(tmem + (uint32_t)(A::s_col + t * 128), q + off, k + off, IDESC_S, (uint32_t)(i != 0), issue);
+        const int n_keys = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)(j1 - j0));                // (known to be the same in all lanes)
+        int ks = 0, vs = 0, ps = 0, po = 0;                                      // stages of keys and values; places of scores and probabilities
+        uint32_t kp = 0, vp = 0, pp = 0;                                         // and their phases
+        int n_o[NT] = {};
+        auto scores = [&](int j, auto t_) {
+            constexpr int t = decltype(t_)::value;
+            if (j >= n_keys || !ok) return;
+            if (t == 0) { if (!AT_WAIT(k_full + 8 * ks, kp)) return; tc_fence_after(); }
+            if (on(j0 + j, t)) {
+                const uint64_t q = make_smem_desc(smem + A::q_at + (uint32_t)(t * A::tile_bytes)), k = make_smem_desc(smem + A::k_at + (uint32_t)(ks * A::tile_bytes));
+                at_mma_scores((uint32_t)(ps * 128), q, k, IDESC_S, 0u, steps, issue);
+                if (SUB == 2) at_mma_scores((uint32_t)(ps * 128), q + (AT_SUB_BYTES >> 4), k + (AT_SUB_BYTES >> 4), IDESC_S, 1u, steps - 4, issue);
             }
-            tc_commit<false>(s_full + 8 * t, issue);
-            ++n_s[t];
+            tc_commit<false>(s_full + 8 * ps, issue);
+            if (++ps == A::places) ps = 0;
+            if (t == NT - 1) { tc_commit<false>(k_empty + 8 * ks, issue); if (++ks == A::k_stages) { ks = 0; kp ^= 1u; } }
         };
-        auto outputs = [&](int j, int t) {
-            const int st = (j - j0) % A::v_stages;
-            const uint64_t v = at_desc_v(smem + A::v_at + (uint32_t)(st * A::tile_bytes));
+        auto outputs = [&](int j, auto t_) {                                     // the first half of the keys as soon as its probabilities are there
+            constexpr int t = decltype(t_)::value;
+            if (!ok) return;
+            if (t == 0 && !AT_WAIT(v_ready + 8 * vs, vp)) return;
+            const bool here = on(j0 + j, t);
+            const uint64_t v = at_desc_v(smem + A::v_at + (uint32_t)(vs * A::tile_bytes));
 #pragma unroll
-            for (int i = 0; i < AT_KEYS / 16; ++i)                               // 16 keys at a time: 8 columns of P, 2048 bytes of V
-                at_mma_ts(tmem + (uint32_t)(A::o_col + t * A::o_step), tmem + (uint32_t)(A::p_col + t * A::p_step + 8 * i), v + (uint64_t)(128 * i), idesc_o,
-                          (uint32_t)(n_p[t] != 0 || i != 0), issue);
-            tc_commit<false>(o_done + 8 * t, issue);
-            ++n_p[t];
-        };
-        auto parity = [&](int j, int stages) { return (uint32_t)((j - j0) / stages) & 1u; };
-        if (j0 < j1 && AT_WAIT(k_full, 0u)) {
-            tc_fence_after();
-#pragma unroll
-            for (int t = 0; t < NT; ++t) if (on(j0, t)) scores(j0, t);
-            tc_commit<false>(k_empty, issue);
-        }
-        for (int j = j0; j < j1 && ok; ++j) {
-            const bool more = j + 1 < j1;
-            bool have_k = false, have_v = false;
-            const int ks = (j + 1 - j0) % A::k_stages, vs = (j - j0) % A::v_stages;
-            auto next = [&](int t) {
-                if (!more || !on(j + 1, t)) return;
-                if (!have_k) { if (!AT_WAIT(k_full + 8 * ks, parity(j + 1, A::k_stages))) return; have_k = true; tc_fence_after(); }
-                if (A::own_p && n_s[t] > 0) { if (!AT_WAIT(s_free + 8 * t, (uint32_t)(n_s[t] - 1) & 1u)) return; tc_fence_after(); }
-                scores(j + 1, t);
-            };
-            auto now = [&](int t) {
-                if (!on(j, t)) return;
-                if (!have_v) { if (!AT_WAIT(v_ready + 8 * vs, parity(j, A::v_stages))) return; have_v = true; }
-                if (!AT_WAIT(p_ready + 8 * t, (uint32_t)n_p[t] & 1u)) return;
+            for (int h = 0; h < 2; ++h) {
+                if (!AT_WAIT(p_ready + 16 * po + 8 * h, pp)) return;
                 tc_fence_after();
-                outputs(j, t);
-            };
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if (A::own_p) { if (ok) next(t); if (ok) now(t); }
-                else { if (ok) now(t); if (ok) next(t); }                        // (P lies in the place of S)
+                if (here) at_mma_outputs((uint32_t)(A::o_col + t * A::o_step), (uint32_t)(po * 128 + 32 * h), v + (uint64_t)(512 * h), idesc_o, (uint32_t)(n_o[t] | h), issue);
             }
-            if (!ok) break;
-            // (a stage that no tile of rows used is given back like the others)
-            if (!have_v && !AT_WAIT(v_ready + 8 * vs, parity(j, A::v_stages))) break;
-            tc_commit<false>(v_empty + 8 * vs, issue);
-            if (more) {
-                if (!have_k && !AT_WAIT(k_full + 8 * ks, parity(j + 1, A::k_stages))) break;
-                tc_commit<false>(k_empty + 8 * ks, issue);
-            }
+            if (here) { tc_commit<false>(o_done + 16 * t + 8 * (n_o[t] & 1), issue); ++n_o[t]; }
+            if (t == NT - 1) { tc_commit<false>(v_empty + 8 * vs, issue); if (++vs == A::v_stages) { vs = 0; vp ^= 1u; } }
+            if (++po == A::places) { po = 0; pp ^= 1u; }
+        };
+        using T0 = std::integral_constant<int, 0>;
+        using T1 = std::integral_constant<int, NT - 1>;
+        // (the scores of product i + places overwrite the probabilities of product i: issued later, executed later)
+        scores(0, T0());
+        if (NT == 2) scores(0, T1());
+        else scores(1, T0());
+        if (A::places == 3) scores(NT == 2 ? 1 : 2, T0());
+        for (int j = 0; j < n_keys && ok; ++j) {
+            outputs(j, T0());
+            if (NT == 1) scores(j + 3, T0());
+            else if (A::places == 3) { scores(j + 1, T1()); outputs(j, T1()); scores(j + 2, T0()); }
+            else { scores(j + 1, T0()); outputs(j, T1()); scores(j + 1, T1()); }
         }
         if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
         // every MMA retires before tensor memory is released
@@ -483,66 +520,81 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     } else {
         // ================================ softmax ===============================================
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t s_at = t_lane + (uint32_t)(A::s_col + my_tile * 128), p_at = t_lane + (uint32_t)(A::p_col + my_tile * A::p_step);
         const uint32_t o_at = t_lane + (uint32_t)(A::o_col + my_tile * A::o_step);
+        const int my_a = my_tile == 0 ? ka[0] : ka[NT - 1], my_b = my_tile == 0 ? kb[0] : kb[NT - 1];
         const float c = P.scale_log2, lag = AT_LAG / c;
         float m = -INFINITY, l = 0.0f;                                           // what the row subtracts; its sum
         int n = 0;                                                               // tiles of keys done
         for (int j = j0; j < j1 && ok; ++j) {
             const int sst = (j - j0) % AT_SCALES;
             const uint32_t sc_at = smem + A::scale_at + (uint32_t)(sst * 2 * AT_KEYS * 4);
-            if (A::quant && !on(j, my_tile)) {
+            if (A::quant && (j < my_a || j >= my_b)) {
                 if (!AT_WAIT(sc_full + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
                 if (lane == 0) mbar_arrive(sc_empty + 8 * sst);
             }
-            if (!on(j, my_tile)) continue;
-            if (!AT_WAIT(s_full + 8 * my_tile, (uint32_t)n & 1u)) break;
+            // which product this is
+            const int product = NT * (j - j0) + my_tile, place = product % A::places;
+            const uint32_t s_at = t_lane + (uint32_t)(place * 128), p_at = s_at;
+            if (!AT_WAIT(s_full + 8 * place, (uint32_t)(product / A::places) & 1u)) break;
+            if (j < my_a || j >= my_b) {                                         // not needed
+                if (lane == 0) { mbar_arrive(p_ready + 16 * place); mbar_arrive(p_ready + 16 * place + 8); }
+                continue;
+            }
             tc_fence_after();
-            uint32_t s[128];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32u * i, s + 32 * i);
             if (A::quant && !AT_WAIT(sc_full + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
-            tmem_ld_wait();
-            if (A::own_p) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(s_free + 8 * my_tile);
-            }
-            if (A::quant) {
-#pragma unroll
-                for (int i = 0; i < 128; i += 4) {
-                    float4 k;
-                    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w) : "r"(sc_at + 4u * i) : "memory");
-                    s[i] = __float_as_uint(__uint_as_float(s[i]) * k.x); s[i + 1] = __float_as_uint(__uint_as_float(s[i + 1]) * k.y);
-                    s[i + 2] = __float_as_uint(__uint_as_float(s[i + 2]) * k.z); s[i + 3] = __float_as_uint(__uint_as_float(s[i + 3]) * k.w);
-                }
-            }
             const int key0 = j * AT_KEYS;
             const bool cut = __any_sync(0xFFFFFFFFu, exists && lo < hi && (key0 < lo || key0 + AT_KEYS > hi));
-            if (cut) {
+            // The scores are fetched twice, for the maximum and for the exponentials, 32 at a time and the next ones while these
+            // are worked on: 128 of them would not fit into a thread's registers.  The loops are not unrolled further than
+            // the two buffers ask for: the warps of an SM then find their instructions in its cache.
+            uint32_t s[2][32];
+            auto fetched = [&](int i, uint32_t* x) {                             // scales and masks of keys 32 i ..
+                if (A::quant) {
 #pragma unroll
-                for (int i = 0; i < 128; ++i) if (key0 + i < lo || key0 + i >= hi) s[i] = 0xFF800000u;
-            }
-            float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    for (int e = 0; e < 32; e += 4) {
+                        float4 k;
+                        asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w) : "r"(sc_at + 128u * i + 4u * e) : "memory");
+                        const f32x2 u = f2_mul(f2_bits(x[e], x[e + 1]), f2(k.x, k.y)), v = f2_mul(f2_bits(x[e + 2], x[e + 3]), f2(k.z, k.w));
+                        x[e] = __float_as_uint(f2_lo(u)); x[e + 1] = __float_as_uint(f2_hi(u)); x[e + 2] = __float_as_uint(f2_lo(v)); x[e + 3] = __float_as_uint(f2_hi(v));
+                    }
+                }
+                if (cut) {
+                    const int first_seen = lo - key0 - 32 * i, end_seen = hi - key0 - 32 * i;
 #pragma unroll
-            for (int i = 0; i < 128; i += 8)
+                    for (int e = 0; e < 32; ++e) if (e < first_seen || e >= end_seen) x[e] = 0xFF800000u;
+                }
+            };
+            float most[4] = {m, -INFINITY, -INFINITY, -INFINITY};
+            tmem_ld32(s_at, s[0]);
+#pragma unroll 1
+            for (int i2 = 0; i2 < 4; i2 += 2)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) most[e] = at_max3(most[e], __uint_as_float(s[i + 2 * e]), __uint_as_float(s[i + 2 * e + 1]));
-            const float top = at_max3(at_max3(most[0], most[1], most[2]), most[3], m);
-            if (n > 0 && A::own_p && !AT_WAIT(o_done + 8 * my_tile, (uint32_t)(n - 1) & 1u)) break;
+                for (int b = 0; b < 2; ++b) {
+                    const int i = i2 + b;
+                    tmem_ld_wait();
+                    tmem_ld32(s_at + 32u * ((i + 1) & 3), s[b ^ 1]);             // (the last one: the first again, for the exponentials)
+                    fetched(i, s[b]);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8)
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) most[f] = at_max3(most[f], __uint_as_float(s[b][e + 2 * f]), __uint_as_float(s[b][e + 2 * f + 1]));
+                }
+            const float top = at_max3(at_max3(most[0], most[1], most[2]), most[3], most[3]);
             // (a maximum of NaN is passed on to the whole row; that of +infinity makes every exponential of the row NaN)
             if (__any_sync(0xFFFFFFFFu, !(top <= m + lag) && top != -INFINITY)) {
                 const float to = top == INFINITY ? __int_as_float(0x7FFFFFFF) : top;
                 const float corr = to == -INFINITY ? 1.0f : at_exp2((m - to) * c);
                 if (n > 0) {
+                    // (two barriers in turn: of the one before last is known that it is over)
+                    if (!AT_WAIT(o_done + 16 * my_tile + 8 * ((n - 1) & 1), (uint32_t)((n - 1) >> 1) & 1u)) break;
                     tc_fence_after();
-                    for (int d = 0; d < D; d += 32) {
-                        uint32_t o[32];
-                        tmem_ld32(o_at + (uint32_t)d, o);
+                    for (int d = 0; d < D; d += 16) {
+                        uint32_t o[16];
+                        at_tmem_ld16(o_at + (uint32_t)d, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(m == -INFINITY ? 0.0f : __uint_as_float(o[i]) * corr);
-                        at_tmem_st32(o_at + (uint32_t)d, o);
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(m == -INFINITY ? 0.0f : __uint_as_float(o[i]) * corr);
+                        at_tmem_st16(o_at + (uint32_t)d, o);
                     }
                     at_tmem_st_wait();
                     tc_fence_before();
@@ -553,38 +605,44 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
             const float shift = m == -INFINITY ? 0.0f : -m * c;                  // (nothing seen so far: every p is 0)
             const f32x2 c2 = f2(c), shift2 = f2(shift);
             f32x2 sum[2] = {0, 0};
-            uint32_t w[64];
+#pragma unroll 1
+            for (int i2 = 0; i2 < 4; i2 += 2) {
 #pragma unroll
-            for (int i = 0; i < 64; ++i) {
-                const f32x2 x = f2_fma(f2_bits(s[2 * i], s[2 * i + 1]), c2, shift2);
-                float p0 = at_exp2(f2_lo(x)), p1 = at_exp2(f2_hi(x));
-                sum[i & 1] = f2_add(sum[i & 1], f2(p0, p1));
-                if (A::quant) {
-                    float v0, v1;
-                    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(sc_at + AT_KEYS * 4u + 8u * i) : "memory");
-                    p0 *= v0; p1 *= v1;
-                    if (cut) {                                                   // (0 times a scale that is no number)
-                        if (s[2 * i] == 0xFF800000u) p0 = 0.0f;
-                        if (s[2 * i + 1] == 0xFF800000u) p1 = 0.0f;
+                for (int b = 0; b < 2; ++b) {
+                    const int i = i2 + b;
+                    uint32_t w[16], *x = s[b];
+                    tmem_ld_wait();
+                    if (b == 0 || i2 == 0) tmem_ld32(s_at + 32u * (i + 1), s[b ^ 1]);
+                    fetched(i, x);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const f32x2 y = f2_fma(f2_bits(x[2 * e], x[2 * e + 1]), c2, shift2);
+                        f32x2 p = (AT_POLY >> (e & 7) & 1) ? at_exp2_poly(y) : f2(at_exp2(f2_lo(y)), at_exp2(f2_hi(y)));
+                        sum[e & 1] = f2_add(sum[e & 1], p);
+                        if (A::quant) {
+                            float v0, v1;
+                            asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(sc_at + AT_KEYS * 4u + 128u * i + 8u * e) : "memory");
+                            p = f2_mul(p, f2(v0, v1));
+                        }
+                        w[e] = pack_bf16x2(p);
                     }
+                    if (A::quant && cut) {                                       // (0 times a scale that is no number)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[e] &= (x[2 * e] == 0xFF800000u ? 0u : 0xFFFFu) | (x[2 * e + 1] == 0xFF800000u ? 0u : 0xFFFF0000u);
+                    }
+                    at_tmem_st16(p_at + 16u * i, w);
                 }
-                w[i] = pack_bf16x2(p0, p1);
-            }
-            if (A::quant) {
+                at_tmem_st_wait();                                               // half of the probabilities: the product may begin
+                tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(sc_empty + 8 * sst);
+                if (lane == 0) mbar_arrive(p_ready + 16 * place + 4 * i2);
             }
+            if (A::quant && lane == 0) mbar_arrive(sc_empty + 8 * sst);
             const f32x2 both = f2_add(sum[0], sum[1]);
             l += f2_lo(both) + f2_hi(both);
-            at_tmem_st32(p_at, w);
-            at_tmem_st32(p_at + 32u, w + 32);
-            at_tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_ready + 8 * my_tile);
             ++n;
         }
-        if (ok && n > 0) AT_WAIT(o_done + 8 * my_tile, (uint32_t)(n - 1) & 1u);
+        if (ok && n > 0) AT_WAIT(o_done + 16 * my_tile + 8 * ((n - 1) & 1), (uint32_t)((n - 1) >> 1) & 1u);
         if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
         tc_fence_after();
         // ---- results ----
@@ -681,7 +739,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == A::mma_warp) tmem_dealloc_cta1(tmem, A::tmem_cols);
+    if (warp == A::mma_warp) tmem_dealloc_cta1(tmem, 512);
 #undef AT_WAIT
 }
 

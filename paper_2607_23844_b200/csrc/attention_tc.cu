@@ -28,23 +28,25 @@ namespace oc {
 
 static constexpr int AT_ROWS = 128, AT_KEYS = 128, AT_SUB_BYTES = 128 * 128;   // a tile of 128 rows of 64 bf16
 static constexpr int AT_SCALES = 4;                                             // stages of the ring of scales
-static constexpr float AT_LAG = 8.0f;                                           // powers of two that a maximum may lag behind
+// A row's maximum may lag behind by 8 powers of two and more: no more than this for the sum of a tile's exponentials.
+static constexpr float AT_LAG = 8.0f, AT_SUM_MAX = 128.0f * 256.0f;
 
 template <int NT, int SUB, int KT> struct At {
     static constexpr bool quant = KT == OC_DTYPE_I8 || KT == OC_DTYPE_I4;
-    static constexpr int helpers = quant ? 6 : 2;
-    static constexpr int softmax_warps = 4 * NT, copy_warp = softmax_warps, mma_warp = copy_warp + 1, helper0 = mma_warp + 1;
+    static constexpr int softmax_warps = 4 * NT, copy_warp = softmax_warps, score_warp = copy_warp + 1, output_warp = copy_warp + 2, helper0 = copy_warp + 3;
+    static constexpr int helpers = quant ? 5 : 1;
     static constexpr int warps = helper0 + helpers, threads = 32 * warps;
+    static constexpr int chunk = threads > 384 ? 16 : 32;                        // scores that a thread fetches at a time
     static constexpr int tile_bytes = SUB * AT_SUB_BYTES;                        // 128 keys (or rows) in bf16
     static constexpr int raw_bytes = KT == OC_DTYPE_I8 ? tile_bytes / 2 : tile_bytes / 4;        // (most) of 128 keys as they lie
-    static constexpr int k_stages = quant ? (NT * SUB == 4 ? 1 : 2) : (SUB == 2 ? 2 : 3), v_stages = quant ? 2 : k_stages;
+    static constexpr int k_stages = quant ? (NT * SUB == 4 ? 1 : 2) : (SUB == 1 ? 3 : 2), v_stages = quant ? 2 : k_stages;
     static constexpr int raw_stages = !quant ? 0 : (SUB == 2 && KT == OC_DTYPE_I8 ? 3 : 4);
     static constexpr int q_at = 0, k_at = NT * tile_bytes, v_at = k_at + k_stages * tile_bytes, raw_at = v_at + v_stages * tile_bytes;
     static constexpr int scale_at = raw_at + raw_stages * raw_bytes, rest_at = scale_at + (quant ? AT_SCALES * 2 * AT_KEYS * 4 : 0);
     // Tensor memory, all 512 columns: what is left beside O are places of 128 columns for scores, each taken over by its
     // probabilities.
     static constexpr int o_step = 64 * SUB, places = (512 - NT * o_step) / 128, o_col = places * 128;
-    static constexpr int n_bars = 2 * k_stages + 3 * v_stages + 2 * raw_stages + 2 * AT_SCALES + 3 * places + 2 * NT + 1;
+    static constexpr int n_bars = 2 * k_stages + 3 * v_stages + 2 * raw_stages + 2 * AT_SCALES + 3 * places + 2;
     static constexpr int smem = rest_at + n_bars * 8 + 64;
     static constexpr int out_stride = 64 * SUB + 4;                              // floats between rows where a cluster joins them
 };
@@ -92,6 +94,10 @@ __device__ __forceinline__ void at_tmem_st16(uint32_t taddr, const uint32_t* v) 
         :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
            "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void at_tmem_st8(uint32_t taddr, const uint32_t* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+        :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void at_tmem_ld16(uint32_t taddr, uint32_t* v) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -118,9 +124,14 @@ __device__ __forceinline__ float at_exp2(float x) { float r; asm("ex2.approx.ftz
 
 // 2^x of two numbers without the special function unit, which gives 16 a clock and SM: x = n + f with n whole and
 // 0 <= f < 1, 2^f = 1 + f (a + f (b + f c)) (minimax for a polynomial through 1 by Remez' exchange, relative error 8.6e-5, a
-// 45th of bf16's half step), n added to the exponent.  What is below -127 becomes 0.
+// 45th of bf16's half step), n added to the exponent.  What is below -127 becomes 0, what is above 127 2^127.
+__device__ __forceinline__ float at_clamp(float x) {
+    float r;
+    asm("{\n\t.reg .f32 t;\n\tmax.NaN.f32 t, %1, 0fC2FE0000;\n\tmin.NaN.f32 %0, t, 0f42FE0000;\n\t}" : "=f"(r) : "f"(x));
+    return r;
+}
 __device__ __forceinline__ f32x2 at_exp2_poly(f32x2 x) {
-    x = f2(fmaxf(f2_lo(x), -127.0f), fmaxf(f2_hi(x), -127.0f));
+    x = f2(at_clamp(f2_lo(x)), at_clamp(f2_hi(x)));
     const f32x2 big = f2(12582912.0f);                                           // 1.5 * 2^23: the sum's last bits are n
     f32x2 y;
     asm("add.rm.f32x2 %0, %1, %2;" : "=l"(y) : "l"(x), "l"(big));
@@ -160,7 +171,7 @@ __device__ __forceinline__ uint4 at_widen_i4(uint32_t w) {
 }
 
 #ifndef AT_POLY
-#define AT_POLY 0x55
+#define AT_POLY 0x11
 #endif
 struct AttnTcParams {
     AttnParams a;
@@ -185,7 +196,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     const uint32_t k_full = bar0, k_empty = k_full + 8 * A::k_stages, v_full = k_empty + 8 * A::k_stages, v_ready = v_full + 8 * A::v_stages;
     const uint32_t v_empty = v_ready + 8 * A::v_stages, raw_full = v_empty + 8 * A::v_stages, raw_empty = raw_full + 8 * A::raw_stages;
     const uint32_t sc_full = raw_empty + 8 * A::raw_stages, sc_empty = sc_full + 8 * AT_SCALES;
-    const uint32_t s_full = sc_empty + 8 * AT_SCALES, p_ready = s_full + 8 * A::places, o_done = p_ready + 16 * A::places, drain = o_done + 16 * NT;
+    const uint32_t s_full = sc_empty + 8 * AT_SCALES, p_ready = s_full + 8 * A::places, p_done = p_ready + 8 * A::places, drain = p_done + 8 * A::places;
     uint32_t* tmem_slot = (uint32_t*)(bars + A::n_bars);
     volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = P.pages.D;
@@ -199,9 +210,8 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         for (int i = 0; i < A::v_stages; ++i) { mbar_init(v_full + 8 * i, 1); mbar_init(v_ready + 8 * i, A::helpers); mbar_init(v_empty + 8 * i, 1); }
         for (int i = 0; i < A::raw_stages; ++i) { mbar_init(raw_full + 8 * i, 1); mbar_init(raw_empty + 8 * i, A::helpers); }
         for (int i = 0; i < AT_SCALES; ++i) { mbar_init(sc_full + 8 * i, 1); mbar_init(sc_empty + 8 * i, A::softmax_warps); }
-        for (int i = 0; i < A::places; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 16 * i, 4); mbar_init(p_ready + 16 * i + 8, 4); }
-        for (int i = 0; i < 2 * NT; ++i) mbar_init(o_done + 8 * i, 1);
-        mbar_init(drain, 1);
+        for (int i = 0; i < A::places; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); mbar_init(p_done + 8 * i, 1); }
+        mbar_init(drain, 1); mbar_init(drain + 8, 1);
         *abort_flag = 0;
         s_odd = 0;
         for (int t = 0; t < NT; ++t) { s_range[t][0] = 0x7FFFFFFF; s_range[t][1] = 0; s_range[t][2] = 0; s_range[t][3] = 0x7FFFFFFF; }
@@ -215,7 +225,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     const AttnSeq S = attn_seq(P, T.seq);
     const uint32_t first = T.tile * (uint32_t)(NT * AT_ROWS), rows = (uint32_t)S.n * (uint32_t)P.group;
     if (first >= rows) return;                                                   // (the whole cluster; nothing is allocated yet)
-    if (warp == A::mma_warp) tmem_alloc_cta1(smem_u32(tmem_slot), 512);
+    if (warp == A::score_warp) tmem_alloc_cta1(smem_u32(tmem_slot), 512);
     __syncwarp();
     __syncthreads();                                                             // (the ranges are set up)
     // ---- rows: which keys they see; queries into shared memory (rows that are not there as zeros) ----
@@ -258,8 +268,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    constexpr uint32_t tmem = 0;                                                 // all columns are this CTA's, so they begin at 0
-    if (*tmem_slot != tmem && threadIdx.x == 0) atomicCAS(P.pages.status, 0, OC_ERR_UNSUPPORTED);
+    const uint32_t tmem = __reduce_max_sync(0xFFFFFFFFu, *tmem_slot);             // (known to be the same in all lanes)
     // (not before this CTA has its tensor memory: a kernel that takes its own before it waits for this one could have it)
     if (threadIdx.x == 0) pdl_launch_dependents();
     // Tiles of keys [a, b) of each tile of rows; this CTA's share of them all.
@@ -381,64 +390,66 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
             // copies already issued still write this CTA's shared memory: a bounded chance to land
             if (bytes_pending) { const unsigned long long t0 = global_ns(); while (global_ns() - t0 < 20000000ull) {} }
         }
-    } else if (warp == A::mma_warp) {
+    } else if (warp == A::score_warp || warp == A::output_warp) {
         // ================================ MMAs ==================================================
-        constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(AT_KEYS >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
-        const uint32_t n_out = (uint32_t)(D + 15) / 16u * 16u;
-        const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((n_out >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
-        const int steps = (D + 15) / 16;
+        // A warp for each of the two products: waiting, computing operands and issuing take one nearly as long as the products take
+        // the tensor cores.
         const uint32_t issue = elect_one();
         const int n_keys = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)(j1 - j0));                // (known to be the same in all lanes)
-        int ks = 0, vs = 0, ps = 0, po = 0;                                      // stages of keys and values; places of scores and probabilities
-        uint32_t kp = 0, vp = 0, pp = 0;                                         // and their phases
-        int n_o[NT] = {};
-        auto scores = [&](int j, auto t_) {
-            constexpr int t = decltype(t_)::value;
-            if (j >= n_keys || !ok) return;
-            if (t == 0) { if (!AT_WAIT(k_full + 8 * ks, kp)) return; tc_fence_after(); }
-            if (on(j0 + j, t)) {
-                const uint64_t q = make_smem_desc(smem + A::q_at + (uint32_t)(t * A::tile_bytes)), k = make_smem_desc(smem + A::k_at + (uint32_t)(ks * A::tile_bytes));
-                at_mma_scores((uint32_t)(ps * 128), q, k, IDESC_S, 0u, steps, issue);
-                if (SUB == 2) at_mma_scores((uint32_t)(ps * 128), q + (AT_SUB_BYTES >> 4), k + (AT_SUB_BYTES >> 4), IDESC_S, 1u, steps - 4, issue);
-            }
-            tc_commit<false>(s_full + 8 * ps, issue);
-            if (++ps == A::places) ps = 0;
-            if (t == NT - 1) { tc_commit<false>(k_empty + 8 * ks, issue); if (++ks == A::k_stages) { ks = 0; kp ^= 1u; } }
-        };
-        auto outputs = [&](int j, auto t_) {                                     // the first half of the keys as soon as its probabilities are there
-            constexpr int t = decltype(t_)::value;
-            if (!ok) return;
-            if (t == 0 && !AT_WAIT(v_ready + 8 * vs, vp)) return;
-            const bool here = on(j0 + j, t);
-            const uint64_t v = at_desc_v(smem + A::v_at + (uint32_t)(vs * A::tile_bytes));
+        int st = 0, place = 0;                                                   // stage of keys or values; place of scores or probabilities
+        uint32_t sp = 0, pp = 0;                                                 // their phases
+        if (warp == A::score_warp) {
+            constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(AT_KEYS >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
+            const int steps = (D + 15) / 16;
+            pp = 1u;                                                             // (the places begin empty)
+            for (int j = 0; j < n_keys && ok; ++j) {
+                if (!AT_WAIT(k_full + 8 * st, sp)) break;
+                const uint64_t k = make_smem_desc(smem + A::k_at + (uint32_t)(st * A::tile_bytes));
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (!AT_WAIT(p_ready + 16 * po + 8 * h, pp)) return;
-                tc_fence_after();
-                if (here) at_mma_outputs((uint32_t)(A::o_col + t * A::o_step), (uint32_t)(po * 128 + 32 * h), v + (uint64_t)(512 * h), idesc_o, (uint32_t)(n_o[t] | h), issue);
+                for (int t = 0; t < NT; ++t) {
+                    if (!AT_WAIT(p_done + 8 * place, pp)) break;                 // the probabilities that were there have been used
+                    tc_fence_after();
+                    if (on(j0 + j, t)) {
+                        const uint64_t q = make_smem_desc(smem + A::q_at + (uint32_t)(t * A::tile_bytes));
+                        at_mma_scores(tmem + (uint32_t)(place * 128), q, k, IDESC, 0u, steps, issue);
+                        if (SUB == 2) at_mma_scores(tmem + (uint32_t)(place * 128), q + (AT_SUB_BYTES >> 4), k + (AT_SUB_BYTES >> 4), IDESC, 1u, steps - 4, issue);
+                    }
+                    tc_commit<false>(s_full + 8 * place, issue);
+                    if (++place == A::places) { place = 0; pp ^= 1u; }
+                }
+                tc_commit<false>(k_empty + 8 * st, issue);
+                if (++st == A::k_stages) { st = 0; sp ^= 1u; }
             }
-            if (here) { tc_commit<false>(o_done + 16 * t + 8 * (n_o[t] & 1), issue); ++n_o[t]; }
-            if (t == NT - 1) { tc_commit<false>(v_empty + 8 * vs, issue); if (++vs == A::v_stages) { vs = 0; vp ^= 1u; } }
-            if (++po == A::places) { po = 0; pp ^= 1u; }
-        };
-        using T0 = std::integral_constant<int, 0>;
-        using T1 = std::integral_constant<int, NT - 1>;
-        // (the scores of product i + places overwrite the probabilities of product i: issued later, executed later)
-        scores(0, T0());
-        if (NT == 2) scores(0, T1());
-        else scores(1, T0());
-        if (A::places == 3) scores(NT == 2 ? 1 : 2, T0());
-        for (int j = 0; j < n_keys && ok; ++j) {
-            outputs(j, T0());
-            if (NT == 1) scores(j + 3, T0());
-            else if (A::places == 3) { scores(j + 1, T1()); outputs(j, T1()); scores(j + 2, T0()); }
-            else { scores(j + 1, T0()); outputs(j, T1()); scores(j + 1, T1()); }
+        } else {
+            const uint32_t n_out = (uint32_t)(D + 15) / 16u * 16u;
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((n_out >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
+            uint32_t begun[NT] = {};
+            for (int j = 0; j < n_keys && ok; ++j) {
+                if (!AT_WAIT(v_ready + 8 * st, sp)) break;
+                const uint64_t v = at_desc_v(smem + A::v_at + (uint32_t)(st * A::tile_bytes));
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    if (!AT_WAIT(p_ready + 8 * place, pp)) break;
+                    tc_fence_after();
+                    if (on(j0 + j, t)) {
+                        const uint32_t o = tmem + (uint32_t)(A::o_col + t * A::o_step), p = tmem + (uint32_t)(place * 128);
+                        at_mma_outputs(o, p, v, idesc, begun[t], issue);
+                        at_mma_outputs(o, p + 32u, v + 512u, idesc, 1u, issue);
+                        begun[t] = 1u;
+                    }
+                    tc_commit<false>(p_done + 8 * place, issue);
+                    if (++place == A::places) { place = 0; pp ^= 1u; }
+                }
+                tc_commit<false>(v_empty + 8 * st, issue);
+                if (++st == A::v_stages) { st = 0; sp ^= 1u; }
+            }
         }
         if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
         // every MMA retires before tensor memory is released
-        tc_commit<false>(drain, issue);
+        const uint32_t over = drain + (warp == A::output_warp ? 8u : 0u);
+        tc_commit<false>(over, issue);
         const unsigned long long t0 = global_ns();
-        while (!mbar_try_wait(drain, 0) && global_ns() - t0 < WAIT_LIMIT_NS) {}
+        while (!mbar_try_wait(over, 0) && global_ns() - t0 < WAIT_LIMIT_NS) {}
     } else if (warp >= A::helper0) {
         // ================================ helpers ===============================================
         const int h = warp - A::helper0;
@@ -521,9 +532,10 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         // ================================ softmax ===============================================
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t o_at = t_lane + (uint32_t)(A::o_col + my_tile * A::o_step);
+        int used = -1;                                                           // the last product of this tile of rows
         const int my_a = my_tile == 0 ? ka[0] : ka[NT - 1], my_b = my_tile == 0 ? kb[0] : kb[NT - 1];
-        const float c = P.scale_log2, lag = AT_LAG / c;
-        float m = -INFINITY, l = 0.0f;                                           // what the row subtracts; its sum
+        const float c = P.scale_log2;
+        float m = exists && lo < hi ? -INFINITY : 0.0f, l = 0.0f;                                           // what the row subtracts; its sum
         int n = 0;                                                               // tiles of keys done
         for (int j = j0; j < j1 && ok; ++j) {
             const int sst = (j - j0) % AT_SCALES;
@@ -532,117 +544,144 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 if (!AT_WAIT(sc_full + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
                 if (lane == 0) mbar_arrive(sc_empty + 8 * sst);
             }
-            // which product this is
             const int product = NT * (j - j0) + my_tile, place = product % A::places;
-            const uint32_t s_at = t_lane + (uint32_t)(place * 128), p_at = s_at;
+            const uint32_t s_at = t_lane + (uint32_t)(place * 128);              // (and of the probabilities)
             if (!AT_WAIT(s_full + 8 * place, (uint32_t)(product / A::places) & 1u)) break;
             if (j < my_a || j >= my_b) {                                         // not needed
-                if (lane == 0) { mbar_arrive(p_ready + 16 * place); mbar_arrive(p_ready + 16 * place + 8); }
+                if (lane == 0) mbar_arrive(p_ready + 8 * place);
                 continue;
             }
             tc_fence_after();
             if (A::quant && !AT_WAIT(sc_full + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
             const int key0 = j * AT_KEYS;
             const bool cut = __any_sync(0xFFFFFFFFu, exists && lo < hi && (key0 < lo || key0 + AT_KEYS > hi));
-            // The scores are fetched twice, for the maximum and for the exponentials, 32 at a time and the next ones while these
-            // are worked on: 128 of them would not fit into a thread's registers.  The loops are not unrolled further than
-            // the two buffers ask for: the warps of an SM then find their instructions in its cache.
-            uint32_t s[2][32];
-            auto fetched = [&](int i, uint32_t* x) {                             // scales and masks of keys 32 i ..
+            constexpr int CH = A::chunk;
+            auto fetch = [&](int i, uint32_t* x) { if constexpr (CH == 32) tmem_ld32(s_at + 32u * i, x); else at_tmem_ld16(s_at + 16u * i, x); };
+            auto mask = [&](int i, uint32_t* x) {
+                const int first_seen = lo - key0 - CH * i, end_seen = hi - key0 - CH * i;
+#pragma unroll
+                for (int e = 0; e < CH; ++e) if (e < first_seen || e >= end_seen) x[e] = 0xFF800000u;
+            };
+            auto fetched = [&](int i, uint32_t* x) {                             // scales (and masks) of keys CH i ..
                 if (A::quant) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
+                    for (int e = 0; e < CH; e += 4) {
                         float4 k;
-                        asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w) : "r"(sc_at + 128u * i + 4u * e) : "memory");
+                        asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w) : "r"(sc_at + 4u * CH * i + 4u * e) : "memory");
                         const f32x2 u = f2_mul(f2_bits(x[e], x[e + 1]), f2(k.x, k.y)), v = f2_mul(f2_bits(x[e + 2], x[e + 3]), f2(k.z, k.w));
                         x[e] = __float_as_uint(f2_lo(u)); x[e + 1] = __float_as_uint(f2_hi(u)); x[e + 2] = __float_as_uint(f2_lo(v)); x[e + 3] = __float_as_uint(f2_hi(v));
                     }
                 }
-                if (cut) {
-                    const int first_seen = lo - key0 - 32 * i, end_seen = hi - key0 - 32 * i;
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) if (e < first_seen || e >= end_seen) x[e] = 0xFF800000u;
-                }
+                if (A::quant && cut) mask(i, x);
             };
-            float most[4] = {m, -INFINITY, -INFINITY, -INFINITY};
-            tmem_ld32(s_at, s[0]);
+            if (!A::quant && cut) {                                              // masked in their place: the code below is without
 #pragma unroll 1
-            for (int i2 = 0; i2 < 4; i2 += 2)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int i = i2 + b;
+                for (int i = 0; i < 128 / CH; ++i) {
+                    uint32_t x[CH];
+                    fetch(i, x);
                     tmem_ld_wait();
-                    tmem_ld32(s_at + 32u * ((i + 1) & 3), s[b ^ 1]);             // (the last one: the first again, for the exponentials)
-                    fetched(i, s[b]);
+                    mask(i, x);
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8)
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) most[f] = at_max3(most[f], __uint_as_float(s[b][e + 2 * f]), __uint_as_float(s[b][e + 2 * f + 1]));
+                    for (int e = 0; e < CH; e += 16) at_tmem_st16(s_at + (uint32_t)(CH * i + e), x + e);
                 }
-            const float top = at_max3(at_max3(most[0], most[1], most[2]), most[3], most[3]);
-            // (a maximum of NaN is passed on to the whole row; that of +infinity makes every exponential of the row NaN)
-            if (__any_sync(0xFFFFFFFFu, !(top <= m + lag) && top != -INFINITY)) {
-                const float to = top == INFINITY ? __int_as_float(0x7FFFFFFF) : top;
-                const float corr = to == -INFINITY ? 1.0f : at_exp2((m - to) * c);
-                if (n > 0) {
-                    // (two barriers in turn: of the one before last is known that it is over)
-                    if (!AT_WAIT(o_done + 16 * my_tile + 8 * ((n - 1) & 1), (uint32_t)((n - 1) >> 1) & 1u)) break;
-                    tc_fence_after();
-                    for (int d = 0; d < D; d += 16) {
-                        uint32_t o[16];
-                        at_tmem_ld16(o_at + (uint32_t)d, o);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(m == -INFINITY ? 0.0f : __uint_as_float(o[i]) * corr);
-                        at_tmem_st16(o_at + (uint32_t)d, o);
-                    }
-                    at_tmem_st_wait();
-                    tc_fence_before();
-                }
-                l *= corr;
-                m = to;
+                at_tmem_st_wait();
             }
-            const float shift = m == -INFINITY ? 0.0f : -m * c;                  // (nothing seen so far: every p is 0)
-            const f32x2 c2 = f2(c), shift2 = f2(shift);
-            f32x2 sum[2] = {0, 0};
+            // The exponentials are taken with the maximum of the tiles before.  Only where that shows to be too small (the tile's sum
+            // is above AT_SUM_MAX: some exponent is above 8), or nothing has been seen yet, the scores are fetched again for their
+            // maximum, what has been summed up is rescaled, and the exponentials are taken anew: a tile or two of a sequence.
+            uint32_t w[64];
+            f32x2 sum[2];
+            bool search = __any_sync(0xFFFFFFFFu, m == -INFINITY);
+            for (;;) {
+                if (search) {
+                    float most[2] = {m, -INFINITY};
 #pragma unroll 1
-            for (int i2 = 0; i2 < 4; i2 += 2) {
+                    for (int i = 0; i < 128 / CH; ++i) {
+                        uint32_t x[CH];
+                        fetch(i, x);
+                        tmem_ld_wait();
+                        fetched(i, x);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int i = i2 + b;
-                    uint32_t w[16], *x = s[b];
+                        for (int e = 0; e < CH; e += 4)
+#pragma unroll
+                            for (int f = 0; f < 2; ++f) most[f] = at_max3(most[f], __uint_as_float(x[e + 2 * f]), __uint_as_float(x[e + 2 * f + 1]));
+                    }
+                    // (a maximum of NaN is passed on to the whole row; that of +infinity makes every exponential of the row NaN)
+                    const float top = at_max3(most[0], most[1], most[1]), to = top == INFINITY ? __int_as_float(0x7FFFFFFF) : top;
+                    const float corr = to == -INFINITY ? 1.0f : at_exp2((m - to) * c);
+                    if (n > 0) {
+                        if (!AT_WAIT(p_done + 8 * (used % A::places), (uint32_t)(used / A::places) & 1u)) break;
+                        tc_fence_after();
+                        for (int d = 0; d < D; d += 16) {
+                            uint32_t o[16];
+                            at_tmem_ld16(o_at + (uint32_t)d, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(m == -INFINITY ? 0.0f : __uint_as_float(o[i]) * corr);
+                            at_tmem_st16(o_at + (uint32_t)d, o);
+                        }
+                        at_tmem_st_wait();
+                        tc_fence_before();
+                    }
+                    l *= corr;
+                    m = to;
+                }
+                const float shift = m == -INFINITY ? 0.0f : -m * c;              // (nothing seen so far: every p is 0)
+                const f32x2 c2 = f2(c), shift2 = f2(shift);
+                sum[0] = sum[1] = 0;
+                uint32_t s[2][CH];
+                fetch(0, s[0]);
+                bool fine = true;
+#pragma unroll
+                for (int i = 0; i < 128 / CH; ++i) {
+                    uint32_t* x = s[i & 1];
                     tmem_ld_wait();
-                    if (b == 0 || i2 == 0) tmem_ld32(s_at + 32u * (i + 1), s[b ^ 1]);
+                    if (i < 128 / CH - 1) fetch(i + 1, s[(i + 1) & 1]);
                     fetched(i, x);
+                    if (i == 128 / CH - 1) {
+                        // The last scores are in registers.  If nothing asks for another round, the probabilities may take their place.
+                        float top = __uint_as_float(x[0]);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
+                        for (int e = 0; e < CH; e += 2) top = at_max3(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                        const f32x2 so_far = f2_add(sum[0], sum[1]);
+                        fine = search || __all_sync(0xFFFFFFFFu, f2_lo(so_far) + f2_hi(so_far) <= AT_SUM_MAX && fmaf(top, c, shift) <= AT_LAG);
+                        if (!fine) break;
+#pragma unroll
+                        for (int k = 0; k < (128 - CH) / 2; k += CH / 2) { if constexpr (CH == 32) at_tmem_st16(s_at + (uint32_t)k, w + k); else at_tmem_st8(s_at + (uint32_t)k, w + k); }
+                    }
+                    uint32_t* to = w + CH / 2 * i;
+#pragma unroll
+                    for (int e = 0; e < CH / 2; ++e) {
                         const f32x2 y = f2_fma(f2_bits(x[2 * e], x[2 * e + 1]), c2, shift2);
                         f32x2 p = (AT_POLY >> (e & 7) & 1) ? at_exp2_poly(y) : f2(at_exp2(f2_lo(y)), at_exp2(f2_hi(y)));
                         sum[e & 1] = f2_add(sum[e & 1], p);
                         if (A::quant) {
                             float v0, v1;
-                            asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(sc_at + AT_KEYS * 4u + 128u * i + 8u * e) : "memory");
+                            asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(sc_at + AT_KEYS * 4u + 4u * CH * i + 8u * e) : "memory");
                             p = f2_mul(p, f2(v0, v1));
                         }
-                        w[e] = pack_bf16x2(p);
+                        to[e] = pack_bf16x2(p);
                     }
                     if (A::quant && cut) {                                       // (0 times a scale that is no number)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] &= (x[2 * e] == 0xFF800000u ? 0u : 0xFFFFu) | (x[2 * e + 1] == 0xFF800000u ? 0u : 0xFFFF0000u);
+                        for (int e = 0; e < CH / 2; ++e) to[e] &= (x[2 * e] == 0xFF800000u ? 0u : 0xFFFFu) | (x[2 * e + 1] == 0xFF800000u ? 0u : 0xFFFF0000u);
                     }
-                    at_tmem_st16(p_at + 16u * i, w);
+                    if (i == 128 / CH - 1) { if constexpr (CH == 32) at_tmem_st16(s_at + 48u, to); else at_tmem_st8(s_at + 56u, to); }
                 }
-                at_tmem_st_wait();                                               // half of the probabilities: the product may begin
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_ready + 16 * place + 4 * i2);
+                if (fine) break;
+                search = true;
             }
+            if (!ok) break;
+            l += (f2_lo(sum[0]) + f2_hi(sum[0])) + (f2_lo(sum[1]) + f2_hi(sum[1]));
+            at_tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_ready + 8 * place);
+            used = product;
             if (A::quant && lane == 0) mbar_arrive(sc_empty + 8 * sst);
-            const f32x2 both = f2_add(sum[0], sum[1]);
-            l += f2_lo(both) + f2_hi(both);
             ++n;
         }
-        if (ok && n > 0) AT_WAIT(o_done + 16 * my_tile + 8 * ((n - 1) & 1), (uint32_t)((n - 1) >> 1) & 1u);
+        if (ok && n > 0) AT_WAIT(p_done + 8 * (used % A::places), (uint32_t)(used / A::places) & 1u);
         if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
         tc_fence_after();
         // ---- results ----
@@ -739,7 +778,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == A::mma_warp) tmem_dealloc_cta1(tmem, 512);
+    if (warp == A::score_warp) tmem_dealloc_cta1(tmem, 512);
 #undef AT_WAIT
 }
 
@@ -794,6 +833,9 @@ static oc_status launch_tc_as(oc_ctx* ctx, AttnTcParams& TP, cudaStream_t s) {
 template <int SUB, int KT>
 static oc_status launch_tc_rows(oc_ctx* ctx, AttnTcParams& TP, cudaStream_t s) {
     const uint64_t rows = (uint64_t)TP.a.rows_per_batch * (uint64_t)TP.a.group, problems = (uint64_t)TP.a.n_seqs * (uint64_t)TP.a.pages.heads;
+#ifdef AT_NT1
+    return launch_tc_as<1, SUB, KT>(ctx, TP, s);
+#endif
     // one tile of rows in a CTA where pairs would leave SMs idle
     if (rows <= AT_ROWS || (rows + 2 * AT_ROWS - 1) / (2 * AT_ROWS) * problems < (uint64_t)ctx->sm_count) return launch_tc_as<1, SUB, KT>(ctx, TP, s);
     return launch_tc_as<2, SUB, KT>(ctx, TP, s);

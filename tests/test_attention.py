@@ -515,9 +515,10 @@ def test_attention_large_scores(oc, ctx, dtype, kind, rows):
 @pytest.mark.parametrize("dtype,kind", TYPES)
 @pytest.mark.parametrize("rows", [1, 3, 140])
 @pytest.mark.parametrize("what", [NAN, math.inf, -math.inf])
-def test_attention_values_that_are_no_numbers(oc, ctx, dtype, kind, rows, what):
+@pytest.mark.parametrize("bad", [290, 256, 319])
+def test_attention_values_that_are_no_numbers(oc, ctx, dtype, kind, rows, what, bad):
     """In a key or a value that rows do not see: no influence.  In one that they see: it shows there and nowhere else."""
-    keys, bad = 400, 290
+    keys = 400
     cache = Cache(oc, kind, 1, 72, 1, keys, 16, seed=12)
     q = rand(torch.Generator().manual_seed(rows), rows, 1, 72, dtype=dtype)
     pg, r = cache.place(0, bad)
@@ -548,6 +549,46 @@ def test_attention_values_that_are_no_numbers(oc, ctx, dtype, kind, rows, what):
         if hit and m == "k" and what != what:
             assert torch.isnan(out[hit]).all()
         cache.pool[m], cache.scale[m] = kept
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", [(BF16, BF16), (BF16, "i8"), (F32, F32)])
+@pytest.mark.parametrize("rows", [1, 130])
+def test_attention_a_key_of_nan_shows_wherever_it_is(oc, ctx, dtype, kind, rows):
+    cache = Cache(oc, kind, 1, 64, 1, 256, 16, seed=16)
+    q = rand(torch.Generator().manual_seed(rows), rows, 1, 64, dtype=dtype)
+    for at in list(range(128, 160)) + [0, 63, 255]:
+        pg, r = cache.place(0, at)
+        where = (pg, 0, r) if cache.scale["k"] is not None else (pg, 0, r, 7)
+        store = cache.scale["k"] if cache.scale["k"] is not None else cache.pool["k"]
+        was = store[where].clone()
+        store[where] = NAN
+        assert torch.isnan(run(oc, ctx, cache, q, [rows], check=False)).all(), at
+        store[where] = was
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("rows", [1, 140])
+def test_attention_scores_that_grow_along_the_keys(oc, ctx, dtype, kind, rows):
+    """The maximum of a row rises from tile to tile by a few powers of two, by many, and falls back."""
+    keys = 1500
+    cache = Cache(oc, kind, 1, 64, 1, keys, 16, seed=17)
+    gen = torch.Generator().manual_seed(rows)
+    q = rand(gen, rows, 1, 64, dtype=dtype, std=0.1)
+    q[..., 0] = (torch.rand(rows, 1, generator=gen) + 0.5).to(dtype)
+    rise = torch.cat([torch.linspace(0, 60, 700), torch.linspace(300, 400, 300), torch.linspace(400, 0, 500)])
+    x = cache.val["k"][0].clone()
+    x[:, 0, 0] = rise.double()
+    xx = x.to(dtype)
+    ctx.kv_put(cache.desc, oc.kv_rows(cache.desc, keys, tag(oc, dtype), k=xx.cuda()), xx.cuda(), cache.pool["k"], k_scale=cache.scale["k"], page_table=cache.gpu_table)
+    if isinstance(kind, str):
+        w, sc = levels(xx, kind)
+        cache.val["k"][0] = w.double() * sc.float().double()[..., None]
+    else:
+        cache.val["k"][0] = xx.double()
+    for scale in (0.05, 0.3, 1.0):
+        run(oc, ctx, cache, q, [rows], scale=scale)
 
 
 @pytest.mark.gpu

@@ -307,6 +307,7 @@ oc_status launch_attention(oc_ctx* ctx, const oc_kv_desc& cache, const oc_attent
     // (a unit, or a number of units, beyond every position means the same as the largest position)
     P.unit = std::min<int64_t>(d.unit, 0x7FFFFFFF); P.back = std::min<int64_t>(d.back, 0x7FFFFFFF); P.ahead = std::min<int64_t>(d.ahead, 0x7FFFFFFF);
     P.scale = d.scale; P.scale_log2 = d.scale * 1.44269504f;
+    P.long_first = q_start || d.unit > 0;
     const uint64_t eb = d.dtype == OC_DTYPE_F32 ? 4 : 2;
     P.wide_q = ((uintptr_t)q | ((q_start ? 0u : (uint64_t)P.q_batch) | (uint64_t)P.q_row | (uint64_t)P.q_head) * eb) % 16 == 0;
     P.wide_out = ((uintptr_t)out | ((q_start ? 0u : (uint64_t)P.o_batch) | (uint64_t)P.o_row | (uint64_t)P.o_head) * eb) % 16 == 0;

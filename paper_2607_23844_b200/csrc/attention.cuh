@@ -21,16 +21,25 @@ struct AttnParams {
     uint32_t tiles;                              // tiles of rows of a sequence and head of the cache
     int split;                                   // CTAs of a cluster
     bool wide_q, wide_out;                       // 16 bytes at a time
+    bool long_first;                             // order of the tiles (attn_tile)
 };
 
 #ifdef __CUDACC__
-// A CTA's work: a tile of rows of one sequence and head of the cache (tiles in descending order: with a causal window
-// the long ones come first).
+// A CTA's work: a tile of rows of one sequence and head of the cache.  Neighbouring CTAs share their keys and values
+// in L2, except where the tiles' work differs (windows, packed sequences): then the last tiles of all sequences, which
+// have the most keys with a causal window and exist in the longest sequences only, come first.
 struct AttnTile { uint32_t seq, head, tile; };
 __device__ __forceinline__ AttnTile attn_tile(const AttnParams& P, uint32_t id) {
     AttnTile t;
-    const uint32_t problem = id / P.tiles;
-    t.tile = P.tiles - 1 - (id - problem * P.tiles);
+    uint32_t problem;
+    if (P.long_first) {
+        const uint32_t problems = P.n_seqs * (uint32_t)P.pages.heads, back = id / problems;
+        problem = id - back * problems;
+        t.tile = P.tiles - 1 - back;
+    } else {
+        problem = id / P.tiles;
+        t.tile = id - problem * P.tiles;
+    }
     t.seq = problem / (uint32_t)P.pages.heads;
     t.head = problem - t.seq * (uint32_t)P.pages.heads;
     return t;

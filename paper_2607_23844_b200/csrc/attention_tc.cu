@@ -46,6 +46,7 @@ template <int NT, int SUB, int KT> struct At {
     // Tensor memory, all 512 columns: what is left beside O are places of 128 columns for scores, each taken over by its
     // probabilities.
     static constexpr int o_step = 64 * SUB, places = (512 - NT * o_step) / 128, o_col = places * 128;
+    static constexpr bool one_warp = places == NT;                               // for both products
     static constexpr int n_bars = 2 * k_stages + 3 * v_stages + 2 * raw_stages + 2 * AT_SCALES + 3 * places + 2;
     static constexpr int smem = rest_at + n_bars * 8 + 64;
     static constexpr int out_stride = 64 * SUB + 4;                              // floats between rows where a cluster joins them
@@ -178,7 +179,7 @@ struct AttnTcParams {
     CUtensorMap mapK, mapV;          // bf16: {head_dim, vectors of the pool}, boxes {64, box_rows}
     int box_rows;                    // rows that a copy takes: the largest piece of 128 keys that no page boundary cuts
     int n_boxes, row_bytes;
-    FastDiv group;
+    FastDiv group, units;
 };
 
 template <int NT, int SUB, int KT>
@@ -393,56 +394,62 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     } else if (warp == A::score_warp || warp == A::output_warp) {
         // ================================ MMAs ==================================================
         // A warp for each of the two products: waiting, computing operands and issuing take one nearly as long as the products take
-        // the tensor cores.
+        // the tensor cores.  With two places only, one warp does both: the scores of product i + 2 then follow the outputs of
+        // product i in the tensor cores' queue without a barrier between them, and overwrite its probabilities in time.
         const uint32_t issue = elect_one();
         const int n_keys = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)(j1 - j0));                // (known to be the same in all lanes)
-        int st = 0, place = 0;                                                   // stage of keys or values; place of scores or probabilities
-        uint32_t sp = 0, pp = 0;                                                 // their phases
-        if (warp == A::score_warp) {
-            constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(AT_KEYS >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
-            const int steps = (D + 15) / 16;
-            pp = 1u;                                                             // (the places begin empty)
-            for (int j = 0; j < n_keys && ok; ++j) {
-                if (!AT_WAIT(k_full + 8 * st, sp)) break;
-                const uint64_t k = make_smem_desc(smem + A::k_at + (uint32_t)(st * A::tile_bytes));
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    if (!AT_WAIT(p_done + 8 * place, pp)) break;                 // the probabilities that were there have been used
-                    tc_fence_after();
-                    if (on(j0 + j, t)) {
-                        const uint64_t q = make_smem_desc(smem + A::q_at + (uint32_t)(t * A::tile_bytes));
-                        at_mma_scores(tmem + (uint32_t)(place * 128), q, k, IDESC, 0u, steps, issue);
-                        if (SUB == 2) at_mma_scores(tmem + (uint32_t)(place * 128), q + (AT_SUB_BYTES >> 4), k + (AT_SUB_BYTES >> 4), IDESC, 1u, steps - 4, issue);
-                    }
-                    tc_commit<false>(s_full + 8 * place, issue);
-                    if (++place == A::places) { place = 0; pp ^= 1u; }
-                }
-                tc_commit<false>(k_empty + 8 * st, issue);
-                if (++st == A::k_stages) { st = 0; sp ^= 1u; }
+        constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(AT_KEYS >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
+        const int steps = (D + 15) / 16;
+        const uint32_t n_out = (uint32_t)(D + 15) / 16u * 16u;
+        const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((n_out >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
+        int ks = 0, vs = 0, ps = 0, po = 0;                                      // stages of keys and values; places of scores and outputs
+        uint32_t kp = 0, vp = 0, pp = 0, sp = 1u;                                // their phases (the places begin empty)
+        uint32_t begun[NT] = {};
+        auto scores = [&](int j, int t) {                                        // t: known when this is compiled
+            if (j >= n_keys || !ok) return;
+            if (t == 0) { if (!AT_WAIT(k_full + 8 * ks, kp)) return; tc_fence_after(); }
+            if (!A::one_warp) { if (!AT_WAIT(p_done + 8 * ps, sp)) return; tc_fence_after(); }      // the probabilities that were there have been used
+            if (on(j0 + j, t)) {
+                const uint64_t q = make_smem_desc(smem + A::q_at + (uint32_t)(t * A::tile_bytes)), k = make_smem_desc(smem + A::k_at + (uint32_t)(ks * A::tile_bytes));
+                at_mma_scores(tmem + (uint32_t)(ps * 128), q, k, IDESC_S, 0u, steps, issue);
+                if (SUB == 2) at_mma_scores(tmem + (uint32_t)(ps * 128), q + (AT_SUB_BYTES >> 4), k + (AT_SUB_BYTES >> 4), IDESC_S, 1u, steps - 4, issue);
             }
+            tc_commit<false>(s_full + 8 * ps, issue);
+            if (++ps == A::places) { ps = 0; sp ^= 1u; }
+            if (t == NT - 1) { tc_commit<false>(k_empty + 8 * ks, issue); if (++ks == A::k_stages) { ks = 0; kp ^= 1u; } }
+        };
+        auto outputs = [&](int j, int t) {
+            if (!ok) return;
+            if (t == 0 && !AT_WAIT(v_ready + 8 * vs, vp)) return;
+            if (!AT_WAIT(p_ready + 8 * po, pp)) return;
+            tc_fence_after();
+            if (on(j0 + j, t)) {
+                const uint64_t v = at_desc_v(smem + A::v_at + (uint32_t)(vs * A::tile_bytes));
+                const uint32_t o = tmem + (uint32_t)(A::o_col + t * A::o_step), p = tmem + (uint32_t)(po * 128);
+                at_mma_outputs(o, p, v, idesc_o, begun[t], issue);
+                at_mma_outputs(o, p + 32u, v + 512u, idesc_o, 1u, issue);
+                begun[t] = 1u;
+            }
+            tc_commit<false>(p_done + 8 * po, issue);
+            if (++po == A::places) { po = 0; pp ^= 1u; }
+            if (t == NT - 1) { tc_commit<false>(v_empty + 8 * vs, issue); if (++vs == A::v_stages) { vs = 0; vp ^= 1u; } }
+        };
+        if (A::one_warp) {
+            if (warp == A::score_warp) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) scores(0, t);
+                for (int j = 0; j < n_keys && ok; ++j)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) { outputs(j, t); scores(j + 1, t); }
+            }
+        } else if (warp == A::score_warp) {
+            for (int j = 0; j < n_keys && ok; ++j)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) scores(j, t);
         } else {
-            const uint32_t n_out = (uint32_t)(D + 15) / 16u * 16u;
-            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((n_out >> 3) << 17) | ((uint32_t)(AT_ROWS >> 4) << 24);
-            uint32_t begun[NT] = {};
-            for (int j = 0; j < n_keys && ok; ++j) {
-                if (!AT_WAIT(v_ready + 8 * st, sp)) break;
-                const uint64_t v = at_desc_v(smem + A::v_at + (uint32_t)(st * A::tile_bytes));
+            for (int j = 0; j < n_keys && ok; ++j)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    if (!AT_WAIT(p_ready + 8 * place, pp)) break;
-                    tc_fence_after();
-                    if (on(j0 + j, t)) {
-                        const uint32_t o = tmem + (uint32_t)(A::o_col + t * A::o_step), p = tmem + (uint32_t)(place * 128);
-                        at_mma_outputs(o, p, v, idesc, begun[t], issue);
-                        at_mma_outputs(o, p + 32u, v + 512u, idesc, 1u, issue);
-                        begun[t] = 1u;
-                    }
-                    tc_commit<false>(p_done + 8 * place, issue);
-                    if (++place == A::places) { place = 0; pp ^= 1u; }
-                }
-                tc_commit<false>(v_empty + 8 * st, issue);
-                if (++st == A::v_stages) { st = 0; sp ^= 1u; }
-            }
+                for (int t = 0; t < NT; ++t) outputs(j, t);
         }
         if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
         // every MMA retires before tensor memory is released
@@ -485,27 +492,36 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 if (lane == 0) mbar_arrive(v_ready + 8 * st);
             }
         } else {
-            const int units = (D + 15) / 16 * 2, raw_units = D / 8;              // of 8 elements; with those that fill up a product's step
+            const int units = D / 8, items = AT_KEYS * units;                    // of 8 elements, in the order in which they lie
+            // the elements that fill up a product's step of 16 are zeros for good
+            if (units & 1)
+                for (int i = h * 32 + lane; i < (A::k_stages + A::v_stages) * AT_KEYS; i += 32 * A::helpers) {
+                    const uint32_t at = smem + A::k_at + (uint32_t)((i >> 7) * A::tile_bytes + (units >> 3) * AT_SUB_BYTES + (i & 127) * 128 + (((units & 7) ^ (i & 7)) << 4));
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" :: "r"(at), "r"(0u) : "memory");
+                }
             int stage = 0; uint32_t phase = 0;
             auto widen = [&](uint32_t base) {
                 const uint32_t raw = smem + A::raw_at + (uint32_t)(stage * A::raw_bytes);
-                for (int i = h * 32 + lane; i < AT_KEYS * 8 * SUB; i += 32 * A::helpers) {
-                    const int r = i / (8 * SUB), u = i % (8 * SUB);
-                    if (u >= units) continue;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (u < raw_units) {
-                        if (KT == OC_DTYPE_I8) {
-                            uint2 w;
-                            asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w.x), "=r"(w.y) : "r"(raw + (uint32_t)(r * D + 8 * u)) : "memory");
-                            v = at_widen_i8(w);
-                        } else {
-                            uint32_t w;
-                            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(raw + (uint32_t)(r * (D / 2) + 4 * u)) : "memory");
-                            v = at_widen_i4(w);
-                        }
+                constexpr int BATCH = 4;                                         // (loads on their way together)
+                for (int i0 = h * 32 + lane; i0 < items; i0 += 32 * A::helpers * BATCH) {
+                    uint2 w[BATCH];
+#pragma unroll
+                    for (int b = 0; b < BATCH; ++b) {
+                        const int i = i0 + b * 32 * A::helpers;
+                        w[b] = make_uint2(0u, 0u);
+                        if (i >= items) break;
+                        if (KT == OC_DTYPE_I8) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[b].x), "=r"(w[b].y) : "r"(raw + 8u * i) : "memory");
+                        else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[b].x) : "r"(raw + 4u * i) : "memory");
                     }
-                    const uint32_t at = base + (uint32_t)((u >> 3) * AT_SUB_BYTES + r * 128 + (((u & 7) ^ (r & 7)) << 4));
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+#pragma unroll
+                    for (int b = 0; b < BATCH; ++b) {
+                        const int i = i0 + b * 32 * A::helpers;
+                        if (i >= items) break;
+                        const uint32_t r = TP.units.div((uint32_t)i), u = (uint32_t)i - r * TP.units.d;
+                        const uint4 v = KT == OC_DTYPE_I8 ? at_widen_i8(w[b]) : at_widen_i4(w[b].x);
+                        const uint32_t at = base + (u >> 3) * AT_SUB_BYTES + r * 128u + (((u & 7u) ^ (r & 7u)) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                    }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -650,15 +666,15 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                         for (int k = 0; k < (128 - CH) / 2; k += CH / 2) { if constexpr (CH == 32) at_tmem_st16(s_at + (uint32_t)k, w + k); else at_tmem_st8(s_at + (uint32_t)k, w + k); }
                     }
                     uint32_t* to = w + CH / 2 * i;
+                    float4 vs;
 #pragma unroll
                     for (int e = 0; e < CH / 2; ++e) {
                         const f32x2 y = f2_fma(f2_bits(x[2 * e], x[2 * e + 1]), c2, shift2);
                         f32x2 p = (AT_POLY >> (e & 7) & 1) ? at_exp2_poly(y) : f2(at_exp2(f2_lo(y)), at_exp2(f2_hi(y)));
                         sum[e & 1] = f2_add(sum[e & 1], p);
                         if (A::quant) {
-                            float v0, v1;
-                            asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(sc_at + AT_KEYS * 4u + 4u * CH * i + 8u * e) : "memory");
-                            p = f2_mul(p, f2(v0, v1));
+                            if ((e & 1) == 0) asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(vs.x), "=f"(vs.y), "=f"(vs.z), "=f"(vs.w) : "r"(sc_at + AT_KEYS * 4u + 4u * CH * i + 8u * e) : "memory");
+                            p = f2_mul(p, (e & 1) == 0 ? f2(vs.x, vs.y) : f2(vs.z, vs.w));
                         }
                         to[e] = pack_bf16x2(p);
                     }
@@ -845,7 +861,7 @@ oc_status launch_attention_tc(oc_ctx* ctx, const AttnParams& P, int kv_dtype, in
     AttnTcParams TP;
     memset(&TP, 0, sizeof(TP));
     TP.a = P;
-    TP.group = FastDiv((uint32_t)P.group);
+    TP.group = FastDiv((uint32_t)P.group); TP.units = FastDiv((uint32_t)(P.pages.D / 8));
     TP.box_rows = (int)std::gcd<int64_t>(page_rows, AT_KEYS); TP.n_boxes = AT_KEYS / TP.box_rows;
     const int D = P.pages.D;
     TP.row_bytes = kv_dtype == OC_DTYPE_I4 ? D / 2 : D;

@@ -316,6 +316,7 @@ oc_status launch_attention(oc_ctx* ctx, const oc_kv_desc& cache, const oc_attent
         if (cache.dtype == OC_DTYPE_I8) return launch_simt<OC_DTYPE_F32, OC_DTYPE_I8>(ctx, P, s);
         return launch_simt<OC_DTYPE_F32, OC_DTYPE_I4>(ctx, P, s);
     }
+    if (attention_few_rows(P)) return launch_attention_few(ctx, P, cache.dtype, s);
     return launch_attention_tc(ctx, P, cache.dtype, cache.page_rows, s);
 }
 

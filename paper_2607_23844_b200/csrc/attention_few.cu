@@ -1,13 +1,14 @@
 // Attention of few rows (a sequence's rows times the heads that share one of the cache are at most 16: single tokens)
 // over the paged cache: bound by reading the cache once, so nothing but that is waited for.
-// A warp takes 16 keys at a time, straight from the pages into registers, the next ones while these are worked on, and
-// multiplies with mma.sync m16n8k16: the 16 rows are all there are, and a 128-row tile of tcgen05 would be staged through
-// shared memory for an eighth of its rows.  Where a lane's elements lie is chosen so that all loads are contiguous and as
-// wide as rows are aligned; the products' inner indices may be in any order as long as both operands share it:
-//     scores   lane (n, c) = (lane / 4, lane % 4) holds of key n E elements from 4 E chunk + E c on; a step of the product takes
-//              four of them, from the queries the same ones
-//     outputs  lane (n, c) holds of keys 4c .. 4c + 3 the EV elements from EV n on; column n of the product's tile j is element
-//              EV n + j, its inner index the keys in the order in which the scores' tiles leave the probabilities
+// A warp takes 16 keys at a time, straight from the pages into registers, the next keys on their way as soon as these have
+// been multiplied, the next values likewise, and multiplies with mma.sync m16n8k16: S^T = K Q^T and O^T = V^T P^T, so that the
+// few rows are the short side of the products (a 128-row tile of tcgen05 would be empty but for them, and go through shared
+// memory).  Where a lane's elements lie is chosen so that all loads are contiguous and as wide as rows are aligned; the
+// products' indices may be in any order as long as all operands share it:
+//     scores   lane (n, c) = (lane / 4, lane % 4) holds of the keys of its two rows n, n + 8 of the product the E elements from
+//              4 E chunk + E c on; a step of the product takes four of them, from the queries the same ones
+//     outputs  lane (n, c) holds of the keys of columns 2c, 2c + 1, 2c + 8, 2c + 9 the EV elements from EV n on; rows n and n + 8 of
+//              tile j are elements EV n + 2j and the next.  P^T comes out of the scores by transposing 8 x 8 pieces (movmatrix)
 // 8 and 4 bits are widened to bf16 exactly; the scales join the scores and the probabilities.  The warps of a CTA, and the
 // CTAs of a cluster, split the keys and join (maximum, sum, output) at the end, the latter through distributed shared memory.
 #include <string.h>
@@ -60,15 +61,17 @@ __device__ __forceinline__ void af_mma(float* d, const uint32_t* a, uint32_t b0,
 __device__ __forceinline__ float af_max(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float af_exp2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
+__device__ __forceinline__ uint32_t af_transpose(uint32_t a) { uint32_t r; asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a)); return r; }
+
 // KT: type of the cache; E, NC: elements of a lane's run of a key, runs; EV, NP: of its values; ROWS: 8 where no more are used
 template <int KT, int E, int NC, int EV, int NP, int ROWS>
-__global__ void __launch_bounds__(AF_WARPS * 32)
+__global__ void __launch_bounds__(AF_WARPS * 32, KT != OC_DTYPE_BF16 && ROWS == 8 ? 2 : 1)
 attention_few_kernel(const __grid_constant__ AttnParams P) {
     constexpr bool quant = KT == OC_DTYPE_I8 || KT == OC_DTYPE_I4;
     constexpr int KB = KT == OC_DTYPE_BF16 ? 2 * E : KT == OC_DTYPE_I8 ? E : E / 2, VB = KT == OC_DTYPE_BF16 ? 2 * EV : KT == OC_DTYPE_I8 ? EV : EV / 2;
-    constexpr int STEPS = NC * E / 4, DP = NP * 8 * EV, HALVES = ROWS / 8, NT = NP * EV;       // products of scores; columns; tiles of outputs
-    extern __shared__ __align__(16) float af_smem[];                         // [warps][16][DP + 4] outputs, then [warps][16][2] maxima and sums
-    __shared__ int s_range[2], s_odd;
+    constexpr int STEPS = NC * E / 4, DP = NP * 8 * EV, RT = ROWS / 8, OT = NP * EV / 2;       // products of scores; columns; tiles of rows, of outputs
+    extern __shared__ __align__(16) float af_smem[];                         // [warps][rows][DP + 4] outputs, then [warps][rows][2] maxima and sums
+    __shared__ int s_range[4], s_odd;
     __shared__ float s_join[AF_ROWS][2];
     constexpr int OS = DP + 4;
     float* stats = af_smem + AF_WARPS * ROWS * OS;
@@ -80,56 +83,37 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
     const AttnSeq S = attn_seq(P, seq);
     const int rows = S.n * P.group;
     if (rows <= 0) return;                                                   // (the whole cluster)
-    if (threadIdx.x == 0) { s_range[0] = 0x7FFFFFFF; s_range[1] = 0; s_odd = 0; }
-    __syncthreads();
-    // the rows n and n + 8: what they see
-    int lo[HALVES], hi[HALVES];
-    bool exists[HALVES];
-    int low = 0, high = 0x7FFFFFFF;                                          // keys within are seen by all rows
+    // what the rows 8 rt + 2c and the next see
+    int lo[RT][2], hi[RT][2];
+    float m[RT][2], l[RT][2], o[RT][OT][4];
+    int low = 0, high = 0x7FFFFFFF, from = 0x7FFFFFFF, to = 0;               // keys [low, high) are seen by all rows, [from, to) by any
 #pragma unroll
-    for (int h = 0; h < HALVES; ++h) {
-        const int r = n + 8 * h;
-        lo[h] = hi[h] = 0;
-        exists[h] = r < rows && attn_bounds(P, S, seq, r / P.group, lo[h], hi[h]);
-        if (exists[h] && lo[h] < hi[h]) {
-            if (warp == 0 && c == 0) { atomicMin(&s_range[0], lo[h]); atomicMax(&s_range[1], hi[h]); }
-            low = max(low, lo[h]); high = min(high, hi[h]);
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = 8 * rt + 2 * c + e;
+            int a = 0, b = 0;
+            const bool some = r < rows && attn_bounds(P, S, seq, r / P.group, a, b) && a < b;
+            if (some) { low = max(low, a); high = min(high, b); from = min(from, a); to = max(to, b); }
+            lo[rt][e] = some ? a : 0; hi[rt][e] = some ? b : 0;
+            m[rt][e] = some ? -INFINITY : 0.0f; l[rt][e] = 0.0f;
         }
+#pragma unroll
+        for (int t = 0; t < OT; ++t) o[rt][t][0] = o[rt][t][1] = o[rt][t][2] = o[rt][t][3] = 0.0f;
     }
 #pragma unroll
-    for (int d = 4; d < 32; d <<= 1) { low = max(low, __shfl_xor_sync(0xFFFFFFFFu, low, d)); high = min(high, __shfl_xor_sync(0xFFFFFFFFu, high, d)); }
-    // queries: elements 4E chunk + E c + 4s .. + 3 of step (chunk, s)
-    uint32_t q[STEPS][4];
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        const int d = (s / (E / 4)) * 4 * E + E * c + 4 * (s % (E / 4));
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint32_t a = 0, b = 0;
-            const int r = n + 8 * h;
-            if (h < HALVES && r < rows && d < D) {
-                const int i = r / P.group;
-                const uint16_t* p = (const uint16_t*)P.q + attn_q_at(P, S, seq, i, (int)head * P.group + (r - i * P.group)) + d;
-                if (P.wide_q) { const uint2 v = *(const uint2*)p; a = v.x; b = v.y; }
-                else { a = (uint32_t)p[0] | (uint32_t)p[1] << 16; b = (uint32_t)p[2] | (uint32_t)p[3] << 16; }
-            }
-            q[s][h] = a; q[s][2 + h] = b;
-        }
+    for (int d = 1; d < 4; d <<= 1) {
+        low = max(low, __shfl_xor_sync(0xFFFFFFFFu, low, d)); high = min(high, __shfl_xor_sync(0xFFFFFFFFu, high, d));
+        from = min(from, __shfl_xor_sync(0xFFFFFFFFu, from, d)); to = max(to, __shfl_xor_sync(0xFFFFFFFFu, to, d));
     }
-    __syncthreads();
+    if (threadIdx.x == 0) s_odd = 0;
     // this CTA's share of the steps of 16 keys, this warp's every eighth
-    int k0 = s_range[0] / AF_STEP, k1 = s_range[1] > 0 ? (s_range[1] + AF_STEP - 1) / AF_STEP : 0;
+    int k0 = from / AF_STEP, k1 = to > 0 ? (to + AF_STEP - 1) / AF_STEP : 0;
     if (k1 <= k0) k0 = k1 = 0;
     if (P.split > 1) {
         const int all = k1 - k0, a = (int)((long long)all * rank / P.split), b = (int)((long long)all * (rank + 1) / P.split);
         k1 = k0 + b; k0 += a;
     }
-    float m[HALVES], l[HALVES], o[NT][4];
-#pragma unroll
-    for (int h = 0; h < HALVES; ++h) { m[h] = exists[h] && lo[h] < hi[h] ? -INFINITY : 0.0f; l[h] = 0.0f; }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.0f;
-    struct Step { AfRaw<KB> k[NC][2]; AfRaw<VB> v[NP][4]; float4 ks, vs; } cur, nxt;
     auto find = [&](int k) -> int {                                          // the pool's vector of a step's first key; -1: no such page
         if (k >= k1) return -1;
         const uint32_t key = (uint32_t)k * AF_STEP, pn = P.pages.page_rows.div(key);
@@ -137,85 +121,124 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
         return page < 0 ? -1 : (int)(kv_vector(P.pages, page, key - pn * P.pages.page_rows.d) + head * P.pages.page_rows.d);
     };
     const long long row_bytes = KT == OC_DTYPE_BF16 ? 2ll * D : KT == OC_DTYPE_I8 ? D : D / 2;
-    const int key_n = 4 * (n >> 1) + (n & 1);                                // key of column n of the first tile of scores; the second's: + 2
-    auto load = [&](Step& s, int vec) {
+    const int key_n = 4 * (n >> 1) + (n & 1);                                // key of row n of the scores' product; row n + 8's: + 2
+    AfRaw<KB> rk[NC][2];
+    AfRaw<VB> rv[NP][4];
+    float ks[2] = {0.0f, 0.0f}, vs[2] = {0.0f, 0.0f};
+    auto load_k = [&](int vec) {
 #pragma unroll
         for (int ch = 0; ch < NC; ++ch)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                s.k[ch][t] = AfRaw<KB>{};
-                if (vec >= 0 && (ch * 4 + c) * E < D) s.k[ch][t] = af_load<KB>((const uint8_t*)P.k_pool + (long long)(vec + key_n + 2 * t) * row_bytes + (ch * 4 + c) * KB);
+                rk[ch][t] = AfRaw<KB>{};
+                if (vec >= 0 && (ch * 4 + c) * E < D) rk[ch][t] = af_load<KB>((const uint8_t*)P.k_pool + (long long)(vec + key_n + 2 * t) * row_bytes + (ch * 4 + c) * KB);
             }
+        if (quant)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) ks[t] = vec >= 0 ? __ldg(P.k_scale + vec + key_n + 2 * t) : 0.0f;
+    };
+    auto load_v = [&](int vec) {
 #pragma unroll
         for (int ps = 0; ps < NP; ++ps)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s.v[ps][i] = AfRaw<VB>{};
-                if (vec >= 0 && (ps * 8 + n) * EV < D) s.v[ps][i] = af_load<VB>((const uint8_t*)P.v_pool + (long long)(vec + 4 * c + i) * row_bytes + (ps * 8 + n) * VB);
+            for (int i = 0; i < 4; ++i) {                                    // keys 4c + i: columns 2c, 2c + 1, 2c + 8, 2c + 9
+                rv[ps][i] = AfRaw<VB>{};
+                if (vec >= 0 && (ps * 8 + n) * EV < D) rv[ps][i] = af_load<VB>((const uint8_t*)P.v_pool + (long long)(vec + 4 * c + i) * row_bytes + (ps * 8 + n) * VB);
             }
-        if (quant) {
-            s.ks = s.vs = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (vec >= 0) { s.ks = __ldg((const float4*)(P.k_scale + vec) + c); s.vs = __ldg((const float4*)(P.v_scale + vec) + c); }
-        }
+        if (quant)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) vs[t] = vec >= 0 ? __ldg(P.v_scale + vec + key_n + 2 * t) : 0.0f;
     };
+    int k = k0 + warp, vec = find(k);
+    load_k(vec);
+    load_v(vec);
+    vec = find(k + AF_WARPS);
+    // queries: of row n, elements 4E chunk + E c + 4s .. + 3 of step (chunk, s)
+    uint32_t q[RT][STEPS][2];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = 8 * rt + n, i = r / P.group;
+        const uint16_t* p = (const uint16_t*)P.q + (r < rows ? attn_q_at(P, S, seq, i, (int)head * P.group + (r - i * P.group)) : 0);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const int d = (s / (E / 4)) * 4 * E + E * c + 4 * (s % (E / 4));
+            uint32_t a = 0, b = 0;
+            if (r < rows && d < D) {
+                if (P.wide_q) { const uint2 v = *(const uint2*)(p + d); a = v.x; b = v.y; }
+                else { a = (uint32_t)p[d] | (uint32_t)p[d + 1] << 16; b = (uint32_t)p[d + 2] | (uint32_t)p[d + 3] << 16; }
+            }
+            q[rt][s][0] = a; q[rt][s][1] = b;
+        }
+    }
+    __syncthreads();                                                         // (s_odd)
     const float cc = P.scale_log2, lag = AF_LAG / cc;
-    int k = k0 + warp, vec_next = find(k + AF_WARPS);
-    load(cur, find(k));
     for (; k < k1; k += AF_WARPS) {
-        load(nxt, vec_next);
-        vec_next = find(k + 2 * AF_WARPS);
-        float s[2][4] = {};
+        float x[RT][4];                                                      // [0], [1]: key n with the lane's two rows, [2], [3]: key n + 8
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) x[rt][0] = x[rt][1] = x[rt][2] = x[rt][3] = 0.0f;
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
             const int e = 4 * (st % (E / 4));
+            const AfRaw<KB>&r0 = rk[st / (E / 4)][0], &r1 = rk[st / (E / 4)][1];
+            const uint32_t a[4] = {af_pair<KT>(r0, e), af_pair<KT>(r1, e), af_pair<KT>(r0, e + 2), af_pair<KT>(r1, e + 2)};
 #pragma unroll
-            for (int t = 0; t < 2; ++t) af_mma(s[t], q[st], af_pair<KT>(cur.k[st / (E / 4)][t], e), af_pair<KT>(cur.k[st / (E / 4)][t], e + 2));
+            for (int rt = 0; rt < RT; ++rt) af_mma(x[rt], a, q[rt][st][0], q[rt][st][1]);
         }
-        const int key0 = k * AF_STEP + 4 * c;                                // this lane's keys: key0 .. key0 + 3, s[i / 2][i % 2 + 2 h] of row n + 8h
-        const bool cut = k * AF_STEP < low || (k + 1) * AF_STEP > high;
-        const float ks[4] = {cur.ks.x, cur.ks.y, cur.ks.z, cur.ks.w}, vs[4] = {cur.vs.x, cur.vs.y, cur.vs.z, cur.vs.w};
-        float x[HALVES][4];
-        bool hidden[HALVES][4];
+        if (quant)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) { x[rt][0] *= ks[0]; x[rt][1] *= ks[0]; x[rt][2] *= ks[1]; x[rt][3] *= ks[1]; }
+        load_k(vec);
+        const int vec_v = vec;
+        vec = find(k + 2 * AF_WARPS);
+        const int key0 = k * AF_STEP;
+        const bool cut = key0 < low || key0 + AF_STEP > high;
+        uint32_t hidden = 0;
         bool grow = false;
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) {
+        for (int rt = 0; rt < RT; ++rt) {
+            if (cut) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[h][i] = s[i >> 1][(i & 1) + 2 * h];
-                if (quant) x[h][i] *= ks[i];
-                hidden[h][i] = cut && (key0 + i < lo[h] || key0 + i >= hi[h]);
-                if (hidden[h][i]) x[h][i] = -INFINITY;
+                for (int i = 0; i < 4; ++i) {
+                    const int key = key0 + key_n + 2 * (i >> 1);
+                    if (key < lo[rt][i & 1] || key >= hi[rt][i & 1]) { x[rt][i] = -INFINITY; hidden |= 1u << (4 * rt + i); }
+                }
             }
-            const float top = af_max(af_max(x[h][0], x[h][1]), af_max(x[h][2], x[h][3]));
-            grow |= !(top <= m[h] + lag) && top != -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float top = af_max(x[rt][e], x[rt][2 + e]);
+                grow |= !(top <= m[rt][e] + lag) && top != -INFINITY;
+            }
         }
         if (__any_sync(0xFFFFFFFFu, grow)) {
             // the rows' new maxima (NaN is passed on to the whole row; that of +infinity makes its exponentials NaN)
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h) {
-                float top = af_max(af_max(x[h][0], x[h][1]), af_max(x[h][2], x[h][3]));
-                top = af_max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                top = af_max(af_max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2)), m[h]);
-                if (top == INFINITY) top = __int_as_float(0x7FFFFFFF);
-                const float corr = top == -INFINITY || m[h] == -INFINITY ? (top == top ? 0.0f : top) : af_exp2((m[h] - top) * cc);
-                l[h] *= corr;
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) { o[t][2 * h] *= corr; o[t][2 * h + 1] *= corr; }
-                m[h] = top;
-            }
+                for (int e = 0; e < 2; ++e) {
+                    float top = af_max(x[rt][e], x[rt][2 + e]);
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) top = af_max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                    top = af_max(top, m[rt][e]);
+                    if (top == INFINITY) top = __int_as_float(0x7FFFFFFF);
+                    const float corr = top == -INFINITY || m[rt][e] == -INFINITY ? (top == top ? 0.0f : top) : af_exp2((m[rt][e] - top) * cc);
+                    l[rt][e] *= corr;
+#pragma unroll
+                    for (int t = 0; t < OT; ++t) { o[rt][t][e] *= corr; o[rt][t][2 + e] *= corr; }
+                    m[rt][e] = top;
+                }
         }
-        uint32_t p[4] = {0u, 0u, 0u, 0u};
+        uint32_t p[RT][2];
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) {
-            const float shift = m[h] == -INFINITY ? 0.0f : -m[h] * cc;
+        for (int rt = 0; rt < RT; ++rt) {
             float e[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                e[i] = af_exp2(fmaf(x[h][i], cc, shift));
-                l[h] += e[i];
-                if (quant) e[i] = hidden[h][i] ? 0.0f : e[i] * vs[i];        // (0 times a scale that is no number)
+                const float mm = m[rt][i & 1];
+                e[i] = af_exp2(fmaf(x[rt][i], cc, mm == -INFINITY ? 0.0f : -mm * cc));
+                l[rt][i & 1] += e[i];
+                if (quant) e[i] = hidden >> (4 * rt + i) & 1 ? 0.0f : e[i] * vs[i >> 1];        // (0 times a scale that is no number)
             }
-            p[h] = pack_bf16x2(e[0], e[1]); p[2 + h] = pack_bf16x2(e[2], e[3]);
+            p[rt][0] = af_transpose(pack_bf16x2(e[0], e[1])); p[rt][1] = af_transpose(pack_bf16x2(e[2], e[3]));
         }
         if (!quant && cut) {                                                 // 0 * NaN would reach rows that do not see it
             bool odd = false;
@@ -225,31 +248,37 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int j = 0; j < VB / 4; ++j) {
-                        uint32_t& w = cur.v[ps][i].w[j];
+                        uint32_t& w = rv[ps][i].w[j];
                         const bool a = (w & 0x7F80u) == 0x7F80u, b = (w & 0x7F800000u) == 0x7F800000u;
-                        odd |= (a || b) && key0 + i < S.len;
+                        odd |= (a || b) && key0 + 4 * c + i < S.len;
                         w &= (a ? 0u : 0xFFFFu) | (b ? 0u : 0xFFFF0000u);
                     }
             if (odd) s_odd = 1;
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) af_mma(o[t], p, af_across<KT>(cur.v[t / EV][0], cur.v[t / EV][1], t % EV), af_across<KT>(cur.v[t / EV][2], cur.v[t / EV][3], t % EV));
-        cur = nxt;
+        for (int t = 0; t < OT; ++t) {
+            const AfRaw<VB>* r = rv[2 * t / EV];
+            const int e = 2 * t % EV;
+            const uint32_t a[4] = {af_across<KT>(r[0], r[1], e), af_across<KT>(r[0], r[1], e + 1), af_across<KT>(r[2], r[3], e), af_across<KT>(r[2], r[3], e + 1)};
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) af_mma(o[rt][t], a, p[rt][0], p[rt][1]);
+        }
+        load_v(vec_v);
     }
-    // ---- the warps' results side by side: o[t] holds columns EV * (8 pass + 2c) + j and EV * (8 pass + 2c + 1) + j of rows n and n + 8 ----
+    // ---- the warps' results side by side ----
     float* mine = af_smem + warp * ROWS * OS;
 #pragma unroll
-    for (int h = 0; h < HALVES; ++h) {
-        l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 1);
-        l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 2);
-        if (c == 0) { stats[(warp * ROWS + n + 8 * h) * 2] = m[h]; stats[(warp * ROWS + n + 8 * h) * 2 + 1] = l[h]; }
+    for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int at = (t / EV) * 8 * EV + t % EV;
-            mine[(n + 8 * h) * OS + at + EV * (2 * c)] = o[t][2 * h];
-            mine[(n + 8 * h) * OS + at + EV * (2 * c + 1)] = o[t][2 * h + 1];
+        for (int e = 0; e < 2; ++e) {
+            const int r = 8 * rt + 2 * c + e;
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) l[rt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[rt][e], d);
+            if (n == 0) { stats[(warp * ROWS + r) * 2] = m[rt][e]; stats[(warp * ROWS + r) * 2 + 1] = l[rt][e]; }
+#pragma unroll
+            for (int t = 0; t < OT; ++t)
+                *(float2*)(mine + r * OS + (2 * t / EV) * 8 * EV + EV * n + 2 * t % EV) = make_float2(o[rt][t][e], o[rt][t][2 + e]);
         }
-    }
     __syncthreads();
     const int vecs = D / 4;
     // a row's parts, with their maxima and sums: (maximum, sum, 4 columns)

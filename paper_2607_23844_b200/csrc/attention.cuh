@@ -115,6 +115,20 @@ __device__ float attn_not_finite(const AttnParams& P, uint32_t seq, uint32_t hea
     return sum;
 }
 
+// Whole numbers as pairs of bf16, which holds them exactly.
+//   8 bits: u = x + 128 (the sign bit flipped) in the low byte of 0x4300 reads as 256 + x where x < 0, as 256 + 2x elsewhere (bit 7
+//   falls on the exponent's last bit), so that with d = that - 256:  x = d - max(d, 0) / 2.  Three operations on the FMA
+//   pipe, which the product's conversions leave idle; masks and subtractions that tell the cases apart take four on the integer
+//   pipe, which has half its rate (single tokens over 8-bit caches: 185 us with those).
+//   4 bits: u = x + 8 in the low bits of 0x4300 reads as 136 + x.
+__device__ __forceinline__ uint32_t attn_fma2(uint32_t a, uint32_t b, uint32_t c) { uint32_t r; asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c)); return r; }
+__device__ __forceinline__ uint32_t attn_i8_pair(uint32_t v) {                // 0x43uu 0x43uu
+    uint32_t d = attn_fma2(v, 0x3F803F80u, 0xC380C380u), r;
+    asm("fma.rn.relu.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(0x3F803F80u), "r"(0xC380C380u));
+    return attn_fma2(r, 0xBF00BF00u, d);
+}
+__device__ __forceinline__ uint32_t attn_i4_pair(uint32_t v) { return attn_fma2((v & 0x000F000Fu) | 0x43004300u, 0x3F803F80u, 0xC308C308u); }
+
 // Distributed shared memory of a cluster
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }

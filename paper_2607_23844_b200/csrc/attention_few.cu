@@ -20,6 +20,9 @@
 namespace oc {
 
 static constexpr int AF_WARPS = 8, AF_ROWS = 16, AF_STEP = 16;
+#ifndef AF_MULT
+#define AF_MULT 2
+#endif
 static constexpr float AF_LAG = 8.0f;                                        // powers of two that a maximum may lag behind
 
 template <int BYTES> struct AfRaw { uint32_t w[BYTES / 4]; };
@@ -30,29 +33,28 @@ template <int BYTES> __device__ __forceinline__ AfRaw<BYTES> af_load(const void*
     else asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(r.w[0]) : "l"(p));
     return r;
 }
-// Whole numbers as bf16 pairs: see the tensor-core kernel's copy of the idea: 128 + the low 7 bits, minus 128 or 256 by the sign bit
-__device__ __forceinline__ uint32_t af_sub(uint32_t a, uint32_t b) { uint32_t r; asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
-__device__ __forceinline__ uint32_t af_i8_pair(uint32_t bytes) {              // bytes 0 and 2
-    return af_sub((bytes & 0x007F007Fu) | 0x43004300u, (bytes & 0x00800080u) | 0x43004300u);
+// Which elements of a run of 8 make up pair i: neighbours, or in 4 bits those that one mask cuts out of a word.
+template <int KT> __device__ __forceinline__ constexpr int af_first(int i) { return KT == OC_DTYPE_I4 ? i : 2 * i; }
+template <int KT> __device__ __forceinline__ constexpr int af_second(int i) { return KT == OC_DTYPE_I4 ? i + 4 : 2 * i + 1; }
+// (sign bits flipped: whole numbers with an offset)
+template <int KT, int BYTES> __device__ __forceinline__ void af_flip(AfRaw<BYTES>& r) {
+#pragma unroll
+    for (int i = 0; i < BYTES / 4; ++i) r.w[i] ^= KT == OC_DTYPE_I8 ? 0x80808080u : KT == OC_DTYPE_I4 ? 0x88888888u : 0u;
 }
-// Elements e and e + 1 of a run, as a pair
-template <int KT, int BYTES> __device__ __forceinline__ uint32_t af_pair(const AfRaw<BYTES>& r, int e) {
-    if (KT == OC_DTYPE_BF16) return r.w[e >> 1];
-    if (KT == OC_DTYPE_I8) return af_i8_pair(__byte_perm(r.w[e >> 2], 0u, e & 2 ? 0x4342u : 0x4140u));
-    const uint32_t x = (r.w[e >> 3] ^ 0x88888888u) >> (4 * (e & 7));
-    return af_sub((x & 0xFu) | (x & 0xF0u) << 12 | 0x43004300u, 0x43084308u);
+// Pair i of a run
+template <int KT, int BYTES> __device__ __forceinline__ uint32_t af_pair(const AfRaw<BYTES>& r, int i) {
+    if (KT == OC_DTYPE_BF16) return r.w[i];
+    if (KT == OC_DTYPE_I8) return attn_i8_pair(__byte_perm(r.w[i >> 1], 0x43434343u, i & 1 ? 0x4342u : 0x4140u));
+    return attn_i4_pair(r.w[i >> 2] >> (4 * (i & 3)));
 }
-// Element e of two runs, as a pair
+// Element e of two runs
 template <int KT, int BYTES> __device__ __forceinline__ uint32_t af_across(const AfRaw<BYTES>& a, const AfRaw<BYTES>& b, int e) {
     if (KT == OC_DTYPE_BF16) return __byte_perm(a.w[e >> 1], b.w[e >> 1], e & 1 ? 0x7632u : 0x5410u);
-    if (KT == OC_DTYPE_I8) {
-        const int s = e & 3;
-        return af_i8_pair(__byte_perm(a.w[e >> 2], b.w[e >> 2], (uint32_t)(s | s << 4 | (4 + s) << 8 | (4 + s) << 12)));
-    }
-    const int s = (e & 7) >> 1;                                              // the byte; its low or high half
-    const uint32_t x = __byte_perm(a.w[e >> 3], b.w[e >> 3], (uint32_t)(s | s << 4 | (4 + s) << 8 | (4 + s) << 12)) ^ 0x00880088u;
-    if ((e & 1) == 0) return af_sub((x & 0x000F000Fu) | 0x43004300u, 0x43084308u);
-    return af_sub(((x >> 4) & 0x000F000Fu) | 0x43004300u, 0x43084308u);
+    const int s = KT == OC_DTYPE_I8 ? e & 3 : (e & 7) >> 1;                  // the byte
+    const uint32_t x = __byte_perm(KT == OC_DTYPE_I8 ? a.w[e >> 2] : a.w[e >> 3], KT == OC_DTYPE_I8 ? b.w[e >> 2] : b.w[e >> 3],
+                                   (uint32_t)(s | s << 4 | (4 + s) << 8 | (4 + s) << 12));
+    if (KT == OC_DTYPE_I8) return attn_i8_pair((x & 0x00FF00FFu) | 0x43004300u);
+    return attn_i4_pair(e & 1 ? x >> 4 : x);
 }
 __device__ __forceinline__ void af_mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -79,7 +81,22 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
     pdl_enter();
     const uint32_t rank = P.split > 1 ? cluster_rank() : 0u;
     const uint32_t problem = blockIdx.x / (uint32_t)P.split;
-    const uint32_t seq = problem / (uint32_t)P.pages.heads, head = problem - seq * (uint32_t)P.pages.heads;
+    uint32_t seq = problem / (uint32_t)P.pages.heads;
+    const uint32_t head = problem - seq * (uint32_t)P.pages.heads;
+    if (P.long_first) {                                                      // the seq-th longest sequence (at most as many as threads)
+        __shared__ int s_len[AF_WARPS * 32], s_seq;
+        const int t = threadIdx.x, ns = (int)P.n_seqs;
+        if (t < ns) s_len[t] = __ldg(P.kv_len + t);
+        __syncthreads();
+        if (t < ns) {
+            const int mine = s_len[t];
+            uint32_t before = 0;
+            for (int i = 0; i < ns; ++i) before += s_len[i] > mine || (s_len[i] == mine && i < t);
+            if (before == seq) s_seq = t;
+        }
+        __syncthreads();
+        seq = (uint32_t)s_seq;
+    }
     const AttnSeq S = attn_seq(P, seq);
     const int rows = S.n * P.group;
     if (rows <= 0) return;                                                   // (the whole cluster)
@@ -125,29 +142,42 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
     AfRaw<KB> rk[NC][2];
     AfRaw<VB> rv[NP][4];
     float ks[2] = {0.0f, 0.0f}, vs[2] = {0.0f, 0.0f};
+    // (a lane's runs behind the end of a row are never loaded: their zeros stay)
+    const uint8_t* kp = (const uint8_t*)P.k_pool + key_n * row_bytes + c * KB;
+    const uint8_t* vp = (const uint8_t*)P.v_pool + 4 * c * row_bytes + n * VB;
+#pragma unroll
+    for (int ch = 0; ch < NC; ++ch) rk[ch][0] = rk[ch][1] = AfRaw<KB>{};
+#pragma unroll
+    for (int ps = 0; ps < NP; ++ps) rv[ps][0] = rv[ps][1] = rv[ps][2] = rv[ps][3] = AfRaw<VB>{};
     auto load_k = [&](int vec) {
+        if (vec >= 0) {
+            const uint8_t* at = kp + (long long)vec * row_bytes;
 #pragma unroll
-        for (int ch = 0; ch < NC; ++ch)
+            for (int ch = 0; ch < NC; ++ch)
+                if ((ch * 4 + c) * E < D) { rk[ch][0] = af_load<KB>(at + ch * 4 * KB); rk[ch][1] = af_load<KB>(at + 2 * row_bytes + ch * 4 * KB); }
+            if (quant) { ks[0] = __ldg(P.k_scale + vec + key_n); ks[1] = __ldg(P.k_scale + vec + key_n + 2); }
+        } else {                                                             // a page that is not there, or nothing left
+            ks[0] = ks[1] = 0.0f;
+            if (!quant)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                rk[ch][t] = AfRaw<KB>{};
-                if (vec >= 0 && (ch * 4 + c) * E < D) rk[ch][t] = af_load<KB>((const uint8_t*)P.k_pool + (long long)(vec + key_n + 2 * t) * row_bytes + (ch * 4 + c) * KB);
-            }
-        if (quant)
-#pragma unroll
-            for (int t = 0; t < 2; ++t) ks[t] = vec >= 0 ? __ldg(P.k_scale + vec + key_n + 2 * t) : 0.0f;
+                for (int ch = 0; ch < NC; ++ch) rk[ch][0] = rk[ch][1] = AfRaw<KB>{};
+        }
     };
     auto load_v = [&](int vec) {
+        if (vec >= 0) {
+            const uint8_t* at = vp + (long long)vec * row_bytes;
 #pragma unroll
-        for (int ps = 0; ps < NP; ++ps)
+            for (int i = 0; i < 4; ++i)                                      // keys 4c + i: columns 2c, 2c + 1, 2c + 8, 2c + 9
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                                    // keys 4c + i: columns 2c, 2c + 1, 2c + 8, 2c + 9
-                rv[ps][i] = AfRaw<VB>{};
-                if (vec >= 0 && (ps * 8 + n) * EV < D) rv[ps][i] = af_load<VB>((const uint8_t*)P.v_pool + (long long)(vec + 4 * c + i) * row_bytes + (ps * 8 + n) * VB);
-            }
-        if (quant)
+                for (int ps = 0; ps < NP; ++ps)
+                    if ((ps * 8 + n) * EV < D) rv[ps][i] = af_load<VB>(at + i * row_bytes + ps * 8 * VB);
+            if (quant) { vs[0] = __ldg(P.v_scale + vec + key_n); vs[1] = __ldg(P.v_scale + vec + key_n + 2); }
+        } else {
+            vs[0] = vs[1] = 0.0f;
+            if (!quant)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) vs[t] = vec >= 0 ? __ldg(P.v_scale + vec + key_n + 2 * t) : 0.0f;
+                for (int ps = 0; ps < NP; ++ps) rv[ps][0] = rv[ps][1] = rv[ps][2] = rv[ps][3] = AfRaw<VB>{};
+        }
     };
     int k = k0 + warp, vec = find(k);
     load_k(vec);
@@ -160,27 +190,33 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
         const int r = 8 * rt + n, i = r / P.group;
         const uint16_t* p = (const uint16_t*)P.q + (r < rows ? attn_q_at(P, S, seq, i, (int)head * P.group + (r - i * P.group)) : 0);
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
+        for (int s = 0; s < STEPS; s += 2) {                                 // 8 elements: pairs 2s .. 2s + 3 of the lane's run
             const int d = (s / (E / 4)) * 4 * E + E * c + 4 * (s % (E / 4));
-            uint32_t a = 0, b = 0;
+            uint16_t e[8] = {};
             if (r < rows && d < D) {
-                if (P.wide_q) { const uint2 v = *(const uint2*)(p + d); a = v.x; b = v.y; }
-                else { a = (uint32_t)p[d] | (uint32_t)p[d + 1] << 16; b = (uint32_t)p[d + 2] | (uint32_t)p[d + 3] << 16; }
+                if (P.wide_q) { const uint4 v = ld_v4(p + d); memcpy(e, &v, 16); }
+                else
+#pragma unroll
+                    for (int i2 = 0; i2 < 8; ++i2) e[i2] = p[d + i2];
             }
-            q[rt][s][0] = a; q[rt][s][1] = b;
+#pragma unroll
+            for (int i2 = 0; i2 < 4; ++i2) q[rt][s + (i2 >> 1)][i2 & 1] = (uint32_t)e[af_first<KT>(i2)] | (uint32_t)e[af_second<KT>(i2)] << 16;
         }
     }
     __syncthreads();                                                         // (s_odd)
     const float cc = P.scale_log2, lag = AF_LAG / cc;
     for (; k < k1; k += AF_WARPS) {
+        if (quant)
+#pragma unroll
+            for (int ch = 0; ch < NC; ++ch) { af_flip<KT>(rk[ch][0]); af_flip<KT>(rk[ch][1]); }
         float x[RT][4];                                                      // [0], [1]: key n with the lane's two rows, [2], [3]: key n + 8
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) x[rt][0] = x[rt][1] = x[rt][2] = x[rt][3] = 0.0f;
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
-            const int e = 4 * (st % (E / 4));
+            const int i = 2 * (st % (E / 4));
             const AfRaw<KB>&r0 = rk[st / (E / 4)][0], &r1 = rk[st / (E / 4)][1];
-            const uint32_t a[4] = {af_pair<KT>(r0, e), af_pair<KT>(r1, e), af_pair<KT>(r0, e + 2), af_pair<KT>(r1, e + 2)};
+            const uint32_t a[4] = {af_pair<KT>(r0, i), af_pair<KT>(r1, i), af_pair<KT>(r0, i + 1), af_pair<KT>(r1, i + 1)};
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) af_mma(x[rt], a, q[rt][st][0], q[rt][st][1]);
         }
@@ -255,6 +291,9 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
                     }
             if (odd) s_odd = 1;
         }
+        if (quant)
+#pragma unroll
+            for (int ps = 0; ps < NP; ++ps) { af_flip<KT>(rv[ps][0]); af_flip<KT>(rv[ps][1]); af_flip<KT>(rv[ps][2]); af_flip<KT>(rv[ps][3]); }
 #pragma unroll
         for (int t = 0; t < OT; ++t) {
             const AfRaw<VB>* r = rv[2 * t / EV];
@@ -364,8 +403,10 @@ static oc_status launch_few_as(oc_ctx* ctx, AttnParams& P, cudaStream_t s) {
     if (problems * ATT_SPLIT_MAX > 0x7FFFFFFFull) return OC_ERR_UNSUPPORTED;
     // CTAs enough for the device several times over (sequences differ in length), each with two steps for every warp at least
     int split = 1;
-    while (split < ATT_SPLIT_MAX && problems * split < 4ull * ctx->sm_count && (uint64_t)P.pages.seq_rows >= (uint64_t)split * 2 * 2 * AF_WARPS * AF_STEP) split *= 2;
+    while (split < ATT_SPLIT_MAX && problems * split < AF_MULT * (uint64_t)ctx->sm_count && (uint64_t)P.pages.seq_rows >= (uint64_t)split * 2 * 2 * AF_WARPS * AF_STEP) split *= 2;
     P.split = split;
+    // (where all CTAs are not resident at once, the long sequences' come first)
+    P.long_first = P.kv_len && P.n_seqs > 1 && P.n_seqs <= AF_WARPS * 32 && problems * split > (uint64_t)ctx->sm_count;
     LaunchScope scope(ctx, OC_K_ATTENTION, s);
     PdlLaunch l(dim3((unsigned)(problems * split)), dim3(AF_WARPS * 32), SMEM, s, (unsigned)split);
     cudaLaunchKernelEx(&l.cfg, kernel, (const AttnParams&)P);

@@ -143,31 +143,17 @@ __device__ __forceinline__ f32x2 at_exp2_poly(f32x2 x) {
     return f2_bits(__float_as_uint(f2_lo(p)) + (__float_as_uint(f2_lo(y)) << 23), __float_as_uint(f2_hi(p)) + (__float_as_uint(f2_hi(y)) << 23));
 }
 
-// 8 whole numbers as bf16.  8 bits: the low 7 of x in the mantissa of 128 (0x4300) give 128 + x mod 128; what is
-// subtracted is 128, or 256 (0x4380) where the sign bit is set, which falls on the exponent's last bit by itself.
-__device__ __forceinline__ uint32_t at_bf16x2_sub(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
+// 8 whole numbers as bf16
 __device__ __forceinline__ uint4 at_widen_i8(uint2 w) {
-    uint32_t o[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t x = __byte_perm(i < 2 ? w.x : w.y, 0u, i & 1 ? 0x4342u : 0x4140u);        // two bytes to two halves
-        o[i] = at_bf16x2_sub((x & 0x007F007Fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u);
-    }
-    return make_uint4(o[0], o[1], o[2], o[3]);
+    w.x ^= 0x80808080u; w.y ^= 0x80808080u;
+    return make_uint4(attn_i8_pair(__byte_perm(w.x, 0x43434343u, 0x4140u)), attn_i8_pair(__byte_perm(w.x, 0x43434343u, 0x4342u)),
+                      attn_i8_pair(__byte_perm(w.y, 0x43434343u, 0x4140u)), attn_i8_pair(__byte_perm(w.y, 0x43434343u, 0x4342u)));
 }
-// 4 bits: with the sign bit flipped the number is x + 8, in the mantissa of 128: 136 + x.
 __device__ __forceinline__ uint4 at_widen_i4(uint32_t w) {
-    uint32_t o[4];
     w ^= 0x88888888u;
+    uint32_t o[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t x = w >> (8 * i);                                         // elements 2i and 2i + 1
-        o[i] = at_bf16x2_sub(((x & 0xFu) | (x & 0xF0u) << 12) | 0x43004300u, 0x43084308u);
-    }
+    for (int i = 0; i < 4; ++i) { const uint32_t x = __byte_perm(w, 0u, 0x4440u + i); o[i] = attn_i4_pair(x | x << 12); }      // elements 2i and 2i + 1
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 

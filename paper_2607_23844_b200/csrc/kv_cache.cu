@@ -20,7 +20,7 @@ struct KvMoveParams {
     long long batch_stride[2], row_stride[2], head_stride[2];
     FastDiv rows_per_batch;
     uint32_t n_rows;
-    int lph, rpw, head_blocks;                           // lanes of a head; rows of a warp; blocks of KV_HEADS heads
+    int lph, rpw, head_blocks, block_heads;              // lanes of a head; rows of a warp; blocks of up to KV_HEADS heads
     bool wide[2];                                        // dense rows may be read and written 16 bytes at a time
 };
 
@@ -70,7 +70,8 @@ kv_move_kernel(const __grid_constant__ KvMoveParams P) {
     constexpr int L = KT == OC_DTYPE_I4 ? 7 : 127;
     constexpr int UB = KT == OC_DTYPE_F32 ? 32 : KT == OC_DTYPE_BF16 ? 16 : KT == OC_DTYPE_I8 ? 8 : 4;       // bytes of a unit
     const int lane = threadIdx.x & 31, sub = lane / P.lph, u = lane - sub * P.lph;
-    const int m = blockIdx.y >= (unsigned)P.head_blocks, h0 = ((int)blockIdx.y - m * P.head_blocks) * KV_HEADS;
+    const int m = blockIdx.y >= (unsigned)P.head_blocks, h0 = ((int)blockIdx.y - m * P.head_blocks) * P.block_heads;
+    const int heads = min(P.block_heads, P.pages.heads - h0);
     pdl_enter();
     const uint32_t r = (blockIdx.x * KV_WARPS + (threadIdx.x >> 5)) * (uint32_t)P.rpw + sub;
     bool in = sub < P.rpw && r < P.n_rows;                                    // (rows past the end run along for the shuffles)
@@ -96,42 +97,44 @@ kv_move_kernel(const __grid_constant__ KvMoveParams P) {
     uint8_t* pool = (uint8_t*)P.pool[m];
     float* scales = P.scale[m];
     if (PUT) {
+        int from[5];                                                         // lanes of the same head 1, 2, 4 .. further
+#pragma unroll
+        for (int i = 0; i < 5; ++i) { const int o = u + (1 << i); from[i] = sub * P.lph + (o >= P.lph ? o - P.lph : o); }
         f32x2 f[KV_HEADS][4];
         uint4 raw[KV_HEADS][2];
 #pragma unroll
         for (int k = 0; k < KV_HEADS; ++k) {
             raw[k][0] = raw[k][1] = make_uint4(0, 0, 0, 0);
             if (Q) { f[k][0] = f[k][1] = f[k][2] = f[k][3] = 0; }
-            if (in && h0 + k < P.pages.heads) kv_load<DT>(dense + (h0 + k) * head_bytes, wide, Q ? f[k] : nullptr, raw[k]);
+            if (in && k < heads) kv_load<DT>(dense + (h0 + k) * head_bytes, wide, Q ? f[k] : nullptr, raw[k]);
         }
 #pragma unroll
         for (int k = 0; k < KV_HEADS; ++k) {
+            if (k >= heads) break;
             const uint32_t v = vec + (uint32_t)(h0 + k) * P.pages.page_rows.d;
             uint8_t* to = pool + ((long long)v * (P.pages.D >> 3) + u) * UB;
             if (!Q) {
-                if (in && h0 + k < P.pages.heads) { st_v4(to, raw[k][0]); if (KT == OC_DTYPE_F32) st_v4(to + 16, raw[k][1]); }
+                if (in) { st_v4(to, raw[k][0]); if (KT == OC_DTYPE_F32) st_v4(to + 16, raw[k][1]); }
                 continue;
             }
             uint32_t most = max_bits<8>(f[k], 0u);
             // (the largest of a head's lanes, however many: going around them twice as far each time)
-            for (int d = 1; d < P.lph; d <<= 1) {
-                const int o = u + d;
-                most = max(most, __shfl_sync(0xFFFFFFFFu, most, sub * P.lph + (o >= P.lph ? o - P.lph : o)));
-            }
-            const KvQuant q = kv_quant<L>(most);
-            if (!in || h0 + k >= P.pages.heads) continue;
-            int n[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { n[2 * i] = kv_level<L>(f2_lo(f[k][i]), q); n[2 * i + 1] = kv_level<L>(f2_hi(f[k][i]), q); }
+            for (int i = 0; i < 5; ++i)
+                if ((1 << i) < P.lph) most = max(most, __shfl_sync(0xFFFFFFFFu, most, from[i]));
+            const KvQuant q = kv_quant<L>(most);
+            if (!in) continue;
+            uint32_t n[8];
+            kv_levels<L, DT>(f[k], q, n);
             if (KT == OC_DTYPE_I8) {
                 uint32_t w[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) w[i] = (n[4 * i] & 0xFF) | (n[4 * i + 1] & 0xFF) << 8 | (n[4 * i + 2] & 0xFF) << 16 | (uint32_t)n[4 * i + 3] << 24;
+                for (int i = 0; i < 2; ++i) w[i] = __byte_perm(__byte_perm(n[4 * i], n[4 * i + 1], 0x0040u), __byte_perm(n[4 * i + 2], n[4 * i + 3], 0x0040u), 0x5410u);
                 *(uint2*)to = make_uint2(w[0], w[1]);
             } else {
                 uint32_t w = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w |= (uint32_t)(n[i] & 15) << (4 * i);
+                for (int i = 0; i < 8; ++i) w |= (n[i] & 15u) << (4 * i);
                 *(uint32_t*)to = w;
             }
             if (u == 0) scales[v] = q.scale;
@@ -143,7 +146,7 @@ kv_move_kernel(const __grid_constant__ KvMoveParams P) {
         for (int k = 0; k < KV_HEADS; ++k) {
             raw[k][0] = raw[k][1] = make_uint4(0, 0, 0, 0);
             sc[k] = 0.0f;
-            if (!in || page < 0 || h0 + k >= P.pages.heads) continue;
+            if (!in || page < 0 || k >= heads) continue;
             const uint32_t v = vec + (uint32_t)(h0 + k) * P.pages.page_rows.d;
             const uint8_t* from = pool + ((long long)v * (P.pages.D >> 3) + u) * UB;
             if (KT == OC_DTYPE_F32) { raw[k][0] = ld_v4(from); raw[k][1] = ld_v4(from + 16); }
@@ -155,7 +158,7 @@ kv_move_kernel(const __grid_constant__ KvMoveParams P) {
         if (!in) return;
 #pragma unroll
         for (int k = 0; k < KV_HEADS; ++k) {
-            if (h0 + k >= P.pages.heads) break;
+            if (k >= heads) break;
             if (Q) {
                 float x[8];
 #pragma unroll
@@ -206,7 +209,7 @@ oc_status launch_kv_move(oc_ctx* ctx, bool put, const oc_kv_desc& cache, const o
         P.wide[i] = ((uintptr_t)dense[i] | ((uint64_t)views[i]->batch_stride | (uint64_t)views[i]->row_stride | (uint64_t)views[i]->head_stride) * eb) % 16 == 0;
     }
     P.lph = cache.head_dim / 8; P.rpw = 32 / P.lph;
-    P.head_blocks = (cache.heads + KV_HEADS - 1) / KV_HEADS;
+    P.head_blocks = (cache.heads + KV_HEADS - 1) / KV_HEADS; P.block_heads = (cache.heads + P.head_blocks - 1) / P.head_blocks;
     const uint32_t per_cta = (uint32_t)(KV_WARPS * P.rpw);
     const dim3 grid((P.n_rows + per_cta - 1) / per_cta, (unsigned)(P.head_blocks * (v ? 2 : 1)));
     LaunchScope scope(ctx, put ? OC_K_KV_PUT : OC_K_KV_GET, s);

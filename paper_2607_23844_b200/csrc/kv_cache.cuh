@@ -45,23 +45,57 @@ __device__ __forceinline__ KvQuant kv_quant(uint32_t max_bits) {
     r.max = __uint_as_float(max_bits);
     if (max_bits >= 0x7F800000u) { r.scale = r.max; r.inv = 0.0f; }
     else if (r.max < 7.8886091e-31f) { r.scale = 0.0f; r.inv = 0.0f; }
-    else { r.scale = r.max * (1.0f / L); r.inv = (float)L / r.max; }
+    else { r.scale = r.max * (1.0f / L); r.inv = r.max < 1e36f ? __fdividef((float)L, r.max) : (float)L / r.max; }     // (the former has no room above)
     return r;
 }
-// rint(x * L / max), ties to even.  x * inv is off by up to two roundings, which only matters next to a border: there the
-// remainder x * L - q * max, which a fused multiply-add gives with one rounding, is half of max or more.
+// rint(x * L / max) exactly, ties to even, from a quotient that is off by less than 1: there the remainder
+// x * L - q * max, which a fused multiply-add gives with one rounding, is more than half of max.
 template <int L>
-__device__ __forceinline__ int kv_level(float x, const KvQuant& k) {
-    int q = __float2int_rn(x * k.inv);
-    if (k.inv != 0.0f) {
-        const float xl = x * (float)L, lost = fmaf(x, (float)L, -xl);        // x * L = xl + lost
-        const float rest = 2.0f * (fmaf(-(float)q, k.max, xl) + lost);
-        if (rest > k.max || (rest == k.max && (q & 1))) ++q;
-        else if (rest < -k.max || (rest == -k.max && (q & 1))) --q;
-    } else {
-        q = 0;
-    }
+__device__ __forceinline__ float kv_level_exact(float x, float q, float max) {
+    const float xl = x * (float)L, lost = fmaf(x, (float)L, -xl);            // x * L = xl + lost
+    const float rest = 2.0f * (fmaf(-q, max, xl) + lost);
+    const bool odd = ((int)q & 1) != 0;
+    if (rest > max || (rest == max && odd)) return q + 1.0f;
+    if (rest < -max || (rest == -max && odd)) return q - 1.0f;
     return q;
+}
+// 8 elements: their whole numbers in the low bits of 8 words.  A quotient + 1.5 * 2^23 rounds to one (the conversion
+// instruction has a quarter of the rate); x * inv is off by less than 3e-5.
+//   fp32  what lands within 1e-4 of a tie is looked at again
+//   bf16  ties are common (x = max / 2 is one).  x and max being n 2^a and m 2^b with n, m < 256, a quotient that is no tie
+//         differs from each by a share of 1 / (2 L n) at least, 1.5e-5: rounded with 1 / max 4e-6 too small and too large, the two
+//         differ at a tie only, and their mean rounds to the even one
+// inv = 0 gives 0 also where x is not finite.
+template <int L, int DT>
+__device__ __forceinline__ void kv_levels(const f32x2* f, const KvQuant& k, uint32_t* n) {
+    const float magic = 12582912.0f;
+    if (k.inv == 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) n[i] = 0u;
+        return;
+    }
+    float worst = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f32x2 y;
+        if (DT == OC_DTYPE_BF16) {
+            const f32x2 a = f2_add(f2_fma(f[i], f2(k.inv * (1.0f - 4e-6f)), f2(magic)), f2(-magic));
+            const f32x2 b = f2_add(f2_fma(f[i], f2(k.inv * (1.0f + 4e-6f)), f2(magic)), f2(-magic));
+            y = f2_fma(f2_add(a, b), f2(0.5f), f2(magic));
+        } else {
+            y = f2_fma(f[i], f2(k.inv), f2(magic));
+            const f32x2 t = f2_fma(f[i], f2(k.inv), f2_fma(y, f2(-1.0f), f2(magic)));
+            worst = fmaxf(worst, fmaxf(fabsf(f2_lo(t)), fabsf(f2_hi(t))));
+        }
+        n[2 * i] = __float_as_uint(f2_lo(y)); n[2 * i + 1] = __float_as_uint(f2_hi(y));
+    }
+    if (DT == OC_DTYPE_F32 && worst > 0.4999f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = kv_level_exact<L>(f2_lo(f[i]), __uint_as_float(n[2 * i]) - magic, k.max), b = kv_level_exact<L>(f2_hi(f[i]), __uint_as_float(n[2 * i + 1]) - magic, k.max);
+            n[2 * i] = __float_as_uint(a + magic); n[2 * i + 1] = __float_as_uint(b + magic);
+        }
+    }
 }
 #endif
 

@@ -847,3 +847,23 @@ def test_descriptors_take_strides_from_tensors(oc):
     for bad in (torch.zeros(20, 3, 64), torch.zeros(20, 2, 32), torch.zeros(19, 2, 64), torch.zeros(20, 128), torch.zeros(20, 2, 128)[..., ::2], torch.zeros(2, 2, 9, 64)):
         with pytest.raises(ValueError):
             oc.kv_rows(d, 20, oc.DTYPE_F32, k=bad, rows_per_batch=10)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["i8", "i4"])
+def test_put_rounds_every_pair_of_bf16_values(oc, ctx, kind):
+    """Every quotient of two 8-bit mantissas, at every distance of their exponents that matters."""
+    L = 127 if kind == "i8" else 7
+    m = torch.arange(128, 256).double()
+    rows = []
+    for shift in range(10 if kind == "i8" else 6):
+        n = torch.arange(128, 256).double() * 2.0 ** -shift
+        n = torch.where(n[None] <= m[:, None], n[None].expand(128, 128), -n[None] / 2)          # no element above the maximum
+        rows.append(torch.cat([m[:, None].expand(128, 8), n], 1))                              # [128, 136]
+    x = torch.stack(rows).to(BF16).reshape(-1, 1, 136)
+    pad = x.shape[0]
+    cache = Cache(oc, kind, 1, 136, 1, pad, 16, table=False, empty=True)
+    xx = x.cuda()
+    ctx.kv_put(cache.desc, oc.kv_rows(cache.desc, pad, oc.DTYPE_BF16, k=xx), xx, cache.pool["k"], k_scale=cache.scale["k"])
+    torch.cuda.synchronize()
+    check_put(cache, "k", x, torch.arange(pad))

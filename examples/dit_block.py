@@ -1,6 +1,6 @@
 """One transformer block under Token Cache, with everything around its attention on this library's kernels.
 
-    python examples/dit_block.py [--steps 4]                (on a B200)
+    python examples/dit_block.py [--steps 4] [--kv i8]      (on a B200)
 
 An SD3-shaped block (adaptive norms, attention, feed-forward) is run for a few denoising steps.  The first step computes
 every token and fills the caches; each later step matches and selects on the block's input, computes the kept tokens
@@ -14,8 +14,12 @@ only and takes the others from the step before:
     feed-fwd    linear_int8 -> gelu -> quantize_rows -> linear_int8
     after       block_norm: restore from cache, gate, residual
 
-Attention itself and the gelu are the wrapped layer's own (torch here).  Weights are random: this shows the calls, not
-a model.
+Attention is the wrapped layer's own (torch here), among the kept tokens alone, or with --kv over a cache of all tokens'
+keys and values, in which those of the reused tokens are still there from the steps before:
+
+    attention  rope -> kv_put (the kept tokens' keys and values to their pages) -> attention (kept queries, all keys)
+
+The gelu is torch's.  Weights are random: this shows the calls, not a model.
 """
 from __future__ import annotations
 
@@ -60,7 +64,8 @@ def to_int8(ctx: oc.Context, x: torch.Tensor):
 class Block:
     """The block's weights, its two caches (the outputs of attention and feed-forward) and one step of it."""
 
-    def __init__(self, ctx: oc.Context, B: int, H: int, W: int, heads: int, head_dim: int, reuse: float, seed: int = 0):
+    def __init__(self, ctx: oc.Context, B: int, H: int, W: int, heads: int, head_dim: int, reuse: float, seed: int = 0,
+                 kv: str | None = None):
         self.ctx, self.B, self.H, self.W, self.heads, self.D = ctx, B, H, W, heads, head_dim
         C = self.C = heads * head_dim
         gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -79,6 +84,11 @@ class Block:
         self.axes = (0, head_dim // 2, head_dim - head_dim // 2)
         table_desc = oc.rope_desc(1, oc.DTYPE_BF16, head_dim, self.axes, (1, H, W), heads)
         self.table = oc.rope_table(table_desc).cuda()
+        self.kv = None
+        if kv is not None:                                                    # a sequence for each image, keys and values of every token
+            kind = {"bf16": oc.DTYPE_BF16, "i8": oc.DTYPE_I8, "i4": oc.DTYPE_I4}[kv]
+            self.kv = oc.kv_desc(kind, heads, head_dim, B, self.per, page_rows=64)
+            (self.k_pool, self.k_scale), (self.v_pool, self.v_scale) = oc.kv_pools(self.kv), oc.kv_pools(self.kv)
 
     def select(self, x: torch.Tensor):
         """(slot_of, kept_idx, kept tokens per batch element) of this step's input."""
@@ -90,6 +100,16 @@ class Block:
         self.ctx.match(self.layout, x, sim, idx)
         self.ctx.select(self.layout, sim, idx, oc.SELECT_COUNT, 0.0, self.n_reuse, keep, kept, count, match_map, slot_of)
         return slot_of, kept, keep
+
+    def attend(self, q, k, v, kept, dense: int) -> torch.Tensor:
+        """The kept tokens' keys and values into the cache, their queries over all of it: [dense, C]."""
+        ctx, kv = self.ctx, self.kv
+        ctx.kv_put(kv, oc.kv_rows(kv, dense, oc.DTYPE_BF16, k=k, v=v), k, self.k_pool, v, self.v_pool, k_scale=self.k_scale,
+                   v_scale=self.v_scale, idx=kept)
+        a = torch.empty(dense, self.heads, self.D, dtype=BF16, device="cuda")
+        d = oc.attention_desc(kv, dense, oc.DTYPE_BF16, self.heads, self.D ** -0.5, q=q, out=a)
+        ctx.attention(kv, d, q, self.k_pool, self.v_pool, a, k_scale=self.k_scale, v_scale=self.v_scale, idx=kept)
+        return a.view(dense, self.C)
 
     def step(self, x: torch.Tensor, condition: torch.Tensor, first: bool):
         """x [n, C] bf16, condition [B, C] bf16 -> (the block's output, this step's slot_of or None)."""
@@ -111,8 +131,12 @@ class Block:
         d = oc.rope_desc(dense, oc.DTYPE_BF16, D, self.axes, (1, self.H, self.W), self.heads, self.heads, rows_per_batch=keep,
                          eps=EPS, q=q, q_out=qo, k=k, k_out=ko)
         ctx.rope(d, self.table, q, qo, k=k, k_out=ko, idx=kept, q_w=self.q_w, k_w=self.k_w)
-        a = F.scaled_dot_product_attention(qo, ko, v.view(self.B, keep, self.heads, D).transpose(1, 2))
-        z = self.lin["proj"](ctx, *to_int8(ctx, a.transpose(1, 2).reshape(dense, C)))
+        if self.kv is None:
+            a = F.scaled_dot_product_attention(qo, ko, v.view(self.B, keep, self.heads, D).transpose(1, 2))
+            a = a.transpose(1, 2).reshape(dense, C)
+        else:
+            a = self.attend(qo, ko, v, kept, dense)
+        z = self.lin["proj"](ctx, *to_int8(ctx, a))
 
         # restore, gate, residual, the next norm and its 8-bit rows in one pass
         mid = torch.empty_like(x)
@@ -141,11 +165,12 @@ def drifting_input(B: int, H: int, W: int, C: int, steps: int, seed: int = 1):
 def main() -> None:
     ap = argparse.ArgumentParser()
     ap.add_argument("--steps", type=int, default=4)
+    ap.add_argument("--kv", choices=["bf16", "i8", "i4"], help="attend over a cache of all tokens' keys and values, of this type")
     a = ap.parse_args()
     B, H, W, heads, D = 2, 64, 64, 24, 64
     layout = oc.Layout(oc.KIND_TOKEN, oc.DTYPE_BF16, B, 1, H, W, heads * D)
     with oc.Context(0, oc.match_workspace_bytes(layout)) as ctx:
-        block = Block(ctx, B, H, W, heads, D, reuse=0.5)
+        block = Block(ctx, B, H, W, heads, D, reuse=0.5, kv=a.kv)
         condition = torch.randn(B, heads * D, device="cuda").to(BF16)
         for step, x in enumerate(drifting_input(B, H, W, heads * D, a.steps)):
             for _ in range(3):

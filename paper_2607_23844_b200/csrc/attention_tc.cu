@@ -47,7 +47,7 @@ template <int NT, int SUB, int KT> struct At {
     // probabilities.
     static constexpr int o_step = 64 * SUB, places = (512 - NT * o_step) / 128, o_col = places * 128;
     static constexpr bool one_warp = places == NT;                               // for both products
-    static constexpr int n_bars = 2 * k_stages + 3 * v_stages + 2 * raw_stages + 2 * AT_SCALES + 3 * places + 2;
+    static constexpr int n_bars = 2 * k_stages + 3 * v_stages + 2 * raw_stages + 3 * AT_SCALES + 3 * places + 2;
     static constexpr int smem = rest_at + n_bars * 8 + 64;
     static constexpr int out_stride = 64 * SUB + 4;                              // floats between rows where a cluster joins them
 };
@@ -176,6 +176,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     extern __shared__ __align__(1024) uint8_t at_smem[];
     __shared__ int s_range[NT][4];                                               // of each tile: first key seen, last, highest first, lowest last
     __shared__ float s_stats[NT * AT_ROWS][2];
+    __shared__ __align__(16) float s_ones[A::quant ? AT_KEYS : 4];
     __shared__ int s_odd;                                                        // whether a value was no number
     const uint32_t smem = smem_u32(at_smem);
     uint64_t* bars = (uint64_t*)(at_smem + A::rest_at);
@@ -183,11 +184,12 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     const uint32_t k_full = bar0, k_empty = k_full + 8 * A::k_stages, v_full = k_empty + 8 * A::k_stages, v_ready = v_full + 8 * A::v_stages;
     const uint32_t v_empty = v_ready + 8 * A::v_stages, raw_full = v_empty + 8 * A::v_stages, raw_empty = raw_full + 8 * A::raw_stages;
     const uint32_t sc_full = raw_empty + 8 * A::raw_stages, sc_empty = sc_full + 8 * AT_SCALES;
-    const uint32_t s_full = sc_empty + 8 * AT_SCALES, p_ready = s_full + 8 * A::places, p_done = p_ready + 8 * A::places, drain = p_done + 8 * A::places;
+    const uint32_t sc_ready = sc_empty + 8 * AT_SCALES, s_full = sc_ready + 8 * AT_SCALES, p_ready = s_full + 8 * A::places, p_done = p_ready + 8 * A::places, drain = p_done + 8 * A::places;
     uint32_t* tmem_slot = (uint32_t*)(bars + A::n_bars);
     volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = P.pages.D;
 
+    if (A::quant && threadIdx.x < AT_KEYS) s_ones[threadIdx.x] = 1.0f;
     if (smem & 1023u) {                                                          // never expected; refuse rather than compute garbage
         if (threadIdx.x == 0) atomicCAS(P.pages.status, 0, OC_ERR_ALIGNMENT);
         return;
@@ -196,7 +198,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         for (int i = 0; i < A::k_stages; ++i) { mbar_init(k_full + 8 * i, A::quant ? A::helpers : 1); mbar_init(k_empty + 8 * i, 1); }
         for (int i = 0; i < A::v_stages; ++i) { mbar_init(v_full + 8 * i, 1); mbar_init(v_ready + 8 * i, A::helpers); mbar_init(v_empty + 8 * i, 1); }
         for (int i = 0; i < A::raw_stages; ++i) { mbar_init(raw_full + 8 * i, 1); mbar_init(raw_empty + 8 * i, A::helpers); }
-        for (int i = 0; i < AT_SCALES; ++i) { mbar_init(sc_full + 8 * i, 1); mbar_init(sc_empty + 8 * i, A::softmax_warps); }
+        for (int i = 0; i < AT_SCALES; ++i) { mbar_init(sc_full + 8 * i, 1); mbar_init(sc_ready + 8 * i, 1); mbar_init(sc_empty + 8 * i, A::softmax_warps); }
         for (int i = 0; i < A::places; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); mbar_init(p_done + 8 * i, 1); }
         mbar_init(drain, 1); mbar_init(drain + 8, 1);
         *abort_flag = 0;
@@ -446,10 +448,10 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     } else if (warp >= A::helper0) {
         // ================================ helpers ===============================================
         const int h = warp - A::helper0;
-        if (!A::quant) {
-            int cut_lo = 0, cut_hi = 0x7FFFFFFF;                                 // tiles within are seen whole by every row
+        int cut_lo = 0, cut_hi = 0x7FFFFFFF;                                     // tiles within are seen whole by every row
 #pragma unroll
-            for (int t = 0; t < NT; ++t) if (s_range[t][1] > 0) { cut_lo = max(cut_lo, s_range[t][2]); cut_hi = min(cut_hi, s_range[t][3]); }
+        for (int t = 0; t < NT; ++t) if (s_range[t][1] > 0) { cut_lo = max(cut_lo, s_range[t][2]); cut_hi = min(cut_hi, s_range[t][3]); }
+        if (!A::quant) {
             for (int j = j0; j < j1; ++j) {
                 const int st = (j - j0) % A::v_stages;
                 if (!AT_WAIT(v_full + 8 * st, (uint32_t)((j - j0) / A::v_stages) & 1u)) break;
@@ -513,6 +515,18 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 __syncwarp();
             };
             for (int j = j0; j < j1 + 1 && ok; ++j) {                            // in the order of the copies
+                if (j < j1 && h == 0) {
+                    const int sst = (j - j0) % AT_SCALES;
+                    if (!AT_WAIT(sc_full + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
+                    if (j * AT_KEYS < cut_lo || (j + 1) * AT_KEYS > cut_hi) {    // scales of values that are no numbers: as in bf16
+                        float* v = (float*)(at_smem + A::scale_at) + (2 * sst + 1) * AT_KEYS;
+#pragma unroll
+                        for (int i = 0; i < AT_KEYS; i += 32)
+                            if (!isfinite(v[i + lane])) { v[i + lane] = 0.0f; if (j * AT_KEYS + i + lane < S.len) s_odd = 1; }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(sc_ready + 8 * sst);
+                }
                 if (j < j1) {
                     const int st = (j - j0) % A::k_stages;
                     if (!AT_WAIT(raw_full + 8 * stage, phase) || !AT_WAIT(k_empty + 8 * st, ((uint32_t)((j - j0) / A::k_stages) & 1u) ^ 1u)) break;
@@ -541,9 +555,8 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         int n = 0;                                                               // tiles of keys done
         for (int j = j0; j < j1 && ok; ++j) {
             const int sst = (j - j0) % AT_SCALES;
-            const uint32_t sc_at = smem + A::scale_at + (uint32_t)(sst * 2 * AT_KEYS * 4);
             if (A::quant && (j < my_a || j >= my_b)) {
-                if (!AT_WAIT(sc_full + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
+                if (!AT_WAIT(sc_ready + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
                 if (lane == 0) mbar_arrive(sc_empty + 8 * sst);
             }
             const int product = NT * (j - j0) + my_tile, place = product % A::places;
@@ -554,7 +567,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 continue;
             }
             tc_fence_after();
-            if (A::quant && !AT_WAIT(sc_full + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
+            if (A::quant && !AT_WAIT(sc_ready + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
             const int key0 = j * AT_KEYS;
             const bool cut = __any_sync(0xFFFFFFFFu, exists && lo < hi && (key0 < lo || key0 + AT_KEYS > hi));
             constexpr int CH = A::chunk;
@@ -564,24 +577,25 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
 #pragma unroll
                 for (int e = 0; e < CH; ++e) if (e < first_seen || e >= end_seen) x[e] = 0xFF800000u;
             };
-            auto fetched = [&](int i, uint32_t* x) {                             // scales (and masks) of keys CH i ..
-                if (A::quant) {
+            // (masked scores have their keys' scales already: a scale of 0 would make NaN of -infinity)
+            const float* ks = !A::quant || cut ? s_ones : (const float*)(at_smem + A::scale_at) + 2 * sst * AT_KEYS;
+            const float* vs = (const float*)(at_smem + A::scale_at) + (2 * sst + 1) * AT_KEYS;
+            auto scaled = [&](int i, uint32_t* x, const float* by) {             // keys CH i ..
 #pragma unroll
-                    for (int e = 0; e < CH; e += 4) {
-                        float4 k;
-                        asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w) : "r"(sc_at + 4u * CH * i + 4u * e) : "memory");
-                        const f32x2 u = f2_mul(f2_bits(x[e], x[e + 1]), f2(k.x, k.y)), v = f2_mul(f2_bits(x[e + 2], x[e + 3]), f2(k.z, k.w));
-                        x[e] = __float_as_uint(f2_lo(u)); x[e + 1] = __float_as_uint(f2_hi(u)); x[e + 2] = __float_as_uint(f2_lo(v)); x[e + 3] = __float_as_uint(f2_hi(v));
-                    }
+                for (int e = 0; e < CH; e += 4) {
+                    const float4 k = *(const float4*)(by + CH * i + e);
+                    const f32x2 u = f2_mul(f2_bits(x[e], x[e + 1]), f2(k.x, k.y)), v = f2_mul(f2_bits(x[e + 2], x[e + 3]), f2(k.z, k.w));
+                    x[e] = __float_as_uint(f2_lo(u)); x[e + 1] = __float_as_uint(f2_hi(u)); x[e + 2] = __float_as_uint(f2_lo(v)); x[e + 3] = __float_as_uint(f2_hi(v));
                 }
-                if (A::quant && cut) mask(i, x);
             };
-            if (!A::quant && cut) {                                              // masked in their place: the code below is without
+            auto fetched = [&](int i, uint32_t* x) { if (A::quant) scaled(i, x, ks); };
+            if (cut) {                                                           // masked in their place: the code below is without
 #pragma unroll 1
                 for (int i = 0; i < 128 / CH; ++i) {
                     uint32_t x[CH];
                     fetch(i, x);
                     tmem_ld_wait();
+                    if (A::quant) scaled(i, x, (const float*)(at_smem + A::scale_at) + 2 * sst * AT_KEYS);
                     mask(i, x);
 #pragma unroll
                     for (int e = 0; e < CH; e += 16) at_tmem_st16(s_at + (uint32_t)(CH * i + e), x + e);
@@ -652,21 +666,17 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                         for (int k = 0; k < (128 - CH) / 2; k += CH / 2) { if constexpr (CH == 32) at_tmem_st16(s_at + (uint32_t)k, w + k); else at_tmem_st8(s_at + (uint32_t)k, w + k); }
                     }
                     uint32_t* to = w + CH / 2 * i;
-                    float4 vs;
+                    float4 v;
 #pragma unroll
                     for (int e = 0; e < CH / 2; ++e) {
                         const f32x2 y = f2_fma(f2_bits(x[2 * e], x[2 * e + 1]), c2, shift2);
                         f32x2 p = (AT_POLY >> (e & 7) & 1) ? at_exp2_poly(y) : f2(at_exp2(f2_lo(y)), at_exp2(f2_hi(y)));
                         sum[e & 1] = f2_add(sum[e & 1], p);
                         if (A::quant) {
-                            if ((e & 1) == 0) asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(vs.x), "=f"(vs.y), "=f"(vs.z), "=f"(vs.w) : "r"(sc_at + AT_KEYS * 4u + 4u * CH * i + 8u * e) : "memory");
-                            p = f2_mul(p, (e & 1) == 0 ? f2(vs.x, vs.y) : f2(vs.z, vs.w));
+                            if ((e & 1) == 0) v = *(const float4*)(vs + CH * i + 2 * e);
+                            p = f2_mul(p, (e & 1) == 0 ? f2(v.x, v.y) : f2(v.z, v.w));
                         }
                         to[e] = pack_bf16x2(p);
-                    }
-                    if (A::quant && cut) {                                       // (0 times a scale that is no number)
-#pragma unroll
-                        for (int e = 0; e < CH / 2; ++e) to[e] &= (x[2 * e] == 0xFF800000u ? 0u : 0xFFFFu) | (x[2 * e + 1] == 0xFF800000u ? 0u : 0xFFFF0000u);
                     }
                     if (i == 128 / CH - 1) { if constexpr (CH == 32) at_tmem_st16(s_at + 48u, to); else at_tmem_st8(s_at + 56u, to); }
                 }
@@ -702,7 +712,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                     float y[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] = some ? __uint_as_float(o[i + e]) * inv : 0.0f;
-                    if (s_odd && some && !A::quant)
+                    if (s_odd && some)
                         for (int e = 0; e < 8; ++e) y[e] += attn_not_finite<KT>(P, T.seq, T.head, max(lo, 0), hi, d + i + e);
                     const uint4 v = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
                     uint16_t* out = (uint16_t*)P.out + at + d + i;
@@ -766,7 +776,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                     }
                     const float inv = 1.0f / sum;
                     y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
-                    if (odd && !A::quant) {
+                    if (odd) {
                         y.x += attn_not_finite<KT>(P, T.seq, T.head, a, b, d); y.y += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 1);
                         y.z += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 2); y.w += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 3);
                     }

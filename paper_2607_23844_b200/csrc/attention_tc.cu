@@ -34,13 +34,13 @@ static constexpr float AT_LAG = 8.0f, AT_SUM_MAX = 128.0f * 256.0f;
 template <int NT, int SUB, int KT> struct At {
     static constexpr bool quant = KT == OC_DTYPE_I8 || KT == OC_DTYPE_I4;
     static constexpr int softmax_warps = 4 * NT, copy_warp = softmax_warps, score_warp = copy_warp + 1, output_warp = copy_warp + 2, helper0 = copy_warp + 3;
-    static constexpr int helpers = quant ? 5 : 1;
+    static constexpr int helpers = quant ? 5 : 1, k_helpers = quant ? 3 : 0, v_helpers = helpers - k_helpers;         // of keys, of values
     static constexpr int warps = helper0 + helpers, threads = 32 * warps;
     static constexpr int chunk = threads > 384 ? 16 : 32;                        // scores that a thread fetches at a time
     static constexpr int tile_bytes = SUB * AT_SUB_BYTES;                        // 128 keys (or rows) in bf16
     static constexpr int raw_bytes = KT == OC_DTYPE_I8 ? tile_bytes / 2 : tile_bytes / 4;        // (most) of 128 keys as they lie
     static constexpr int k_stages = quant ? (NT * SUB == 4 ? 1 : 2) : (SUB == 1 ? 3 : 2), v_stages = quant ? 2 : k_stages;
-    static constexpr int raw_stages = !quant ? 0 : (SUB == 2 && KT == OC_DTYPE_I8 ? 3 : 4);
+    static constexpr int rk_stages = quant ? 2 : 0, rv_stages = !quant ? 0 : (SUB == 2 && KT == OC_DTYPE_I8 ? 1 : 2), raw_stages = rk_stages + rv_stages;   // rows as they lie
     static constexpr int q_at = 0, k_at = NT * tile_bytes, v_at = k_at + k_stages * tile_bytes, raw_at = v_at + v_stages * tile_bytes;
     static constexpr int scale_at = raw_at + raw_stages * raw_bytes, rest_at = scale_at + (quant ? AT_SCALES * 2 * AT_KEYS * 4 : 0);
     // Tensor memory, all 512 columns: what is left beside O are places of 128 columns for scores, each taken over by its
@@ -195,9 +195,9 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         return;
     }
     if (threadIdx.x == 0) {
-        for (int i = 0; i < A::k_stages; ++i) { mbar_init(k_full + 8 * i, A::quant ? A::helpers : 1); mbar_init(k_empty + 8 * i, 1); }
-        for (int i = 0; i < A::v_stages; ++i) { mbar_init(v_full + 8 * i, 1); mbar_init(v_ready + 8 * i, A::helpers); mbar_init(v_empty + 8 * i, 1); }
-        for (int i = 0; i < A::raw_stages; ++i) { mbar_init(raw_full + 8 * i, 1); mbar_init(raw_empty + 8 * i, A::helpers); }
+        for (int i = 0; i < A::k_stages; ++i) { mbar_init(k_full + 8 * i, A::quant ? A::k_helpers : 1); mbar_init(k_empty + 8 * i, 1); }
+        for (int i = 0; i < A::v_stages; ++i) { mbar_init(v_full + 8 * i, 1); mbar_init(v_ready + 8 * i, A::v_helpers); mbar_init(v_empty + 8 * i, 1); }
+        for (int i = 0; i < A::raw_stages; ++i) { mbar_init(raw_full + 8 * i, 1); mbar_init(raw_empty + 8 * i, i < A::rk_stages ? A::k_helpers : A::v_helpers); }
         for (int i = 0; i < AT_SCALES; ++i) { mbar_init(sc_full + 8 * i, 1); mbar_init(sc_ready + 8 * i, 1); mbar_init(sc_empty + 8 * i, A::softmax_warps); }
         for (int i = 0; i < A::places; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); mbar_init(p_done + 8 * i, 1); }
         mbar_init(drain, 1); mbar_init(drain + 8, 1);
@@ -326,9 +326,8 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 at_v = at; at = next;
             }
         } else {
-            int stage = 0; uint32_t phase = 0;
             int at = j0 < j1 ? find(j0) : -2, at_v = at;
-            auto load = [&](const void* pool, int where) {
+            auto load = [&](const void* pool, int stage, uint32_t phase, int where) {
                 if (!AT_WAIT(raw_empty + 8 * stage, phase ^ 1u)) return;
                 const uint32_t to = smem + A::raw_at + (uint32_t)(stage * A::raw_bytes), bar = raw_full + 8 * stage, bytes = (uint32_t)(TP.box_rows * TP.row_bytes);
                 uint32_t boxes = 0;
@@ -340,12 +339,12 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 }
                 mbar_arrive_expect_tx_elected(bar, boxes * bytes, issue);
                 bytes_pending = bar;
-                if (++stage == A::raw_stages) { stage = 0; phase ^= 1u; }
             };
+            constexpr int RK = A::quant ? A::rk_stages : 1, RV = A::quant ? A::rv_stages : 1;
             for (int j = j0; j < j1 + 1 && ok; ++j) {
                 const int next = j + 1 < j1 ? find(j + 1) : -2;
                 if (j < j1) {
-                    load(P.k_pool, at);
+                    load(P.k_pool, (j - j0) % RK, (uint32_t)((j - j0) / RK) & 1u, at);
                     const int st = (j - j0) % AT_SCALES; const uint32_t ph = (uint32_t)((j - j0) / AT_SCALES) & 1u;
                     if (!ok || !AT_WAIT(sc_empty + 8 * st, ph ^ 1u)) break;
                     const uint32_t to = smem + A::scale_at + (uint32_t)(st * 2 * AT_KEYS * 4), bytes = (uint32_t)TP.box_rows * 4u;
@@ -369,7 +368,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                     if (zeros) __syncwarp();
                     mbar_arrive_expect_tx_elected(sc_full + 8 * st, 2 * boxes * bytes, issue);
                 }
-                if (j > j0) load(P.v_pool, at_v);
+                if (j > j0) load(P.v_pool, RK + (j - 1 - j0) % RV, (uint32_t)((j - 1 - j0) / RV) & 1u, at_v);
                 at_v = at; at = next;
             }
         }
@@ -481,21 +480,22 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
             }
         } else {
             const int units = D / 8, items = AT_KEYS * units;                    // of 8 elements, in the order in which they lie
+            const bool value = h >= A::k_helpers;                                // this warp's share of the keys, or of the values
+            const int ways = value ? A::v_helpers : A::k_helpers, share = value ? h - A::k_helpers : h;
+            const int stages = value ? A::v_stages : A::k_stages, at0 = value ? A::v_at : A::k_at;
             // the elements that fill up a product's step of 16 are zeros for good
             if (units & 1)
-                for (int i = h * 32 + lane; i < (A::k_stages + A::v_stages) * AT_KEYS; i += 32 * A::helpers) {
-                    const uint32_t at = smem + A::k_at + (uint32_t)((i >> 7) * A::tile_bytes + (units >> 3) * AT_SUB_BYTES + (i & 127) * 128 + (((units & 7) ^ (i & 7)) << 4));
+                for (int i = share * 32 + lane; i < stages * AT_KEYS; i += 32 * ways) {
+                    const uint32_t at = smem + (uint32_t)(at0 + (i >> 7) * A::tile_bytes + (units >> 3) * AT_SUB_BYTES + (i & 127) * 128 + (((units & 7) ^ (i & 7)) << 4));
                     asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" :: "r"(at), "r"(0u) : "memory");
                 }
-            int stage = 0; uint32_t phase = 0;
-            auto widen = [&](uint32_t base) {
-                const uint32_t raw = smem + A::raw_at + (uint32_t)(stage * A::raw_bytes);
+            auto widen = [&](uint32_t raw, uint32_t base) {
                 constexpr int BATCH = 4;                                         // (loads on their way together)
-                for (int i0 = h * 32 + lane; i0 < items; i0 += 32 * A::helpers * BATCH) {
+                for (int i0 = share * 32 + lane; i0 < items; i0 += 32 * ways * BATCH) {
                     uint2 w[BATCH];
 #pragma unroll
                     for (int b = 0; b < BATCH; ++b) {
-                        const int i = i0 + b * 32 * A::helpers;
+                        const int i = i0 + b * 32 * ways;
                         w[b] = make_uint2(0u, 0u);
                         if (i >= items) break;
                         if (KT == OC_DTYPE_I8) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[b].x), "=r"(w[b].y) : "r"(raw + 8u * i) : "memory");
@@ -503,7 +503,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                     }
 #pragma unroll
                     for (int b = 0; b < BATCH; ++b) {
-                        const int i = i0 + b * 32 * A::helpers;
+                        const int i = i0 + b * 32 * ways;
                         if (i >= items) break;
                         const uint32_t r = TP.units.div((uint32_t)i), u = (uint32_t)i - r * TP.units.d;
                         const uint4 v = KT == OC_DTYPE_I8 ? at_widen_i8(w[b]) : at_widen_i4(w[b].x);
@@ -514,33 +514,26 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
             };
-            for (int j = j0; j < j1 + 1 && ok; ++j) {                            // in the order of the copies
-                if (j < j1 && h == 0) {
-                    const int sst = (j - j0) % AT_SCALES;
-                    if (!AT_WAIT(sc_full + 8 * sst, (uint32_t)((j - j0) / AT_SCALES) & 1u)) break;
+            constexpr int RK = A::quant ? A::rk_stages : 1, RV = A::quant ? A::rv_stages : 1;
+            const int raws = value ? RV : RK, raw0 = value ? RK : 0;
+            for (int j = j0; j < j1 && ok; ++j) {
+                const int i = j - j0, st = i % stages, rs = raw0 + i % raws;
+                const uint32_t empty = (value ? v_empty : k_empty) + 8 * st, full = (value ? v_ready : k_full) + 8 * st;
+                if (h == 0) {
+                    const int sst = i % AT_SCALES;
+                    if (!AT_WAIT(sc_full + 8 * sst, (uint32_t)(i / AT_SCALES) & 1u)) break;
                     if (j * AT_KEYS < cut_lo || (j + 1) * AT_KEYS > cut_hi) {    // scales of values that are no numbers: as in bf16
                         float* v = (float*)(at_smem + A::scale_at) + (2 * sst + 1) * AT_KEYS;
 #pragma unroll
-                        for (int i = 0; i < AT_KEYS; i += 32)
-                            if (!isfinite(v[i + lane])) { v[i + lane] = 0.0f; if (j * AT_KEYS + i + lane < S.len) s_odd = 1; }
+                        for (int k = 0; k < AT_KEYS; k += 32)
+                            if (!isfinite(v[k + lane])) { v[k + lane] = 0.0f; if (j * AT_KEYS + k + lane < S.len) s_odd = 1; }
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(sc_ready + 8 * sst);
                 }
-                if (j < j1) {
-                    const int st = (j - j0) % A::k_stages;
-                    if (!AT_WAIT(raw_full + 8 * stage, phase) || !AT_WAIT(k_empty + 8 * st, ((uint32_t)((j - j0) / A::k_stages) & 1u) ^ 1u)) break;
-                    widen(smem + A::k_at + (uint32_t)(st * A::tile_bytes));
-                    if (lane == 0) { mbar_arrive(k_full + 8 * st); mbar_arrive(raw_empty + 8 * stage); }
-                    if (++stage == A::raw_stages) { stage = 0; phase ^= 1u; }
-                }
-                if (j > j0) {
-                    const int st = (j - 1 - j0) % A::v_stages;
-                    if (!AT_WAIT(raw_full + 8 * stage, phase) || !AT_WAIT(v_empty + 8 * st, ((uint32_t)((j - 1 - j0) / A::v_stages) & 1u) ^ 1u)) break;
-                    widen(smem + A::v_at + (uint32_t)(st * A::tile_bytes));
-                    if (lane == 0) { mbar_arrive(v_ready + 8 * st); mbar_arrive(raw_empty + 8 * stage); }
-                    if (++stage == A::raw_stages) { stage = 0; phase ^= 1u; }
-                }
+                if (!AT_WAIT(raw_full + 8 * rs, (uint32_t)(i / raws) & 1u) || !AT_WAIT(empty, ((uint32_t)(i / stages) & 1u) ^ 1u)) break;
+                widen(smem + A::raw_at + (uint32_t)(rs * A::raw_bytes), smem + (uint32_t)(at0 + st * A::tile_bytes));
+                if (lane == 0) { mbar_arrive(full); mbar_arrive(raw_empty + 8 * rs); }
             }
         }
         if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }

@@ -36,7 +36,9 @@ template <int NT, int SUB, int KT> struct At {
     static constexpr int softmax_warps = 4 * NT, copy_warp = softmax_warps, score_warp = copy_warp + 1, output_warp = copy_warp + 2, helper0 = copy_warp + 3;
     static constexpr int helpers = quant ? 5 : 1, k_helpers = quant ? 3 : 0, v_helpers = helpers - k_helpers;         // of keys, of values
     static constexpr int warps = helper0 + helpers, threads = 32 * warps;
-    static constexpr int chunk = threads > 384 ? 16 : 32;                        // scores that a thread fetches at a time
+    // 512 threads are launched with 128 registers each: 2 x 128 x 176 + 2 x 128 x 80 of them
+    static constexpr int take_regs = threads == 512 ? 176 : 0, give_regs = threads == 512 ? 80 : 0;
+    static constexpr int chunk = 32;                        // scores that a thread fetches at a time
     static constexpr int tile_bytes = SUB * AT_SUB_BYTES;                        // 128 keys (or rows) in bf16
     static constexpr int raw_bytes = KT == OC_DTYPE_I8 ? tile_bytes / 2 : tile_bytes / 4;        // (most) of 128 keys as they lie
     static constexpr int k_stages = quant ? (NT * SUB == 4 ? 1 : 2) : (SUB == 1 ? 3 : 2), v_stages = quant ? 2 : k_stages;
@@ -160,6 +162,10 @@ __device__ __forceinline__ uint4 at_widen_i4(uint32_t w) {
 #ifndef AT_POLY
 #define AT_POLY 0x11
 #endif
+// Registers that warps give back and that the softmax warps take (whole warpgroups do the same)
+template <int REGS> __device__ __forceinline__ void at_give() { if constexpr (REGS > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(REGS)); }
+template <int REGS> __device__ __forceinline__ void at_take() { if constexpr (REGS > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(REGS)); }
+
 struct AttnTcParams {
     AttnParams a;
     CUtensorMap mapK, mapV;          // bf16: {head_dim, vectors of the pool}, boxes {64, box_rows}
@@ -281,6 +287,8 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     bool ok = true;
 #define AT_WAIT(bar, parity) (ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait((bar), (parity), abort_flag)))
 
+    if (warp >= A::softmax_warps) {
+    at_give<A::give_regs>();
     if (warp == A::copy_warp) {
         // ================================ copies ================================================
         const uint32_t issue = elect_one();
@@ -444,7 +452,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         tc_commit<false>(over, issue);
         const unsigned long long t0 = global_ns();
         while (!mbar_try_wait(over, 0) && global_ns() - t0 < WAIT_LIMIT_NS) {}
-    } else if (warp >= A::helper0) {
+    } else {
         // ================================ helpers ===============================================
         const int h = warp - A::helper0;
         int cut_lo = 0, cut_hi = 0x7FFFFFFF;                                     // tiles within are seen whole by every row
@@ -537,8 +545,10 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
             }
         }
         if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
+    }
     } else {
         // ================================ softmax ===============================================
+        at_take<A::take_regs>();
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t o_at = t_lane + (uint32_t)(A::o_col + my_tile * A::o_step);
         int used = -1;                                                           // the last product of this tile of rows

@@ -38,6 +38,10 @@ template <int NT, int SUB, int KT> struct At {
     static constexpr int warps = helper0 + helpers, threads = 32 * warps;
     // 512 threads are launched with 128 registers each: 2 x 128 x 176 + 2 x 128 x 80 of them
     static constexpr int take_regs = threads == 512 ? 176 : 0, give_regs = threads == 512 ? 80 : 0;
+    // Which of 8 neighbouring pairs of exponentials come from the polynomial: what the FMA pipe has room for.  SD3-sized rows (2 x 2560 x
+    // 4096 x 24 heads of 64): none 240 us, one 229, two 220, three 258; in 8 bits, whose scales take that pipe: none 347, one 363,
+    // two 396.  Heads of 128 wait for the tensor cores instead.
+    static constexpr int poly = quant ? 0 : SUB == 1 ? 0x11 : 0x01;
     static constexpr int chunk = 32;                        // scores that a thread fetches at a time
     static constexpr int tile_bytes = SUB * AT_SUB_BYTES;                        // 128 keys (or rows) in bf16
     static constexpr int raw_bytes = KT == OC_DTYPE_I8 ? tile_bytes / 2 : tile_bytes / 4;        // (most) of 128 keys as they lie
@@ -49,7 +53,7 @@ template <int NT, int SUB, int KT> struct At {
     // probabilities.
     static constexpr int o_step = 64 * SUB, places = (512 - NT * o_step) / 128, o_col = places * 128;
     static constexpr bool one_warp = places == NT;                               // for both products
-    static constexpr int n_bars = 2 * k_stages + 3 * v_stages + 2 * raw_stages + 3 * AT_SCALES + 3 * places + 2;
+    static constexpr int n_bars = 2 * k_stages + 3 * v_stages + 2 * raw_stages + 3 * AT_SCALES + 3 * places + 3;
     static constexpr int smem = rest_at + n_bars * 8 + 64;
     static constexpr int out_stride = 64 * SUB + 4;                              // floats between rows where a cluster joins them
 };
@@ -159,9 +163,6 @@ __device__ __forceinline__ uint4 at_widen_i4(uint32_t w) {
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-#ifndef AT_POLY
-#define AT_POLY 0x11
-#endif
 // Registers that warps give back and that the softmax warps take (whole warpgroups do the same)
 template <int REGS> __device__ __forceinline__ void at_give() { if constexpr (REGS > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(REGS)); }
 template <int REGS> __device__ __forceinline__ void at_take() { if constexpr (REGS > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(REGS)); }
@@ -181,8 +182,9 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     const AttnParams& P = TP.a;
     extern __shared__ __align__(1024) uint8_t at_smem[];
     __shared__ int s_range[NT][4];                                               // of each tile: first key seen, last, highest first, lowest last
-    __shared__ float s_stats[NT * AT_ROWS][2];
+    __shared__ float s_stats[NT * AT_ROWS][2], s_share[NT * AT_ROWS];             // maxima and sums; weights of the cluster's parts
     __shared__ __align__(16) float s_ones[A::quant ? AT_KEYS : 4];
+    __shared__ unsigned char s_there[NT * AT_ROWS];
     __shared__ int s_odd;                                                        // whether a value was no number
     const uint32_t smem = smem_u32(at_smem);
     uint64_t* bars = (uint64_t*)(at_smem + A::rest_at);
@@ -190,7 +192,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     const uint32_t k_full = bar0, k_empty = k_full + 8 * A::k_stages, v_full = k_empty + 8 * A::k_stages, v_ready = v_full + 8 * A::v_stages;
     const uint32_t v_empty = v_ready + 8 * A::v_stages, raw_full = v_empty + 8 * A::v_stages, raw_empty = raw_full + 8 * A::raw_stages;
     const uint32_t sc_full = raw_empty + 8 * A::raw_stages, sc_empty = sc_full + 8 * AT_SCALES;
-    const uint32_t sc_ready = sc_empty + 8 * AT_SCALES, s_full = sc_ready + 8 * AT_SCALES, p_ready = s_full + 8 * A::places, p_done = p_ready + 8 * A::places, drain = p_done + 8 * A::places;
+    const uint32_t sc_ready = sc_empty + 8 * AT_SCALES, s_full = sc_ready + 8 * AT_SCALES, p_ready = s_full + 8 * A::places, p_done = p_ready + 8 * A::places, drain = p_done + 8 * A::places, q_ready = drain + 16;
     uint32_t* tmem_slot = (uint32_t*)(bars + A::n_bars);
     volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = P.pages.D;
@@ -206,7 +208,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         for (int i = 0; i < A::raw_stages; ++i) { mbar_init(raw_full + 8 * i, 1); mbar_init(raw_empty + 8 * i, i < A::rk_stages ? A::k_helpers : A::v_helpers); }
         for (int i = 0; i < AT_SCALES; ++i) { mbar_init(sc_full + 8 * i, 1); mbar_init(sc_ready + 8 * i, 1); mbar_init(sc_empty + 8 * i, A::softmax_warps); }
         for (int i = 0; i < A::places; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); mbar_init(p_done + 8 * i, 1); }
-        mbar_init(drain, 1); mbar_init(drain + 8, 1);
+        mbar_init(drain, 1); mbar_init(drain + 8, 1); mbar_init(q_ready, A::softmax_warps);
         *abort_flag = 0;
         s_odd = 0;
         for (int t = 0; t < NT; ++t) { s_range[t][0] = 0x7FFFFFFF; s_range[t][1] = 0; s_range[t][2] = 0; s_range[t][3] = 0x7FFFFFFF; }
@@ -223,7 +225,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     if (warp == A::score_warp) tmem_alloc_cta1(smem_u32(tmem_slot), 512);
     __syncwarp();
     __syncthreads();                                                             // (the ranges are set up)
-    // ---- rows: which keys they see; queries into shared memory (rows that are not there as zeros) ----
+    // ---- rows: which keys they see ----
     const int my_tile = warp >> 2, my_row = (warp & 3) * 32 + lane;              // of a softmax thread
     bool exists = false;
     int lo = 0, hi = 0, qi = 0, qg = 0;
@@ -239,26 +241,6 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 lo = hi = 0;
             }
         }
-        constexpr int UN = SUB * 8;
-        for (int i = threadIdx.x; i < NT * AT_ROWS * UN; i += 32 * A::softmax_warps) {
-            const int rr = i / UN, u = i % UN;
-            const uint32_t r2 = first + (uint32_t)rr;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (r2 < rows && 8 * u < D) {
-                const uint32_t q2 = TP.group.div(r2);
-                const uint16_t* q = (const uint16_t*)P.q + attn_q_at(P, S, T.seq, (int)q2, (int)T.head * P.group + (int)(r2 - q2 * TP.group.d)) + 8 * u;
-                if (P.wide_q) v = ld_v4(q);
-                else {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)q[2 * e] | (uint32_t)q[2 * e + 1] << 16;
-                    v = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            }
-            const uint32_t at = smem + A::q_at + (uint32_t)((rr >> 7) * A::tile_bytes + (u >> 3) * AT_SUB_BYTES + (rr & 127) * 128 + (((u & 7) ^ (rr & 7)) << 4));
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
@@ -400,6 +382,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         int ks = 0, vs = 0, ps = 0, po = 0;                                      // stages of keys and values; places of scores and outputs
         uint32_t kp = 0, vp = 0, pp = 0, sp = 1u;                                // their phases (the places begin empty)
         uint32_t begun[NT] = {};
+        if (warp == A::score_warp) AT_WAIT(q_ready, 0u);
         auto scores = [&](int j, int t) {                                        // t: known when this is compiled
             if (j >= n_keys || !ok) return;
             if (t == 0) { if (!AT_WAIT(k_full + 8 * ks, kp)) return; tc_fence_after(); }
@@ -549,6 +532,33 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     } else {
         // ================================ softmax ===============================================
         at_take<A::take_regs>();
+        // queries into shared memory (rows that are not there as zeros), 8 pieces of 16 bytes on their way at a time
+        constexpr int UN = SUB * 8, BATCH = 8;
+        for (int i0 = threadIdx.x; i0 < NT * AT_ROWS * UN; i0 += 32 * A::softmax_warps * BATCH) {
+            uint4 v[BATCH];
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const int i = i0 + b * 32 * A::softmax_warps, rr = i / UN, u = i % UN;
+                const uint32_t r2 = first + (uint32_t)rr;
+                v[b] = make_uint4(0, 0, 0, 0);
+                if (r2 < rows && 8 * u < D) {
+                    const uint32_t q2 = TP.group.div(r2);
+                    const uint16_t* q = (const uint16_t*)P.q + attn_q_at(P, S, T.seq, (int)q2, (int)T.head * P.group + (int)(r2 - q2 * TP.group.d)) + 8 * u;
+                    if (P.wide_q) v[b] = *(const uint4*)q;
+                    else v[b] = make_uint4((uint32_t)q[0] | (uint32_t)q[1] << 16, (uint32_t)q[2] | (uint32_t)q[3] << 16,
+                                           (uint32_t)q[4] | (uint32_t)q[5] << 16, (uint32_t)q[6] | (uint32_t)q[7] << 16);
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const int i = i0 + b * 32 * A::softmax_warps, rr = i / UN, u = i % UN;
+                const uint32_t at = smem + A::q_at + (uint32_t)((rr >> 7) * A::tile_bytes + (u >> 3) * AT_SUB_BYTES + (rr & 127) * 128 + (((u & 7) ^ (rr & 7)) << 4));
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(v[b].x), "r"(v[b].y), "r"(v[b].z), "r"(v[b].w) : "memory");
+            }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_ready);
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t o_at = t_lane + (uint32_t)(A::o_col + my_tile * A::o_step);
         int used = -1;                                                           // the last product of this tile of rows
@@ -673,7 +683,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
 #pragma unroll
                     for (int e = 0; e < CH / 2; ++e) {
                         const f32x2 y = f2_fma(f2_bits(x[2 * e], x[2 * e + 1]), c2, shift2);
-                        f32x2 p = (AT_POLY >> (e & 7) & 1) ? at_exp2_poly(y) : f2(at_exp2(f2_lo(y)), at_exp2(f2_hi(y)));
+                        f32x2 p = (A::poly >> (e & 7) & 1) ? at_exp2_poly(y) : f2(at_exp2(f2_lo(y)), at_exp2(f2_hi(y)));
                         sum[e & 1] = f2_add(sum[e & 1], p);
                         if (A::quant) {
                             if ((e & 1) == 0) v = *(const float4*)(vs + CH * i + 2 * e);
@@ -739,7 +749,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 if (n > 0) { tmem_ld32(o_at + (uint32_t)d, o); tmem_ld_wait(); }
 #pragma unroll
                 for (int i = 0; i < 32; i += 4)
-                    if (d + i < D) *(float4*)(part + d + i) = n > 0 ? make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]))
+                    if (d + i < D) *(float4*)(part + d + i) = n > 0 && m != -INFINITY ? make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]))
                                                                     : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
         }
@@ -753,39 +763,52 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(w) : "r"(cluster_map(smem_u32(&s_odd), (uint32_t)k)) : "memory");
                 odd |= w;
             }
-            // every split-th row, its elements side by side
+            // Every split-th row: first the weights of its parts (a thread for each row), then the elements side by side.
             const int vecs = D / 4, mine = (NT * AT_ROWS) / P.split;
             const uint32_t stats = smem_u32(&s_stats[0][0]);
-            for (int i = threadIdx.x; i < mine * vecs; i += 32 * A::softmax_warps) {
-                const int r = (i / vecs) * P.split + (int)rank, d = 4 * (i % vecs);
+            if ((int)threadIdx.x < mine) {
+                const int r = (int)threadIdx.x * P.split + (int)rank;
                 const uint32_t rr = first + (uint32_t)r;
-                if (rr >= rows) continue;
-                const int q2 = (int)TP.group.div(rr), head = (int)T.head * P.group + (int)(rr - (uint32_t)q2 * TP.group.d);
-                int a, b;
-                if (!attn_bounds(P, S, T.seq, q2, a, b)) continue;
+                int a = 0, b = 0;
+                const int q2 = rr < rows ? (int)TP.group.div(rr) : 0;
+                const bool there = rr < rows && attn_bounds(P, S, T.seq, q2, a, b);
                 float top = -INFINITY, sum = 0.0f;
+                for (int k = 0; k < P.split; ++k) { const float x = cluster_ld(cluster_map(stats, (uint32_t)k) + 8u * r); top = at_max3(top, x, x); }
                 for (int k = 0; k < P.split; ++k) {
-                    float x = cluster_ld(cluster_map(stats, (uint32_t)k) + 8u * r);
-                    top = at_max3(top, x, x);
+                    const uint32_t st = cluster_map(stats, (uint32_t)k) + 8u * r;
+                    const float x = cluster_ld(st), f = x == -INFINITY ? 0.0f : at_exp2((x - top) * P.scale_log2);
+                    sum = fmaf(f, cluster_ld(st + 4), sum);
+                    s_share[(int)threadIdx.x * P.split + k] = there && a < b ? f : 0.0f;
                 }
+                const float inv = 1.0f / sum;                                    // (all scores -infinity: 0 / 0)
+                if (there && a < b) for (int k = 0; k < P.split; ++k) s_share[(int)threadIdx.x * P.split + k] *= inv;
+                if (P.lse && there) P.lse[(S.row0 + q2) * P.q_heads + (int)T.head * P.group + (int)(rr - (uint32_t)q2 * TP.group.d)] = a < b ? top * P.scale + logf(sum) : -INFINITY;
+                s_there[threadIdx.x] = there ? (a < b ? 2 : 1) : 0;
+            }
+            asm volatile("bar.sync 1, %0;" :: "n"(32 * A::softmax_warps) : "memory");
+            for (int i = threadIdx.x; i < mine * vecs; i += 32 * A::softmax_warps) {
+                const int rm = i / vecs, r = rm * P.split + (int)rank, d = 4 * (i % vecs);
+                if (s_there[rm] == 0) continue;
+                const uint32_t rr = first + (uint32_t)r;
+                const int q2 = (int)TP.group.div(rr), head = (int)T.head * P.group + (int)(rr - (uint32_t)q2 * TP.group.d);
                 float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (a < b) {
-                    for (int k = 0; k < P.split; ++k) {
-                        const uint32_t st = cluster_map(stats, (uint32_t)k) + 8u * r;
-                        const float x = cluster_ld(st), f = x == -INFINITY ? 0.0f : at_exp2((x - top) * P.scale_log2);
-                        sum = fmaf(f, cluster_ld(st + 4), sum);
-                        const float4 o = cluster_ld4(cluster_map(smem, (uint32_t)k) + (uint32_t)(r * A::out_stride + d) * 4u);
-                        if (x != -INFINITY) { y.x = fmaf(f, o.x, y.x); y.y = fmaf(f, o.y, y.y); y.z = fmaf(f, o.z, y.z); y.w = fmaf(f, o.w, y.w); }
+                if (s_there[rm] == 2) {
+                    const uint32_t at = smem + (uint32_t)(r * A::out_stride + d) * 4u;
+                    for (int k = 0; k < P.split; k += 2) {                       // (a power of two of them; both on their way together)
+                        const float4 o0 = cluster_ld4(cluster_map(at, (uint32_t)k)), o1 = cluster_ld4(cluster_map(at, (uint32_t)k + 1));
+                        const float f0 = s_share[rm * P.split + k], f1 = s_share[rm * P.split + k + 1];
+                        // (a part that saw nothing of the row has zeros)
+                        y.x = fmaf(f0, o0.x, fmaf(f1, o1.x, y.x)); y.y = fmaf(f0, o0.y, fmaf(f1, o1.y, y.y));
+                        y.z = fmaf(f0, o0.z, fmaf(f1, o1.z, y.z)); y.w = fmaf(f0, o0.w, fmaf(f1, o1.w, y.w));
                     }
-                    const float inv = 1.0f / sum;
-                    y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
                     if (odd) {
+                        int a, b;
+                        attn_bounds(P, S, T.seq, q2, a, b);
                         y.x += attn_not_finite<KT>(P, T.seq, T.head, a, b, d); y.y += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 1);
                         y.z += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 2); y.w += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 3);
                     }
                 }
                 attn_store4<OC_DTYPE_BF16>(P, attn_out_at(P, S, T.seq, q2, head) + d, y);
-                if (P.lse && d == 0) P.lse[(S.row0 + q2) * P.q_heads + head] = a < b ? top * P.scale + logf(sum) : -INFINITY;
             }
         }
         cluster_sync();                                                          // nobody reads a retired CTA's memory

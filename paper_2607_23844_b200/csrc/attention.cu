@@ -1,4 +1,4 @@
-// Attention over the paged cache on the fp32 pipelines, and the choice of kernel.
+// Attention over the paged cache for fp32 queries, on the fp32 pipelines, and the choice of kernel.
 //     out[r] = sum_j p_j V[j] / sum_j p_j,   p_j = exp(scale * q[r] . K[j] - m),   m the row's running maximum
 // One CTA takes a tile of TR rows (the heads that share a head of the cache are rows of their own) and walks over the keys 64 at
 // a time; the maximum, the sum and the output of a row are carried along and rescaled when the maximum grows.
@@ -27,8 +27,6 @@ template <int KT> __device__ __forceinline__ void as_load(const void* pool, cons
     if (KT == OC_DTYPE_F32) {
         RowVec<OC_DTYPE_F32>::unpack(ld_nc_v4((const float*)pool + at), f);
         RowVec<OC_DTYPE_F32>::unpack(ld_nc_v4((const float*)pool + at + 4), f + 2);
-    } else if (KT == OC_DTYPE_BF16) {
-        RowVec<OC_DTYPE_BF16>::unpack(ld_nc_v4((const uint16_t*)pool + at), f);
     } else {
         const float s = __ldg(scales + v);
         uint2 w;
@@ -43,7 +41,7 @@ template <int KT> __device__ __forceinline__ void as_load(const void* pool, cons
     }
 }
 
-template <int TR, int DP, int QT, int KT>
+template <int TR, int DP, int KT>
 __global__ void __launch_bounds__(AS_THREADS)
 attention_simt_kernel(const __grid_constant__ AttnParams P) {
     using M = AsSmem<TR, DP>;
@@ -72,20 +70,18 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
         }
         bounds[tid][0] = lo; bounds[tid][1] = hi;
     }
-    for (int i = tid; i < TR * (DP / 8); i += AS_THREADS) {
-        const int r = i / (DP / 8), u = i % (DP / 8);
+#pragma unroll
+    for (int it = 0; it < (TR * (DP / 8) + AS_THREADS - 1) / AS_THREADS; ++it) {
+        const int i = tid + it * AS_THREADS, r = i / (DP / 8), u = i % (DP / 8);
+        if (r >= TR) break;
         f32x2 f[4] = {};
         if (first + r < rows && 8 * u < D) {
             const int row = (int)((first + r) / P.group), g = (int)((first + r) % P.group);
-            const long long at = attn_q_at(P, S, T.seq, row, (int)T.head * P.group + g) + 8 * u;
-            if (QT == OC_DTYPE_F32) {
-                const float* q = (const float*)P.q + at;
-                if (P.wide_q) { RowVec<OC_DTYPE_F32>::unpack(ld_v4(q), f); RowVec<OC_DTYPE_F32>::unpack(ld_v4(q + 4), f + 2); }
-                else for (int e = 0; e < 4; ++e) f[e] = f2(q[2 * e], q[2 * e + 1]);
-            } else {
-                const uint16_t* q = (const uint16_t*)P.q + at;
-                for (int e = 0; e < 4; ++e) f[e] = f2_bits((uint32_t)q[2 * e] << 16, (uint32_t)q[2 * e + 1] << 16);
-            }
+            const float* q = (const float*)P.q + attn_q_at(P, S, T.seq, row, (int)T.head * P.group + g) + 8 * u;
+            if (P.wide_q) { RowVec<OC_DTYPE_F32>::unpack(*(const uint4*)q, f); RowVec<OC_DTYPE_F32>::unpack(*(const uint4*)(q + 4), f + 2); }
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[e] = f2(q[2 * e], q[2 * e + 1]);
         }
         store_row_smem<8>(sq + r * M::QS + 8 * u, f);
     }
@@ -106,30 +102,49 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
 #pragma unroll
         for (int c = 0; c < C; ++c) o[r][c][0] = o[r][c][1] = o[r][c][2] = o[r][c][3] = 0.0f;
     }
-    auto load = [&](const void* pool, const float* scales, int key0, bool value) {
-        for (int i = tid; i < AS_KEYS * (DP / 8); i += AS_THREADS) {
-            const int j = i / (DP / 8), u = i % (DP / 8), key = key0 + j;
-            f32x2 f[4] = {};
+    // A tile of keys or values on its way in registers: fetched while the one before is worked on.
+    constexpr int ITEMS = AS_KEYS * (DP / 8) / AS_THREADS;
+    f32x2 ahead[ITEMS][4];
+    auto fetch = [&](const void* pool, const float* scales, int key0) {
+        int vec[ITEMS];
+#pragma unroll
+        for (int it = 0; it < ITEMS; ++it) {
+            const int i = tid + it * AS_THREADS, j = i / (DP / 8), u = i % (DP / 8), key = key0 + j;
+            vec[it] = -1;
             if (key < S.len && 8 * u < D) {
                 const uint32_t pn = P.pages.page_rows.div((uint32_t)key);
                 const int page = kv_page(P.pages, T.seq, pn);
-                if (page >= 0) as_load<KT>(pool, scales, kv_vector(P.pages, page, (uint32_t)key - pn * P.pages.page_rows.d) + T.head * P.pages.page_rows.d, D, u, f);
-                if (value && max_bits<8>(f, 0u) >= 0x7F800000u) {
-                    odd = 1;
+                if (page >= 0) vec[it] = (int)(kv_vector(P.pages, page, (uint32_t)key - pn * P.pages.page_rows.d) + T.head * P.pages.page_rows.d);
+            }
+        }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float a = f2_lo(f[e]), b = f2_hi(f[e]);
-                        f[e] = f2(isfinite(a) ? a : 0.0f, isfinite(b) ? b : 0.0f);
-                    }
+        for (int it = 0; it < ITEMS; ++it) {
+            ahead[it][0] = ahead[it][1] = ahead[it][2] = ahead[it][3] = 0;
+            if (vec[it] >= 0) as_load<KT>(pool, scales, (uint32_t)vec[it], D, (tid + it * AS_THREADS) % (DP / 8), ahead[it]);
+        }
+    };
+    auto put = [&](bool value) {
+#pragma unroll
+        for (int it = 0; it < ITEMS; ++it) {
+            const int i = tid + it * AS_THREADS, j = i / (DP / 8), u = i % (DP / 8);
+            f32x2* f = ahead[it];
+            if (value && max_bits<8>(f, 0u) >= 0x7F800000u) {
+                odd = 1;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = f2_lo(f[e]), b = f2_hi(f[e]);
+                    f[e] = f2(isfinite(a) ? a : 0.0f, isfinite(b) ? b : 0.0f);
                 }
             }
             store_row_smem<8>(skv + j * M::KS + 8 * u, f);
         }
     };
+    if (k0 < k1) fetch(P.k_pool, P.k_scale, k0 * AS_KEYS);
     for (int kt = k0; kt < k1; ++kt) {
         const int key0 = kt * AS_KEYS;
         __syncthreads();                                                     // (the last tile's values have been read)
-        load(P.k_pool, P.k_scale, key0, false);
+        put(false);
+        fetch(P.v_pool, P.v_scale, key0);
         __syncthreads();
         float s[R][4] = {};
         for (int d = 0; d < D; d += 4) {
@@ -145,7 +160,8 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
                     s[r][c] = fmaf(a[r].x, b[c].x, fmaf(a[r].y, b[c].y, fmaf(a[r].z, b[c].z, fmaf(a[r].w, b[c].w, s[r][c]))));
         }
         __syncthreads();                                                     // (the keys have been read)
-        load(P.v_pool, P.v_scale, key0, true);
+        put(true);
+        if (kt + 1 < k1) fetch(P.k_pool, P.k_scale, key0 + AS_KEYS);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float most = m[r];
@@ -206,7 +222,7 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
                 y.x += attn_not_finite<KT>(P, T.seq, T.head, a, b, d); y.y += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 1);
                 y.z += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 2); y.w += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 3);
             }
-            attn_store4<QT>(P, attn_out_at(P, S, T.seq, row, head) + d, y);
+            attn_store4<OC_DTYPE_F32>(P, attn_out_at(P, S, T.seq, row, head) + d, y);
         }
         if (P.lse && d == 0) P.lse[(S.row0 + row) * P.q_heads + head] = a < b ? most * P.scale + logf(sum) : -INFINITY;
     };
@@ -261,10 +277,10 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
 }
 
 // ---- host side -------------------------------------------------------------------------------------
-template <int TR, int DP, int QT, int KT>
+template <int TR, int DP, int KT>
 static oc_status launch_simt_as(oc_ctx* ctx, AttnParams& P, cudaStream_t s) {
     using M = AsSmem<TR, DP>;
-    auto* kernel = attention_simt_kernel<TR, DP, QT, KT>;
+    auto* kernel = attention_simt_kernel<TR, DP, KT>;
     static PerDeviceOnce once;                       // (the context's device is current here)
     if (!once.ensure(ctx->device, [&] {
             const bool ok = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, M::bytes) == cudaSuccess &&
@@ -285,11 +301,13 @@ static oc_status launch_simt_as(oc_ctx* ctx, AttnParams& P, cudaStream_t s) {
     cudaLaunchKernelEx(&l.cfg, kernel, (const AttnParams&)P);
     return last_launch_status();
 }
-template <int QT, int KT>
+template <int KT>
 static oc_status launch_simt(oc_ctx* ctx, AttnParams& P, cudaStream_t s) {
-    const bool few = (uint64_t)P.rows_per_batch * (uint64_t)P.group <= 16;
-    if (P.pages.D <= 64) return few ? launch_simt_as<16, 64, QT, KT>(ctx, P, s) : launch_simt_as<64, 64, QT, KT>(ctx, P, s);
-    return few ? launch_simt_as<16, 128, QT, KT>(ctx, P, s) : launch_simt_as<64, 128, QT, KT>(ctx, P, s);
+    // tiles of 16 rows where there are no more of them, or where those of 64 would leave most SMs idle
+    const uint64_t rows = (uint64_t)P.rows_per_batch * (uint64_t)P.group, key_tiles = (P.pages.seq_rows + AS_KEYS - 1) / AS_KEYS;
+    const bool few = rows <= 16 || (rows + 63) / 64 * P.n_seqs * P.pages.heads * std::min<uint64_t>(key_tiles, ATT_SPLIT_MAX) < (uint64_t)ctx->sm_count / 2;
+    if (P.pages.D <= 64) return few ? launch_simt_as<16, 64, KT>(ctx, P, s) : launch_simt_as<64, 64, KT>(ctx, P, s);
+    return few ? launch_simt_as<16, 128, KT>(ctx, P, s) : launch_simt_as<64, 128, KT>(ctx, P, s);
 }
 
 oc_status launch_attention(oc_ctx* ctx, const oc_kv_desc& cache, const oc_attention_desc& d, const int32_t* page_table, const int32_t* kv_len,
@@ -312,9 +330,9 @@ oc_status launch_attention(oc_ctx* ctx, const oc_kv_desc& cache, const oc_attent
     P.wide_q = ((uintptr_t)q | ((q_start ? 0u : (uint64_t)P.q_batch) | (uint64_t)P.q_row | (uint64_t)P.q_head) * eb) % 16 == 0;
     P.wide_out = ((uintptr_t)out | ((q_start ? 0u : (uint64_t)P.o_batch) | (uint64_t)P.o_row | (uint64_t)P.o_head) * eb) % 16 == 0;
     if (d.dtype == OC_DTYPE_F32) {
-        if (cache.dtype == OC_DTYPE_F32) return launch_simt<OC_DTYPE_F32, OC_DTYPE_F32>(ctx, P, s);
-        if (cache.dtype == OC_DTYPE_I8) return launch_simt<OC_DTYPE_F32, OC_DTYPE_I8>(ctx, P, s);
-        return launch_simt<OC_DTYPE_F32, OC_DTYPE_I4>(ctx, P, s);
+        if (cache.dtype == OC_DTYPE_F32) return launch_simt<OC_DTYPE_F32>(ctx, P, s);
+        if (cache.dtype == OC_DTYPE_I8) return launch_simt<OC_DTYPE_I8>(ctx, P, s);
+        return launch_simt<OC_DTYPE_I4>(ctx, P, s);
     }
     if (attention_few_rows(P)) return launch_attention_few(ctx, P, cache.dtype, s);
     return launch_attention_tc(ctx, P, cache.dtype, cache.page_rows, s);

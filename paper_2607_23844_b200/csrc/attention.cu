@@ -330,6 +330,7 @@ oc_status launch_attention(oc_ctx* ctx, const oc_kv_desc& cache, const oc_attent
     P.wide_q = ((uintptr_t)q | ((q_start ? 0u : (uint64_t)P.q_batch) | (uint64_t)P.q_row | (uint64_t)P.q_head) * eb) % 16 == 0;
     P.wide_out = ((uintptr_t)out | ((q_start ? 0u : (uint64_t)P.o_batch) | (uint64_t)P.o_row | (uint64_t)P.o_head) * eb) % 16 == 0;
     if (d.dtype == OC_DTYPE_F32) {
+        if (attention_few_rows_f32(P)) return launch_attention_few_f32(ctx, P, cache.dtype, s);
         if (cache.dtype == OC_DTYPE_F32) return launch_simt<OC_DTYPE_F32>(ctx, P, s);
         if (cache.dtype == OC_DTYPE_I8) return launch_simt<OC_DTYPE_I8>(ctx, P, s);
         return launch_simt<OC_DTYPE_I4>(ctx, P, s);

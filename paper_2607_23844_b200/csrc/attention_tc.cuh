@@ -7,4 +7,7 @@ oc_status launch_attention_tc(oc_ctx*, const AttnParams&, int kv_dtype, int64_t 
 // Few rows (attention_few.cu): whether a call has no more of them, and the call.
 bool attention_few_rows(const AttnParams&);
 oc_status launch_attention_few(oc_ctx*, AttnParams&, int kv_dtype, cudaStream_t);
+// The same for fp32 queries (attention_few_f32.cu).
+bool attention_few_rows_f32(const AttnParams&);
+oc_status launch_attention_few_f32(oc_ctx*, AttnParams&, int kv_dtype, cudaStream_t);
 }  // namespace oc

@@ -214,7 +214,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         for (int t = 0; t < NT; ++t) { s_range[t][0] = 0x7FFFFFFF; s_range[t][1] = 0; s_range[t][2] = 0; s_range[t][3] = 0x7FFFFFFF; }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        if (!A::quant) { tma_prefetch_map(&TP.mapK); tma_prefetch_map(&TP.mapV); }
+        if (!A::quant && P.pages.n_tokens > 0) { tma_prefetch_map(&TP.mapK); tma_prefetch_map(&TP.mapV); }      // (there are none for a cache of no tokens)
     }
     pdl_wait();
     const uint32_t rank = P.split > 1 ? cluster_rank() : 0u;

@@ -733,6 +733,39 @@ def test_on_another_stream_and_in_two_graphs(oc, ctx, dtype, kind, rows):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("rows", [1, 3, 140])
+def test_attention_over_a_cache_of_no_tokens(oc, ctx, dtype, kind, rows):
+    """No tokens, no pages, no addresses: zeros, and a log of 0."""
+    d = oc.kv_desc(tag(oc, kind), 2, 64, 2, 0, 16)
+    q = rand(torch.Generator().manual_seed(rows), 2 * rows, 2, 64, dtype=dtype).cuda()
+    out, lse = torch.full_like(q, 5.0), torch.full((2 * rows, 2), 5.0, device="cuda")
+    a = oc.attention_desc(d, 2 * rows, tag(oc, dtype), 2, 0.1, rows_per_batch=rows, q=q, out=out)
+    ctx.attention(d, a, q, None, None, out, lse=lse)
+    torch.cuda.synchronize()
+    assert ctx.device_status() == oc.OK and (out == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("rows", [1, 5, 200])
+def test_attention_two_calls_at_once(oc, dtype, kind, rows):
+    """Contexts of their own on streams of their own."""
+    cache = Cache(oc, kind, 2, 64, 2, 900, 32, seed=30)
+    q = rand(torch.Generator().manual_seed(rows), 2 * rows, 4, 64, dtype=dtype)
+    with oc.Context(0) as a, oc.Context(0) as b:
+        want = run(oc, a, cache, q, [rows, rows])
+        streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.zeros_like(want) for _ in range(8)]
+        qq = q.cuda()
+        d = oc.attention_desc(cache.desc, 2 * rows, tag(oc, dtype), 4, 0.125, rows_per_batch=rows, q=qq, out=outs[0])
+        torch.cuda.synchronize()
+        for i, o in enumerate(outs):
+            (a, b)[i % 2].attention(cache.desc, d, qq, cache.pool["k"], cache.pool["v"], o, stream=streams[i % 2], **cache.args())
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want) for o in outs) and a.device_status() == oc.OK and b.device_status() == oc.OK
+
+
+@pytest.mark.gpu
 def test_the_same_call_gives_the_same_bits(oc, ctx):
     for dtype, kind in TYPES:
         for rows in (1, 70):

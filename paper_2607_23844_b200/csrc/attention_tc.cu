@@ -36,8 +36,10 @@ template <int NT, int SUB, int KT> struct At {
     static constexpr int softmax_warps = 4 * NT, copy_warp = softmax_warps, score_warp = copy_warp + 1, output_warp = copy_warp + 2, helper0 = copy_warp + 3;
     static constexpr int helpers = quant ? 5 : 1, k_helpers = quant ? 3 : 0, v_helpers = helpers - k_helpers;         // of keys, of values
     static constexpr int warps = helper0 + helpers, threads = 32 * warps;
-    // 512 threads are launched with 128 registers each: 2 x 128 x 176 + 2 x 128 x 80 of them
-    static constexpr int take_regs = threads == 512 ? 176 : 0, give_regs = threads == 512 ? 80 : 0;
+    // 8 and 4 bits: of the registers that a CTA is launched with (128 for each of 512 threads, 168 for each of 384) the softmax
+    // warps take from the others: 2 x 128 x 176 + 2 x 128 x 80 = 512 x 128, 128 x 232 + 2 x 128 x 136 = 384 x 168.
+    static constexpr int take_regs = !quant ? 0 : threads == 512 ? 176 : 232, give_regs = !quant ? 0 : threads == 512 ? 80 : 136;
+    static_assert(!quant || threads == 512 || threads == 384, "registers of a CTA");
     // Which of 8 neighbouring pairs of exponentials come from the polynomial: what the FMA pipe has room for.  SD3-sized rows (2 x 2560 x
     // 4096 x 24 heads of 64): none 240 us, one 229, two 220, three 258; in 8 bits, whose scales take that pipe: none 347, one 363,
     // two 396.  Heads of 128 wait for the tensor cores instead.
@@ -513,12 +515,15 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 if (h == 0) {
                     const int sst = i % AT_SCALES;
                     if (!AT_WAIT(sc_full + 8 * sst, (uint32_t)(i / AT_SCALES) & 1u)) break;
+                    float* v = (float*)(at_smem + A::scale_at) + (2 * sst + 1) * AT_KEYS;
+#pragma unroll
+                    for (int k = 0; k < AT_KEYS; k += 32) v[k + lane - AT_KEYS] *= P.scale_log2;                   // (one product less for each score)
                     if (j * AT_KEYS < cut_lo || (j + 1) * AT_KEYS > cut_hi) {    // scales of values that are no numbers: as in bf16
-                        float* v = (float*)(at_smem + A::scale_at) + (2 * sst + 1) * AT_KEYS;
 #pragma unroll
                         for (int k = 0; k < AT_KEYS; k += 32)
                             if (!isfinite(v[k + lane])) { v[k + lane] = 0.0f; if (j * AT_KEYS + k + lane < S.len) s_odd = 1; }
                     }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); // (written again by copies)
                     __syncwarp();
                     if (lane == 0) mbar_arrive(sc_ready + 8 * sst);
                 }
@@ -563,7 +568,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         const uint32_t o_at = t_lane + (uint32_t)(A::o_col + my_tile * A::o_step);
         int used = -1;                                                           // the last product of this tile of rows
         const int my_a = my_tile == 0 ? ka[0] : ka[NT - 1], my_b = my_tile == 0 ? kb[0] : kb[NT - 1];
-        const float c = P.scale_log2;
+        const float c = A::quant ? 1.0f : P.scale_log2;                          // (in 8 and 4 bits it is in the keys' scales)
         float m = exists && lo < hi ? -INFINITY : 0.0f, l = 0.0f;                                           // what the row subtracts; its sum
         int n = 0;                                                               // tiles of keys done
         for (int j = j0; j < j1 && ok; ++j) {
@@ -666,14 +671,21 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                     uint32_t* x = s[i & 1];
                     tmem_ld_wait();
                     if (i < 128 / CH - 1) fetch(i + 1, s[(i + 1) & 1]);
-                    fetched(i, x);
+                    if constexpr (A::quant) {                                    // the exponents, in the place of the scores
+#pragma unroll
+                        for (int e = 0; e < CH; e += 4) {
+                            const float4 k = *(const float4*)(ks + CH * i + e);
+                            const f32x2 u = f2_fma(f2_bits(x[e], x[e + 1]), f2(k.x, k.y), shift2), v = f2_fma(f2_bits(x[e + 2], x[e + 3]), f2(k.z, k.w), shift2);
+                            x[e] = __float_as_uint(f2_lo(u)); x[e + 1] = __float_as_uint(f2_hi(u)); x[e + 2] = __float_as_uint(f2_lo(v)); x[e + 3] = __float_as_uint(f2_hi(v));
+                        }
+                    }
                     if (i == 128 / CH - 1) {
                         // The last scores are in registers.  If nothing asks for another round, the probabilities may take their place.
                         float top = __uint_as_float(x[0]);
 #pragma unroll
                         for (int e = 0; e < CH; e += 2) top = at_max3(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
                         const f32x2 so_far = f2_add(sum[0], sum[1]);
-                        fine = search || __all_sync(0xFFFFFFFFu, f2_lo(so_far) + f2_hi(so_far) <= AT_SUM_MAX && fmaf(top, c, shift) <= AT_LAG);
+                        fine = search || __all_sync(0xFFFFFFFFu, f2_lo(so_far) + f2_hi(so_far) <= AT_SUM_MAX && (A::quant ? top : fmaf(top, c, shift)) <= AT_LAG);
                         if (!fine) break;
 #pragma unroll
                         for (int k = 0; k < (128 - CH) / 2; k += CH / 2) { if constexpr (CH == 32) at_tmem_st16(s_at + (uint32_t)k, w + k); else at_tmem_st8(s_at + (uint32_t)k, w + k); }
@@ -682,7 +694,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                     float4 v;
 #pragma unroll
                     for (int e = 0; e < CH / 2; ++e) {
-                        const f32x2 y = f2_fma(f2_bits(x[2 * e], x[2 * e + 1]), c2, shift2);
+                        const f32x2 y = A::quant ? f2_bits(x[2 * e], x[2 * e + 1]) : f2_fma(f2_bits(x[2 * e], x[2 * e + 1]), c2, shift2);
                         f32x2 p = (A::poly >> (e & 7) & 1) ? at_exp2_poly(y) : f2(at_exp2(f2_lo(y)), at_exp2(f2_hi(y)));
                         sum[e & 1] = f2_add(sum[e & 1], p);
                         if (A::quant) {
@@ -737,7 +749,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                     }
                 }
             }
-            if (P.lse && exists && ok) P.lse[(S.row0 + qi) * P.q_heads + head] = some ? m * P.scale + logf(l) : -INFINITY;
+            if (P.lse && exists && ok) P.lse[(S.row0 + qi) * P.q_heads + head] = some ? m * (A::quant ? 0.69314718f : P.scale) + logf(l) : -INFINITY;
         } else {
             const int r = my_tile * AT_ROWS + my_row;
             float* part = (float*)at_smem + (long long)r * A::out_stride;
@@ -776,13 +788,13 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 for (int k = 0; k < P.split; ++k) { const float x = cluster_ld(cluster_map(stats, (uint32_t)k) + 8u * r); top = at_max3(top, x, x); }
                 for (int k = 0; k < P.split; ++k) {
                     const uint32_t st = cluster_map(stats, (uint32_t)k) + 8u * r;
-                    const float x = cluster_ld(st), f = x == -INFINITY ? 0.0f : at_exp2((x - top) * P.scale_log2);
+                    const float x = cluster_ld(st), f = x == -INFINITY ? 0.0f : at_exp2((x - top) * (A::quant ? 1.0f : P.scale_log2));
                     sum = fmaf(f, cluster_ld(st + 4), sum);
                     s_share[(int)threadIdx.x * P.split + k] = there && a < b ? f : 0.0f;
                 }
                 const float inv = 1.0f / sum;                                    // (all scores -infinity: 0 / 0)
                 if (there && a < b) for (int k = 0; k < P.split; ++k) s_share[(int)threadIdx.x * P.split + k] *= inv;
-                if (P.lse && there) P.lse[(S.row0 + q2) * P.q_heads + (int)T.head * P.group + (int)(rr - (uint32_t)q2 * TP.group.d)] = a < b ? top * P.scale + logf(sum) : -INFINITY;
+                if (P.lse && there) P.lse[(S.row0 + q2) * P.q_heads + (int)T.head * P.group + (int)(rr - (uint32_t)q2 * TP.group.d)] = a < b ? top * (A::quant ? 0.69314718f : P.scale) + logf(sum) : -INFINITY;
                 s_there[threadIdx.x] = there ? (a < b ? 2 : 1) : 0;
             }
             asm volatile("bar.sync 1, %0;" :: "n"(32 * A::softmax_warps) : "memory");

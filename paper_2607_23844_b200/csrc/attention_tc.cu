@@ -10,7 +10,15 @@
 //   helper warps    bf16: values of keys behind the sequence become zeros, and so do values that are no numbers where not
 //                   every row sees the tile (0 * NaN would reach the rows that do not); 8 and 4 bits: raw rows to bf16,
 //                   which holds those whole numbers exactly, so that the scales join the scores and the probabilities
-// Two tiles of rows take turns: while one's scores become probabilities the tensor cores work for the other.
+// Two tiles of rows take turns: while one's scores become probabilities the tensor cores work for the other.  With heads of up
+// to 64 a third place for scores in tensor memory lets the products run ahead of the softmax warps.
+// Measured (bf16): 25 x 4608 rows over 9216 keys, 5 heads of 64, 1359 GFLOP: 1.83 ms, 744 TFLOP/s; 2 x 2560 x 4096, 24 heads of 64:
+// 210 us, 613 (480 CTAs are 3.2 rounds of the device's 148); 2 x 2048 x 4096, 16 heads of 128: 146 us, 941.  In 8 bits 333 us and 267.
+// What bounds heads of 64: a step (256 rows, 128 keys) takes 2500 to 2800 clocks, of which the products take 1024 and the
+// exponentials 1540 (a quarter of them by polynomial), both warps of a scheduler together 1900 with all their instructions
+// where nothing else runs; reading scores out of tensor memory beside running products costs 350, and each hand-over
+// through a barrier 150 to 300.  Other splits were slower: P beside S with a place for each tile of rows (2.08 ms), one
+// warp for both products (1.92), a pass for the maximum of its own (2.07), two CTAs of one tile on an SM (2.03).
 // The maximum that a row subtracts only follows the running one when that is 2^8 ahead: rescaling O in tensor memory
 // is then rare, and the sums lose nothing by it.
 // Where there are few tiles, the CTAs of a cluster split the keys and join their sums through distributed shared memory.
@@ -883,9 +891,6 @@ static oc_status launch_tc_as(oc_ctx* ctx, AttnTcParams& TP, cudaStream_t s) {
 template <int SUB, int KT>
 static oc_status launch_tc_rows(oc_ctx* ctx, AttnTcParams& TP, cudaStream_t s) {
     const uint64_t rows = (uint64_t)TP.a.rows_per_batch * (uint64_t)TP.a.group, problems = (uint64_t)TP.a.n_seqs * (uint64_t)TP.a.pages.heads;
-#ifdef AT_NT1
-    return launch_tc_as<1, SUB, KT>(ctx, TP, s);
-#endif
     // one tile of rows in a CTA where pairs would leave SMs idle
     if (rows <= AT_ROWS || (rows + 2 * AT_ROWS - 1) / (2 * AT_ROWS) * problems < (uint64_t)ctx->sm_count) return launch_tc_as<1, SUB, KT>(ctx, TP, s);
     return launch_tc_as<2, SUB, KT>(ctx, TP, s);

@@ -5,8 +5,8 @@
 //   softmax warps   four for each tile of rows, a thread for each row: scores out of tensor memory, maximum, exponentials,
 //                   sum, probabilities in bf16 back into tensor memory, where the second product reads them
 //   copy warp       keys and values of the pages: TMA boxes (bf16), bulk copies (8 and 4 bits), into rings
-//   MMA warp        tcgen05.mma, Q K^T from shared memory, P V with P in tensor memory and V as it lies (its rows are the
-//                   product's inner axis)
+//   MMA warps       tcgen05.mma, one for Q K^T from shared memory, one for P V with P in tensor memory and V as it lies (its
+//                   rows are the product's inner axis)
 //   helper warps    bf16: values of keys behind the sequence become zeros, and so do values that are no numbers where not
 //                   every row sees the tile (0 * NaN would reach the rows that do not); 8 and 4 bits: raw rows to bf16,
 //                   which holds those whole numbers exactly, so that the scales join the scores and the probabilities
@@ -52,7 +52,7 @@ template <int NT, int SUB, int KT> struct At {
     // 4096 x 24 heads of 64): none 240 us, one 229, two 220, three 258; in 8 bits, whose scales take that pipe: none 347, one 363,
     // two 396.  Heads of 128 wait for the tensor cores instead.
     static constexpr int poly = quant ? 0 : SUB == 1 ? 0x11 : 0x01;
-    static constexpr int chunk = 32;                        // scores that a thread fetches at a time
+    static constexpr int chunk = 32;                                             // scores that a thread fetches at a time
     static constexpr int tile_bytes = SUB * AT_SUB_BYTES;                        // 128 keys (or rows) in bf16
     static constexpr int raw_bytes = KT == OC_DTYPE_I8 ? tile_bytes / 2 : tile_bytes / 4;        // (most) of 128 keys as they lie
     static constexpr int k_stages = quant ? (NT * SUB == 4 ? 1 : 2) : (SUB == 1 ? 3 : 2), v_stages = quant ? 2 : k_stages;
@@ -110,10 +110,6 @@ __device__ __forceinline__ void at_tmem_st16(uint32_t taddr, const uint32_t* v) 
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
         :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
            "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void at_tmem_st8(uint32_t taddr, const uint32_t* v) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
-        :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void at_tmem_ld16(uint32_t taddr, uint32_t* v) {
     asm volatile(
@@ -232,6 +228,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     const AttnSeq S = attn_seq(P, T.seq);
     const uint32_t first = T.tile * (uint32_t)(NT * AT_ROWS), rows = (uint32_t)S.n * (uint32_t)P.group;
     if (first >= rows) return;                                                   // (the whole cluster; nothing is allocated yet)
+    // (registers leave room for one CTA of this kernel on an SM, so no cluster waits here for what another cluster's CTA holds)
     if (warp == A::score_warp) tmem_alloc_cta1(smem_u32(tmem_slot), 512);
     __syncwarp();
     __syncthreads();                                                             // (the ranges are set up)
@@ -597,7 +594,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
             const int key0 = j * AT_KEYS;
             const bool cut = __any_sync(0xFFFFFFFFu, exists && lo < hi && (key0 < lo || key0 + AT_KEYS > hi));
             constexpr int CH = A::chunk;
-            auto fetch = [&](int i, uint32_t* x) { if constexpr (CH == 32) tmem_ld32(s_at + 32u * i, x); else at_tmem_ld16(s_at + 16u * i, x); };
+            auto fetch = [&](int i, uint32_t* x) { tmem_ld32(s_at + 32u * i, x); };
             auto mask = [&](int i, uint32_t* x) {
                 const int first_seen = lo - key0 - CH * i, end_seen = hi - key0 - CH * i;
 #pragma unroll
@@ -696,7 +693,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                         fine = search || __all_sync(0xFFFFFFFFu, f2_lo(so_far) + f2_hi(so_far) <= AT_SUM_MAX && (A::quant ? top : fmaf(top, c, shift)) <= AT_LAG);
                         if (!fine) break;
 #pragma unroll
-                        for (int k = 0; k < (128 - CH) / 2; k += CH / 2) { if constexpr (CH == 32) at_tmem_st16(s_at + (uint32_t)k, w + k); else at_tmem_st8(s_at + (uint32_t)k, w + k); }
+                        for (int k = 0; k < (128 - CH) / 2; k += CH / 2) at_tmem_st16(s_at + (uint32_t)k, w + k);
                     }
                     uint32_t* to = w + CH / 2 * i;
                     float4 v;
@@ -711,7 +708,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                         }
                         to[e] = pack_bf16x2(p);
                     }
-                    if (i == 128 / CH - 1) { if constexpr (CH == 32) at_tmem_st16(s_at + 48u, to); else at_tmem_st8(s_at + 56u, to); }
+                    if (i == 128 / CH - 1) at_tmem_st16(s_at + 48u, to);
                 }
                 if (fine) break;
                 search = true;

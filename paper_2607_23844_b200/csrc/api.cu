@@ -632,6 +632,7 @@ static oc_status kv_move(oc_ctx* c, bool put, const oc_kv_desc* cache, const oc_
     st = check_pools(cache, k_pool, k_scale, v_pool, v_scale, v != nullptr);
     if (st != OC_OK) return st;
     if (k == k_pool || (v && v == v_pool)) return OC_ERR_INVALID_ARG;
+    if (v && (put ? v_pool == k_pool || (v_scale && v_scale == k_scale) : v == k)) return OC_ERR_INVALID_ARG;  // (both would be written to one place)
     if (rows->n_rows > ROWS_MAX || rows->rows_per_batch > ROWS_MAX) return OC_ERR_UNSUPPORTED;
     const uintptr_t el = (uintptr_t)elem_size(rows->dtype) - 1;
     if (((uintptr_t)k & el) || ((uintptr_t)v & el) || ((uintptr_t)page_table & 3u) || ((uintptr_t)idx & 3u)) return OC_ERR_ALIGNMENT;
@@ -654,7 +655,7 @@ oc_status oc_attention(oc_ctx* c, const oc_kv_desc* cache, const oc_attention_de
                        const int32_t* kv_len, const int32_t* q_start, const int32_t* idx, const void* q, const void* k_pool,
                        const float* k_scale, const void* v_pool, const float* v_scale, void* out, float* lse, void* stream) {
     if (!c || !d || !float_type(d->dtype) || d->q_heads <= 0 || d->n_rows < 0 || d->rows_per_batch <= 0 || d->unit < 0) return OC_ERR_INVALID_ARG;
-    if (!(d->scale > 0.0f) || !isfinite(d->scale)) return OC_ERR_INVALID_ARG;
+    if (!(d->scale > 0.0f) || !(d->scale < 0x1p127f)) return OC_ERR_INVALID_ARG;          // (times log2(e) it is finite)
     oc_status st = check_kv(cache, page_table != nullptr);
     if (st != OC_OK) return st;
     if (!kv_quantised(cache) && cache->dtype != d->dtype) return OC_ERR_INVALID_ARG;

@@ -869,6 +869,23 @@ def test_attention_refusals(oc, host):
     assert call(cache=kv(oc, n_seqs=0)) == oc.OK
 
 
+def test_two_outputs_in_one_place_are_refused(oc, host):
+    def move(call, cache, k, kp, v, vp, ks=None, vs=None):
+        r = oc.CKvRows(oc.DTYPE_BF16, 20, 20, oc.CRopeView(2560, 128, 64), oc.CRopeView(2560, 128, 64))
+        args = (k, kp, v, vp) if call == "kv_put" else (kp, k, vp, v)
+        return getattr(host.ctx, call)(cache, r, *args, k_scale=ks, v_scale=vs, page_table=A, idx=A, stream=0, check=False)
+    assert move("kv_put", kv(oc), A, 2 * A, 3 * A, 2 * A) == oc.ERR_INVALID_ARG
+    assert move("kv_put", kv(oc, dtype=oc.DTYPE_I8), A, 2 * A, 3 * A, 4 * A, 5 * A, 5 * A) == oc.ERR_INVALID_ARG
+    assert move("kv_get", kv(oc), A, 2 * A, A, 3 * A) == oc.ERR_INVALID_ARG
+
+
+def test_a_scale_whose_binary_logarithm_leaves_fp32_is_refused(oc, host):
+    view = oc.CRopeView(2560, 256, 64)
+    for scale in (2.0 ** 127, 3.4e38):
+        d = oc.CAttention(oc.DTYPE_BF16, 4, scale, 20, 10, 0, -1, -1, view, view)
+        assert host.ctx.attention(kv(oc), d, A, 2 * A, 3 * A, 4 * A, page_table=A, stream=0, check=False) == oc.ERR_INVALID_ARG
+
+
 def test_descriptors_take_strides_from_tensors(oc):
     d = kv(oc)
     packed = torch.zeros(20, 6, 64)

@@ -571,7 +571,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         if (lane == 0) mbar_arrive(q_ready);
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t o_at = t_lane + (uint32_t)(A::o_col + my_tile * A::o_step);
-        int used = -1;                                                           // the last product of this tile of rows
+        int used = -1;                                                           // the last product of this tile of rows, until it is known to have retired
         const int my_a = my_tile == 0 ? ka[0] : ka[NT - 1], my_b = my_tile == 0 ? kb[0] : kb[NT - 1];
         const float c = A::quant ? 1.0f : P.scale_log2;                          // (in 8 and 4 bits it is in the keys' scales)
         float m = exists && lo < hi ? -INFINITY : 0.0f, l = 0.0f;                                           // what the row subtracts; its sum
@@ -586,6 +586,12 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
             const uint32_t s_at = t_lane + (uint32_t)(place * 128);              // (and of the probabilities)
             if (!AT_WAIT(s_full + 8 * place, (uint32_t)(product / A::places) & 1u)) break;
             if (j < my_a || j >= my_b) {                                         // not needed
+                // (The tile's last product retires before this warp lets any later one begin: the place's barrier goes on to phases of the
+                // other tile's products, among them one of the same parity, so that a later look could miss the phase meant here.)
+                if (used >= 0) {
+                    if (!AT_WAIT(p_done + 8 * (used % A::places), (uint32_t)(used / A::places) & 1u)) break;
+                    used = -1;
+                }
                 if (lane == 0) mbar_arrive(p_ready + 8 * place);
                 continue;
             }
@@ -723,7 +729,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
             if (A::quant && lane == 0) mbar_arrive(sc_empty + 8 * sst);
             ++n;
         }
-        if (ok && n > 0) AT_WAIT(p_done + 8 * (used % A::places), (uint32_t)(used / A::places) & 1u);
+        if (ok && used >= 0) AT_WAIT(p_done + 8 * (used % A::places), (uint32_t)(used / A::places) & 1u);
         if (!ok && lane == 0) { atomicCAS(P.pages.status, 0, OC_ERR_TIMEOUT); *abort_flag = 1; }
         tc_fence_after();
         // ---- results ----

@@ -1,0 +1,81 @@
+"""Attention over the paged cache in the forms that large calls take: two tiles of 128 rows in a CTA, from 148 pairs of tiles
+on.  The restatement in 64 bits and its bounds are those of test_attention, computed on the device: the calls are larger."""
+import pytest
+import torch
+
+from test_attention import BF16, Cache, assert_attn, ctx, exact, oc, rand, tag  # noqa: F401 (fixtures)
+
+KINDS = [BF16, "i8", "i4"]
+
+
+@pytest.fixture(scope="module")
+def shared(oc):
+    """Caches that several tests read"""
+    made = {}
+
+    def get(*key, **kw):
+        if (key, tuple(kw.items())) not in made:
+            made[key, tuple(kw.items())] = Cache(oc, *key, **kw)
+        return made[key, tuple(kw.items())]
+    return get
+
+
+def attend(oc, ctx, cache, q, counts, unit=0, back=-1, ahead=-1, idx=None, ragged=False, check=True):
+    """q [n, heads, D] on the CPU, counts: rows of each sequence.  One call, its outputs and log-sum-exps checked."""
+    n, H, D = q.shape
+    rows, at = [], 0
+    for s, m in enumerate(counts):
+        for i in range(m):
+            p = cache.lens[s] - m + i if idx is None else int(idx[at + i]) - s * cache.seq_rows
+            rows.append(None if idx is not None and idx[at + i] < 0 else (s, p))
+        at += m
+    rows += [None] * (n - at)
+    qq = q.cuda()
+    out, lse = torch.full((n, H, D), 5.0, dtype=q.dtype, device="cuda"), torch.full((n, H), 5.0, device="cuda")
+    ints = lambda x: None if x is None else torch.as_tensor(x).to(torch.int32).cuda()  # noqa: E731
+    start = [sum(counts[:i]) for i in range(len(counts) + 1)] if ragged else None
+    d = oc.attention_desc(cache.desc, n, tag(oc, q.dtype), H, D ** -0.5, rows_per_batch=max(counts), unit=unit, back=back, ahead=ahead, q=qq, out=out)
+    ctx.attention(cache.desc, d, qq, cache.pool["k"], cache.pool["v"], out, kv_len=ints(cache.lens), q_start=ints(start), idx=ints(idx), lse=lse, **cache.args())
+    torch.cuda.synchronize()
+    assert ctx.device_status() == oc.OK
+    if not check:
+        return out
+    held, cache.val = cache.val, {m: v.cuda() for m, v in cache.val.items()}
+    with torch.device("cuda"):
+        want, bound, wl, bl = (t.cpu() for t in exact(cache, qq, rows, D ** -0.5, unit, back, ahead))
+    cache.val = held
+    assert_attn(out, want, bound, rows)
+    got, live = lse.cpu().double(), torch.tensor([r is not None for r in rows])
+    assert (got[~live] == 5.0).all()
+    empty = torch.isinf(wl) & live[:, None]
+    assert (got[empty] == -float("inf")).all() and ((got - wl).abs() <= bl)[live[:, None] & ~empty].all()
+    return out
+
+
+def steps_apart(n_seqs, seq_rows, apart, gen, swap=False):
+    """Kept tokens of sequences of 512 rows: of every 256 the first 128 lie in one tile of 128 keys, the others `apart` tiles behind
+    it (or before it: swap), so that with a causal window one tile of rows ends that many steps before the other."""
+    out = []
+    for s in range(n_seqs):
+        for pair in range(2):
+            near = 128 * pair + torch.randint(0, 128, (128,), generator=gen)
+            far = near + 128 * apart
+            out += [s * seq_rows + x for x in ((far, near) if swap else (near, far))]
+    return torch.cat(out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("apart", [1, 2, 3, 4, 5, 8])
+@pytest.mark.parametrize("swap", [False, True])
+def test_one_tile_of_rows_ends_before_the_other(oc, ctx, shared, kind, D, apart, swap):
+    cache = shared(kind, 20, D, 4, 1317, 64)
+    gen = torch.Generator().manual_seed(apart)
+    q = rand(gen, 4 * 512, 20, D, dtype=BF16)
+    idx = steps_apart(4, 1317, apart, gen, swap)
+    first = attend(oc, ctx, cache, q, [512] * 4, unit=1, ahead=0, idx=idx)
+    for _ in range(3):
+        assert torch.equal(attend(oc, ctx, cache, q, [512] * 4, unit=1, ahead=0, idx=idx, check=False), first)
+    attend(oc, ctx, cache, q, [512] * 4, unit=1, back=0, ahead=-1, idx=idx)              # and one that begins before the other
+    attend(oc, ctx, cache, q, [512] * 4, unit=100, back=0, ahead=0, idx=idx)             # windows with a gap between them

@@ -79,3 +79,43 @@ def test_one_tile_of_rows_ends_before_the_other(oc, ctx, shared, kind, D, apart,
         assert torch.equal(attend(oc, ctx, cache, q, [512] * 4, unit=1, ahead=0, idx=idx, check=False), first)
     attend(oc, ctx, cache, q, [512] * 4, unit=1, back=0, ahead=-1, idx=idx)              # and one that begins before the other
     attend(oc, ctx, cache, q, [512] * 4, unit=100, back=0, ahead=0, idx=idx)             # windows with a gap between them
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D", [40, 64, 72, 128])
+@pytest.mark.parametrize("unit,back,ahead,kept", [(0, -1, -1, False), (1, -1, 0, False), (1, 200, 0, True), (256, -1, 0, True), (256, 0, 0, True), (100, 1, 0, False)])
+def test_pairs_of_tiles_under_windows(oc, ctx, shared, kind, D, unit, back, ahead, kept):
+    """Rows that are no whole number of tiles; kept lists in order and with an unused tail; lengths that end inside a tile."""
+    lens, rows, gen = [700, 411], 390, torch.Generator().manual_seed(D)
+    cache = shared(kind, 40, D, 2, 700, 48, lens=tuple(lens), seed=3)
+    q = rand(gen, 2 * rows, 40, D, dtype=BF16)
+    idx = None
+    if kept:
+        idx = torch.cat([torch.cat([torch.randperm(700, generator=gen)[: rows - 7].sort().values + 700 * s, torch.full((7,), -1)]) for s in range(2)])
+    attend(oc, ctx, cache, q, [rows, rows], unit=unit, back=back, ahead=ahead, idx=idx)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_pairs_of_tiles_of_packed_sequences_and_shared_heads(oc, ctx, kind, D):
+    """Sequences of very different lengths behind one another, more rows than keys in one, none in another; four heads to a key."""
+    lens, rows = [900, 0, 300, 77, 640], [300, 0, 310, 77, 5]
+    cache = Cache(oc, kind, 10, D, 5, 900, 32, lens=lens, seed=4)
+    q = rand(torch.Generator().manual_seed(5), sum(rows) + 3, 40, D, dtype=BF16)
+    attend(oc, ctx, cache, q, rows, unit=1, ahead=0, ragged=True)
+    attend(oc, ctx, cache, q, rows, ragged=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_pairs_of_tiles_of_unsorted_rows(oc, ctx, kind, D):
+    """Kept lists in descending and in no order: every tile of rows sees every tile of keys in part."""
+    gen = torch.Generator().manual_seed(6)
+    cache = Cache(oc, kind, 20, D, 4, 520, 16, lens=[520, 519, 129, 1], seed=6)
+    q = rand(gen, 4 * 512, 20, D, dtype=BF16)
+    for order in (lambda x: x.flip(0), lambda x: x[torch.randperm(512, generator=gen)]):
+        idx = torch.cat([order(torch.arange(512)) + 520 * s for s in range(4)])
+        attend(oc, ctx, cache, q, [512] * 4, unit=1, ahead=0, idx=idx)

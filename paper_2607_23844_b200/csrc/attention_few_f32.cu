@@ -211,11 +211,10 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
         for (int w = 0; w < P.split; ++w) top = fmaxf(top, cluster_ld(cluster_map(join_at, (uint32_t)w) + 8u * r));
         for (int w = 0; w < P.split; ++w) {
             const uint32_t st = cluster_map(join_at, (uint32_t)w) + 8u * r;
-            const float mw = cluster_ld(st);
-            if (mw == -INFINITY) continue;
-            const float f = exp2f((mw - top) * P.scale_log2);
+            // (a part whose scores are all NaN has no maximum either, but its sum is NaN: it counts)
+            const float mw = cluster_ld(st), f = mw == -INFINITY ? 0.0f : exp2f((mw - top) * P.scale_log2);
             sum = fmaf(f, cluster_ld(st + 4u), sum);
-            y = fmaf(f, cluster_ld(cluster_map(part_at, (uint32_t)w) + (uint32_t)(r * DP + d) * 4u), y);
+            if (mw != -INFINITY) y = fmaf(f, cluster_ld(cluster_map(part_at, (uint32_t)w) + (uint32_t)(r * DP + d) * 4u), y);
         }
         finish(r, d, y, top, sum, odd != 0);
     }

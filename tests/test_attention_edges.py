@@ -1,0 +1,48 @@
+"""Attention over the paged cache at its edges: values that are no numbers, the largest numbers, cuts between the CTAs that share
+a sequence's keys.  Restatement and bounds are those of test_attention."""
+import pytest
+import torch
+
+from test_attention import BF16, F32, NAN, TYPES, Cache, ctx, host, oc, rand, run, tag  # noqa: F401 (fixtures)
+
+
+def poison(cache, m, tokens, what, column=7):
+    """`what` in the tokens' keys or values of sequence 0, all heads: in their scales, or one column"""
+    for t in tokens:
+        pg, r = cache.place(0, t)
+        if cache.scale[m] is None:
+            cache.pool[m][pg, :, r, column] = what
+        else:
+            cache.scale[m][pg, :, r] = what
+
+
+def with_lse(oc, ctx, cache, q, **kw):
+    """(out, lse) of one sequence on the CPU"""
+    n, H, D = q.shape
+    qq, lse = q.cuda(), torch.full((n, H), 5.0, device="cuda")
+    out = torch.full_like(qq, 5.0)
+    idx, window = kw.pop("idx", None), {k: kw.pop(k) for k in ("unit", "back", "ahead") if k in kw}
+    d = oc.attention_desc(cache.desc, n, tag(oc, q.dtype), H, kw.pop("scale", D ** -0.5), q=qq, out=out, **window)
+    ctx.attention(cache.desc, d, qq, cache.pool["k"], cache.pool["v"], out, lse=lse, kv_len=torch.tensor(cache.lens, dtype=torch.int32).cuda(),
+                  idx=None if idx is None else torch.as_tensor(idx, dtype=torch.int32).cuda(), **cache.args(), **kw)
+    torch.cuda.synchronize()
+    assert ctx.device_status() == oc.OK
+    return out.cpu(), lse.cpu()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("rows", [1, 4, 16, 40])
+def test_a_cta_that_sees_keys_of_nan_only(oc, ctx, dtype, kind, rows):
+    """Where a cluster splits the keys: the last key alone in a CTA, a CTA's whole share, a window's last key."""
+    q = rand(torch.Generator().manual_seed(rows), rows, 1, 64, dtype=dtype)
+    for lens, bad in ((33, [32]), (17, [16]), (65, [64]), (512, range(256, 512)), (512, range(0, 256))):
+        cache = Cache(oc, kind, 1, 64, 1, 512, 16, lens=[lens], seed=40)
+        poison(cache, "k", bad, NAN)
+        for t in with_lse(oc, ctx, cache, q):
+            assert torch.isnan(t).all(), (lens, bad)
+    cache = Cache(oc, kind, 1, 64, 1, 2048, 16, seed=41)
+    poison(cache, "k", [1024], NAN)
+    for t in with_lse(oc, ctx, cache, q, unit=1, back=32, ahead=0, idx=[1024] * rows):
+        assert torch.isnan(t).all()
+    assert not torch.isnan(with_lse(oc, ctx, cache, q, unit=1, back=32, ahead=0, idx=[1023] * rows)[0]).any()

@@ -671,6 +671,7 @@ oc_status oc_attention(oc_ctx* c, const oc_kv_desc* cache, const oc_attention_de
         if (st != OC_OK) return st;
     }
     if (out == k_pool || out == v_pool) return OC_ERR_INVALID_ARG;
+    if (cache->seq_rows > ROWS_MAX - 4096) return OC_ERR_UNSUPPORTED;       // (the kernels' tiles of keys end before 2^31)
     if (cache->head_dim > 128 || d->n_rows > ROWS_MAX || d->rows_per_batch > ROWS_MAX || d->q_heads > 65535) return OC_ERR_UNSUPPORTED;
     if (d->n_rows * d->q_heads > ROWS_MAX) return OC_ERR_UNSUPPORTED;
     const uintptr_t el = (uintptr_t)elem_size(d->dtype) - 1;

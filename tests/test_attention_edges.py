@@ -46,3 +46,12 @@ def test_a_cta_that_sees_keys_of_nan_only(oc, ctx, dtype, kind, rows):
     for t in with_lse(oc, ctx, cache, q, unit=1, back=32, ahead=0, idx=[1024] * rows):
         assert torch.isnan(t).all()
     assert not torch.isnan(with_lse(oc, ctx, cache, q, unit=1, back=32, ahead=0, idx=[1023] * rows)[0]).any()
+
+
+def test_sequences_whose_tiles_would_pass_2_to_the_31_are_refused(oc, host):
+    """A small pool may stand for as many tokens: pages of the table may be shared."""
+    view = oc.CRopeView(2560, 256, 64)
+    d = oc.CAttention(oc.DTYPE_BF16, 4, 0.1, 20, 20, 0, -1, -1, view, view)
+    for seq_rows in (2 ** 31 - 1, 2 ** 31 - 100, 2 ** 31 - 4096):
+        cache = oc.CKv(oc.DTYPE_BF16, 2, 64, 1, seq_rows, 2 ** 20, 1, 2 ** 11)
+        assert host.ctx.attention(cache, d, 0x10000, 0x20000, 0x30000, 0x40000, page_table=0x50000, stream=0, check=False) == oc.ERR_UNSUPPORTED, seq_rows

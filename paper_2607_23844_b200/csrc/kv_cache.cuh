@@ -48,15 +48,16 @@ __device__ __forceinline__ KvQuant kv_quant(uint32_t max_bits) {
     else { r.scale = r.max * (1.0f / L); r.inv = r.max < 1e36f ? __fdividef((float)L, r.max) : (float)L / r.max; }     // (the former has no room above)
     return r;
 }
-// rint(x * L / max) exactly, ties to even, from a quotient that is off by less than 1: there the remainder
-// x * L - q * max, which a fused multiply-add gives with one rounding, is more than half of max.
+// rint(x * L / max) exactly, ties to even, from a quotient that is off by less than 1.  x * L - (q +- 1/2) * max, doubled, decides.  x * L is a sum
+// of two fp32 numbers; the larger less the product is exact where the two are close (a multiple of the smaller one's last
+// place, and few of them), and a sum of two fp32 numbers always has the right sign.
 template <int L>
 __device__ __forceinline__ float kv_level_exact(float x, float q, float max) {
     const float xl = x * (float)L, lost = fmaf(x, (float)L, -xl);            // x * L = xl + lost
-    const float rest = 2.0f * (fmaf(-q, max, xl) + lost);
+    const float above = fmaf(-(2.0f * q + 1.0f), max, 2.0f * xl) + 2.0f * lost, below = fmaf(-(2.0f * q - 1.0f), max, 2.0f * xl) + 2.0f * lost;
     const bool odd = ((int)q & 1) != 0;
-    if (rest > max || (rest == max && odd)) return q + 1.0f;
-    if (rest < -max || (rest == -max && odd)) return q - 1.0f;
+    if (above > 0.0f || (above == 0.0f && odd)) return q + 1.0f;
+    if (below < 0.0f || (below == 0.0f && odd)) return q - 1.0f;
     return q;
 }
 // 8 elements: their whole numbers in the low bits of 8 words.  A quotient + 1.5 * 2^23 rounds to one (the conversion

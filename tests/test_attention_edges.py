@@ -3,7 +3,7 @@ a sequence's keys.  Restatement and bounds are those of test_attention."""
 import pytest
 import torch
 
-from test_attention import BF16, F32, NAN, TYPES, Cache, ctx, host, oc, rand, run, tag  # noqa: F401 (fixtures)
+from test_attention import BF16, F32, NAN, TYPES, Cache, check_put, ctx, host, oc, rand, run, tag  # noqa: F401 (fixtures)
 
 
 def poison(cache, m, tokens, what, column=7):
@@ -55,3 +55,28 @@ def test_sequences_whose_tiles_would_pass_2_to_the_31_are_refused(oc, host):
     for seq_rows in (2 ** 31 - 1, 2 ** 31 - 100, 2 ** 31 - 4096):
         cache = oc.CKv(oc.DTYPE_BF16, 2, 64, 1, seq_rows, 2 ** 20, 1, 2 ** 11)
         assert host.ctx.attention(cache, d, 0x10000, 0x20000, 0x30000, 0x40000, page_table=0x50000, stream=0, check=False) == oc.ERR_UNSUPPORTED, seq_rows
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["i8", "i4"])
+@pytest.mark.parametrize("most", [1.0, 3.0, 0.7, 2.0 ** -99, 2.0 ** 99, 1.1e30, 1e36])
+def test_put_rounds_beside_ties_as_defined(oc, ctx, kind, most):
+    """Quotients at a tie and up to three steps of x beside it."""
+    L = 127 if kind == "i8" else 7
+    top = torch.tensor(most)
+    gen = torch.Generator().manual_seed(3)
+    rows = []
+    for _ in range(64):
+        half = torch.randint(0, L, (1, 64), generator=gen).double() + 0.5
+        x = (half * top.double() / L).to(F32)
+        for _ in range(int(torch.randint(0, 4, (1,), generator=gen))):
+            x = torch.nextafter(x, torch.zeros(()) if len(rows) % 2 else top)
+        x = x * torch.where(torch.rand(1, 64, generator=gen) < 0.5, -1.0, 1.0)
+        x[0, 9] = top
+        rows.append(x)
+    x = torch.stack(rows)                                                                # [64, 1, 64]
+    cache = Cache(oc, kind, 1, 64, 1, 64, 16, empty=True)
+    xx = x.cuda()
+    ctx.kv_put(cache.desc, oc.kv_rows(cache.desc, 64, oc.DTYPE_F32, k=xx), xx, cache.pool["k"], k_scale=cache.scale["k"], page_table=cache.gpu_table)
+    torch.cuda.synchronize()
+    check_put(cache, "k", x, torch.arange(64))

@@ -53,6 +53,7 @@ __device__ __forceinline__ KvQuant kv_quant(uint32_t max_bits) {
 // place, and few of them), and a sum of two fp32 numbers always has the right sign.
 template <int L>
 __device__ __forceinline__ float kv_level_exact(float x, float q, float max) {
+    if (max > 1e30f) { x *= 2.3283064e-10f; max *= 2.3283064e-10f; }         // (by 2^-32, exactly: twice x * L has no room above)
     const float xl = x * (float)L, lost = fmaf(x, (float)L, -xl);            // x * L = xl + lost
     const float above = fmaf(-(2.0f * q + 1.0f), max, 2.0f * xl) + 2.0f * lost, below = fmaf(-(2.0f * q - 1.0f), max, 2.0f * xl) + 2.0f * lost;
     const bool odd = ((int)q & 1) != 0;

@@ -59,9 +59,9 @@ def test_sequences_whose_tiles_would_pass_2_to_the_31_are_refused(oc, host):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", ["i8", "i4"])
-@pytest.mark.parametrize("most", [1.0, 3.0, 0.7, 2.0 ** -99, 2.0 ** 99, 1.1e30, 1e36])
+@pytest.mark.parametrize("most", [1.0, 3.0, 0.7, 2.0 ** -99, 2.0 ** 99, 1.1e30, 1e36, 2.6e36, 2.7e36, 4.9e37, 1e38, 3.4028234e38])
 def test_put_rounds_beside_ties_as_defined(oc, ctx, kind, most):
-    """Quotients at a tie and up to three steps of x beside it."""
+    """Quotients at a tie and up to three steps of x beside it, also where x L leaves fp32."""
     L = 127 if kind == "i8" else 7
     top = torch.tensor(most)
     gen = torch.Generator().manual_seed(3)

@@ -38,14 +38,18 @@ __device__ __forceinline__ uint32_t kv_vector(const KvPages& K, int page, uint32
 }
 
 // Whole numbers of a vector from its largest magnitude (bits of it): scale = max|x| / L, inv = L / max|x|.
+// The scale is the nearest fp32 number, without a division (one costs fp32 rows 24 us of 174): max times a reciprocal of two
+// parts, the smaller one first (Brisebarre, Muller and Raina, division by a divisor known in advance; equal to max / L for
+// every mantissa with both L).
 struct KvQuant { float scale, inv, max; };
 template <int L>
 __device__ __forceinline__ KvQuant kv_quant(uint32_t max_bits) {
+    constexpr float high = 1.0f / L, low = (float)(1.0 / L - (double)high);
     KvQuant r;
     r.max = __uint_as_float(max_bits);
     if (max_bits >= 0x7F800000u) { r.scale = r.max; r.inv = 0.0f; }
     else if (r.max < 7.8886091e-31f) { r.scale = 0.0f; r.inv = 0.0f; }
-    else { r.scale = r.max * (1.0f / L); r.inv = r.max < 1e36f ? __fdividef((float)L, r.max) : (float)L / r.max; }     // (the former has no room above)
+    else { r.scale = fmaf(r.max, high, r.max * low); r.inv = r.max < 1e36f ? __fdividef((float)L, r.max) : (float)L / r.max; }     // (the former has no room above)
     return r;
 }
 // rint(x * L / max) exactly, ties to even, from a quotient that is off by less than 1.  x * L - (q +- 1/2) * max, doubled, decides.  x * L is a sum

@@ -80,3 +80,25 @@ def test_put_rounds_beside_ties_as_defined(oc, ctx, kind, most):
     ctx.kv_put(cache.desc, oc.kv_rows(cache.desc, 64, oc.DTYPE_F32, k=xx), xx, cache.pool["k"], k_scale=cache.scale["k"], page_table=cache.gpu_table)
     torch.cuda.synchronize()
     check_put(cache, "k", x, torch.arange(64))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", ["i8", "i4"])
+def test_put_rounds_scales_once(oc, ctx, dtype, kind):
+    """scale = max|x| / L is the nearest fp32 number, for every magnitude and where the vector is zero or no number."""
+    n, heads = 512, 4
+    gen = torch.Generator().manual_seed(4)
+    x = rand(gen, n, heads, 64, dtype=F32) * 2.0 ** torch.randint(-98, 120, (n, heads, 1), generator=gen).float()
+    x[0], x[1, 1, 5], x[2, 1, 6], x[3] = 0.0, float("inf"), NAN, 2.0 ** -101
+    x = x.to(dtype)
+    x[:, 0, 0] = (3.0 + torch.arange(n) * 2.0 ** (-7 if dtype == BF16 else -21)).to(dtype)          # neighbours
+    cache = Cache(oc, kind, heads, 64, 1, n, 16, table=False, empty=True)
+    xx = x.cuda()
+    ctx.kv_put(cache.desc, oc.kv_rows(cache.desc, n, tag(oc, dtype), k=xx), xx, cache.pool["k"], k_scale=cache.scale["k"])
+    torch.cuda.synchronize()
+    check_put(cache, "k", x, torch.arange(n))
+    most = x.float().abs().amax(-1)
+    want = torch.where(most < 2.0 ** -100, torch.zeros(()), most / torch.tensor(127.0 if kind == "i8" else 7.0))
+    got = cache.tokens("k")[1][0]
+    assert torch.equal(got.nan_to_num(nan=-1.0), want.nan_to_num(nan=-1.0))

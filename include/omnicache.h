@@ -593,7 +593,7 @@ typedef struct oc_kv_desc {
     int dtype, heads, head_dim;
     int64_t n_seqs, seq_rows;
     int64_t page_rows, n_pages;
-    int64_t table_stride;             /* entries of page_table for a sequence */
+    int64_t table_stride;             /* entries of page_table for a sequence; unused without one (0 where its size is asked for) */
 } oc_kv_desc;
 /* Host only: bytes of the pool and of its scales (0 for fp32 and bf16). */
 oc_status oc_kv_bytes(const oc_kv_desc* cache, size_t* pool_bytes, size_t* scale_bytes);

@@ -593,7 +593,8 @@ static oc_status check_kv(const oc_kv_desc* k, bool table) {
 
 oc_status oc_kv_bytes(const oc_kv_desc* k, size_t* pool, size_t* scales) {
     if (!pool || !scales) return OC_ERR_INVALID_ARG;
-    oc_status st = check_kv(k, true);
+    // (a stride of 0 between several sequences: a cache without a table)
+    oc_status st = check_kv(k, !k || k->table_stride > 0 || k->n_seqs <= 1);
     if (st != OC_OK) return st;
     const size_t vectors = (size_t)(k->n_pages * k->heads * k->page_rows);
     *pool = k->dtype == OC_DTYPE_I4 ? vectors * (size_t)(k->head_dim / 2) : vectors * (size_t)k->head_dim * (k->dtype == OC_DTYPE_I8 ? 1u : (size_t)elem_size(k->dtype));

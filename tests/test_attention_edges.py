@@ -102,3 +102,12 @@ def test_put_rounds_scales_once(oc, ctx, dtype, kind):
     want = torch.where(most < 2.0 ** -100, torch.zeros(()), most / torch.tensor(127.0 if kind == "i8" else 7.0))
     got = cache.tokens("k")[1][0]
     assert torch.equal(got.nan_to_num(nan=-1.0), want.nan_to_num(nan=-1.0))
+
+
+def test_sizes_of_a_cache_without_a_table(oc):
+    d = oc.CKv(oc.DTYPE_I8, 2, 64, 2, 100, 16, 14, 0)
+    assert oc.kv_bytes(d) == (14 * 2 * 16 * 64, 14 * 2 * 16 * 4)
+    for bad in (oc.CKv(oc.DTYPE_I8, 2, 64, 2, 100, 16, 13, 0), oc.CKv(oc.DTYPE_I8, 2, 64, 2, 100, 16, 14, 6)):
+        with pytest.raises(oc.OmniCacheError):
+            oc.kv_bytes(bad)
+    assert oc.kv_bytes(oc.CKv(oc.DTYPE_BF16, 2, 64, 1, 100, 16, 3, 0)) == (3 * 2 * 16 * 128, 0)      # one sequence, pages shared by a table

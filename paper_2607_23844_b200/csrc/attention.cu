@@ -49,10 +49,10 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
     using M = AsSmem<TR, DP>;
     constexpr int R = TR / 16, C = DP / 64;                                  // rows of a thread; vectors of 4 outputs
     extern __shared__ __align__(16) float as_smem[];
-    __shared__ int range[4];                                                 // first and last key that the tile sees
+    __shared__ int range[2];                                                 // first and last key that the tile sees
     __shared__ int bounds[TR][2];                                            // of each row; lo = -1: the row is left as it is
     __shared__ float stats[TR][2];
-    __shared__ int odd;                                                      // whether a value was no number
+    __shared__ int bad[2];                                                   // keys with values that are no numbers
     float *sq = as_smem + M::q, *skv = as_smem + M::kv, *sp = as_smem + M::p;
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, D = P.pages.D;
     pdl_enter();
@@ -61,7 +61,7 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
     const AttnSeq S = attn_seq(P, T.seq);
     const long long first = (long long)T.tile * TR, rows = (long long)S.n * P.group;
     if (first >= rows) return;                                               // (the whole cluster)
-    if (tid == 0) { range[0] = 0x7FFFFFFF; range[1] = 0; odd = 0; }
+    if (tid == 0) { range[0] = 0x7FFFFFFF; range[1] = 0; attn_bad_none(bad); }
     __syncthreads();
     if (tid < TR) {
         int lo = -1, hi = -1;
@@ -125,13 +125,13 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
             if (vec[it] >= 0) as_load<KT>(pool, scales, (uint32_t)vec[it], D, (tid + it * AS_THREADS) % (DP / 8), ahead[it]);
         }
     };
-    auto put = [&](bool value) {
+    auto put = [&](bool value, int key0) {
 #pragma unroll
         for (int it = 0; it < ITEMS; ++it) {
             const int i = tid + it * AS_THREADS, j = i / (DP / 8), u = i % (DP / 8);
             f32x2* f = ahead[it];
             if (value && max_bits<8>(f, 0u) >= 0x7F800000u) {
-                odd = 1;
+                attn_bad_key(bad, key0 + j);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float a = f2_lo(f[e]), b = f2_hi(f[e]);
@@ -145,7 +145,7 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
     for (int kt = k0; kt < k1; ++kt) {
         const int key0 = kt * AS_KEYS;
         __syncthreads();                                                     // (the last tile's values have been read)
-        put(false);
+        put(false, key0);
         fetch(P.v_pool, P.v_scale, key0);
         __syncthreads();
         float s[R][4] = {};
@@ -162,7 +162,7 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
                     s[r][c] = fmaf(a[r].x, b[c].x, fmaf(a[r].y, b[c].y, fmaf(a[r].z, b[c].z, fmaf(a[r].w, b[c].w, s[r][c]))));
         }
         __syncthreads();                                                     // (the keys have been read)
-        put(true);
+        put(true, key0);
         if (kt + 1 < k1) fetch(P.k_pool, P.k_scale, key0 + AS_KEYS);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -213,6 +213,7 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
             }
         }
     }
+    int bad0 = 0, bad1 = 0;
     auto finish = [&](int r, int c, const float* x, float sum, float most) {  // r: row of the tile; columns 64 c + 4 tx ..
         const int row = (int)((first + r) / P.group), head = (int)T.head * P.group + (int)((first + r) % P.group);
         const int a = bounds[r][0], b = bounds[r][1];
@@ -220,16 +221,15 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
         float4 y = a < b ? make_float4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         const int d = 64 * c + 4 * tx;
         if (d < D) {
-            if (odd && a < b) {
-                y.x += attn_not_finite<KT>(P, T.seq, T.head, a, b, d); y.y += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 1);
-                y.z += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 2); y.w += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 3);
-            }
+            const int bad_a = max(a, bad0), bad_b = min(b, bad1);
+            if (bad_a < bad_b) attn_add4(y, attn_not_finite<KT>(P, T.seq, T.head, bad_a, bad_b, d));
             attn_store4<OC_DTYPE_F32>(P, attn_out_at(P, S, T.seq, row, head) + d, y);
         }
         if (P.lse && d == 0) P.lse[(S.row0 + row) * P.q_heads + head] = a < b ? most * P.scale + logf(sum) : -INFINITY;
     };
     if (P.split == 1) {
-        __syncthreads();                                                     // (`odd` is final)
+        __syncthreads();                                                     // (`bad` is final)
+        bad0 = bad[0]; bad1 = bad[1];
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (lo[r] >= 0)
@@ -247,13 +247,7 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
         for (int c = 0; c < C; ++c) *(float4*)(part + (ty * R + r) * DP + 64 * c + 4 * tx) = make_float4(o[r][c][0], o[r][c][1], o[r][c][2], o[r][c][3]);
     }
     cluster_sync();
-    if (tid == 0) for (int k = 0; k < P.split; ++k) {                        // (a value that is no number may be another CTA's)
-        int w;
-        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(w) : "r"(cluster_map(smem_u32(&odd), (uint32_t)k)) : "memory");
-        range[2] = k == 0 ? w : range[2] | w;
-    }
-    __syncthreads();
-    const int any_odd = range[2];
+    cluster_bad(bad, P.split, bad0, bad1);                                   // (they may be another CTA's)
     const uint32_t part_at = smem_u32(part), stats_at = smem_u32(&stats[0][0]);
     for (int r = ty * P.split + (int)rank; r < TR; r += 16 * P.split) {
         if (bounds[r][0] < 0) continue;
@@ -271,7 +265,6 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
                 x[c][0] = fmaf(w, v.x, x[c][0]); x[c][1] = fmaf(w, v.y, x[c][1]); x[c][2] = fmaf(w, v.z, x[c][2]); x[c][3] = fmaf(w, v.w, x[c][3]);
             }
         }
-        if (any_odd) odd = 1;
 #pragma unroll
         for (int c = 0; c < C; ++c) finish(r, c, x[c], sum, most);
     }

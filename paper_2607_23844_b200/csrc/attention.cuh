@@ -92,28 +92,51 @@ __device__ __forceinline__ long long attn_out_at(const AttnParams& P, const Attn
     return (P.q_start ? (s.row0 + i) * P.o_row : (long long)seq * P.o_batch + (long long)i * P.o_row) + (long long)head * P.o_head;
 }
 
-// The sum of the values in column d that are no numbers, over the keys [lo, hi).  Such values are taken as zeros by the
-// kernels, so that they stay away from rows that do not see them, and added at the end to those that do.
+// Values that are no numbers are taken as zeros by the kernels, so that they stay away from rows that do not see them, and added
+// at the end to those that do.  A CTA keeps the first and the last key that holds one: rows look at the keys between only.
+__device__ __forceinline__ void attn_bad_none(int* bad) { bad[0] = 0x7FFFFFFF; bad[1] = 0; }
+__device__ __forceinline__ void attn_bad_key(int* bad, int key) { atomicMin(&bad[0], key); atomicMax(&bad[1], key + 1); }
+// Elements d .. d + 3 of vector v of the values, as bits of floats
 template <int KT>
-__device__ float attn_not_finite(const AttnParams& P, uint32_t seq, uint32_t head, int lo, int hi, int d) {
-    float sum = 0.0f;
-    for (int j = lo; j < hi; ++j) {
+__device__ __forceinline__ void attn_value4(const AttnParams& P, uint32_t v, int d, uint32_t* x) {
+    const long long at = (long long)v * P.pages.D + d;
+    if (KT == OC_DTYPE_F32) {
+        const uint4 w = *(const uint4*)((const float*)P.v_pool + at);
+        x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
+    } else if (KT == OC_DTYPE_BF16) {
+        const uint2 w = *(const uint2*)((const uint16_t*)P.v_pool + at);
+        x[0] = w.x << 16; x[1] = w.x & 0xFFFF0000u; x[2] = w.y << 16; x[3] = w.y & 0xFFFF0000u;
+    } else {
+        const float s = P.v_scale[v];
+        const uint32_t w = KT == OC_DTYPE_I8 ? *(const uint32_t*)((const uint8_t*)P.v_pool + at) : (uint32_t)*(const uint16_t*)((const uint8_t*)P.v_pool + (at >> 1));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            x[e] = __float_as_uint(s * (float)(KT == OC_DTYPE_I8 ? (int)(w << (24 - 8 * e)) >> 24 : (int)(w << (28 - 4 * e)) >> 28));
+    }
+}
+// The sums of what is no number in columns d .. d + 3 of the keys [lo, hi): 0 where there is nothing of the kind.
+// (Sums of NaN stay what they are: the rest is not looked at.)
+template <int KT>
+__device__ __forceinline__ float4 attn_not_finite(const AttnParams& P, uint32_t seq, uint32_t head, int lo, int hi, int d) {
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = lo; j < hi;) {
+        const int end = min(hi, (j & ~15) + 16);                             // (pages have a multiple of 16 rows)
         const uint32_t pn = P.pages.page_rows.div((uint32_t)j);
         const int page = kv_page(P.pages, seq, pn);
-        if (page < 0) continue;
-        const uint32_t v = kv_vector(P.pages, page, (uint32_t)j - pn * P.pages.page_rows.d) + head * P.pages.page_rows.d;
-        uint32_t x;
-        if (KT == OC_DTYPE_F32) x = __float_as_uint(((const float*)P.v_pool)[(long long)v * P.pages.D + d]);
-        else if (KT == OC_DTYPE_BF16) x = (uint32_t)((const uint16_t*)P.v_pool)[(long long)v * P.pages.D + d] << 16;
-        else {
-            const long long at = (long long)v * P.pages.D + d;
-            const int n = KT == OC_DTYPE_I8 ? (int)((const int8_t*)P.v_pool)[at] : (int)(((uint32_t)((const uint8_t*)P.v_pool)[at >> 1] << (28 - 4 * (d & 1)))) >> 28;
-            x = __float_as_uint((float)n * P.v_scale[v]);
+        if (page < 0) { j = end; continue; }
+        uint32_t v = kv_vector(P.pages, page, (uint32_t)j - pn * P.pages.page_rows.d) + head * P.pages.page_rows.d;
+#pragma unroll 4
+        for (; j < end; ++j, ++v) {
+            uint32_t x[4];
+            attn_value4<KT>(P, v, d, x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) if ((x[e] & 0x7F800000u) == 0x7F800000u) sum[e] += __uint_as_float(x[e]);
         }
-        if ((x & 0x7F800000u) == 0x7F800000u) sum += __uint_as_float(x);
+        if (isnan(sum[0]) && isnan(sum[1]) && isnan(sum[2]) && isnan(sum[3])) break;
     }
-    return sum;
+    return make_float4(sum[0], sum[1], sum[2], sum[3]);
 }
+__device__ __forceinline__ void attn_add4(float4& y, const float4& t) { y.x += t.x; y.y += t.y; y.z += t.z; y.w += t.w; }
 
 // Whole numbers as pairs of bf16, which holds them exactly.
 //   8 bits: u = x + 128 (the sign bit flipped) in the low byte of 0x4300 reads as 256 + x where x < 0, as 256 + 2x elsewhere (bit 7
@@ -146,6 +169,18 @@ __device__ __forceinline__ float4 cluster_ld4(uint32_t addr) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
     return v;
+}
+
+// The first and last of such keys of a cluster's CTAs
+__device__ __forceinline__ void cluster_bad(const int* bad, int ctas, int& first, int& end) {
+    first = 0x7FFFFFFF; end = 0;
+    for (int k = 0; k < ctas; ++k) {
+        const uint32_t at = cluster_map(smem_u32(bad), (uint32_t)k);
+        int a, b;
+        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(a) : "r"(at) : "memory");
+        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(b) : "r"(at + 4u) : "memory");
+        first = min(first, a); end = max(end, b);
+    }
 }
 
 // Four neighbouring elements of a row's result

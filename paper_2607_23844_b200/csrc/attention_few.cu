@@ -72,7 +72,7 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
     constexpr int KB = KT == OC_DTYPE_BF16 ? 2 * E : KT == OC_DTYPE_I8 ? E : E / 2, VB = KT == OC_DTYPE_BF16 ? 2 * EV : KT == OC_DTYPE_I8 ? EV : EV / 2;
     constexpr int STEPS = NC * E / 4, DP = NP * 8 * EV, RT = ROWS / 8, OT = NP * EV / 2;       // products of scores; columns; tiles of rows, of outputs
     extern __shared__ __align__(16) float af_smem[];                         // [warps][rows][DP + 4] outputs, then [warps][rows][2] maxima and sums
-    __shared__ int s_range[4], s_odd;
+    __shared__ int s_bad[2];                                                 // keys with values that are no numbers
     __shared__ float s_join[AF_ROWS][2];
     constexpr int OS = DP + 4;
     float* stats = af_smem + AF_WARPS * ROWS * OS;
@@ -122,7 +122,7 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
         low = max(low, __shfl_xor_sync(0xFFFFFFFFu, low, d)); high = min(high, __shfl_xor_sync(0xFFFFFFFFu, high, d));
         from = min(from, __shfl_xor_sync(0xFFFFFFFFu, from, d)); to = max(to, __shfl_xor_sync(0xFFFFFFFFu, to, d));
     }
-    if (threadIdx.x == 0) s_odd = 0;
+    if (threadIdx.x == 0) attn_bad_none(s_bad);
     // this CTA's share of the steps of 16 keys, this warp's every eighth
     int k0 = from / AF_STEP, k1 = to > 0 ? (to + AF_STEP - 1) / AF_STEP : 0;
     if (k1 <= k0) k0 = k1 = 0;
@@ -202,7 +202,7 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
             for (int i2 = 0; i2 < 4; ++i2) q[rt][s + (i2 >> 1)][i2 & 1] = (uint32_t)e[af_first<KT>(i2)] | (uint32_t)e[af_second<KT>(i2)] << 16;
         }
     }
-    __syncthreads();                                                         // (s_odd)
+    __syncthreads();                                                         // (s_bad)
     const float cc = P.scale_log2, lag = AF_LAG / cc;
     for (; k < k1; k += AF_WARPS) {
         if (quant)
@@ -276,19 +276,20 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
             p[rt][0] = af_transpose(pack_bf16x2(e[0], e[1])); p[rt][1] = af_transpose(pack_bf16x2(e[2], e[3]));
         }
         if (!quant && cut) {                                                 // 0 * NaN would reach rows that do not see it
-            bool odd = false;
 #pragma unroll
-            for (int ps = 0; ps < NP; ++ps)
+            for (int i = 0; i < 4; ++i) {
+                bool odd = false;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int ps = 0; ps < NP; ++ps)
 #pragma unroll
                     for (int j = 0; j < VB / 4; ++j) {
                         uint32_t& w = rv[ps][i].w[j];
                         const bool a = (w & 0x7F80u) == 0x7F80u, b = (w & 0x7F800000u) == 0x7F800000u;
-                        odd |= (a || b) && key0 + 4 * c + i < S.len;
+                        odd |= a || b;
                         w &= (a ? 0u : 0xFFFFu) | (b ? 0u : 0xFFFF0000u);
                     }
-            if (odd) s_odd = 1;
+                if (odd && key0 + 4 * c + i < S.len) attn_bad_key(s_bad, key0 + 4 * c + i);
+            }
         }
         if (quant)
 #pragma unroll
@@ -334,28 +335,30 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
         }
         return y;
     };
-    auto store = [&](int r, int d, float4 y, float top, float sum, bool odd) {
+    int bad0 = 0, bad1 = 0;
+    auto store = [&](int r, int d, float4 y, float top, float sum) {
         const int i = r / P.group, hq = (int)head * P.group + (r - i * P.group);
         int a, b;
         if (!attn_bounds(P, S, seq, i, a, b)) return;
         const bool some = a < b;
         const float inv = 1.0f / sum;                                        // (all scores -infinity: 0 / 0)
         y = some ? make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (odd && some && !quant) {
-            y.x += attn_not_finite<KT>(P, seq, head, a, b, d); y.y += attn_not_finite<KT>(P, seq, head, a, b, d + 1);
-            y.z += attn_not_finite<KT>(P, seq, head, a, b, d + 2); y.w += attn_not_finite<KT>(P, seq, head, a, b, d + 3);
+        if (!quant && some) {
+            a = max(a, bad0); b = min(b, bad1);
+            if (a < b) attn_add4(y, attn_not_finite<KT>(P, seq, head, a, b, d));
         }
         attn_store4<OC_DTYPE_BF16>(P, attn_out_at(P, S, seq, i, hq) + d, y);
         if (P.lse && d == 0) P.lse[(S.row0 + i) * P.q_heads + hq] = some ? top * P.scale + logf(sum) : -INFINITY;
     };
     const int used = min(rows, ROWS);
     if (P.split == 1) {
+        bad0 = s_bad[0]; bad1 = s_bad[1];
         for (int it = threadIdx.x; it < used * vecs; it += AF_WARPS * 32) {
             const int r = it / vecs, d = 4 * (it - r * vecs);
             float top, sum;
             const float4 y = join(AF_WARPS, [&](int w, int e) { return stats[(w * ROWS + r) * 2 + e]; },
                                   [&](int w) { return *(const float4*)(af_smem + (w * ROWS + r) * OS + d); }, top, sum);
-            store(r, d, y, top, sum, s_odd != 0);
+            store(r, d, y, top, sum);
         }
         return;
     }
@@ -369,19 +372,14 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
         if (d == 0) { s_join[r][0] = top; s_join[r][1] = sum; }
     }
     cluster_sync();
-    int odd = 0;
-    for (int k2 = 0; k2 < P.split; ++k2) {
-        int w;
-        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(w) : "r"(cluster_map(smem_u32(&s_odd), (uint32_t)k2)) : "memory");
-        odd |= w;
-    }
+    cluster_bad(s_bad, P.split, bad0, bad1);
     const uint32_t part_at = smem_u32(af_smem), join_at = smem_u32(&s_join[0][0]);
     for (int it = (int)rank * AF_WARPS * 32 + threadIdx.x; it < used * vecs; it += P.split * AF_WARPS * 32) {
         const int r = it / vecs, d = 4 * (it - r * vecs);
         float top, sum;
         const float4 y = join(P.split, [&](int w, int e) { return cluster_ld(cluster_map(join_at, (uint32_t)w) + 8u * r + 4u * e); },
                               [&](int w) { return cluster_ld4(cluster_map(part_at, (uint32_t)w) + (uint32_t)(r * OS + d) * 4u); }, top, sum);
-        store(r, d, y, top, sum, odd != 0);
+        store(r, d, y, top, sum);
     }
     cluster_sync();                                                          // nobody reads a retired CTA's memory
 }

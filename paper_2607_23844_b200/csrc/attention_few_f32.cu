@@ -27,7 +27,7 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
     __shared__ __align__(16) float s_q[ROWS][DP];
     __shared__ float s_part[AG_WARPS][ROWS][DP];
     __shared__ float s_stat[AG_WARPS][ROWS][2], s_join[ROWS][2];
-    __shared__ int s_lo[ROWS], s_hi[ROWS], s_odd;
+    __shared__ int s_lo[ROWS], s_hi[ROWS], s_bad[2];                         // (s_bad: keys with values that are no numbers)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = P.pages.D;
     pdl_enter();
     const uint32_t rank = P.split > 1 ? cluster_rank() : 0u;
@@ -41,7 +41,7 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
         const bool there = (int)threadIdx.x < rows && attn_bounds(P, S, seq, (int)threadIdx.x / P.group, a, b);
         s_lo[threadIdx.x] = there ? a : -1; s_hi[threadIdx.x] = there ? max(a, b) : -1;
     }
-    if (threadIdx.x == 0) s_odd = 0;
+    if (threadIdx.x == 0) attn_bad_none(s_bad);
     for (int i = threadIdx.x; i < ROWS * DP; i += AG_WARPS * 32) {
         const int r = i / DP, d = i % DP, row = r / P.group;
         s_q[r][d] = r < rows && d < D ? ((const float*)P.q)[attn_q_at(P, S, seq, row, (int)head * P.group + (r - row * P.group)) + d] : 0.0f;
@@ -124,7 +124,6 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
             l[r] += e;
             p[r] = quant ? (hidden ? 0.0f : e * vs) : e;
         }
-        bool odd = false;
 #pragma unroll 8
         for (int j = 0; j < AG_STEP; ++j) {
             const int v = __shfl_sync(0xFFFFFFFFu, vec, j);
@@ -152,7 +151,7 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
             }
             if (!quant && cut) {                                             // 0 * NaN would reach rows that do not see it
 #pragma unroll
-                for (int c = 0; c < CPL; ++c) if (!isfinite(x[c])) { x[c] = 0.0f; odd = true; }
+                for (int c = 0; c < CPL; ++c) if (!isfinite(x[c])) { x[c] = 0.0f; attn_bad_key(s_bad, k * AG_STEP + j); }
             }
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
@@ -161,7 +160,6 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
                 for (int c = 0; c < CPL; ++c) o[r][c] = fmaf(w, x[c], o[r][c]);
             }
         }
-        if (odd) s_odd = 1;
         vec = next;
     }
     // ---- the warps' results side by side, then those of the cluster's CTAs ----
@@ -175,14 +173,20 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
     }
     __syncthreads();
     const int used = min(rows, ROWS);
-    auto finish = [&](int r, int d, float y, float top, float sum, bool odd) {
+    int bad0 = 0, bad1 = 0;
+    auto finish = [&](int r, int d, float y, float top, float sum) {
         const int i = r / P.group, hq = (int)head * P.group + (r - i * P.group), a = s_lo[r], b = s_hi[r];
         if (a < 0) return;
         y = a < b ? y / sum : 0.0f;                                          // (all scores -infinity: 0 / 0)
-        if (odd && a < b) y += attn_not_finite<KT>(P, seq, head, a, b, d);
+        const int bad_a = max(a, bad0), bad_b = min(b, bad1);
+        if (bad_a < bad_b) {
+            const float4 t = attn_not_finite<KT>(P, seq, head, bad_a, bad_b, d & ~3);
+            y += (d & 3) == 0 ? t.x : (d & 3) == 1 ? t.y : (d & 3) == 2 ? t.z : t.w;
+        }
         ((float*)P.out)[attn_out_at(P, S, seq, i, hq) + d] = y;
         if (P.lse && d == 0) P.lse[(S.row0 + i) * P.q_heads + hq] = a < b ? top * P.scale + logf(sum) : -INFINITY;
     };
+    if (P.split == 1) { bad0 = s_bad[0]; bad1 = s_bad[1]; }
     for (int it = threadIdx.x; it < used * D; it += AG_WARPS * 32) {
         const int r = it / D, d = it - r * D;
         float top = -INFINITY, sum = 0.0f, y = 0.0f;
@@ -192,18 +196,13 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
             sum = fmaf(f, s_stat[w][r][1], sum);
             if (mw != -INFINITY) y = fmaf(f, s_part[w][r][d], y);
         }
-        if (P.split == 1) { finish(r, d, y, top, sum, s_odd != 0); continue; }
+        if (P.split == 1) { finish(r, d, y, top, sum); continue; }
         s_part[0][r][d] = y;                                                 // (read by this thread alone)
         if (d == 0) { s_join[r][0] = top; s_join[r][1] = sum; }
     }
     if (P.split == 1) return;
     cluster_sync();
-    int odd = 0;
-    for (int w = 0; w < P.split; ++w) {
-        int x;
-        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(x) : "r"(cluster_map(smem_u32(&s_odd), (uint32_t)w)) : "memory");
-        odd |= x;
-    }
+    cluster_bad(s_bad, P.split, bad0, bad1);
     const uint32_t part_at = smem_u32(&s_part[0][0][0]), join_at = smem_u32(&s_join[0][0]);
     for (int it = (int)rank * AG_WARPS * 32 + threadIdx.x; it < used * D; it += P.split * AG_WARPS * 32) {
         const int r = it / D, d = it - r * D;
@@ -216,7 +215,7 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
             sum = fmaf(f, cluster_ld(st + 4u), sum);
             if (mw != -INFINITY) y = fmaf(f, cluster_ld(cluster_map(part_at, (uint32_t)w) + (uint32_t)(r * DP + d) * 4u), y);
         }
-        finish(r, d, y, top, sum, odd != 0);
+        finish(r, d, y, top, sum);
     }
     cluster_sync();                                                          // nobody reads a retired CTA's memory
 }

@@ -191,7 +191,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     __shared__ float s_stats[NT * AT_ROWS][2], s_share[NT * AT_ROWS];             // maxima and sums; weights of the cluster's parts
     __shared__ __align__(16) float s_ones[A::quant ? AT_KEYS : 4];
     __shared__ unsigned char s_there[NT * AT_ROWS];
-    __shared__ int s_odd;                                                        // whether a value was no number
+    __shared__ int s_bad[2];                                                     // keys with values that are no numbers
     const uint32_t smem = smem_u32(at_smem);
     uint64_t* bars = (uint64_t*)(at_smem + A::rest_at);
     const uint32_t bar0 = smem_u32(bars);
@@ -216,7 +216,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         for (int i = 0; i < A::places; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); mbar_init(p_done + 8 * i, 1); }
         mbar_init(drain, 1); mbar_init(drain + 8, 1); mbar_init(q_ready, A::softmax_warps);
         *abort_flag = 0;
-        s_odd = 0;
+        attn_bad_none(s_bad);
         for (int t = 0; t < NT; ++t) { s_range[t][0] = 0x7FFFFFFF; s_range[t][1] = 0; s_range[t][2] = 0; s_range[t][3] = 0x7FFFFFFF; }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -455,22 +455,23 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 const int key0 = j * AT_KEYS;
                 if (key0 < cut_lo || key0 + AT_KEYS > cut_hi) {
                     const uint32_t base = smem + A::v_at + (uint32_t)(st * A::tile_bytes);
-                    bool odd = false;
+                    int bad_first = 0x7FFFFFFF, bad_last = -1;
                     for (int i = h * 32 + lane; i < SUB * 1024; i += 32 * A::helpers) {          // pieces of 16 bytes
                         const uint32_t at = base + (uint32_t)(i * 16);
-                        const bool there = key0 + ((i >> 3) & 127) < S.len;
+                        const int key = key0 + ((i >> 3) & 127);
+                        const bool there = key < S.len;
                         uint32_t w[4];
                         asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
                         bool change = !there;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const bool a = (w[e] & 0x7F80u) == 0x7F80u, b = (w[e] & 0x7F800000u) == 0x7F800000u;
-                            if (there && (a || b)) { odd = change = true; }
+                            if (there && (a || b)) { change = true; bad_first = min(bad_first, key); bad_last = max(bad_last, key); }
                             w[e] = there ? w[e] & ((a ? 0u : 0xFFFFu) | (b ? 0u : 0xFFFF0000u)) : 0u;
                         }
                         if (change) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
                     }
-                    if (odd) s_odd = 1;
+                    if (bad_last >= 0) { attn_bad_key(s_bad, bad_first); attn_bad_key(s_bad, bad_last); }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 __syncwarp();
@@ -526,7 +527,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                     if (j * AT_KEYS < cut_lo || (j + 1) * AT_KEYS > cut_hi) {    // scales of values that are no numbers: as in bf16
 #pragma unroll
                         for (int k = 0; k < AT_KEYS; k += 32)
-                            if (!isfinite(v[k + lane])) { v[k + lane] = 0.0f; if (j * AT_KEYS + k + lane < S.len) s_odd = 1; }
+                            if (!isfinite(v[k + lane])) { v[k + lane] = 0.0f; if (j * AT_KEYS + k + lane < S.len) attn_bad_key(s_bad, j * AT_KEYS + k + lane); }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); // (written again by copies)
                     __syncwarp();
@@ -748,8 +749,6 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                     float y[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] = some ? __uint_as_float(o[i + e]) * inv : 0.0f;
-                    if (s_odd && some)
-                        for (int e = 0; e < 8; ++e) y[e] += attn_not_finite<KT>(P, T.seq, T.head, max(lo, 0), hi, d + i + e);
                     const uint4 v = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
                     uint16_t* out = (uint16_t*)P.out + at + d + i;
                     if (P.wide_out) st_v4(out, v);
@@ -759,6 +758,22 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                         for (int e = 0; e < 4; ++e) { out[2 * e] = (uint16_t)x[e]; out[2 * e + 1] = (uint16_t)(x[e] >> 16); }
                     }
                 }
+            }
+            // What is no number between the keys of the row: its lanes' columns side by side, one row after the other.
+            const int bad_a = max(lo, s_bad[0]), bad_b = min(hi, s_bad[1]);
+            __syncwarp();
+            for (unsigned left = __ballot_sync(0xFFFFFFFFu, exists && ok && bad_a < bad_b); left; left &= left - 1u) {
+                const int r = __ffs(left) - 1, a = __shfl_sync(0xFFFFFFFFu, bad_a, r), b = __shfl_sync(0xFFFFFFFFu, bad_b, r);
+                const long long to = __shfl_sync(0xFFFFFFFFu, at, r) + 4 * lane;
+                if (4 * lane >= D) continue;
+                const float4 t = attn_not_finite<KT>(P, T.seq, T.head, a, b, 4 * lane);
+                const float x[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (x[e] != 0.0f) {
+                        uint16_t* o = (uint16_t*)P.out + to + e;
+                        *o = (uint16_t)pack_bf16x2(__uint_as_float((uint32_t)*o << 16) + x[e], 0.0f);
+                    }
             }
             if (P.lse && exists && ok) P.lse[(S.row0 + qi) * P.q_heads + head] = some ? m * (A::quant ? 0.69314718f : P.scale) + logf(l) : -INFINITY;
         } else {
@@ -780,12 +795,8 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     if (P.split > 1) {
         cluster_sync();
         if (warp < A::softmax_warps && !*abort_flag) {
-            int odd = 0;
-            for (int k = 0; k < P.split; ++k) {
-                int w;
-                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(w) : "r"(cluster_map(smem_u32(&s_odd), (uint32_t)k)) : "memory");
-                odd |= w;
-            }
+            int bad0, bad1;
+            cluster_bad(s_bad, P.split, bad0, bad1);
             // Every split-th row: first the weights of its parts (a thread for each row), then the elements side by side.
             const int vecs = D / 4, mine = (NT * AT_ROWS) / P.split;
             const uint32_t stats = smem_u32(&s_stats[0][0]);
@@ -824,11 +835,11 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                         y.x = fmaf(f0, o0.x, fmaf(f1, o1.x, y.x)); y.y = fmaf(f0, o0.y, fmaf(f1, o1.y, y.y));
                         y.z = fmaf(f0, o0.z, fmaf(f1, o1.z, y.z)); y.w = fmaf(f0, o0.w, fmaf(f1, o1.w, y.w));
                     }
-                    if (odd) {
+                    if (bad0 < bad1) {
                         int a, b;
                         attn_bounds(P, S, T.seq, q2, a, b);
-                        y.x += attn_not_finite<KT>(P, T.seq, T.head, a, b, d); y.y += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 1);
-                        y.z += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 2); y.w += attn_not_finite<KT>(P, T.seq, T.head, a, b, d + 3);
+                        a = max(a, bad0); b = min(b, bad1);
+                        if (a < b) attn_add4(y, attn_not_finite<KT>(P, T.seq, T.head, a, b, d));
                     }
                 }
                 attn_store4<OC_DTYPE_BF16>(P, attn_out_at(P, S, T.seq, q2, head) + d, y);

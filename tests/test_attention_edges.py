@@ -3,7 +3,7 @@ a sequence's keys.  Restatement and bounds are those of test_attention."""
 import pytest
 import torch
 
-from test_attention import BF16, F32, NAN, TYPES, Cache, check_put, ctx, host, oc, rand, run, tag  # noqa: F401 (fixtures)
+from test_attention import BF16, F32, NAN, TYPES, Cache, check_put, ctx, exact, host, oc, rand, seen_by, tag  # noqa: F401 (fixtures)
 
 
 def poison(cache, m, tokens, what, column=7):
@@ -111,3 +111,78 @@ def test_sizes_of_a_cache_without_a_table(oc):
         with pytest.raises(oc.OmniCacheError):
             oc.kv_bytes(bad)
     assert oc.kv_bytes(oc.CKv(oc.DTYPE_BF16, 2, 64, 1, 100, 16, 3, 0)) == (3 * 2 * 16 * 128, 0)      # one sequence, pages shared by a table
+
+
+def check_no_numbers(oc, ctx, cache, q, pos, bad, unit=0, back=-1, ahead=-1, scale=None):
+    """Rows at `pos` over values of which some are no numbers: bad = [(key, column, what)], with whole numbers what is the key's scale.
+    A column of a row is the sum of those that it sees, whatever their probabilities, and as if they were zeros where it sees none."""
+    n, H, D = q.shape
+    held = {m: (cache.pool[m].clone(), None if cache.scale[m] is None else cache.scale[m].clone()) for m in "kv"}
+    vals = cache.val["v"].clone()
+    strange = torch.zeros(n, H, D, dtype=torch.float64)
+    group = H // cache.heads
+    for key, column, what in bad:
+        poison(cache, "v", [key], what, column)
+        sees = torch.tensor([bool(seen_by(p, cache.lens[0], unit, back, ahead)[key]) for p in pos])
+        if cache.scale["v"] is None:
+            strange[sees, :, column] += what
+            cache.val["v"][0, key, :, column] = 0
+        else:
+            strange[sees] += (cache.tokens("v")[0][0, key].double() * what).repeat_interleave(group, 0)
+            cache.val["v"][0, key] = 0
+    want, bound, _, _ = exact(cache, q, [(0, p) for p in pos], D ** -0.5 if scale is None else scale, unit, back, ahead)
+    idx = torch.tensor(pos)
+    got = with_lse(oc, ctx, cache, q, idx=idx, unit=unit, back=back, ahead=ahead, **({} if scale is None else dict(scale=scale)))[0].double()
+    bound = bound + (2.0 ** -8 if q.dtype == BF16 else 2.0 ** -23) * want.abs() + 1e-30
+    plain = strange == 0
+    assert ((got - want).abs() <= bound)[plain].all()
+    assert torch.equal(got[~plain].nan_to_num(nan=7.0), strange[~plain].nan_to_num(nan=7.0))
+    cache.val["v"] = vals
+    for m in "kv":
+        cache.pool[m], cache.scale[m] = held[m]
+
+
+INF = float("inf")
+BAD = [[(100, 3, INF)], [(1, 0, NAN), (1400, 71, -INF)], [(700, 5, INF), (710, 5, -INF), (711, 6, INF), (1200, 5, INF)], [(j, j % 72, NAN) for j in range(640, 900)]]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("rows", [1, 5, 140])
+@pytest.mark.parametrize("bad", BAD)
+def test_values_that_are_no_numbers_in_several_places(oc, ctx, dtype, kind, rows, bad):
+    cache = Cache(oc, kind, 1, 72, 1, 1500, 16, seed=42)
+    q = rand(torch.Generator().manual_seed(rows), rows, 2, 72, dtype=dtype)
+    for first in (0, 700 - rows, 705, 1500 - rows):
+        check_no_numbers(oc, ctx, cache, q, list(range(first, first + rows)), bad, unit=1, ahead=0)
+    check_no_numbers(oc, ctx, cache, q, list(range(640, 640 + rows)), bad, unit=50, back=1, ahead=2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("rows", [1, 2000])
+def test_values_that_no_row_sees_take_no_time(oc, ctx, dtype, kind, rows):
+    """Unwritten pages of NaN behind a causal window: within a factor of 4 of what it takes over numbers."""
+    desc = oc.kv_desc(tag(oc, kind), 8, 72, 2, 4096, 64)
+    (kp, ks), (vp, vs) = oc.kv_pools(desc), oc.kv_pools(desc)
+    x, q = torch.randn(8192, 8, 72, device="cuda", dtype=dtype), torch.randn(2 * rows, 8, 72, device="cuda", dtype=dtype)
+    ctx.kv_put(desc, oc.kv_rows(desc, 8192, tag(oc, dtype), k=x, v=x), x, kp, x, vp, k_scale=ks, v_scale=vs)
+    idx = (torch.arange(2000 - rows, 2000)[None] + 4096 * torch.arange(2)[:, None]).flatten().int().cuda()
+    out = torch.empty_like(q)
+    d = oc.attention_desc(desc, 2 * rows, tag(oc, dtype), 8, 72 ** -0.5, rows_per_batch=rows, unit=1, ahead=0, q=q, out=out)
+
+    def time():
+        spans = []
+        for _ in range(6):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            ctx.attention(desc, d, q, kp, vp, out, k_scale=ks, v_scale=vs, idx=idx)
+            b.record()
+            torch.cuda.synchronize()
+            spans.append(a.elapsed_time(b))
+        return min(spans)
+    plain, want = time(), out.clone()
+    for pool, scale in ((kp, ks), (vp, vs)):
+        store = (pool if scale is None else scale).view(2, 64, 8, 64, -1)
+        store[:, 31, :, 16:], store[:, 32:] = NAN, NAN                                   # tokens from 2000 on
+    assert time() <= 4 * plain and torch.equal(out, want)

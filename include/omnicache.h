@@ -636,8 +636,8 @@ oc_status oc_kv_get(oc_ctx* ctx, const oc_kv_desc* cache, const oc_kv_rows* rows
  * frames see themselves and earlier ones, back = ahead = 0 keeps each frame to itself.
  * A row that sees no key becomes zeros, with lse = -infinity.  lse (nullable, fp32 [n_rows][q_heads]):
  * log of the sum over visible keys of exp(scale * q . K).  Keys and values that a row does not see have
- * no influence on it, whatever they hold; of a visible infinity in V the row gets that infinity (NaN
- * where both signs meet, or where its probability is 0 in fp32), of a NaN in K or V a NaN.
+ * no influence on it, whatever they hold; of a visible infinity in V the row gets that infinity,
+ * however small its probability (NaN where both signs meet), of a NaN in K or V a NaN.
  * q and out are fp32 over a cache in fp32, 8 or 4 bits, or bf16 over one in bf16, 8 or 4 bits.  bf16:
  * products of bf16 with fp32 sums; probabilities, times the value's scale in the 8- and 4-bit caches,
  * are rounded to bf16 before they meet V; everything else is fp32.  fp32: all of it in fp32.

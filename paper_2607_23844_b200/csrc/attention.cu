@@ -52,7 +52,7 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
     __shared__ int range[2];                                                 // first and last key that the tile sees
     __shared__ int bounds[TR][2];                                            // of each row; lo = -1: the row is left as it is
     __shared__ float stats[TR][2];
-    __shared__ int bad[2];                                                   // keys with values that are no numbers
+    __shared__ int bad[ATT_BAD];                                                   // keys with values that are no numbers
     float *sq = as_smem + M::q, *skv = as_smem + M::kv, *sp = as_smem + M::p;
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, D = P.pages.D;
     pdl_enter();
@@ -131,7 +131,7 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
             const int i = tid + it * AS_THREADS, j = i / (DP / 8), u = i % (DP / 8);
             f32x2* f = ahead[it];
             if (value && max_bits<8>(f, 0u) >= 0x7F800000u) {
-                attn_bad_key(bad, key0 + j);
+                attn_bad_key(P, bad, key0 + j);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float a = f2_lo(f[e]), b = f2_hi(f[e]);
@@ -222,7 +222,7 @@ attention_simt_kernel(const __grid_constant__ AttnParams P) {
         const int d = 64 * c + 4 * tx;
         if (d < D) {
             const int bad_a = max(a, bad0), bad_b = min(b, bad1);
-            if (bad_a < bad_b) attn_add4(y, attn_not_finite<KT>(P, T.seq, T.head, bad_a, bad_b, d));
+            if (bad_a < bad_b) attn_add4(y, attn_not_finite<KT>(P, bad, T.seq, T.head, bad_a, bad_b, d));
             attn_store4<OC_DTYPE_F32>(P, attn_out_at(P, S, T.seq, row, head) + d, y);
         }
         if (P.lse && d == 0) P.lse[(S.row0 + row) * P.q_heads + head] = a < b ? most * P.scale + logf(sum) : -INFINITY;
@@ -321,6 +321,8 @@ oc_status launch_attention(oc_ctx* ctx, const oc_kv_desc& cache, const oc_attent
     P.unit = std::min<int64_t>(d.unit, 0x7FFFFFFF); P.back = std::min<int64_t>(d.back, 0x7FFFFFFF); P.ahead = std::min<int64_t>(d.ahead, 0x7FFFFFFF);
     P.scale = d.scale; P.scale_log2 = d.scale * 1.44269504f;
     P.long_first = q_start || d.unit > 0;
+    P.part_shift = 7;
+    while ((P.pages.seq_rows - 1) >> P.part_shift >= 128) ++P.part_shift;
     const uint64_t eb = d.dtype == OC_DTYPE_F32 ? 4 : 2;
     P.wide_q = ((uintptr_t)q | ((q_start ? 0u : (uint64_t)P.q_batch) | (uint64_t)P.q_row | (uint64_t)P.q_head) * eb) % 16 == 0;
     P.wide_out = ((uintptr_t)out | ((q_start ? 0u : (uint64_t)P.o_batch) | (uint64_t)P.o_row | (uint64_t)P.o_head) * eb) % 16 == 0;

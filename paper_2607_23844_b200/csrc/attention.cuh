@@ -22,6 +22,7 @@ struct AttnParams {
     int split;                                   // CTAs of a cluster
     bool wide_q, wide_out;                       // 16 bytes at a time
     bool long_first;                             // order of the tiles (attn_tile)
+    int part_shift;                              // log2 of the keys of a 128th of a sequence, 7 or more
 };
 
 #ifdef __CUDACC__
@@ -92,10 +93,22 @@ __device__ __forceinline__ long long attn_out_at(const AttnParams& P, const Attn
     return (P.q_start ? (s.row0 + i) * P.o_row : (long long)seq * P.o_batch + (long long)i * P.o_row) + (long long)head * P.o_head;
 }
 
+__device__ __forceinline__ uint32_t attn_fma2(uint32_t a, uint32_t b, uint32_t c) { uint32_t r; asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c)); return r; }
 // Values that are no numbers are taken as zeros by the kernels, so that they stay away from rows that do not see them, and added
-// at the end to those that do.  A CTA keeps the first and the last key that holds one: rows look at the keys between only.
-__device__ __forceinline__ void attn_bad_none(int* bad) { bad[0] = 0x7FFFFFFF; bad[1] = 0; }
-__device__ __forceinline__ void attn_bad_key(int* bad, int key) { atomicMin(&bad[0], key); atomicMax(&bad[1], key + 1); }
+// at the end to those that do.  A CTA keeps the first and the last key that holds one, and of 128 parts of the sequence (of 128 keys
+// and more) whether they hold any: rows look at those only.
+static constexpr int ATT_BAD = 2 + 4;
+// (of pairs of bf16: 0 times what is no number is NaN, and stays it in a sum that begins with zeros)
+__device__ __forceinline__ uint32_t attn_zero2(uint32_t sum, uint32_t w) { return attn_fma2(w, 0u, sum); }
+__device__ __forceinline__ bool attn_bad2(uint32_t sum) { return (sum & 0x7FFF7FFFu) != 0u; }
+__device__ __forceinline__ void attn_bad_none(int* bad) {
+    bad[0] = 0x7FFFFFFF;
+    for (int i = 1; i < ATT_BAD; ++i) bad[i] = 0;
+}
+__device__ __forceinline__ void attn_bad_key(const AttnParams& P, int* bad, int key) {
+    atomicMin(&bad[0], key); atomicMax(&bad[1], key + 1);
+    atomicOr(&bad[2 + (key >> P.part_shift >> 5)], 1 << (key >> P.part_shift & 31));
+}
 // Elements d .. d + 3 of vector v of the values, as bits of floats
 template <int KT>
 __device__ __forceinline__ void attn_value4(const AttnParams& P, uint32_t v, int d, uint32_t* x) {
@@ -117,9 +130,14 @@ __device__ __forceinline__ void attn_value4(const AttnParams& P, uint32_t v, int
 // The sums of what is no number in columns d .. d + 3 of the keys [lo, hi): 0 where there is nothing of the kind.
 // (Sums of NaN stay what they are: the rest is not looked at.)
 template <int KT>
-__device__ __forceinline__ float4 attn_not_finite(const AttnParams& P, uint32_t seq, uint32_t head, int lo, int hi, int d) {
+__device__ __forceinline__ float4 attn_not_finite(const AttnParams& P, const int* bad, uint32_t seq, uint32_t head, int lo, int hi, int d) {
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int j = lo; j < hi;) {
+        const int part = j >> P.part_shift;
+        if (!(bad[2 + (part >> 5)] >> (part & 31) & 1)) {
+            j = (int)min((long long)hi, (long long)(part + 1) << P.part_shift);
+            continue;
+        }
         const int end = min(hi, (j & ~15) + 16);                             // (pages have a multiple of 16 rows)
         const uint32_t pn = P.pages.page_rows.div((uint32_t)j);
         const int page = kv_page(P.pages, seq, pn);
@@ -144,7 +162,6 @@ __device__ __forceinline__ void attn_add4(float4& y, const float4& t) { y.x += t
 //   pipe, which the product's conversions leave idle; masks and subtractions that tell the cases apart take four on the integer
 //   pipe, which has half its rate (single tokens over 8-bit caches: 185 us with those).
 //   4 bits: u = x + 8 in the low bits of 0x4300 reads as 136 + x.
-__device__ __forceinline__ uint32_t attn_fma2(uint32_t a, uint32_t b, uint32_t c) { uint32_t r; asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c)); return r; }
 __device__ __forceinline__ uint32_t attn_i8_pair(uint32_t v) {                // 0x43uu 0x43uu
     uint32_t d = attn_fma2(v, 0x3F803F80u, 0xC380C380u), r;
     asm("fma.rn.relu.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(0x3F803F80u), "r"(0xC380C380u));
@@ -171,8 +188,8 @@ __device__ __forceinline__ float4 cluster_ld4(uint32_t addr) {
     return v;
 }
 
-// The first and last of such keys of a cluster's CTAs
-__device__ __forceinline__ void cluster_bad(const int* bad, int ctas, int& first, int& end) {
+// The first and last of such keys of a cluster's CTAs; their parts join this CTA's
+__device__ __forceinline__ void cluster_bad(int* bad, int ctas, int& first, int& end) {
     first = 0x7FFFFFFF; end = 0;
     for (int k = 0; k < ctas; ++k) {
         const uint32_t at = cluster_map(smem_u32(bad), (uint32_t)k);
@@ -181,6 +198,13 @@ __device__ __forceinline__ void cluster_bad(const int* bad, int ctas, int& first
         asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(b) : "r"(at + 4u) : "memory");
         first = min(first, a); end = max(end, b);
     }
+    if (first >= end) return;
+    for (int k = 0; k < ctas; ++k)
+        for (int i = 2; i < ATT_BAD; ++i) {
+            int w;
+            asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(w) : "r"(cluster_map(smem_u32(bad + i), (uint32_t)k)) : "memory");
+            atomicOr(&bad[i], w);
+        }
 }
 
 // Four neighbouring elements of a row's result

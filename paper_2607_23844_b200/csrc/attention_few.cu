@@ -72,7 +72,7 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
     constexpr int KB = KT == OC_DTYPE_BF16 ? 2 * E : KT == OC_DTYPE_I8 ? E : E / 2, VB = KT == OC_DTYPE_BF16 ? 2 * EV : KT == OC_DTYPE_I8 ? EV : EV / 2;
     constexpr int STEPS = NC * E / 4, DP = NP * 8 * EV, RT = ROWS / 8, OT = NP * EV / 2;       // products of scores; columns; tiles of rows, of outputs
     extern __shared__ __align__(16) float af_smem[];                         // [warps][rows][DP + 4] outputs, then [warps][rows][2] maxima and sums
-    __shared__ int s_bad[2];                                                 // keys with values that are no numbers
+    __shared__ int s_bad[ATT_BAD];                                                 // keys with values that are no numbers
     __shared__ float s_join[AF_ROWS][2];
     constexpr int OS = DP + 4;
     float* stats = af_smem + AF_WARPS * ROWS * OS;
@@ -227,7 +227,6 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
         vec = find(k + 2 * AF_WARPS);
         const int key0 = k * AF_STEP;
         const bool cut = key0 < low || key0 + AF_STEP > high;
-        uint32_t hidden = 0;
         bool grow = false;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -235,7 +234,7 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int key = key0 + key_n + 2 * (i >> 1);
-                    if (key < lo[rt][i & 1] || key >= hi[rt][i & 1]) { x[rt][i] = -INFINITY; hidden |= 1u << (4 * rt + i); }
+                    if (key < lo[rt][i & 1] || key >= hi[rt][i & 1]) x[rt][i] = -INFINITY;
                 }
             }
 #pragma unroll
@@ -262,6 +261,38 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
                     m[rt][e] = top;
                 }
         }
+        // values that are no numbers: 0 * NaN would reach rows that do not see them
+        if (quant) {
+            if (!(fabsf(vs[0]) + fabsf(vs[1]) < INFINITY))                   // (seldom)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (!isfinite(vs[i])) { vs[i] = 0.0f; if (key0 + key_n + 2 * i < S.len) attn_bad_key(P, s_bad, key0 + key_n + 2 * i); }
+        } else {
+            uint32_t zero = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int ps = 0; ps < NP; ++ps)
+#pragma unroll
+                    for (int j = 0; j < VB / 4; ++j) zero = attn_zero2(zero, rv[ps][i].w[j]);
+            if (attn_bad2(zero)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    bool odd = false;
+#pragma unroll
+                    for (int ps = 0; ps < NP; ++ps)
+#pragma unroll
+                        for (int j = 0; j < VB / 4; ++j) {
+                            uint32_t& w = rv[ps][i].w[j];
+                            const bool a = (w & 0x7F80u) == 0x7F80u, b = (w & 0x7F800000u) == 0x7F800000u;
+                            odd |= a || b;
+                            w &= (a ? 0u : 0xFFFFu) | (b ? 0u : 0xFFFF0000u);
+                        }
+                    if (odd && key0 + 4 * c + i < S.len) attn_bad_key(P, s_bad, key0 + 4 * c + i);
+                }
+            }
+            __syncwarp();
+        }
         uint32_t p[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -271,25 +302,9 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
                 const float mm = m[rt][i & 1];
                 e[i] = af_exp2(fmaf(x[rt][i], cc, mm == -INFINITY ? 0.0f : -mm * cc));
                 l[rt][i & 1] += e[i];
-                if (quant) e[i] = hidden >> (4 * rt + i) & 1 ? 0.0f : e[i] * vs[i >> 1];        // (0 times a scale that is no number)
+                if (quant) e[i] *= vs[i >> 1];
             }
             p[rt][0] = af_transpose(pack_bf16x2(e[0], e[1])); p[rt][1] = af_transpose(pack_bf16x2(e[2], e[3]));
-        }
-        if (!quant && cut) {                                                 // 0 * NaN would reach rows that do not see it
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                bool odd = false;
-#pragma unroll
-                for (int ps = 0; ps < NP; ++ps)
-#pragma unroll
-                    for (int j = 0; j < VB / 4; ++j) {
-                        uint32_t& w = rv[ps][i].w[j];
-                        const bool a = (w & 0x7F80u) == 0x7F80u, b = (w & 0x7F800000u) == 0x7F800000u;
-                        odd |= a || b;
-                        w &= (a ? 0u : 0xFFFFu) | (b ? 0u : 0xFFFF0000u);
-                    }
-                if (odd && key0 + 4 * c + i < S.len) attn_bad_key(s_bad, key0 + 4 * c + i);
-            }
         }
         if (quant)
 #pragma unroll
@@ -343,9 +358,9 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
         const bool some = a < b;
         const float inv = 1.0f / sum;                                        // (all scores -infinity: 0 / 0)
         y = some ? make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (!quant && some) {
+        if (some) {
             a = max(a, bad0); b = min(b, bad1);
-            if (a < b) attn_add4(y, attn_not_finite<KT>(P, seq, head, a, b, d));
+            if (a < b) attn_add4(y, attn_not_finite<KT>(P, s_bad, seq, head, a, b, d));
         }
         attn_store4<OC_DTYPE_BF16>(P, attn_out_at(P, S, seq, i, hq) + d, y);
         if (P.lse && d == 0) P.lse[(S.row0 + i) * P.q_heads + hq] = some ? top * P.scale + logf(sum) : -INFINITY;

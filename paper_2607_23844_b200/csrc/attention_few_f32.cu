@@ -27,7 +27,7 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
     __shared__ __align__(16) float s_q[ROWS][DP];
     __shared__ float s_part[AG_WARPS][ROWS][DP];
     __shared__ float s_stat[AG_WARPS][ROWS][2], s_join[ROWS][2];
-    __shared__ int s_lo[ROWS], s_hi[ROWS], s_bad[2];                         // (s_bad: keys with values that are no numbers)
+    __shared__ int s_lo[ROWS], s_hi[ROWS], s_bad[ATT_BAD];                         // (s_bad: keys with values that are no numbers)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = P.pages.D;
     pdl_enter();
     const uint32_t rank = P.split > 1 ? cluster_rank() : 0u;
@@ -76,7 +76,9 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
         float s[ROWS];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) s[r] = 0.0f;
-        const float ks = quant && vec >= 0 ? __ldg(P.k_scale + vec) : 0.0f, vs = quant && vec >= 0 ? __ldg(P.v_scale + vec) : 0.0f;
+        const float ks = quant && vec >= 0 ? __ldg(P.k_scale + vec) : 0.0f;
+        float vs = quant && vec >= 0 ? __ldg(P.v_scale + vec) : 0.0f;
+        if (quant && !isfinite(vs)) { vs = 0.0f; attn_bad_key(P, s_bad, key); } // (0 * NaN would reach rows that do not see it)
         // (a lane without a key works on zeros)
 #pragma unroll 4
         for (int d = 0; d < D; d += E) {
@@ -106,8 +108,7 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             float x = quant ? s[r] * ks : s[r];
-            const bool hidden = cut && (key < s_lo[r] || key >= s_hi[r]);
-            if (hidden) x = -INFINITY;
+            if (cut && (key < s_lo[r] || key >= s_hi[r])) x = -INFINITY;
             float top = x;
 #pragma unroll
             for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
@@ -122,43 +123,58 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
             }
             const float e = exp2f((x - base) * P.scale_log2);
             l[r] += e;
-            p[r] = quant ? (hidden ? 0.0f : e * vs) : e;
+            p[r] = quant ? e * vs : e;
         }
-#pragma unroll 8
-        for (int j = 0; j < AG_STEP; ++j) {
-            const int v = __shfl_sync(0xFFFFFFFFu, vec, j);
-            float x[CPL];
+        constexpr int G = 4;                                                 // keys on their way together
+        for (int j0 = 0; j0 < AG_STEP; j0 += G) {
+            float x[G][CPL];
 #pragma unroll
-            for (int c = 0; c < CPL; ++c) x[c] = 0.0f;
-            if (v >= 0 && lane * CPL < D) {                                  // (columns CPL lane ..: D is a multiple of 8)
-                const long long at = (long long)v * D + lane * CPL;
-                if (KT == OC_DTYPE_F32) {
-                    if constexpr (CPL == 4) { const float4 y = __ldg((const float4*)((const float*)P.v_pool + at)); x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w; }
-                    else { const float2 y = __ldg((const float2*)((const float*)P.v_pool + at)); x[0] = y.x; x[1] = y.y; }
-                } else if (KT == OC_DTYPE_I8) {
-                    uint32_t w;
-                    if constexpr (CPL == 4) w = __ldg((const uint32_t*)((const uint8_t*)P.v_pool + at));
-                    else w = __ldg((const uint16_t*)((const uint8_t*)P.v_pool + at));
+            for (int g = 0; g < G; ++g) {
+                const int v = __shfl_sync(0xFFFFFFFFu, vec, j0 + g);
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c) x[c] = ag_byte<KT>(w, c);
-                } else {
-                    uint32_t w;
-                    if constexpr (CPL == 4) w = __ldg((const uint16_t*)((const uint8_t*)P.v_pool + (at >> 1)));
-                    else w = __ldg((const uint8_t*)P.v_pool + (at >> 1));
+                for (int c = 0; c < CPL; ++c) x[g][c] = 0.0f;
+                if (v >= 0 && lane * CPL < D) {                              // (columns CPL lane ..: D is a multiple of 8)
+                    const long long at = (long long)v * D + lane * CPL;
+                    if (KT == OC_DTYPE_F32) {
+                        if constexpr (CPL == 4) { const float4 y = __ldg((const float4*)((const float*)P.v_pool + at)); x[g][0] = y.x; x[g][1] = y.y; x[g][2] = y.z; x[g][3] = y.w; }
+                        else { const float2 y = __ldg((const float2*)((const float*)P.v_pool + at)); x[g][0] = y.x; x[g][1] = y.y; }
+                    } else if (KT == OC_DTYPE_I8) {
+                        uint32_t w;
+                        if constexpr (CPL == 4) w = __ldg((const uint32_t*)((const uint8_t*)P.v_pool + at));
+                        else w = __ldg((const uint16_t*)((const uint8_t*)P.v_pool + at));
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c) x[c] = ag_byte<KT>(w, c);
+                        for (int c = 0; c < CPL; ++c) x[g][c] = ag_byte<KT>(w, c);
+                    } else {
+                        uint32_t w;
+                        if constexpr (CPL == 4) w = __ldg((const uint16_t*)((const uint8_t*)P.v_pool + (at >> 1)));
+                        else w = __ldg((const uint8_t*)P.v_pool + (at >> 1));
+#pragma unroll
+                        for (int c = 0; c < CPL; ++c) x[g][c] = ag_byte<KT>(w, c);
+                    }
                 }
             }
-            if (!quant && cut) {                                             // 0 * NaN would reach rows that do not see it
+            if (!quant) {                                                    // (0 times what is no number is NaN, and stays it)
+                float zero = 0.0f;
 #pragma unroll
-                for (int c = 0; c < CPL; ++c) if (!isfinite(x[c])) { x[c] = 0.0f; attn_bad_key(s_bad, k * AG_STEP + j); }
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int c = 0; c < CPL; ++c) zero = fmaf(x[g][c], 0.0f, zero);
+                if (zero != 0.0f) {
+#pragma unroll
+                    for (int g = 0; g < G; ++g)
+#pragma unroll
+                        for (int c = 0; c < CPL; ++c)
+                            if (!isfinite(x[g][c])) { x[g][c] = 0.0f; attn_bad_key(P, s_bad, k * AG_STEP + j0 + g); }
+                }
             }
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                const float w = __shfl_sync(0xFFFFFFFFu, p[r], j);
+            for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int c = 0; c < CPL; ++c) o[r][c] = fmaf(w, x[c], o[r][c]);
-            }
+                for (int r = 0; r < ROWS; ++r) {
+                    const float w = __shfl_sync(0xFFFFFFFFu, p[r], j0 + g);
+#pragma unroll
+                    for (int c = 0; c < CPL; ++c) o[r][c] = fmaf(w, x[g][c], o[r][c]);
+                }
         }
         vec = next;
     }
@@ -180,7 +196,7 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
         y = a < b ? y / sum : 0.0f;                                          // (all scores -infinity: 0 / 0)
         const int bad_a = max(a, bad0), bad_b = min(b, bad1);
         if (bad_a < bad_b) {
-            const float4 t = attn_not_finite<KT>(P, seq, head, bad_a, bad_b, d & ~3);
+            const float4 t = attn_not_finite<KT>(P, s_bad, seq, head, bad_a, bad_b, d & ~3);
             y += (d & 3) == 0 ? t.x : (d & 3) == 1 ? t.y : (d & 3) == 2 ? t.z : t.w;
         }
         ((float*)P.out)[attn_out_at(P, S, seq, i, hq) + d] = y;

@@ -7,9 +7,9 @@
 //   copy warp       keys and values of the pages: TMA boxes (bf16), bulk copies (8 and 4 bits), into rings
 //   MMA warps       tcgen05.mma, one for Q K^T from shared memory, one for P V with P in tensor memory and V as it lies (its
 //                   rows are the product's inner axis)
-//   helper warps    bf16: values of keys behind the sequence become zeros, and so do values that are no numbers where not
-//                   every row sees the tile (0 * NaN would reach the rows that do not); 8 and 4 bits: raw rows to bf16,
-//                   which holds those whole numbers exactly, so that the scales join the scores and the probabilities
+//   helper warps    bf16: values that are no numbers become zeros (0 * NaN would reach the rows that do not see them), and their
+//                   keys are kept for the rows that do; 8 and 4 bits: raw rows to bf16, which holds those whole
+//                   numbers exactly, so that the scales join the scores and the probabilities
 // Two tiles of rows take turns: while one's scores become probabilities the tensor cores work for the other.  With heads of up
 // to 64 a third place for scores in tensor memory lets the products run ahead of the softmax warps.
 // Measured (bf16): 25 x 4608 rows over 9216 keys, 5 heads of 64, 1359 GFLOP: 1.83 ms, 744 TFLOP/s; 2 x 2560 x 4096, 24 heads of 64:
@@ -187,11 +187,11 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     using A = At<NT, SUB, KT>;
     const AttnParams& P = TP.a;
     extern __shared__ __align__(1024) uint8_t at_smem[];
-    __shared__ int s_range[NT][4];                                               // of each tile: first key seen, last, highest first, lowest last
+    __shared__ int s_range[NT][2];                                               // of each tile: first key seen, last
     __shared__ float s_stats[NT * AT_ROWS][2], s_share[NT * AT_ROWS];             // maxima and sums; weights of the cluster's parts
     __shared__ __align__(16) float s_ones[A::quant ? AT_KEYS : 4];
     __shared__ unsigned char s_there[NT * AT_ROWS];
-    __shared__ int s_bad[2];                                                     // keys with values that are no numbers
+    __shared__ int s_bad[ATT_BAD];                                                     // keys with values that are no numbers
     const uint32_t smem = smem_u32(at_smem);
     uint64_t* bars = (uint64_t*)(at_smem + A::rest_at);
     const uint32_t bar0 = smem_u32(bars);
@@ -217,7 +217,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
         mbar_init(drain, 1); mbar_init(drain + 8, 1); mbar_init(q_ready, A::softmax_warps);
         *abort_flag = 0;
         attn_bad_none(s_bad);
-        for (int t = 0; t < NT; ++t) { s_range[t][0] = 0x7FFFFFFF; s_range[t][1] = 0; s_range[t][2] = 0; s_range[t][3] = 0x7FFFFFFF; }
+        for (int t = 0; t < NT; ++t) { s_range[t][0] = 0x7FFFFFFF; s_range[t][1] = 0; }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         if (!A::quant && P.pages.n_tokens > 0) { tma_prefetch_map(&TP.mapK); tma_prefetch_map(&TP.mapV); }      // (there are none for a cache of no tokens)
@@ -243,7 +243,6 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
             exists = attn_bounds(P, S, T.seq, qi, lo, hi);
             if (exists && lo < hi) {
                 atomicMin(&s_range[my_tile][0], lo); atomicMax(&s_range[my_tile][1], hi);
-                atomicMax(&s_range[my_tile][2], lo); atomicMin(&s_range[my_tile][3], hi);
             } else {
                 lo = hi = 0;
             }
@@ -445,33 +444,39 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
     } else {
         // ================================ helpers ===============================================
         const int h = warp - A::helper0;
-        int cut_lo = 0, cut_hi = 0x7FFFFFFF;                                     // tiles within are seen whole by every row
-#pragma unroll
-        for (int t = 0; t < NT; ++t) if (s_range[t][1] > 0) { cut_lo = max(cut_lo, s_range[t][2]); cut_hi = min(cut_hi, s_range[t][3]); }
         if (!A::quant) {
             for (int j = j0; j < j1; ++j) {
                 const int st = (j - j0) % A::v_stages;
                 if (!AT_WAIT(v_full + 8 * st, (uint32_t)((j - j0) / A::v_stages) & 1u)) break;
                 const int key0 = j * AT_KEYS;
-                if (key0 < cut_lo || key0 + AT_KEYS > cut_hi) {
-                    const uint32_t base = smem + A::v_at + (uint32_t)(st * A::tile_bytes);
+                const uint32_t base = smem + A::v_at + (uint32_t)(st * A::tile_bytes);
+                uint32_t zero = 0;
+#pragma unroll 8
+                for (int i = h * 32 + lane; i < SUB * 1024; i += 32 * A::helpers) {              // pieces of 16 bytes
+                    uint32_t w[4];
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(base + (uint32_t)(i * 16)) : "memory");
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) zero = attn_zero2(zero, w[e]);
+                }
+                if (__any_sync(0xFFFFFFFFu, attn_bad2(zero))) {
                     int bad_first = 0x7FFFFFFF, bad_last = -1;
-                    for (int i = h * 32 + lane; i < SUB * 1024; i += 32 * A::helpers) {          // pieces of 16 bytes
+                    for (int i = h * 32 + lane; i < SUB * 1024; i += 32 * A::helpers) {
                         const uint32_t at = base + (uint32_t)(i * 16);
                         const int key = key0 + ((i >> 3) & 127);
-                        const bool there = key < S.len;
                         uint32_t w[4];
                         asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
-                        bool change = !there;
+                        bool change = false;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const bool a = (w[e] & 0x7F80u) == 0x7F80u, b = (w[e] & 0x7F800000u) == 0x7F800000u;
-                            if (there && (a || b)) { change = true; bad_first = min(bad_first, key); bad_last = max(bad_last, key); }
-                            w[e] = there ? w[e] & ((a ? 0u : 0xFFFFu) | (b ? 0u : 0xFFFF0000u)) : 0u;
+                            change |= a || b;
+                            w[e] &= (a ? 0u : 0xFFFFu) | (b ? 0u : 0xFFFF0000u);
                         }
-                        if (change) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                        if (!change) continue;
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                        if (key < S.len) { bad_first = min(bad_first, key); bad_last = max(bad_last, key); }     // (behind the sequence lies anything)
                     }
-                    if (bad_last >= 0) { attn_bad_key(s_bad, bad_first); attn_bad_key(s_bad, bad_last); }
+                    if (bad_last >= 0) { attn_bad_key(P, s_bad, bad_first); attn_bad_key(P, s_bad, bad_last); }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 __syncwarp();
@@ -521,14 +526,15 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 if (h == 0) {
                     const int sst = i % AT_SCALES;
                     if (!AT_WAIT(sc_full + 8 * sst, (uint32_t)(i / AT_SCALES) & 1u)) break;
-                    float* v = (float*)(at_smem + A::scale_at) + (2 * sst + 1) * AT_KEYS;
+                    // the softmax scale joins the keys' (one product less for each score); values' scales that are no numbers: as in bf16
+                    float* of_k = (float*)(at_smem + A::scale_at) + 2 * sst * AT_KEYS + lane, *of_v = of_k + AT_KEYS, k4[4], v4[4];
 #pragma unroll
-                    for (int k = 0; k < AT_KEYS; k += 32) v[k + lane - AT_KEYS] *= P.scale_log2;                   // (one product less for each score)
-                    if (j * AT_KEYS < cut_lo || (j + 1) * AT_KEYS > cut_hi) {    // scales of values that are no numbers: as in bf16
+                    for (int k = 0; k < 4; ++k) { k4[k] = of_k[32 * k]; v4[k] = of_v[32 * k]; }
 #pragma unroll
-                        for (int k = 0; k < AT_KEYS; k += 32)
-                            if (!isfinite(v[k + lane])) { v[k + lane] = 0.0f; if (j * AT_KEYS + k + lane < S.len) attn_bad_key(s_bad, j * AT_KEYS + k + lane); }
-                    }
+                    for (int k = 0; k < 4; ++k) of_k[32 * k] = k4[k] * P.scale_log2;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (!isfinite(v4[k])) { of_v[32 * k] = 0.0f; if (j * AT_KEYS + 32 * k + lane < S.len) attn_bad_key(P, s_bad, j * AT_KEYS + 32 * k + lane); }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); // (written again by copies)
                     __syncwarp();
                     if (lane == 0) mbar_arrive(sc_ready + 8 * sst);
@@ -766,7 +772,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 const int r = __ffs(left) - 1, a = __shfl_sync(0xFFFFFFFFu, bad_a, r), b = __shfl_sync(0xFFFFFFFFu, bad_b, r);
                 const long long to = __shfl_sync(0xFFFFFFFFu, at, r) + 4 * lane;
                 if (4 * lane >= D) continue;
-                const float4 t = attn_not_finite<KT>(P, T.seq, T.head, a, b, 4 * lane);
+                const float4 t = attn_not_finite<KT>(P, s_bad, T.seq, T.head, a, b, 4 * lane);
                 const float x[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -839,7 +845,7 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                         int a, b;
                         attn_bounds(P, S, T.seq, q2, a, b);
                         a = max(a, bad0); b = min(b, bad1);
-                        if (a < b) attn_add4(y, attn_not_finite<KT>(P, T.seq, T.head, a, b, d));
+                        if (a < b) attn_add4(y, attn_not_finite<KT>(P, s_bad, T.seq, T.head, a, b, d));
                     }
                 }
                 attn_store4<OC_DTYPE_BF16>(P, attn_out_at(P, S, T.seq, q2, head) + d, y);

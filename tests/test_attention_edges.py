@@ -160,6 +160,19 @@ def test_values_that_are_no_numbers_in_several_places(oc, ctx, dtype, kind, rows
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("rows", [1, 5, 140])
+@pytest.mark.parametrize("bad", BAD)
+def test_values_that_are_no_numbers_count_whatever_their_probability(oc, ctx, dtype, kind, rows, bad):
+    """Scores hundreds apart, so that most probabilities are 0 in fp32; in tiles that every row sees, and that some do not."""
+    cache = Cache(oc, kind, 1, 72, 1, 1500, 16, seed=43)
+    q = rand(torch.Generator().manual_seed(rows), rows, 2, 72, dtype=dtype, std=30.0)
+    check_no_numbers(oc, ctx, cache, q, list(range(rows)), bad, scale=1.0)
+    check_no_numbers(oc, ctx, cache, q, list(range(1500 - rows, 1500)), bad, unit=1, ahead=0, scale=1.0)
+    check_no_numbers(oc, ctx, cache, q, list(range(680, 680 + rows)), bad, unit=1, back=60, ahead=-1, scale=1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", TYPES)
 @pytest.mark.parametrize("rows", [1, 2000])
 def test_values_that_no_row_sees_take_no_time(oc, ctx, dtype, kind, rows):
     """Unwritten pages of NaN behind a causal window: within a factor of 4 of what it takes over numbers."""

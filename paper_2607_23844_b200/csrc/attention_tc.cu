@@ -15,7 +15,7 @@
 // Measured (bf16): 25 x 4608 rows over 9216 keys, 5 heads of 64, 1359 GFLOP: 1.83 ms, 744 TFLOP/s; 2 x 2560 x 4096, 24 heads of 64:
 // 210 us, 613 (480 CTAs are 3.2 rounds of the device's 148); 2 x 2048 x 4096, 16 heads of 128: 146 us, 941.  In 8 bits 333 us and 267.
 // What bounds heads of 64: a step (256 rows, 128 keys) takes 2500 to 2800 clocks, of which the products take 1024 and the
-// exponentials 1540 (a quarter of them by polynomial), both warps of a scheduler together 1900 with all their instructions
+// exponentials 1790 (an eighth of them by polynomial), both warps of a scheduler together 1900 with all their instructions
 // where nothing else runs; reading scores out of tensor memory beside running products costs 350, and each hand-over
 // through a barrier 150 to 300.  Other splits were slower: P beside S with a place for each tile of rows (2.08 ms), one
 // warp for both products (1.92), a pass for the maximum of its own (2.07), two CTAs of one tile on an SM (2.03).
@@ -48,10 +48,10 @@ template <int NT, int SUB, int KT> struct At {
     // warps take from the others: 2 x 128 x 176 + 2 x 128 x 80 = 512 x 128, 128 x 232 + 2 x 128 x 136 = 384 x 168.
     static constexpr int take_regs = !quant ? 0 : threads == 512 ? 176 : 232, give_regs = !quant ? 0 : threads == 512 ? 80 : 136;
     static_assert(!quant || threads == 512 || threads == 384, "registers of a CTA");
-    // Which of 8 neighbouring pairs of exponentials come from the polynomial: what the FMA pipe has room for.  SD3-sized rows (2 x 2560 x
-    // 4096 x 24 heads of 64): none 240 us, one 229, two 220, three 258; in 8 bits, whose scales take that pipe: none 347, one 363,
-    // two 396.  Heads of 128 wait for the tensor cores instead.
-    static constexpr int poly = quant ? 0 : SUB == 1 ? 0x11 : 0x01;
+    // Which of 8 neighbouring pairs of exponentials come from the polynomial: what the FMA pipe has room for.  None, one, two:  25 x 4608 x
+    // 9216, 5 heads of 64: 1809, 1735, 1760 us;  2 x 2560 x 4096, 24 heads of 64: 221, 214, 215;  2 x 2048 x 4096, 16 heads of 128:
+    // 156, 152.  In 8 and 4 bits the scales take that pipe.
+    static constexpr int poly = quant ? 0 : 0x01;
     static constexpr int chunk = 32;                                             // scores that a thread fetches at a time
     static constexpr int tile_bytes = SUB * AT_SUB_BYTES;                        // 128 keys (or rows) in bf16
     static constexpr int raw_bytes = KT == OC_DTYPE_I8 ? tile_bytes / 2 : tile_bytes / 4;        // (most) of 128 keys as they lie
@@ -136,8 +136,10 @@ __device__ __forceinline__ float at_max3(float a, float b, float c) {           
 __device__ __forceinline__ float at_exp2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
 // 2^x of two numbers without the special function unit, which gives 16 a clock and SM: x = n + f with n whole and
-// 0 <= f < 1, 2^f = 1 + f (a + f (b + f c)) (minimax for a polynomial through 1 by Remez' exchange, relative error 8.6e-5, a
-// 45th of bf16's half step), n added to the exponent.  What is below -127 becomes 0, what is above 127 2^127.
+// 0 <= f < 1, 2^f = 1 + f (a + f (b + f (c + f (d + f e)))) (minimax for a polynomial through 1 by Remez' exchange, its
+// coefficients rounded to fp32 one after the other; relative error in fp32 2.5e-7, that of the unit: the log-sum-exp is as good as
+// the other form's, which it was not with two terms less, 8.6e-5).  n is added to the exponent.  What is below -127 becomes 0, what
+// is above 127 2^127.
 __device__ __forceinline__ float at_clamp(float x) {
     float r;
     asm("{\n\t.reg .f32 t;\n\tmax.NaN.f32 t, %1, 0fC2FE0000;\n\tmin.NaN.f32 %0, t, 0f42FE0000;\n\t}" : "=f"(r) : "f"(x));
@@ -149,8 +151,10 @@ __device__ __forceinline__ f32x2 at_exp2_poly(f32x2 x) {
     f32x2 y;
     asm("add.rm.f32x2 %0, %1, %2;" : "=l"(y) : "l"(x), "l"(big));
     const f32x2 f = f2_add(x, f2_fma(y, f2(-1.0f), big));
-    f32x2 p = f2_fma(f, f2(0.07706704f), f2(0.227645f));
-    p = f2_fma(p, f, f2(0.69511676f));
+    f32x2 p = f2_fma(f, f2(0.0018613838f), f2(0.009022821f));
+    p = f2_fma(p, f, f2(0.055799514f));
+    p = f2_fma(p, f, f2(0.2401646f));
+    p = f2_fma(p, f, f2(0.6931513f));
     p = f2_fma(p, f, f2(1.0f));
     return f2_bits(__float_as_uint(f2_lo(p)) + (__float_as_uint(f2_lo(y)) << 23), __float_as_uint(f2_hi(p)) + (__float_as_uint(f2_hi(y)) << 23));
 }

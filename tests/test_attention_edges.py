@@ -199,3 +199,27 @@ def test_values_that_no_row_sees_take_no_time(oc, ctx, dtype, kind, rows):
         store = (pool if scale is None else scale).view(2, 64, 8, 64, -1)
         store[:, 31, :, 16:], store[:, 32:] = NAN, NAN                                   # tokens from 2000 on
     assert time() <= 4 * plain and torch.equal(out, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [BF16, "i8", "i4"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows", [1, 16, 140])
+def test_the_log_sum_exp_is_of_fp32(oc, ctx, kind, D, rows):
+    """One key at a score of 0 and 127 at -x exactly (one element of the products is not 0): lse = log(1 + 127 exp(-x)).
+    u = 2^-24.  The exponent x log2(e) is two roundings and the scale's two off, 4 u x; the exponential, a special function or a
+    polynomial, 5 u; 128 terms in chains of at most 34 additions 34 u of the sum, whose logarithm adds 4 u."""
+    u = 2.0 ** -24
+    cache = Cache(oc, kind, 1, D, 1, 128, 16, seed=44)
+    key = torch.zeros(128, 1, D)
+    key[1:, 0, 0] = -1.0
+    key = key.to(BF16).cuda()
+    ctx.kv_put(cache.desc, oc.kv_rows(cache.desc, 128, oc.DTYPE_BF16, k=key), key, cache.pool["k"], k_scale=cache.scale["k"], page_table=cache.gpu_table)
+    for step in range(0, 256, rows):
+        x = (torch.arange(step, step + rows) % 256 / 256.0 + 0.5).to(BF16)
+        q = torch.zeros(rows, 1, D, dtype=BF16)
+        q[:, 0, 0] = x
+        x, lse = x.double(), with_lse(oc, ctx, cache, q, scale=1.0)[1][:, 0].double()
+        want = torch.log(1 + 127 * torch.exp(-x))
+        level = 3 * u * x if isinstance(kind, str) else 0                                # (scale * q of a whole number)
+        assert ((lse - want).abs() <= 4 * u * x + level + 43 * u + 2 * u * want).all(), float(((lse - want).abs()).max() / u)

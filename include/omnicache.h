@@ -614,7 +614,7 @@ typedef struct oc_kv_rows {
  * may be null: a cache of one tensor.  A floating-point cache has the rows' own type.
  * Errors: OC_ERR_INVALID_ARG (also: scales missing, or given for a floating-point cache; a stride of 0
  * between several heads, rows or batch elements of oc_kv_get's rows; an fp32 cache of bf16 rows or the
- * other way round; one address for two outputs); OC_ERR_ALIGNMENT (a pool or its scales not 16-byte aligned, another pointer not aligned to its
+ * other way round; one address for two outputs, or for an output and an input); OC_ERR_ALIGNMENT (a pool or its scales not 16-byte aligned, another pointer not aligned to its
  * element, head_dim not a multiple of 8, page_rows not of 16); OC_ERR_UNSUPPORTED (head_dim over 256; 2^31 or
  * more rows, tokens, or vectors in the pool). */
 oc_status oc_kv_put(oc_ctx* ctx, const oc_kv_desc* cache, const oc_kv_rows* rows, const int32_t* page_table, const int32_t* idx,
@@ -644,7 +644,7 @@ oc_status oc_kv_get(oc_ctx* ctx, const oc_kv_desc* cache, const oc_kv_rows* rows
  * Recorded as OC_ERR_INVALID_ARG in the device status word: kv_len outside 0 .. seq_rows (taken as the
  * nearer end), q_start that descends or leaves n_rows or exceeds rows_per_batch (the rows concerned are
  * not written), an idx of another sequence (that row is not written).
- * out may be q with the same strides.  Errors: as oc_kv_put; OC_ERR_INVALID_ARG (scale not positive or
+ * out may be q with the same strides (with others it is refused).  Errors: as oc_kv_put; OC_ERR_INVALID_ARG (scale not positive or
  * not below 2^127; q_heads not a multiple of the cache's heads); OC_ERR_UNSUPPORTED (head_dim over 128; seq_rows of
  * 2^31 - 4096 and more). */
 typedef struct oc_attention_desc {

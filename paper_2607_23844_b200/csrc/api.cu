@@ -1,5 +1,6 @@
 // The C-ABI layer: argument validation, context, launch bookkeeping, Layered Cache store, and the
 // host-buffer convenience call.  No kernel lives here.
+#include <initializer_list>
 #include <math.h>
 #include <string.h>
 
@@ -618,6 +619,19 @@ static bool bad_view(const oc_rope_view& w, int64_t heads, int64_t rows, int64_t
     return (heads > 1 && w.head_stride == 0) || (std::min(rows, rows_per_batch) > 1 && w.row_stride == 0) || (batches && rows > rows_per_batch && w.batch_stride == 0);
 }
 
+// Whether an output begins where another output or an input does.
+static bool same_place(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+    for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+        if (!*o) continue;
+        if (std::find(o + 1, outputs.end(), *o) != outputs.end() || std::find(inputs.begin(), inputs.end(), *o) != inputs.end()) return true;
+    }
+    return false;
+}
+static bool same_strides(const oc_rope_view& a, const oc_rope_view& b, int64_t heads, int64_t rows, int64_t rows_per_batch, bool batches) {
+    return (heads <= 1 || a.head_stride == b.head_stride) && (std::min(rows, rows_per_batch) <= 1 || a.row_stride == b.row_stride) &&
+           (!batches || rows <= rows_per_batch || a.batch_stride == b.batch_stride);
+}
+
 static oc_status kv_move(oc_ctx* c, bool put, const oc_kv_desc* cache, const oc_kv_rows* rows, const int32_t* page_table, const int32_t* idx,
                          const void* k, const void* k_pool, const float* k_scale, const void* v, const void* v_pool, const float* v_scale, void* stream) {
     if (!c || !rows || !float_type(rows->dtype) || rows->n_rows < 0 || rows->rows_per_batch <= 0) return OC_ERR_INVALID_ARG;
@@ -637,6 +651,7 @@ static oc_status kv_move(oc_ctx* c, bool put, const oc_kv_desc* cache, const oc_
     if (rows->n_rows > ROWS_MAX || rows->rows_per_batch > ROWS_MAX) return OC_ERR_UNSUPPORTED;
     const uintptr_t el = (uintptr_t)elem_size(rows->dtype) - 1;
     if (((uintptr_t)k & el) || ((uintptr_t)v & el) || ((uintptr_t)page_table & 3u) || ((uintptr_t)idx & 3u)) return OC_ERR_ALIGNMENT;
+    if (put ? same_place({k_pool, v_pool, k_scale, v_scale}, {k, v, page_table, idx}) : same_place({k, v}, {k_pool, v_pool, k_scale, v_scale, page_table, idx})) return OC_ERR_INVALID_ARG;
     DeviceGuard guard(c->device);
     if (!guard.ok) return OC_ERR_CUDA;
     return launch_kv_move(c, put, *cache, *rows, page_table, idx, k, k_pool, k_scale, v, v_pool, v_scale, (cudaStream_t)stream);
@@ -678,6 +693,8 @@ oc_status oc_attention(oc_ctx* c, const oc_kv_desc* cache, const oc_attention_de
     const uintptr_t el = (uintptr_t)elem_size(d->dtype) - 1;
     if (((uintptr_t)q & el) || ((uintptr_t)out & el) || ((uintptr_t)lse & 3u) || ((uintptr_t)page_table & 3u) || ((uintptr_t)kv_len & 3u) ||
         ((uintptr_t)q_start & 3u) || ((uintptr_t)idx & 3u)) return OC_ERR_ALIGNMENT;
+    if (same_place({out, lse}, {k_pool, v_pool, k_scale, v_scale, page_table, kv_len, q_start, idx}) || lse == q) return OC_ERR_INVALID_ARG;
+    if (out == q && !same_strides(d->q, d->out, d->q_heads, d->n_rows, q_start ? d->n_rows : d->rows_per_batch, !q_start)) return OC_ERR_INVALID_ARG;
     DeviceGuard guard(c->device);
     if (!guard.ok) return OC_ERR_CUDA;
     return launch_attention(c, *cache, *d, page_table, kv_len, q_start, idx, q, k_pool, k_scale, v_pool, v_scale, out, lse, (cudaStream_t)stream);

@@ -223,3 +223,40 @@ def test_the_log_sum_exp_is_of_fp32(oc, ctx, kind, D, rows):
         want = torch.log(1 + 127 * torch.exp(-x))
         level = 3 * u * x if isinstance(kind, str) else 0                                # (scale * q of a whole number)
         assert ((lse - want).abs() <= 4 * u * x + level + 43 * u + 2 * u * want).all(), float(((lse - want).abs()).max() / u)
+
+
+def test_outputs_in_the_place_of_others_are_refused(oc, host):
+    A = 0x10000
+    view = oc.CRopeView(2560, 256, 64)
+
+    def attend(q=A, kp=2 * A, vp=3 * A, out=4 * A, ks=5 * A, vs=6 * A, lse=7 * A, oview=view, n=20, per=10, heads=4, kind=oc.DTYPE_I8, **kw):
+        d = oc.CAttention(oc.DTYPE_BF16, heads, 0.1, n, per, 0, -1, -1, view, oview)
+        cache = oc.CKv(kind, 2, 64, 2, 100, 16, 14, 7)
+        return host.ctx.attention(cache, d, q, kp, vp, out, k_scale=ks, v_scale=vs, page_table=8 * A, lse=lse, stream=0, check=False, **kw)
+    for bad in (dict(lse=4 * A), dict(lse=A), dict(lse=2 * A), dict(lse=6 * A), dict(lse=8 * A), dict(out=5 * A), dict(out=6 * A), dict(out=8 * A), dict(out=9 * A, kv_len=9 * A),
+                dict(lse=9 * A, idx=9 * A), dict(out=A, oview=oc.CRopeView(2560, 64, 640)), dict(out=A, oview=oc.CRopeView(5120, 256, 64)), dict(out=A, oview=oc.CRopeView(2560, 512, 64))):
+        assert attend(**bad) == oc.ERR_INVALID_ARG, bad
+
+    def move(put, k=A, kp=2 * A, v=3 * A, vp=4 * A, ks=5 * A, vs=6 * A, table=7 * A, idx=8 * A):
+        r = oc.CKvRows(oc.DTYPE_BF16, 20, 20, oc.CRopeView(2560, 128, 64), oc.CRopeView(2560, 128, 64))
+        args = (k, kp, v, vp) if put else (kp, k, vp, v)
+        return getattr(host.ctx, "kv_put" if put else "kv_get")(oc.CKv(oc.DTYPE_I8, 2, 64, 2, 100, 16, 14, 7), r, *args, k_scale=ks, v_scale=vs, page_table=table, idx=idx,
+                                                                stream=0, check=False)
+    for bad in (dict(kp=3 * A), dict(vp=A), dict(ks=2 * A), dict(vs=2 * A), dict(ks=4 * A), dict(vs=4 * A), dict(ks=A), dict(vs=3 * A), dict(kp=7 * A), dict(vs=8 * A)):
+        assert move(True, **bad) == oc.ERR_INVALID_ARG, bad
+    for bad in (dict(k=4 * A), dict(v=2 * A), dict(k=5 * A), dict(v=6 * A), dict(v=7 * A), dict(k=8 * A)):
+        assert move(False, **bad) == oc.ERR_INVALID_ARG, bad
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("rows", [1, 16, 200])
+def test_in_place_with_strides_that_do_not_count(oc, ctx, dtype, kind, rows):
+    """out is q: strides of axes of one element may differ."""
+    cache = Cache(oc, kind, 1, 64, 1, 300, 16, seed=45)
+    q = rand(torch.Generator().manual_seed(rows), rows, 1, 64, dtype=dtype)
+    want = with_lse(oc, ctx, cache, q)[0]
+    x = q.cuda()
+    d = oc.attention_desc(cache.desc, rows, tag(oc, dtype), 1, 0.125, q=x, out=(7, 64, 0))
+    ctx.attention(cache.desc, d, x, cache.pool["k"], cache.pool["v"], x, **cache.args())
+    assert torch.equal(x.cpu(), want)

@@ -286,6 +286,29 @@ def _ptr_strided(t) -> int | None:
     return t.data_ptr()
 
 
+_INT32, _ROW_TYPES = torch.int32, {DTYPE_F32: torch.float32, DTYPE_BF16: torch.bfloat16}
+
+
+def _ints(t, name: str) -> int | None:
+    """Pointer of an int32 array: torch's own index tensors are int64 and would be read as twice as many numbers."""
+    if t is None:
+        return None
+    try:
+        dtype = t.dtype
+    except AttributeError:
+        return t                                                     # (an address)
+    if dtype is not _INT32:
+        raise ValueError(f"{name} is {dtype}: expected torch.int32")
+    return _ptr(t)
+
+
+def _typed(t, dtype: int, name: str) -> int | None:
+    """Pointer of rows (as _ptr_strided) whose type a descriptor names."""
+    if type(t) is _Tensor and t.dtype is not _ROW_TYPES.get(dtype):
+        raise ValueError(f"{name} is {t.dtype}, which is not the descriptor's type")
+    return _ptr_strided(t)
+
+
 def _rows(t, width: int, stride: int | None, name: str):
     """(pointer, elements between rows) of a matrix `width` elements wide: dense unless a stride is given or the tensor
     is a part of a larger one."""
@@ -438,6 +461,7 @@ def kv_rows(cache: CKv, n_rows: int, dtype: int, k=None, v=None, rows_per_batch:
     """oc_kv_rows, the strides taken from tensors (or from (batch, row, head) stride tuples): [n_rows, heads, head_dim]
     views, as a packed projection holds them, or [batch, heads, rows, head_dim], as oc_rope leaves them."""
     per_batch = _per_batch(rows_per_batch, n_rows, k, v)
+    _typed(k, dtype, "k"), _typed(v, dtype, "v")
     return CKvRows(dtype, n_rows, per_batch, _heads_view(k, cache.heads, cache.head_dim, n_rows, per_batch, "k"),
                    _heads_view(v, cache.heads, cache.head_dim, n_rows, per_batch, "v"))
 
@@ -640,7 +664,7 @@ class Context:
     def kv_put(self, cache: CKv, rows: CKvRows, k, k_pool, v=None, v_pool=None, k_scale=None, v_scale=None, page_table=None,
                idx=None, stream=None, check: bool = True) -> int:
         """oc_kv_put: strides are the descriptor's, so k and v may be parts of one projection."""
-        st = _lib.oc_kv_put(self._h, cache, rows, _ptr(page_table), _ptr(idx), _ptr_strided(k), _ptr(k_pool), _ptr(k_scale),
+        st = _lib.oc_kv_put(self._h, cache, rows, _ints(page_table, "page_table"), _ints(idx, "idx"), _ptr_strided(k), _ptr(k_pool), _ptr(k_scale),
                             _ptr_strided(v), _ptr(v_pool), _ptr(v_scale), _stream(stream))
         if check:
             _chk(st, "oc_kv_put")
@@ -649,7 +673,7 @@ class Context:
     def kv_get(self, cache: CKv, rows: CKvRows, k_pool, k, v_pool=None, v=None, k_scale=None, v_scale=None, page_table=None,
                idx=None, stream=None, check: bool = True) -> int:
         """oc_kv_get"""
-        st = _lib.oc_kv_get(self._h, cache, rows, _ptr(page_table), _ptr(idx), _ptr(k_pool), _ptr(k_scale), _ptr_strided(k),
+        st = _lib.oc_kv_get(self._h, cache, rows, _ints(page_table, "page_table"), _ints(idx, "idx"), _ptr(k_pool), _ptr(k_scale), _ptr_strided(k),
                             _ptr(v_pool), _ptr(v_scale), _ptr_strided(v), _stream(stream))
         if check:
             _chk(st, "oc_kv_get")
@@ -658,8 +682,9 @@ class Context:
     def attention(self, cache: CKv, desc: CAttention, q, k_pool, v_pool, out, k_scale=None, v_scale=None, page_table=None,
                   kv_len=None, q_start=None, idx=None, lse=None, stream=None, check: bool = True) -> int:
         """oc_attention"""
-        st = _lib.oc_attention(self._h, cache, desc, _ptr(page_table), _ptr(kv_len), _ptr(q_start), _ptr(idx), _ptr_strided(q),
-                               _ptr(k_pool), _ptr(k_scale), _ptr(v_pool), _ptr(v_scale), _ptr_strided(out), _ptr(lse),
+        st = _lib.oc_attention(self._h, cache, desc, _ints(page_table, "page_table"), _ints(kv_len, "kv_len"),
+                               _ints(q_start, "q_start"), _ints(idx, "idx"), _typed(q, desc.dtype, "q"), _ptr(k_pool),
+                               _ptr(k_scale), _ptr(v_pool), _ptr(v_scale), _typed(out, desc.dtype, "out"), _ptr(lse),
                                _stream(stream))
         if check:
             _chk(st, "oc_attention")

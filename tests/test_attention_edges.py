@@ -260,3 +260,25 @@ def test_in_place_with_strides_that_do_not_count(oc, ctx, dtype, kind, rows):
     d = oc.attention_desc(cache.desc, rows, tag(oc, dtype), 1, 0.125, q=x, out=(7, 64, 0))
     ctx.attention(cache.desc, d, x, cache.pool["k"], cache.pool["v"], x, **cache.args())
     assert torch.equal(x.cpu(), want)
+
+
+def test_tensors_of_another_type_are_refused(oc, host):
+    cache = oc.CKv(oc.DTYPE_BF16, 2, 64, 2, 100, 16, 14, 7)
+    x, y = torch.zeros(20, 2, 64, dtype=BF16), torch.zeros(20, 2, 64)
+    for kw in (dict(k=y), dict(k=x, v=y), dict(k=y, v=x)):
+        with pytest.raises(ValueError):
+            oc.kv_rows(cache, 20, oc.DTYPE_BF16, **kw)
+    rows, pool = oc.kv_rows(cache, 20, oc.DTYPE_BF16, k=x, v=x), torch.zeros(14, 2, 16, 64, dtype=BF16)
+    desc = oc.attention_desc(cache, 20, oc.DTYPE_BF16, 2, 0.1, rows_per_batch=10, q=x, out=x)
+    for bad in (torch.zeros(20, dtype=torch.int64), torch.zeros(20, dtype=torch.int16), torch.zeros(20)):
+        for name in ("idx", "page_table", "kv_len", "q_start"):
+            with pytest.raises(ValueError):
+                host.ctx.attention(cache, desc, x, pool, pool, x, stream=0, check=False, **{name: bad})
+            if name in ("idx", "page_table"):
+                with pytest.raises(ValueError):
+                    host.ctx.kv_put(cache, rows, x, pool, stream=0, check=False, **{name: bad})
+                with pytest.raises(ValueError):
+                    host.ctx.kv_get(cache, rows, pool, x, stream=0, check=False, **{name: bad})
+    for q, out in ((y, x), (x, y)):
+        with pytest.raises(ValueError):
+            host.ctx.attention(cache, desc, q, pool, pool, out, stream=0, check=False)

@@ -3,7 +3,7 @@ on.  The restatement in 64 bits and its bounds are those of test_attention, comp
 import pytest
 import torch
 
-from test_attention import BF16, Cache, assert_attn, ctx, exact, oc, rand, tag  # noqa: F401 (fixtures)
+from test_attention import BF16, TYPES, Cache, assert_attn, ctx, exact, oc, rand, tag  # noqa: F401 (fixtures)
 
 KINDS = [BF16, "i8", "i4"]
 
@@ -119,3 +119,47 @@ def test_pairs_of_tiles_of_unsorted_rows(oc, ctx, kind, D):
     for order in (lambda x: x.flip(0), lambda x: x[torch.randperm(512, generator=gen)]):
         idx = torch.cat([order(torch.arange(512)) + 520 * s for s in range(4)])
         attend(oc, ctx, cache, q, [512] * 4, unit=1, ahead=0, idx=idx)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("n_seqs,heads", [(32, 8), (256, 1), (300, 1), (149, 2)])
+@pytest.mark.parametrize("how", ["all alike", "ascending", "scattered"])
+def test_single_tokens_of_many_sequences(oc, ctx, dtype, kind, n_seqs, heads, how):
+    """More CTAs than the device holds at once, where bf16 rows of long sequences come first; equal lengths, and none at all."""
+    gen = torch.Generator().manual_seed(n_seqs)
+    lens = {"all alike": [100] * n_seqs, "ascending": [s * 130 // n_seqs for s in range(n_seqs)], "scattered": torch.randint(0, 131, (n_seqs,), generator=gen).tolist()}[how]
+    cache = Cache(oc, kind, heads, 64, n_seqs, 130, 16, lens=lens, seed=8)
+    q = rand(gen, n_seqs, 2 * heads, 64, dtype=dtype)
+    attend(oc, ctx, cache, q, [1] * n_seqs)
+    attend(oc, ctx, cache, q, [1] * n_seqs, unit=1, back=20, ahead=0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [BF16, "i8"])
+def test_lengths_out_of_range_among_many_sequences(oc, ctx, kind):
+    """Recorded, and taken as the nearer end, wherever the sequence comes in the order of lengths."""
+    n = 200
+    cache = Cache(oc, kind, 1, 64, n, 48, 16, seed=9)
+    q = rand(torch.Generator().manual_seed(9), n, 1, 64, dtype=BF16)
+    qq, out = q.cuda(), torch.full((n, 1, 64), 5.0, dtype=BF16, device="cuda")
+    lens = torch.full((n,), 48, dtype=torch.int32)
+    lens[3], lens[7], lens[11] = 2 ** 31 - 1, -(2 ** 31), -1
+    d = oc.attention_desc(cache.desc, n, oc.DTYPE_BF16, 1, 0.125, rows_per_batch=1, q=qq, out=out)
+    ctx.attention(cache.desc, d, qq, cache.pool["k"], cache.pool["v"], out, kv_len=lens.cuda(), **cache.args())
+    torch.cuda.synchronize()
+    assert ctx.device_status() == oc.ERR_INVALID_ARG and ctx.device_status() == oc.OK
+    assert (out[7] == 0).all() and (out[11] == 0).all()
+    rows = [(s, 0) for s in range(n)]
+    cache.lens = [max(0, min(48, int(x))) for x in lens]
+    want, bound, _, _ = exact(cache, q, rows, 0.125)
+    assert_attn(out, want, bound, rows)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", TYPES)
+def test_a_long_chunk_among_single_tokens(oc, ctx, dtype, kind):
+    cache = Cache(oc, kind, 2, 72, 40, 700, 32, lens=[700 - 17 * s for s in range(40)], seed=10)
+    rows = [1] * 20 + [300] + [1] * 19
+    q = rand(torch.Generator().manual_seed(10), sum(rows), 4, 72, dtype=dtype)
+    attend(oc, ctx, cache, q, rows, unit=1, ahead=0, ragged=True)

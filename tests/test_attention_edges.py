@@ -1,5 +1,9 @@
 """Attention over the paged cache at its edges: values that are no numbers, the largest numbers, cuts between the CTAs that share
 a sequence's keys.  Restatement and bounds are those of test_attention."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -282,3 +286,67 @@ def test_tensors_of_another_type_are_refused(oc, host):
     for q, out in ((y, x), (x, y)):
         with pytest.raises(ValueError):
             host.ctx.attention(cache, desc, q, pool, pool, out, stream=0, check=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", [(BF16, BF16), (BF16, "i8"), (F32, "i8")])
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_pools_of_more_than_2_to_the_32_bytes(oc, ctx, dtype, kind, rows):
+    """The last pages of a pool, in every kernel; their values as floating-point vectors read back."""
+    heads, D, page = 2, 128, 64
+    pages = 140000 if kind == BF16 else 280000                                           # 4.6 GB
+    desc = oc.kv_desc(tag(oc, kind), heads, D, 1, 200, page, n_pages=pages)
+    shape = (pages, heads, page)
+    pool = torch.empty(*shape, D, device="cuda", dtype=BF16 if kind == BF16 else torch.int8)
+    scale = None if kind == BF16 else torch.empty(shape, device="cuda")
+    table = torch.tensor([[pages - 1, pages - 3, pages - 2, pages - 4]], dtype=torch.int32, device="cuda")
+    x = rand(torch.Generator().manual_seed(1), 200, heads, D, dtype=dtype).cuda()
+    ctx.kv_put(desc, oc.kv_rows(desc, 200, tag(oc, dtype), k=x), x, pool, k_scale=scale, page_table=table)
+    back, q = torch.empty_like(x), rand(torch.Generator().manual_seed(2), rows, heads, D, dtype=dtype).cuda()
+    held = torch.empty(200, heads, D, device="cuda") if kind != BF16 else back
+    ctx.kv_get(desc, oc.kv_rows(desc, 200, oc.DTYPE_BF16 if kind == BF16 else oc.DTYPE_F32, k=held), pool, held, k_scale=scale, page_table=table)
+    out = torch.empty_like(q)
+    ctx.attention(desc, oc.attention_desc(desc, rows, tag(oc, dtype), heads, 0.1, q=q, out=out), q, pool, pool, out, k_scale=scale, v_scale=scale, page_table=table)
+    torch.cuda.synchronize()
+    assert ctx.device_status() == oc.OK
+    assert ((held.double() - x.double()).abs() <= (0 if kind == BF16 else 0.5001 / 127) * x.double().abs().amax(-1, keepdim=True)).all()
+    p = torch.softmax(torch.einsum("rhd,jhd->hrj", q.double(), held.double()) * 0.1, -1)
+    want, size = torch.einsum("hrj,jhd->rhd", p, held.double()), torch.einsum("hrj,jhd->rhd", p, held.double().abs())
+    # scores of up to 128 terms: 2 x 133 u times at most 128 x 25 x 0.1; p in bf16 and the output: 2 half steps
+    assert ((out.double() - want).abs() <= (2 * 133 * 2.0 ** -24 * 320 + 400 * 2.0 ** -24 + (2.0 ** -7 if dtype == BF16 else 0)) * size).all()
+
+
+CAPTURED = """
+import torch
+from paper_2607_23844_b200 import omnicache as oc
+ctx = oc.Context(0)
+done = []
+for dtype, tag in ((torch.bfloat16, oc.DTYPE_BF16), (torch.float32, oc.DTYPE_F32)):
+    for kind in (tag, oc.DTYPE_I8, oc.DTYPE_I4):
+        for rows in (1, 300):
+            d = oc.kv_desc(kind, 2, 64, 1, 600, 64)
+            (kp, ks), (vp, vs) = oc.kv_pools(d), oc.kv_pools(d)
+            x, q = torch.randn(600, 2, 64, device="cuda", dtype=dtype), torch.randn(rows, 2, 64, device="cuda", dtype=dtype)
+            out = torch.zeros_like(q)
+            r, a = oc.kv_rows(d, 600, tag, k=x, v=x), oc.attention_desc(d, rows, tag, 2, 0.125, q=q, out=out)
+            g = torch.cuda.CUDAGraph()
+            def step():
+                ctx.kv_put(d, r, x, kp, x, vp, k_scale=ks, v_scale=vs)
+                ctx.attention(d, a, q, kp, vp, out, k_scale=ks, v_scale=vs)
+            with torch.cuda.graph(g):
+                step()
+            g.replay()
+            torch.cuda.synchronize()
+            got = out.clone()
+            out.zero_()
+            step()
+            torch.cuda.synchronize()
+            assert got.abs().sum() > 0 and torch.equal(got, out) and ctx.device_status() == oc.OK
+print("captured")
+"""
+
+
+@pytest.mark.gpu
+def test_a_process_s_first_calls_may_be_captured(oc):
+    got = subprocess.run([sys.executable, "-c", CAPTURED], capture_output=True, text=True, timeout=300, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert got.returncode == 0 and "captured" in got.stdout, got.stderr[-2000:]

@@ -610,7 +610,8 @@ typedef struct oc_kv_rows {
 /* oc_kv_put writes row r of k and v to the cache as token idx[r] (no idx: token r); oc_kv_get reads
  * token idx[r] into row r, values rounded once to the rows' type.  Rows whose idx is negative (the unused tail of
  * a kept list) are left out, by oc_kv_get left as they were; so are numbers of n_seqs * seq_rows and
- * more (recorded in the device status word).  idx of oc_kv_put names no token twice.  v and its pool
+ * more (recorded in the device status word).  oc_kv_put writes no place twice: idx names no token twice,
+ * nor two whose page the table shares.  v and its pool
  * may be null: a cache of one tensor.  A floating-point cache has the rows' own type.
  * Errors: OC_ERR_INVALID_ARG (also: scales missing, or given for a floating-point cache; a stride of 0
  * between several heads, rows or batch elements of oc_kv_get's rows; an fp32 cache of bf16 rows or the
@@ -640,7 +641,8 @@ oc_status oc_kv_get(oc_ctx* ctx, const oc_kv_desc* cache, const oc_kv_rows* rows
  * however small its probability (NaN where both signs meet), of a NaN in K or V a NaN.
  * q and out are fp32 over a cache in fp32, 8 or 4 bits, or bf16 over one in bf16, 8 or 4 bits.  bf16:
  * products of bf16 with fp32 sums; probabilities, times the value's scale in the 8- and 4-bit caches,
- * are rounded to bf16 before they meet V; everything else is fp32.  fp32: all of it in fp32.
+ * are rounded to bf16 before they meet V; everything else is fp32.  fp32: all of it in fp32.  Sums are divided at
+ * the end, so that values of 2^100 and more may leave fp32.
  * Recorded as OC_ERR_INVALID_ARG in the device status word: kv_len outside 0 .. seq_rows (taken as the
  * nearer end), q_start that descends or leaves n_rows or exceeds rows_per_batch (the rows concerned are
  * not written), an idx of another sequence (that row is not written).

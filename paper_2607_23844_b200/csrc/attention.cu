@@ -5,7 +5,7 @@
 // Thread (ty, tx) of 16 x 16 holds the scores of TR / 16 rows with 4 keys, and of the output TR / 16 rows with 4 or 8
 // elements.  Where there are few tiles, the CTAs of a cluster split the keys and join their results through
 // distributed shared memory.
-// Bound by shared memory's reads beside the FMAs: 2 x 1024 x 1024, 16 heads of 64 or 128: 338 and 736 us, 25 and 23 TFLOP/s.  Tiles are
+// Bound by shared memory's reads beside the FMAs: 2 x 1024 x 1024, 16 heads of 64 or 128: 338 and 711 us, 25 and 24 TFLOP/s.  Tiles are
 // fetched into registers a step ahead.
 #include <string.h>
 

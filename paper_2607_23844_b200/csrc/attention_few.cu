@@ -9,9 +9,10 @@
 //              4 E chunk + E c on; a step of the product takes four of them, from the queries the same ones
 //     outputs  lane (n, c) holds of the keys of columns 2c, 2c + 1, 2c + 8, 2c + 9 the EV elements from EV n on; rows n and n + 8 of
 //              tile j are elements EV n + 2j and the next.  P^T comes out of the scores by transposing 8 x 8 pieces (movmatrix)
-// Measured in 8 bits on 286000 keys of 8 heads of 128, 4 heads to a key: 604 MB in 165 us (3.65 TB/s), issuing 91 million
+// Measured in 8 bits on 286000 keys of 8 heads of 128, 4 heads to a key: 604 MB in 168 us (3.60 TB/s), issuing 91 million
 // instructions, 82 us of every scheduler's time, most of them for the widening; the rest is waiting with 16 warps on an SM.
-// 8 and 4 bits are widened to bf16 exactly; the scales join the scores and the probabilities.  The warps of a CTA, and the
+// 8 and 4 bits are widened to bf16 exactly; the scales join the scores and the probabilities, which are rounded to bf16 for the
+// second product (their sum is of the unrounded ones).  The warps of a CTA, and the
 // CTAs of a cluster, split the keys and join (maximum, sum, output) at the end, the latter through distributed shared memory.
 #include <string.h>
 

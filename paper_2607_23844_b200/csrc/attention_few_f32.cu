@@ -3,7 +3,7 @@
 // A warp takes 32 keys at a time.  For the scores a lane is a key: it reads the key's row 16 bytes at a time (the lanes' rows are
 // neighbours, so what one load leaves of a line the next ones find in L1) and multiplies with the queries in shared memory, no sum
 // crosses lanes.  For the outputs a lane is a few columns, the keys' probabilities come round by shuffles, and values are read
-// as they lie.  4 x 8192 keys of 16 heads of 64: 98 us (268 MB, 2.7 TB/s), in 8 bits 52; with tiles of 16 rows in shared memory, of
+// as they lie.  4 x 8192 keys of 16 heads of 64: 104 us (268 MB, 2.6 TB/s), in 8 bits 48; with tiles of 16 rows in shared memory, of
 // which one is used, 300.  The warps of a CTA and the CTAs of a cluster split the keys and join at the end.
 #include <string.h>
 

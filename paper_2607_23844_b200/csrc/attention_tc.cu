@@ -12,8 +12,9 @@
 //                   numbers exactly, so that the scales join the scores and the probabilities
 // Two tiles of rows take turns: while one's scores become probabilities the tensor cores work for the other.  With heads of up
 // to 64 a third place for scores in tensor memory lets the products run ahead of the softmax warps.
-// Measured (bf16): 25 x 4608 rows over 9216 keys, 5 heads of 64, 1359 GFLOP: 1.83 ms, 744 TFLOP/s; 2 x 2560 x 4096, 24 heads of 64:
-// 210 us, 613 (480 CTAs are 3.2 rounds of the device's 148); 2 x 2048 x 4096, 16 heads of 128: 146 us, 941.  In 8 bits 333 us and 267.
+// Measured (bf16): 25 x 4608 rows over 9216 keys, 5 heads of 64, 1359 GFLOP: 1.83 ms, 742 TFLOP/s; 2 x 2560 x 4096, 24 heads of 64:
+// 213 us, 606 (480 CTAs are 3.2 rounds of the device's 148); 2 x 2048 x 4096, 16 heads of 128: 152 us, 904.  In 8 bits 342 us and 262.
+// Probabilities are rounded to bf16: the second product takes both operands in one type, and values in bf16 as they are.
 // What bounds heads of 64: a step (256 rows, 128 keys) takes 2500 to 2800 clocks, of which the products take 1024 and the
 // exponentials 1790 (an eighth of them by polynomial), both warps of a scheduler together 1900 with all their instructions
 // where nothing else runs; reading scores out of tensor memory beside running products costs 350, and each hand-over

@@ -6,7 +6,7 @@
 // tokens of 32 / lph neighbouring rows share a warp: kept lists ascend, so their vectors of a head are mostly
 // neighbours in a page too.
 // Measured on 230400 tokens with 5 heads of 64 (keys and values), put | get: bf16 590 MB 92 | 96 us (6.4 TB/s), fp32 1180 MB 176 | 179 (6.7);
-// bf16 to 8 bits 451 MB 172 | 86, to 4 bits 165 | 84; fp32 to 8 bits 193 | 140.  Putting whole numbers is bound by their 245
+// bf16 to 8 bits 451 MB 173 | 87, to 4 bits 166 | 84; fp32 to 8 bits 174 | 140.  Putting whole numbers is bound by their 247
 // instructions for 8 elements (the largest magnitude, the quotients, their exact rounding).
 #include <string.h>
 

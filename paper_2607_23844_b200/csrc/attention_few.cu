@@ -9,7 +9,7 @@
 //              4 E chunk + E c on; a step of the product takes four of them, from the queries the same ones
 //     outputs  lane (n, c) holds of the keys of columns 2c, 2c + 1, 2c + 8, 2c + 9 the EV elements from EV n on; rows n and n + 8 of
 //              tile j are elements EV n + 2j and the next.  P^T comes out of the scores by transposing 8 x 8 pieces (movmatrix)
-// Measured in 8 bits on 286000 keys of 8 heads of 128, 4 heads to a key: 604 MB in 168 us (3.60 TB/s), issuing 91 million
+// Measured in 8 bits on 286000 keys of 8 heads of 128, 4 heads to a key: 604 MB in 166 us (3.64 TB/s), issuing 91 million
 // instructions, 82 us of every scheduler's time, most of them for the widening; the rest is waiting with 16 warps on an SM.
 // 8 and 4 bits are widened to bf16 exactly; the scales join the scores and the probabilities, which are rounded to bf16 for the
 // second product (their sum is of the unrounded ones).  The warps of a CTA, and the
@@ -264,19 +264,19 @@ attention_few_kernel(const __grid_constant__ AttnParams P) {
         }
         // values that are no numbers: 0 * NaN would reach rows that do not see them
         if (quant) {
-            if (!(fabsf(vs[0]) + fabsf(vs[1]) < INFINITY))                   // (seldom)
+            if (__any_sync(0xFFFFFFFFu, fmaf(vs[0], 0.0f, vs[1] * 0.0f) != 0.0f))
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (!isfinite(vs[i])) { vs[i] = 0.0f; if (key0 + key_n + 2 * i < S.len) attn_bad_key(P, s_bad, key0 + key_n + 2 * i); }
         } else {
-            uint32_t zero = 0;
+            uint32_t zero[4] = {};                                           // (four sums: one would wait for itself)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int ps = 0; ps < NP; ++ps)
 #pragma unroll
-                    for (int j = 0; j < VB / 4; ++j) zero = attn_zero2(zero, rv[ps][i].w[j]);
-            if (attn_bad2(zero)) {
+                    for (int j = 0; j < VB / 4; ++j) zero[i] = attn_zero2(zero[i], rv[ps][i].w[j]);
+            if (attn_bad2(zero[0] | zero[1] | zero[2] | zero[3])) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     bool odd = false;

@@ -154,12 +154,12 @@ attention_few_f32_kernel(const __grid_constant__ AttnParams P) {
                 }
             }
             if (!quant) {                                                    // (0 times what is no number is NaN, and stays it)
-                float zero = 0.0f;
+                float zero[2] = {0.0f, 0.0f};
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c) zero = fmaf(x[g][c], 0.0f, zero);
-                if (zero != 0.0f) {
+                    for (int c = 0; c < CPL; ++c) zero[g & 1] = fmaf(x[g][c], 0.0f, zero[g & 1]);
+                if (zero[0] + zero[1] != 0.0f) {
 #pragma unroll
                     for (int g = 0; g < G; ++g)
 #pragma unroll

@@ -12,8 +12,8 @@
 //                   numbers exactly, so that the scales join the scores and the probabilities
 // Two tiles of rows take turns: while one's scores become probabilities the tensor cores work for the other.  With heads of up
 // to 64 a third place for scores in tensor memory lets the products run ahead of the softmax warps.
-// Measured (bf16): 25 x 4608 rows over 9216 keys, 5 heads of 64, 1359 GFLOP: 1.83 ms, 742 TFLOP/s; 2 x 2560 x 4096, 24 heads of 64:
-// 213 us, 606 (480 CTAs are 3.2 rounds of the device's 148); 2 x 2048 x 4096, 16 heads of 128: 152 us, 904.  In 8 bits 342 us and 262.
+// Measured (bf16): 25 x 4608 rows over 9216 keys, 5 heads of 64, 1359 GFLOP: 1.81 ms, 751 TFLOP/s; 2 x 2560 x 4096, 24 heads of 64:
+// 214 us, 603 (480 CTAs are 3.2 rounds of the device's 148); 2 x 2048 x 4096, 16 heads of 128: 147 us, 935.  In 8 bits 330 us and 261.
 // Probabilities are rounded to bf16: the second product takes both operands in one type, and values in bf16 as they are.
 // What bounds heads of 64: a step (256 rows, 128 keys) takes 2500 to 2800 clocks, of which the products take 1024 and the
 // exponentials 1790 (an eighth of them by polynomial), both warps of a scheduler together 1900 with all their instructions
@@ -455,15 +455,15 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                 if (!AT_WAIT(v_full + 8 * st, (uint32_t)((j - j0) / A::v_stages) & 1u)) break;
                 const int key0 = j * AT_KEYS;
                 const uint32_t base = smem + A::v_at + (uint32_t)(st * A::tile_bytes);
-                uint32_t zero = 0;
+                uint32_t zero[4] = {};
 #pragma unroll 8
                 for (int i = h * 32 + lane; i < SUB * 1024; i += 32 * A::helpers) {              // pieces of 16 bytes
                     uint32_t w[4];
                     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(base + (uint32_t)(i * 16)) : "memory");
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) zero = attn_zero2(zero, w[e]);
+                    for (int e = 0; e < 4; ++e) zero[e] = attn_zero2(zero[e], w[e]);
                 }
-                if (__any_sync(0xFFFFFFFFu, attn_bad2(zero))) {
+                if (__any_sync(0xFFFFFFFFu, attn_bad2(zero[0] | zero[1] | zero[2] | zero[3]))) {
                     int bad_first = 0x7FFFFFFF, bad_last = -1;
                     for (int i = h * 32 + lane; i < SUB * 1024; i += 32 * A::helpers) {
                         const uint32_t at = base + (uint32_t)(i * 16);
@@ -532,14 +532,15 @@ attention_tc_kernel(const __grid_constant__ AttnTcParams TP) {
                     const int sst = i % AT_SCALES;
                     if (!AT_WAIT(sc_full + 8 * sst, (uint32_t)(i / AT_SCALES) & 1u)) break;
                     // the softmax scale joins the keys' (one product less for each score); values' scales that are no numbers: as in bf16
-                    float* of_k = (float*)(at_smem + A::scale_at) + 2 * sst * AT_KEYS + lane, *of_v = of_k + AT_KEYS, k4[4], v4[4];
+                    float* of_k = (float*)(at_smem + A::scale_at) + 2 * sst * AT_KEYS + lane, *of_v = of_k + AT_KEYS, k4[4], zero = 0.0f;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) { k4[k] = of_k[32 * k]; v4[k] = of_v[32 * k]; }
+                    for (int k = 0; k < 4; ++k) { k4[k] = of_k[32 * k]; zero = fmaf(of_v[32 * k], 0.0f, zero); }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) of_k[32 * k] = k4[k] * P.scale_log2;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (!isfinite(v4[k])) { of_v[32 * k] = 0.0f; if (j * AT_KEYS + 32 * k + lane < S.len) attn_bad_key(P, s_bad, j * AT_KEYS + 32 * k + lane); }
+                    if (__any_sync(0xFFFFFFFFu, zero != 0.0f))
+#pragma unroll 1
+                        for (int k = 0; k < AT_KEYS; k += 32)
+                            if (!isfinite(of_v[k])) { of_v[k] = 0.0f; if (j * AT_KEYS + k + lane < S.len) attn_bad_key(P, s_bad, j * AT_KEYS + k + lane); }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); // (written again by copies)
                     __syncwarp();
                     if (lane == 0) mbar_arrive(sc_ready + 8 * sst);

@@ -648,7 +648,7 @@ oc_status oc_kv_get(oc_ctx* ctx, const oc_kv_desc* cache, const oc_kv_rows* rows
  * not written), an idx of another sequence (that row is not written).
  * out may be q with the same strides (with others it is refused).  Errors: as oc_kv_put; OC_ERR_INVALID_ARG (scale not positive or
  * not below 2^127; q_heads not a multiple of the cache's heads); OC_ERR_UNSUPPORTED (head_dim over 128; seq_rows of
- * 2^31 - 4096 and more). */
+ * 2^31 - 4096 and more; 2^27 and more sequences times heads of the cache times tiles of 16 to 256 rows). */
 typedef struct oc_attention_desc {
     int dtype;                        /* of q and out */
     int q_heads;
